@@ -9,6 +9,10 @@
  *   wide_attn       head-group-masked causal attention            (Eq. 1; Algorithm 4: prefill and decode forms)
  *   wide_qproj      routed query projection, GEMM-MN              (Eq. 1 under the mask; Algorithm 2)
  *   wide_unpermute  the scatter epilogue as a standalone step     (Algorithm 2, epilogue)
+ * and what serving puts between the projections and the attention (no counterpart in the paper):
+ *   wide_rope         rotary positions of the queries and keys, one or several position axes
+ *   wide_cache_write  keys and values of new tokens into a paged 4-bit cache; wide_cache_read: back
+ *   wide_attn_cache   head-group-masked causal attention of a batch of sequences over that cache
  *
  * General rules
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library never
@@ -41,7 +45,7 @@
 extern "C" {
 #endif
 
-#define WIDE_VERSION 112
+#define WIDE_VERSION 113
 
 #if defined(__GNUC__)
 #define WIDE_API __attribute__((visibility("default")))
@@ -57,6 +61,7 @@ extern "C" {
 #define WIDE_ERR_WORKSPACE (-4)
 #define WIDE_ERR_CUDA (-5)
 #define WIDE_ERR_TIMEOUT (-6)
+#define WIDE_ERR_BAD_INDEX (-7) /* only from wide_status: a page table, length or row start held a value out of range */
 
 /* element types of activations / weights / outputs */
 #define WIDE_BF16 0
@@ -108,8 +113,9 @@ typedef struct wide_ctx wide_ctx;
 WIDE_API int wide_create(wide_ctx** ctx, int device);
 WIDE_API int wide_destroy(wide_ctx* ctx);
 
-/* Synchronise `stream`, read the device status word into *status (WIDE_OK or
- * WIDE_ERR_TIMEOUT) and clear it; after a timeout the context's internal buffers are reset.
+/* Synchronise `stream`, read the device status word into *status (WIDE_OK, WIDE_ERR_TIMEOUT, or
+ * WIDE_ERR_BAD_INDEX from the calls on a cache, see wide_seqs) and clear it; after a timeout the
+ * context's internal buffers are reset.  WIDE_ERR_BAD_INDEX holds nothing up: later calls run as usual.
  * The only call that blocks the host.
  * After a device-side wait has expired the context's counters and accumulators are in an
  * undefined state: until wide_status has been called, every decode-path call on the context
@@ -411,6 +417,131 @@ WIDE_API int wide_attn(wide_ctx* ctx, void* stream, const void* q, const void* k
 WIDE_API int wide_qproj(wide_ctx* ctx, void* stream, const void* x, const void* w, int dtype, int tokens,
                int hidden, int n_out, int group, const int32_t* perm, const int32_t* counts, void* y,
                unsigned flags);
+
+/* flags for wide_rope */
+#define WIDE_FLAG_ROPE_INTERLEAVED 256u /* pair i = channels (2i, 2i + 1); default (i, i + rot_dim / 2) */
+#define WIDE_FLAG_ROPE_INVERSE 512u     /* rotate back: the transpose, so also the gradient with respect to the input */
+
+/*
+ * wide_rope -- rotary positions of the query and key heads of a token, in one launch.
+ * Channel pair i < rot_dim / 2 of every head turns by  a = positions[axis[i], t] * inv_freq[i]:
+ *     (u, w) -> (u cos a - w sin a, u sin a + w cos a)
+ * channels rot_dim .. head_dim - 1 are copied.  With one axis these are ordinary rotary positions; with
+ * several (time, height, width of image and video tokens) every pair follows the axis the table names.
+ *   q [tokens, n_q_heads * head_dim], k [tokens, n_kv_heads * head_dim] (k and k_out may be NULL
+ *       with n_kv_heads 0): dtype bf16 or fp32; rows q_stride / k_stride elements apart (a slice of a
+ *       fused projection), outputs o_q_stride / o_k_stride apart
+ *   positions int32 [n_axes, tokens], any value; inv_freq fp64 [rot_dim / 2], finite; axis int32
+ *       [rot_dim / 2] with values in [0, n_axes), or NULL (all 0).  An axis out of range leaves its pair
+ *       unturned and sets WIDE_ERR_BAD_INDEX.
+ *   q_out may be q and k_out may be k (with equal strides); other overlaps are not allowed.
+ * The angle is reduced exactly (64-bit fixed point, in turns), so far positions lose nothing; the
+ * rotation is fp32, rounded once.
+ * Needs head_dim in {64, 128}, rot_dim % 16 == 0, rot_dim <= head_dim, n_axes <= 8, and every pointer
+ * to q, k and every row of them 16-byte aligned.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA.
+ */
+WIDE_API int wide_rope(wide_ctx* ctx, void* stream, const void* q, const void* k, int dtype, int tokens, int n_q_heads,
+                       int n_kv_heads, int head_dim, int rot_dim, long long q_stride, long long k_stride,
+                       const int32_t* positions, int n_axes, const double* inv_freq, const int32_t* axis, void* q_out,
+                       void* k_out, long long o_q_stride, long long o_k_stride, unsigned flags);
+
+/*
+ * The 4-bit key/value cache.
+ *
+ * Pages of page_size tokens hold keys and values of all KV heads of a layer.  A sub-group of quant_group
+ * neighbouring channels x of a token and head is held as 16 levels  m + s * n,  n = 0..15:
+ *     m = the largest bf16 number <= min x (+0 for 0),     s = the smallest bf16 number >= (max x - m) / 15,
+ *     n = how many of the borders m + (i + 1/2) s, i = 0..14, x reaches   (all n are 0 where s = 0)
+ * so |x - (m + s n)| <= s / 2.  A sub-group that holds an infinity or a NaN reads back as NaN.
+ *
+ * Layout: bytes [n_pages][n_kv_heads][page_size / 16][block], block = 16 * head_dim + 128 * n_sub bytes,
+ * n_sub = head_dim / quant_group.  A block holds 16 tokens of one head: 8 * head_dim bytes of key codes, as many
+ * of value codes, then the parameter words uint32 [16][n_sub] of the keys and of the values (low half
+ * the bits of s, high half those of m).  Token r of a block and channel d have their code at
+ *     keys:    byte ((((d/64 * 8 + r%8) * 4 + d/8%4) * 2 + d/32%2) * 2 + d/4%2) * 4 + d%2 * 2 + r/8
+ *              low nibble where d/2%2 is 0
+ *     values:  byte ((((d/64 * 8 + d/4%8) * 4 + r/2%4) * 2 + d/32%2) * 2 + d/2%2) * 4 + r%2 * 2 + r/8
+ *              low nibble where d%2 is 0
+ * which is the order in which the lanes of a warp hold the operands of the tensor-core instructions
+ * of wide_attn_cache, and gives every token whole bytes of its own.
+ */
+typedef struct wide_cache {
+    void* pages;      /* device, n_pages * wide_cache_page_bytes(...) bytes, 16-byte aligned; needs no initial value */
+    int n_pages;
+    int page_size;    /* tokens of a page: 16, 32, 64, 128 or 256 */
+    int n_kv_heads;   /* <= 256 */
+    int head_dim;     /* 64 or 128 */
+    int quant_group;  /* 32, 64 or 128, <= head_dim */
+} wide_cache;
+
+/*
+ * The sequences of a call and their places in the cache.  Position p of sequence s lies at token
+ * p % page_size of page page_table[s, p / page_size].  kv_lens[s] counts the positions of a sequence
+ * INCLUDING the new ones of this call.  The new tokens are rows [row_start[s], row_start[s + 1]) of the
+ * call's [rows, ...] matrices, at the sequence's last positions; row_start NULL: one row a sequence (row s).
+ * Rows that belong to no sequence are neither read nor written.
+ *
+ * All three arrays are on the device and are checked there.  A sequence whose length is outside
+ * [0, max_pages * page_size], or that has more new rows than positions, or whose rows are not a range
+ * within [0, rows], is left out (wide_attn_cache: its rows, if they are a range, become zero).  A page number outside
+ * [0, n_pages) holds no tokens: writes to it are dropped, reads from it give zeros, attention does
+ * not see its keys.  Each of these sets WIDE_ERR_BAD_INDEX in the context's status (wide_status).
+ * Pages may be shared by sequences that read them.  No position may be written twice in one call
+ * (two sequences with new tokens on one shared page, or overlapping row ranges): what it then holds is not defined.
+ */
+typedef struct wide_seqs {
+    const int32_t* page_table; /* [n_seqs, max_pages] */
+    const int32_t* kv_lens;    /* [n_seqs] */
+    const int32_t* row_start;  /* [n_seqs + 1] or NULL */
+    int n_seqs;                /* <= WIDE_MAX_SEQS */
+    int max_pages;
+} wide_seqs;
+
+#define WIDE_MAX_SEQS 4096
+
+/* Bytes of one page (0 where the shape is not supported). */
+WIDE_API size_t wide_cache_page_bytes(int page_size, int n_kv_heads, int head_dim, int quant_group);
+
+/*
+ * wide_cache_write -- quantise the keys and values of the new tokens and store them.
+ *   k, v [rows, n_kv_heads * head_dim] bf16 or fp32, rows k_stride / v_stride elements apart
+ * wide_cache_read -- the same rows out of the cache, m + s n in fp32 (one rounding), then rounded to the output type; with
+ * row_start = the running sum of kv_lens that is the whole cache of the sequences, as wide_attn reads it.
+ *   k_out, v_out as k, v
+ * Rows and pointers 16-byte aligned.  One launch, no workspace.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA; WIDE_ERR_BAD_INDEX through wide_status.
+ */
+WIDE_API int wide_cache_write(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* k,
+                              const void* v, int dtype, int rows, long long k_stride, long long v_stride);
+WIDE_API int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, void* k_out,
+                             void* v_out, int dtype, int rows, long long k_stride, long long v_stride);
+
+/*
+ * wide_attn_cache -- Eq. 1 under the head-group mask over the 4-bit cache, a batch of sequences in one call.
+ * For the new tokens of every sequence (their keys already written), with the keys and values that
+ * the cache holds:  row i of a sequence with n new rows and length L sees the positions
+ * j <= L - n + i (causal != 0) or all L of them:
+ *     o[i, h, :] = sum_j softmax_j(scale * q[i, h, :] . k[j, h_kv, :]) v[j, h_kv, :],   h_kv = h / (n_q_heads / n_kv_heads)
+ * Pairs (row, h) whose routing group h / heads_per_group is off in mask_bits, and rows that see no key,
+ * give exact zeros; the cache of a KV head that no new row of a sequence uses is not read (sequences of up to 16 new rows).
+ *   q   [rows, n_q_heads * head_dim] bf16, rows q_stride elements apart;  o [rows, n_q_heads * head_dim] bf16, contiguous
+ *   mask_bits [rows, W], n_groups = n_q_heads / heads_per_group <= WIDE_MAX_GROUPS; NULL: all groups on
+ *   scale: multiplies the logits (<= 0 selects 1/sqrt(head_dim))
+ *   workspace: wide_attn_cache_workspace_bytes(...) bytes; needs no initial value and keeps nothing,
+ *       but two calls that can overlap on the GPU need one each
+ * Built for few new rows a sequence (decoding, verifying drafted tokens): up to 16 query rows share one pass
+ * over a KV head, more take several passes.  A long prefill reads the cache back
+ * (wide_cache_read) and runs wide_attn.
+ * Results do not depend on the other sequences of the batch beyond fp32 rounding, and are the same bit for bit in every run.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA; WIDE_ERR_BAD_INDEX and WIDE_ERR_TIMEOUT
+ * through wide_status.
+ */
+WIDE_API size_t wide_attn_cache_workspace_bytes(int rows, int n_q_heads, int n_kv_heads, int head_dim);
+WIDE_API int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* q,
+                             int dtype, int rows, long long q_stride, int n_q_heads, int heads_per_group,
+                             const uint32_t* mask_bits, int causal, float scale, void* o, void* workspace,
+                             size_t workspace_bytes, unsigned flags);
 
 /*
  * wide_unpermute -- scatter epilogue of Algorithm 2 as its own call: packed-sorted rows back to

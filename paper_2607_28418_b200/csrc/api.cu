@@ -36,6 +36,49 @@ size_t acc_scratch(int tokens, int hidden) {
     return wide_align_up(static_cast<size_t>(tokens) * hidden * sizeof(float), 256);
 }
 
+// ---- checks of the calls on a cache
+bool cache_shape_ok(int page_size, int n_kv_heads, int head_dim, int quant_group) {
+    return is_pow2(page_size) && page_size >= 16 && page_size <= 256 && n_kv_heads > 0 && n_kv_heads <= 256 &&
+           (head_dim == 64 || head_dim == 128) && (quant_group == 32 || quant_group == 64 || quant_group == 128) &&
+           quant_group <= head_dim;
+}
+
+// rows of `width` elements, `stride` apart, that 16-byte accesses can walk
+int check_rows(const void* p, long long stride, long long width, int elem) {
+    if (stride < width) return WIDE_ERR_INVALID_ARG;
+    if (!wide_aligned16(p) || (stride * elem) % 16 != 0) return WIDE_ERR_ALIGNMENT;
+    return WIDE_OK;
+}
+
+bool on_device(const wide_ctx* ctx) {
+    int current = -1;
+    return cudaGetDevice(&current) == cudaSuccess && current == ctx->device;
+}
+
+int check_cache(const wide_ctx* ctx, const wide_cache* c, const wide_seqs* q, int rows) {
+    if (!ctx || !c || !q || rows < 0) return WIDE_ERR_INVALID_ARG;
+    if (!c->pages || c->n_pages <= 0 || !q->page_table || !q->kv_lens || q->n_seqs < 0 || q->max_pages <= 0)
+        return WIDE_ERR_INVALID_ARG;
+    if (!q->row_start && rows < q->n_seqs) return WIDE_ERR_INVALID_ARG;
+    if (!cache_shape_ok(c->page_size, c->n_kv_heads, c->head_dim, c->quant_group) || q->n_seqs > WIDE_MAX_SEQS ||
+        rows > (1 << 27))
+        return WIDE_ERR_UNSUPPORTED_SHAPE;
+    return wide_aligned16(c->pages) ? WIDE_OK : WIDE_ERR_ALIGNMENT;
+}
+
+int cache_move(wide_ctx* ctx, void* stream, bool write, const wide_cache* cache, const wide_seqs* seqs, void* k, void* v,
+               int dtype, int rows, long long ks, long long vs) {
+    if (!k || !v || !valid_dtype(dtype)) return WIDE_ERR_INVALID_ARG;
+    int rc = check_cache(ctx, cache, seqs, rows);
+    if (rc != WIDE_OK) return rc;
+    const long long width = static_cast<long long>(cache->n_kv_heads) * cache->head_dim;
+    if ((rc = check_rows(k, ks, width, wide_elem_bytes(dtype))) != WIDE_OK) return rc;
+    if ((rc = check_rows(v, vs, width, wide_elem_bytes(dtype))) != WIDE_OK) return rc;
+    if (!on_device(ctx)) return WIDE_ERR_INVALID_ARG;
+    if (rows == 0 || seqs->n_seqs == 0) return WIDE_OK;
+    return wide_launch_cache_move(ctx, static_cast<cudaStream_t>(stream), write, cache, seqs, k, v, dtype, rows, ks, vs);
+}
+
 }  // namespace
 
 extern "C" {
@@ -50,6 +93,7 @@ const char* wide_strerror(int code) {
         case WIDE_ERR_ALIGNMENT: return "pointer not 16-byte aligned";
         case WIDE_ERR_WORKSPACE: return "workspace missing or too small";
         case WIDE_ERR_CUDA: return "CUDA runtime or driver error";
+        case WIDE_ERR_BAD_INDEX: return "a page table, length, row start or axis held a value out of range";
         case WIDE_ERR_TIMEOUT: return "a bounded device-side wait expired";
         default: return "unknown error code";
     }
@@ -182,9 +226,11 @@ int wide_destroy(wide_ctx* ctx) {
 int wide_status(wide_ctx* ctx, void* stream, int* status) {
     if (!ctx || !status) return WIDE_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    int v = 0;
+    int v = 0, index = 0;
     WIDE_CUDA_CHECK(cudaMemcpyAsync(&v, ctx->d_status, sizeof(int), cudaMemcpyDeviceToHost, s));
+    WIDE_CUDA_CHECK(cudaMemcpyAsync(&index, ctx->d_status + WIDE_STATUS_INDEX, sizeof(int), cudaMemcpyDeviceToHost, s));
     WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_status, 0, sizeof(int), s));
+    WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_status + WIDE_STATUS_INDEX, 0, sizeof(int), s));
     WIDE_CUDA_CHECK(cudaStreamSynchronize(s));
     if (v != WIDE_OK) {
         // a kernel gave up half-way: restore the invariants later calls rely on
@@ -193,7 +239,7 @@ int wide_status(wide_ctx* ctx, void* stream, int* status) {
         WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_tickets, 0, 2048 * sizeof(unsigned), s));
         WIDE_CUDA_CHECK(cudaStreamSynchronize(s));
     }
-    *status = v;
+    *status = v != WIDE_OK ? v : index;
     return WIDE_OK;
 }
 
@@ -439,6 +485,71 @@ int wide_qproj(wide_ctx* ctx, void* stream, const void* x, const void* w, int dt
     if (!wide_aligned16(x) || !wide_aligned16(w) || !wide_aligned16(y)) return WIDE_ERR_ALIGNMENT;
     return wide_launch_linear_mn_tc(ctx, static_cast<cudaStream_t>(stream), x, w, tokens, hidden, n_out, group, perm,
                                     counts, y);
+}
+
+int wide_rope(wide_ctx* ctx, void* stream, const void* q, const void* k, int dtype, int tokens, int n_q_heads, int n_kv_heads,
+              int head_dim, int rot_dim, long long q_stride, long long k_stride, const int32_t* positions, int n_axes,
+              const double* inv_freq, const int32_t* axis, void* q_out, void* k_out, long long o_q_stride,
+              long long o_k_stride, unsigned flags) {
+    if (!ctx || !q || !q_out || !positions || !inv_freq || !valid_dtype(dtype)) return WIDE_ERR_INVALID_ARG;
+    if (tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0 || head_dim <= 0 || rot_dim <= 0 || n_axes <= 0) return WIDE_ERR_INVALID_ARG;
+    if ((n_kv_heads > 0) != (k != nullptr) || (k != nullptr) != (k_out != nullptr)) return WIDE_ERR_INVALID_ARG;
+    if ((head_dim != 64 && head_dim != 128) || rot_dim % 16 != 0 || rot_dim > head_dim || n_axes > 8 || n_q_heads > 4096 ||
+        n_kv_heads > 4096 || tokens > (1 << 27))
+        return WIDE_ERR_UNSUPPORTED_SHAPE;
+    if ((q == q_out && q_stride != o_q_stride) || (k && k == k_out && k_stride != o_k_stride)) return WIDE_ERR_INVALID_ARG;
+    const int elem = wide_elem_bytes(dtype);
+    int rc;
+    if ((rc = check_rows(q, q_stride, static_cast<long long>(n_q_heads) * head_dim, elem)) != WIDE_OK) return rc;
+    if ((rc = check_rows(q_out, o_q_stride, static_cast<long long>(n_q_heads) * head_dim, elem)) != WIDE_OK) return rc;
+    if (k) {
+        if ((rc = check_rows(k, k_stride, static_cast<long long>(n_kv_heads) * head_dim, elem)) != WIDE_OK) return rc;
+        if ((rc = check_rows(k_out, o_k_stride, static_cast<long long>(n_kv_heads) * head_dim, elem)) != WIDE_OK) return rc;
+    }
+    if (!on_device(ctx)) return WIDE_ERR_INVALID_ARG;
+    if (tokens == 0) return WIDE_OK;
+    return wide_launch_rope(ctx, static_cast<cudaStream_t>(stream), q, k, dtype, tokens, n_q_heads, n_kv_heads, head_dim, rot_dim,
+                            q_stride, k_stride, positions, n_axes, inv_freq, axis, q_out, k_out, o_q_stride, o_k_stride, flags);
+}
+
+size_t wide_cache_page_bytes(int page_size, int n_kv_heads, int head_dim, int quant_group) {
+    if (!cache_shape_ok(page_size, n_kv_heads, head_dim, quant_group)) return 0;
+    return static_cast<size_t>(n_kv_heads) * (page_size / 16) * (16 * head_dim + 128 * (head_dim / quant_group));
+}
+
+int wide_cache_write(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* k, const void* v,
+                     int dtype, int rows, long long k_stride, long long v_stride) {
+    return cache_move(ctx, stream, true, cache, seqs, const_cast<void*>(k), const_cast<void*>(v), dtype, rows, k_stride, v_stride);
+}
+
+int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, void* k_out, void* v_out,
+                    int dtype, int rows, long long k_stride, long long v_stride) {
+    return cache_move(ctx, stream, false, cache, seqs, k_out, v_out, dtype, rows, k_stride, v_stride);
+}
+
+size_t wide_attn_cache_workspace_bytes(int rows, int n_q_heads, int n_kv_heads, int head_dim) {
+    if (rows < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0) return 0;
+    return wide_attn_cache_workspace(rows, n_q_heads, n_kv_heads, head_dim);
+}
+
+int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* q, int dtype,
+                    int rows, long long q_stride, int n_q_heads, int heads_per_group, const uint32_t* mask_bits, int causal,
+                    float scale, void* o, void* workspace, size_t workspace_bytes, unsigned flags) {
+    if (!q || !o || !valid_dtype(dtype) || n_q_heads <= 0 || heads_per_group <= 0 || n_q_heads % heads_per_group != 0 || flags != 0)
+        return WIDE_ERR_INVALID_ARG;
+    int rc = check_cache(ctx, cache, seqs, rows);
+    if (rc != WIDE_OK) return rc;
+    if (n_q_heads % cache->n_kv_heads != 0) return WIDE_ERR_INVALID_ARG;
+    if (dtype != WIDE_BF16 || n_q_heads / heads_per_group > WIDE_MAX_GROUPS || n_q_heads > 4096) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    if ((rc = check_rows(q, q_stride, static_cast<long long>(n_q_heads) * cache->head_dim, 2)) != WIDE_OK) return rc;
+    if (!wide_aligned16(o) || !wide_aligned16(workspace)) return WIDE_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < wide_attn_cache_workspace(rows, n_q_heads, cache->n_kv_heads, cache->head_dim))
+        return WIDE_ERR_WORKSPACE;
+    if (!on_device(ctx)) return WIDE_ERR_INVALID_ARG;
+    if (rows == 0 || seqs->n_seqs == 0) return WIDE_OK;
+    if (!(scale > 0.f)) scale = 1.0f / sqrtf(static_cast<float>(cache->head_dim));
+    return wide_launch_attn_cache(ctx, static_cast<cudaStream_t>(stream), cache, seqs, q, rows, q_stride, n_q_heads,
+                                  heads_per_group, mask_bits, causal ? 1 : 0, scale, o, workspace);
 }
 
 int wide_unpermute(wide_ctx* ctx, void* stream, const void* src_packed, const int32_t* perm,

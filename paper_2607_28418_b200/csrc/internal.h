@@ -9,6 +9,8 @@
 
 #include "wide.h"
 
+#define WIDE_STATUS_INDEX 13   // word of d_status
+
 struct wide_prof_rec {
     const char* name;
     cudaEvent_t begin, end;
@@ -20,7 +22,8 @@ struct wide_ctx {
     int* d_status;          // [0] device status word (WIDE_OK or WIDE_ERR_TIMEOUT), [1] reorder ticket,
                             // [4..5] grid-barrier counters of the decode kernels, [6] channel pool of the GEMV decode kernel, [8..9] tile queue of the
                             // 256-row down projection, [10..12] work list of the attention prefill kernel (next item, CTAs done, next block of rows to zero;
-                            // zero between launches) (16 ints in all)
+                            // zero between launches), [13] WIDE_ERR_BAD_INDEX
+                            // once a call on a cache met an index out of range (16 ints in all)
     float* decode_acc;      // fp32 accumulators of the decode path; zero between calls
     size_t decode_acc_floats;
     unsigned* d_tickets;    // 2048 completion counters, zero between calls: [0, 1024) and [1024, 1152) the decode FFN /
@@ -214,3 +217,17 @@ bool wide_attn_decode_fits(int Tq, int Hq, int Hkv);
 int wide_launch_attn_decode(wide_ctx* ctx, cudaStream_t s, const void* q, const void* k, const void* v,
                             const uint32_t* mask_bits, int Tq, int Tk, int Hq, int Hkv, int head_dim, int hpg,
                             int causal, float scale, void* o, unsigned flags);
+
+// Rotary positions (csrc/rope.cu).
+int wide_launch_rope(wide_ctx* ctx, cudaStream_t s, const void* q, const void* k, int dtype, int tokens, int n_q, int n_kv,
+                     int head_dim, int rot, long long qs, long long ks, const int32_t* positions, int n_axes,
+                     const double* inv_freq, const int32_t* axis, void* q_out, void* k_out, long long oqs, long long oks,
+                     unsigned flags);
+
+// The 4-bit cache: rows in (write) or out (csrc/kv_cache.cu), attention over it (csrc/attn_cache.cu).
+int wide_launch_cache_move(wide_ctx* ctx, cudaStream_t s, bool write, const wide_cache* cache, const wide_seqs* seqs, void* k,
+                           void* v, int dtype, int rows, long long ks, long long vs);
+size_t wide_attn_cache_workspace(int rows, int n_q, int n_kv, int head_dim);
+int wide_launch_attn_cache(wide_ctx* ctx, cudaStream_t s, const wide_cache* cache, const wide_seqs* seqs, const void* q,
+                           int rows, long long qs, int n_q, int hpg, const uint32_t* mask_bits, int causal, float scale,
+                           void* o, void* ws);
