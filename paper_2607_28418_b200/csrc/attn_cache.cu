@@ -20,6 +20,8 @@
 //     CTA, then (at most two per CTA) by a second small kernel.  The order of joining is fixed.
 #include <math_constants.h>
 
+#include <type_traits>
+
 #include "cache.cuh"
 #include "ptx.cuh"
 
@@ -42,7 +44,7 @@ struct AttnArgs {
     __nv_bfloat16* o;
     int* status;                   // device status word (timeouts); index errors go to WIDE_STATUS_INDEX
     unsigned long long wait_ns;
-    int stages, plan_words;        // plan_words: words of a sequence's head mask
+    int plan_words;                // words of a sequence's head mask
     unsigned char* plan;           // the plan in the workspace, or NULL: every CTA makes its own in shared memory
     float* heads;                  // partial results of warps whose first item began before their piece
     float* parts;                  // [CTA][2] partial results of CTAs
@@ -61,6 +63,12 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// d = a * b
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     uint32_t d;
@@ -88,54 +96,65 @@ __device__ __forceinline__ void lds_words(uint32_t a, uint32_t (&w)[N]) {
     if (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[N > 1]), "=r"(w[N > 2 ? 2 : 0]), "=r"(w[N > 3 ? 3 : 0]) : "r"(a));
 }
 
+// Up to one 128-byte line a thread of the grid.
+__device__ __forceinline__ void prefetch_l2(const void* p, size_t bytes) {
+    const size_t at = (static_cast<size_t>(blockIdx.x) * blockDim.x + threadIdx.x) * 128;
+    if (p && at < bytes) asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const char*>(p) + at));
+}
+
 // ------------------------------------------------------------------------------------------------ the plan
 // offsets[s] = units (16-key blocks of items) of the sequences before s, masks[s] = KV heads in use.
 struct Plan {
     long long* offsets;
-    uint32_t* masks;
+    uint32_t *masks, *groups;
 };
-__device__ __forceinline__ Plan plan_at(unsigned char* p, int n_seqs) {
-    return Plan{reinterpret_cast<long long*>(p), reinterpret_cast<uint32_t*>(p + 8 * (n_seqs + 1))};
+__device__ __forceinline__ Plan plan_at(unsigned char* p, int n_seqs, int plan_words) {
+    uint32_t* m = reinterpret_cast<uint32_t*>(p + 8 * (n_seqs + 1));
+    return Plan{reinterpret_cast<long long*>(p), m, m + n_seqs * plan_words};
 }
-size_t plan_bytes(int n_seqs, int words) { return 8 * static_cast<size_t>(n_seqs + 1) + 4 * static_cast<size_t>(n_seqs) * words; }
+size_t plan_bytes(int n_seqs, int plan_words, int words) {
+    return 8 * static_cast<size_t>(n_seqs + 1) + 4 * static_cast<size_t>(n_seqs) * (plan_words + words);
+}
 
 __device__ __forceinline__ int row_blocks(int n_rows, int share, int rows_per) { return (n_rows * share + rows_per - 1) / rows_per; }
 
-// Does any new row of the sequence use KV head h?  Looked at for up to 16 new rows.
-__device__ __forceinline__ bool head_used(const AttnArgs& a, const SeqInfo& i, int h) {
-    if (!a.mask_bits || i.n_rows > 16) return true;
-    const int g0 = h * a.share / a.hpg, g1 = (h * a.share + a.share - 1) / a.hpg;
-    bool any = false;
-    for (int r = 0; r < i.n_rows; ++r)
-        for (int g = g0; g <= g1; ++g) any |= wide_mask_bit(a.mask_bits, a.words, i.row0 + r, g);
-    return any;
-}
-
+// Two rounds of loads (lengths, masks; one thread a sequence), then arithmetic.  Up to 16 new rows are looked at
+// for the KV heads in use; of more rows all heads are taken.
 template <int ROWS>
 __device__ void make_plan(const AttnArgs& a, const Plan& p, long long* part, bool report) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
-    // a warp per sequence: lanes are heads
-    for (int s = warp; s < a.q.n_seqs; s += n_warps) {
-        const SeqInfo i = wide_seq_info(a.q, s, a.c.page_shift);
-        if (i.bad && report && lane == 0) atomicExch(a.status + WIDE_STATUS_INDEX, WIDE_ERR_BAD_INDEX);
-        int used = 0;
-        const bool some = i.n_rows > 0 && i.len > 0;
-        for (int w = 0; w < a.plan_words; ++w) {
-            const int h = 32 * w + lane;
-            const uint32_t m = __ballot_sync(0xffffffffu, some && h < a.c.n_kv_heads && head_used(a, i, h));
-            used += __popc(m);
-            if (lane == 0) p.masks[s * a.plan_words + w] = m;
-        }
-        if (lane == 0)
-            p.offsets[s] = static_cast<long long>(used) * ((i.len + 15) >> 4) * (some ? row_blocks(i.n_rows, a.share, ROWS) : 0);
-    }
-    __syncthreads();
-    // exclusive sums
     const int per = (a.q.n_seqs + blockDim.x - 1) / blockDim.x;
     const int s0 = min(a.q.n_seqs, tid * per), s1 = min(a.q.n_seqs, s0 + per);
+    for (int s = s0; s < s1; ++s) {
+        const SeqInfo i = wide_seq_info(a.q, s, a.c.page_shift);
+        if (i.bad && report) atomicExch(a.status + WIDE_STATUS_INDEX, WIDE_ERR_BAD_INDEX);
+        const bool some = i.n_rows > 0 && i.len > 0;
+        const int looked = a.mask_bits && i.n_rows <= 16 ? i.n_rows : 0;
+        for (int w = 0; w < a.words; ++w) {      // groups that any new row uses
+            uint32_t m = some && looked == 0 ? 0xffffffffu : 0u;
+            if (some)
+                for (int r = 0; r < looked; ++r) m |= a.mask_bits[static_cast<size_t>(i.row0 + r) * a.words + w];
+            p.groups[s * a.words + w] = m;
+        }
+        p.offsets[s] = some ? static_cast<long long>((i.len + 15) >> 4) * row_blocks(i.n_rows, a.share, ROWS) : 0;   // of one head
+    }
+    __syncthreads();
+    for (int x = warp; x < a.q.n_seqs * a.plan_words; x += n_warps) {     // lanes are KV heads
+        const int s = x / a.plan_words, w = x - s * a.plan_words, h = 32 * w + lane;
+        bool any = false;
+        if (h < a.c.n_kv_heads) {
+            const int g1 = (h * a.share + a.share - 1) / a.hpg;
+            for (int g = h * a.share / a.hpg; g <= g1; ++g) any |= (p.groups[s * a.words + (g >> 5)] >> (g & 31)) & 1u;
+        }
+        const uint32_t m = __ballot_sync(0xffffffffu, any);
+        if (lane == 0) p.masks[x] = m;
+    }
+    __syncthreads();
     long long sum = 0;
     for (int s = s0; s < s1; ++s) {
-        const long long n = p.offsets[s];
+        int used = 0;
+        for (int w = 0; w < a.plan_words; ++w) used += __popc(p.masks[s * a.plan_words + w]);
+        const long long n = p.offsets[s] * used;
         p.offsets[s] = sum;
         sum += n;
     }
@@ -160,7 +179,7 @@ __device__ void make_plan(const AttnArgs& a, const Plan& p, long long* part, boo
 template <int ROWS>
 __global__ void __launch_bounds__(1024) attn_cache_plan_kernel(AttnArgs a) {
     __shared__ long long part[32];
-    make_plan<ROWS>(a, plan_at(a.plan, a.q.n_seqs), part, true);
+    make_plan<ROWS>(a, plan_at(a.plan, a.q.n_seqs, a.plan_words), part, true);
 }
 
 // A place on the line of units: block `blk` of an item.
@@ -196,11 +215,19 @@ __device__ Cursor locate(const AttnArgs& a, const Plan& p, long long u) {
     }
     k.seq = lo;
     enter_seq<ROWS>(a, k);
-    long long r = u - p.offsets[lo];
-    const long long item = r / k.n_blk;
-    k.blk = static_cast<int>(r - item * k.n_blk);
-    int nth = static_cast<int>(item / k.n_rb);
-    k.rb = static_cast<int>(item - static_cast<long long>(nth) * k.n_rb);
+    const long long r = u - p.offsets[lo];
+    int nth;
+    if (r <= 0x7fffffffLL) {
+        const int r32 = static_cast<int>(r), item = r32 / k.n_blk;
+        k.blk = r32 - item * k.n_blk;
+        nth = k.n_rb == 1 ? item : item / k.n_rb;
+        k.rb = item - nth * k.n_rb;
+    } else {
+        const long long item = r / k.n_blk;
+        k.blk = static_cast<int>(r - item * k.n_blk);
+        nth = static_cast<int>(item / k.n_rb);
+        k.rb = static_cast<int>(item - static_cast<long long>(nth) * k.n_rb);
+    }
     k.kvh = next_head(a, p, lo, 0);
     for (; nth > 0; --nth) k.kvh = next_head(a, p, lo, k.kvh + 1);
     return k;
@@ -238,21 +265,39 @@ __device__ __forceinline__ RowOut row_out(const AttnArgs& a, const SeqInfo& i, i
 
 __host__ __device__ constexpr int slot_floats(int rows, int D) { return rows * (D + 4); }   // rows of D values, then m and l of each
 
-// Joins `n` partial results of one item, the e-th at at(e): out rows, or a partial again (dst).
+// Joins `n` partial results of one item, the e-th at at(e): out rows, or a partial again (dst).  weights is
+// shared memory for (n + 1) * ROWS pairs; all `n_threads` threads of the CTA take part.
 template <int ROWS, int D, typename At>
-__device__ __forceinline__ void join(const AttnArgs& a, int seq, int kvh, int rb, int n, const At& at, float* dst, int tid, int n_threads) {
-    const SeqInfo info = wide_seq_info(a.q, seq, a.c.page_shift);
-    for (int i = tid; i < ROWS * (D / 4); i += n_threads) {
-        const int r = i / (D / 4), d = i % (D / 4) * 4;
-        float m = -CUDART_INF_F;
-        for (int e = 0; e < n; ++e) m = fmaxf(m, at(e)[ROWS * D + 2 * r]);
+__device__ __forceinline__ void join(const AttnArgs& a, int seq, int kvh, int rb, int n, const At& at, float* dst, float2* weights, int part,
+                                     int parts) {
+    const int tid = threadIdx.x, n_threads = blockDim.x;
+    for (int i = tid; i < n * ROWS; i += n_threads)
+        weights[i] = *reinterpret_cast<const float2*>(at(i / ROWS) + ROWS * D + 2 * (i % ROWS));
+    __syncthreads();
+    // row r: maximum, sum; each piece's weight
+    if (tid < ROWS) {
+        float m = -CUDART_INF_F, l = 0.f;
+        for (int e = 0; e < n; ++e) m = fmaxf(m, weights[e * ROWS + tid].x);
         const float m_use = m == -CUDART_INF_F ? 0.f : m;
-        float l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
         for (int e = 0; e < n; ++e) {
-            const float* p = at(e);
-            const float w = exp2_fast(p[ROWS * D + 2 * r] - m_use);
-            const float4 v = *reinterpret_cast<const float4*>(p + r * D + d);
-            l = fmaf(p[ROWS * D + 2 * r + 1], w, l);
+            const float2 v = weights[e * ROWS + tid];
+            const float w = exp2_fast(v.x - m_use);
+            weights[e * ROWS + tid].x = w;
+            l = fmaf(v.y, w, l);
+        }
+        weights[n * ROWS + tid].x = l;
+        if (dst) *reinterpret_cast<float2*>(dst + ROWS * D + 2 * tid) = make_float2(m, l);
+    }
+    __syncthreads();
+    const SeqInfo info = wide_seq_info(a.q, seq, a.c.page_shift);
+    for (int i = tid + part * n_threads; i < ROWS * (D / 4); i += n_threads * parts) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int e = 0; e < n; ++e) {
+            const float w = weights[e * ROWS + r].x;
+            const float4 v = *reinterpret_cast<const float4*>(at(e) + r * D + d);
             x[0] = fmaf(v.x, w, x[0]);
             x[1] = fmaf(v.y, w, x[1]);
             x[2] = fmaf(v.z, w, x[2]);
@@ -260,16 +305,13 @@ __device__ __forceinline__ void join(const AttnArgs& a, int seq, int kvh, int rb
         }
         if (dst) {
             *reinterpret_cast<float4*>(dst + r * D + d) = make_float4(x[0], x[1], x[2], x[3]);
-            if (d == 0) {
-                dst[ROWS * D + 2 * r] = m;
-                dst[ROWS * D + 2 * r + 1] = l;
-            }
         } else {
             const RowOut ro = row_out(a, info, kvh, rb * ROWS + r, D);
             if (!ro.o) continue;
-            const float inv = ro.on && l != 0.f ? 1.f / l : 0.f;
+            const float sum = weights[n * ROWS + r].x;
             uint2 w = make_uint2(0, 0);
-            if (inv != 0.f) {
+            if (ro.on && sum != 0.f) {
+                const float inv = 1.f / sum;
                 const __nv_bfloat162 b0 = __floats2bfloat162_rn(x[0] * inv, x[1] * inv), b1 = __floats2bfloat162_rn(x[2] * inv, x[3] * inv);
                 w = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
             }
@@ -279,34 +321,121 @@ __device__ __forceinline__ void join(const AttnArgs& a, int seq, int kvh, int rb
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
-template <int D, int G, int NB, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_constant__ AttnArgs a) {
+template <int D, int G, int NB, int WARPS, int STAGES>
+__global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int kRows = 8 * NB;
     constexpr int kNS = D / G;
     constexpr int kSteps = D / 16;              // k16 steps of a key, m16 tiles of a value
     constexpr int kSB = 16 * D + 128 * kNS;     // bytes of a block
     constexpr int kStage = kBlk * kSB;
+    constexpr uint32_t kFull = (1u << kBlk) - 1u;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ uint64_t bars[WARPS * 8];
-    __shared__ long long part[WARPS];
+    __shared__ uint64_t bars[WARPS][2][8];      // per warp and stage: [0] data has arrived, [1] data has been read
+    __shared__ uint32_t here_of[WARPS][8];      // which blocks of the stage have a page
+    __shared__ long long part[WARPS + 1];
     __shared__ int s_abort;
     // per warp two partial results: [0] of an item that began before the piece (in global memory), [1] of the
     // piece's last item (over the ring).  state: 0 none, else 1 | begins here << 1 | ends here << 2
+    __shared__ const float* e_at[WARPS];        // the pieces of one item, at most one of a warp
+    __shared__ float2 weights[(WARPS + 1) * kRows];
     __shared__ int e_state[WARPS][2], e_seq[WARPS][2], e_kvh[WARPS][2], e_rb[WARPS][2];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    unsigned char* ring = smem + kPlanSmem + static_cast<size_t>(warp) * a.stages * kStage;
-    const uint32_t ring_a = smem_u32(ring), bar_a = smem_u32(&bars[warp * 8]);
-    if (lane < a.stages) mbar_init(bar_a + 8 * lane, 1);
+    if (tid < WARPS * STAGES) {
+        mbar_init(smem_u32(&bars[tid / STAGES][0][tid % STAGES]), 1);
+        mbar_init(smem_u32(&bars[tid / STAGES][1][tid % STAGES]), 1);
+    }
     if (tid < 2 * WARPS) e_state[tid >> 1][tid & 1] = 0;
     if (tid == 0) s_abort = 0;
     fence_barrier_init();
-    const Plan plan = plan_at(a.plan ? a.plan : smem, a.q.n_seqs);
+    // All CTAs together bring what the plan will lead to (masks, page table, queries) into L2 while it is made.
+    prefetch_l2(a.mask_bits, static_cast<size_t>(a.q.rows) * a.words * 4);
+    prefetch_l2(a.q.page_table, static_cast<size_t>(a.q.n_seqs) * a.q.max_pages * 4);
+    prefetch_l2(a.qm, (static_cast<size_t>(a.q.rows - 1) * a.qs + a.n_q * D) * 2);
+    const Plan plan = plan_at(a.plan ? a.plan : smem, a.q.n_seqs, a.plan_words);
     __syncthreads();
     if (!a.plan) make_plan<kRows>(a, plan, part, blockIdx.x == 0);
 
+    // the line of units, cut for the CTAs that are worth using (16 units each at least) and their warps
+    const long long total = plan.offsets[a.q.n_seqs];
+    const int ctas = static_cast<int>(min(static_cast<long long>(gridDim.x), (total + 15) / 16)), cta = blockIdx.x;
+    const int who = warp < WARPS ? warp : min(lane, WARPS - 1);    // a lane of the last warp feeds one of the others
+    long long u0 = 0, u1 = 0;
+    if (cta < ctas) {
+        const long long share = total <= 0x7fffffffLL ? static_cast<int>(total) / ctas : total / ctas;
+        const int more = static_cast<int>(total - share * ctas);
+        const long long c0 = share * cta + min(cta, more);
+        const int n = static_cast<int>(share + (cta < more ? 1 : 0));
+        const int each = n / WARPS, extra = n - each * WARPS;
+        u0 = c0 + each * who + min(who, extra);
+        u1 = u0 + each + (who < extra ? 1 : 0);
+    }
+    if (warp == WARPS) {
+        // ---- the feeding warp: lane w keeps the ring of warp w full
+        int left = lane < WARPS ? static_cast<int>(u1 - u0) : 0, issued = 0;
+        const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
+        const uint32_t bar0 = smem_u32(&bars[who][0][0]), ring_a = smem_u32(smem + kPlanSmem) + who * (STAGES * kStage);
+        Cursor ic{};
+        if (left > 0) ic = locate<kRows>(a, plan, u0);
+        int slot = 0;
+        uint32_t parity = 1;           // of the slot's previous reading
+        uint64_t since = globaltimer_ns();
+        while (__any_sync(0xffffffffu, left > 0)) {
+            const bool free_slot = left > 0 && (issued < STAGES || mbar_try_wait(bar0 + 64 + 8 * slot, parity));
+            if (!__any_sync(0xffffffffu, free_slot)) {
+                if (*reinterpret_cast<volatile int*>(&s_abort)) break;
+                if (globaltimer_ns() - since > a.wait_ns) s_abort = 1;
+                continue;
+            }
+            since = globaltimer_ns();
+            if (free_slot) {
+                const int nb = min(min(kBlk, ic.n_blk - ic.blk), left);
+                if (nb <= 0) {         // only if a length changes under the running kernel
+                    left = 0;
+                } else {
+                    const int32_t* table = a.q.page_table + static_cast<size_t>(ic.seq) * a.q.max_pages;
+                    int page[kBlk];
+#pragma unroll
+                    for (int b = 0; b < kBlk; ++b) page[b] = b < nb ? table[(ic.blk + b) >> sub_shift] : -1;
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int b = 0; b < kBlk; ++b) m |= static_cast<unsigned>(page[b]) < static_cast<unsigned>(a.c.n_pages) ? 1u << b : 0u;
+                    if (m != (1u << nb) - 1u) atomicExch(a.status + WIDE_STATUS_INDEX, WIDE_ERR_BAD_INDEX);
+                    here_of[lane][slot] = m;
+                    const uint32_t bar = bar0 + 8 * slot;
+                    mbar_arrive_expect_tx(bar, __popc(m) * kSB);
+                    auto from = [&](int b) {
+                        return a.c.pages + (((static_cast<size_t>(page[b]) * a.c.n_kv_heads + ic.kvh) << sub_shift) + ((ic.blk + b) & sub_mask)) * kSB;
+                    };
+                    const uint32_t to = ring_a + slot * kStage;
+                    if (m == kFull && page[0] == page[1]) {      // neighbours within a page
+                        bulk_load(to, from(0), kStage, bar);
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < kBlk; ++b)
+                            if ((m >> b) & 1u) bulk_load(to + b * kSB, from(b), kSB, bar);
+                    }
+                    if (++slot == STAGES) {
+                        slot = 0;
+                        parity ^= 1u;
+                    }
+                    ++issued;
+                    ic.blk += nb;
+                    left -= nb;
+                    if (ic.blk == ic.n_blk && left > 0) next_item<kRows>(a, plan, ic);
+                }
+            }
+            __syncwarp();
+        }
+        if (*reinterpret_cast<volatile int*>(&s_abort)) {
+            // copies may still be on their way into this CTA's shared memory
+            volatile int never = 0;
+            for (int i = max(0, issued - STAGES); i < issued; ++i) mbar_wait(bar0 + 8 * (i % STAGES), (i / STAGES) & 1, a.wait_ns, &never);
+        }
+    }
+
     // rows that no item writes: KV heads that a sequence does not use, sequences that are left out
-    for (int s = blockIdx.x; s < a.q.n_seqs; s += gridDim.x) {
+    for (int s = blockIdx.x; s < a.q.n_seqs && warp < WARPS; s += gridDim.x) {
         const SeqInfo i = wide_seq_info(a.q, s, a.c.page_shift);
         const int per_row = a.n_q * (D / 8);
         for (long long x = tid; x < static_cast<long long>(i.n_rows) * per_row; x += 32 * WARPS) {
@@ -316,102 +445,58 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
         }
     }
 
-    // the line of units, cut for the CTAs that are worth using (16 units each at least) and their warps
-    const long long total = plan.offsets[a.q.n_seqs];
-    const long long ctas = min(static_cast<long long>(gridDim.x), (total + 15) / 16);
-    const bool idle = blockIdx.x >= ctas;
-    const long long c0 = idle ? 0 : total * blockIdx.x / ctas, c1 = idle ? 0 : total * (blockIdx.x + 1) / ctas;
-    const long long u0 = c0 + (c1 - c0) * warp / WARPS, u1 = c0 + (c1 - c0) * (warp + 1) / WARPS;
+    if (warp < WARPS && u0 < u1) {
+        Cursor cc = locate<kRows>(a, plan, u0);
+        int to_use = static_cast<int>(u1 - u0), slot = 0;
+        uint32_t parity = 0;
+        bool ok = true;
+        const uint32_t bar0 = smem_u32(&bars[warp][0][0]), ring_a = smem_u32(smem + kPlanSmem) + warp * (STAGES * kStage);
+        const uint32_t lane16 = lane * 16, params = 16 * D + 4 * kNS * g;
 
-    bool ok = true;
-    if (u0 < u1) {
-        Cursor ic = locate<kRows>(a, plan, u0), cc = ic;
-        long long to_issue = u1 - u0, to_use = u1 - u0;
-        int issued = 0, used = 0;      // stages
-        uint32_t live = 0;             // kBlk bits a stage, newest lowest: which of its blocks have a page
-        int pt_seq = -1, pt_first = 0, pt = 0;   // page numbers [pt_first, pt_first + 32) of sequence pt_seq, one a lane
-
-        auto issue = [&]() {
-            const int nb = static_cast<int>(min(static_cast<long long>(min(kBlk, ic.n_blk - ic.blk)), to_issue));
-            if (nb <= 0) {      // only if a length changes under the running kernel
-                to_issue = 0;
-                return;
-            }
-            const int first = (ic.blk << 4) >> a.c.page_shift, last = ((ic.blk + nb - 1) << 4) >> a.c.page_shift;
-            if (pt_seq != ic.seq || first < pt_first || last >= pt_first + 32) {
-                pt_seq = ic.seq;
-                pt_first = first;
-                pt = first + lane < a.q.max_pages ? a.q.page_table[static_cast<size_t>(ic.seq) * a.q.max_pages + first + lane] : -1;
-            }
-            const int blk = ic.blk + min(lane, nb - 1);
-            const int page = __shfl_sync(0xffffffffu, pt, ((blk << 4) >> a.c.page_shift) - pt_first);
-            const bool good = static_cast<unsigned>(page) < static_cast<unsigned>(a.c.n_pages) && lane < nb;
-            const uint32_t m = __ballot_sync(0xffffffffu, good);
-            if (m != (1u << nb) - 1u && lane == 0) atomicExch(a.status + WIDE_STATUS_INDEX, WIDE_ERR_BAD_INDEX);
-            live = (live << kBlk) | m;
-            const int slot = issued % a.stages;
-            const uint32_t bar = bar_a + 8 * slot;
-            if (lane == 0) mbar_arrive_expect_tx(bar, __popc(m) * kSB);
-            __syncwarp();
-            if (good) {
-                const int sub = blk & ((1 << (a.c.page_shift - 4)) - 1);
-                const size_t at = (((static_cast<size_t>(page) * a.c.n_kv_heads + ic.kvh) << (a.c.page_shift - 4)) + sub) * kSB;
-                bulk_load(ring_a + slot * kStage + lane * kSB, a.c.pages + at, kSB, bar);
-            }
-            ++issued;
-            ic.blk += nb;
-            to_issue -= nb;
-            if (ic.blk == ic.n_blk && to_issue > 0) next_item<kRows>(a, plan, ic);
-        };
-        for (int s = 0; s < a.stages && to_issue > 0; ++s) issue();
-
-        while (to_use > 0 && ok) {
+        while (true) {
             // ---- an item, or the part of it that lies in this piece
             const SeqInfo info = wide_seq_info(a.q, cc.seq, a.c.page_shift);
             const int first_blk = cc.blk;
-            const int end_blk = static_cast<int>(min(static_cast<long long>(cc.n_blk), cc.blk + to_use));
+            const int end_blk = min(cc.n_blk, cc.blk + to_use);
             if (end_blk <= first_blk) break;
             uint32_t qf[NB][kSteps][2];
             float qsum[NB][kNS][2], qscale[NB][2];   // of this lane's score columns 2t, 2t + 1
-            int last_key[NB][2];
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 const int rr = cc.rb * kRows + 8 * n + g, tok = rr / a.share, h = cc.kvh * a.share + rr - tok * a.share;
-                uint4 w[kSteps / 2];
-                float top = 0.f, sum[kNS];
-                bool finite = true;
+                uint4 qw[kSteps / 2];      // 8 channels of every 32
 #pragma unroll
                 for (int i = 0; i < kSteps / 2; ++i) {
-                    w[i] = make_uint4(0, 0, 0, 0);
+                    qw[i] = make_uint4(0, 0, 0, 0);
                     if (tok < info.n_rows)
-                        w[i] = *reinterpret_cast<const uint4*>(a.qm + (info.row0 + tok) * a.qs + h * D + 32 * i + 8 * t);
+                        qw[i] = *reinterpret_cast<const uint4*>(a.qm + (info.row0 + tok) * a.qs + h * D + 32 * i + 8 * t);
                 }
+                uint32_t top = 0;
+                float sum[kNS];
 #pragma unroll
                 for (int i = 0; i < kNS; ++i) sum[i] = 0.f;
 #pragma unroll
                 for (int i = 0; i < kSteps / 2; ++i) {
-                    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                    const uint32_t x[4] = {qw[i].x, qw[i].y, qw[i].z, qw[i].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float lo = __uint_as_float(x[e] << 16), hi = __uint_as_float(x[e] & 0xFFFF0000u);
-                        top = fmaxf(top, fmaxf(fabsf(lo), fabsf(hi)));
-                        finite = finite && fabsf(lo) <= 3.4e38f && fabsf(hi) <= 3.4e38f;
-                        sum[32 * i / G] += lo + hi;
+                        top = max(top, max((x[e] << 16) & 0x7FFFFFFFu, x[e] & 0x7FFF0000u));   // orders NaN above all numbers
+                        sum[32 * i / G] += __uint_as_float(x[e] << 16) + __uint_as_float(x[e] & 0xFFFF0000u);
                     }
                 }
 #pragma unroll
                 for (int o = 1; o < 4; o <<= 1) {
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    finite = __shfl_xor_sync(0xffffffffu, finite ? 1 : 0, o) && finite;
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
 #pragma unroll
                     for (int i = 0; i < kNS; ++i) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], o);
                 }
+                const bool finite = top < 0x7F800000u;
                 // the row times 2^-e has its largest number in [2^14, 2^15)
-                const int e = min(100, max(-100, static_cast<int>((__float_as_uint(top) >> 23) & 255) - 127 - 14));
+                const int e = min(100, max(-100, static_cast<int>(top >> 23) - 127 - 14));
                 const float down = pow2(-e);
 #pragma unroll
                 for (int i = 0; i < kSteps / 2; ++i) {
-                    const uint32_t x[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+                    const uint32_t x[4] = {qw[i].x, qw[i].y, qw[i].z, qw[i].w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         // words 0, 1 of step 2i: channels 0, 1 and 2, 3 (whose codes come 16 times too large); 2, 3: step 2i + 1
@@ -427,15 +512,14 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 #pragma unroll
                     for (int i = 0; i < kNS; ++i)
                         qsum[n][i][c] = __shfl_sync(0xffffffffu, finite ? sum[i] * a.scale_log2e : CUDART_NAN_F, src);
-                    const int rc = cc.rb * kRows + 8 * n + 2 * t + c;
-                    last_key[n][c] = a.causal ? min(info.len - 1, info.len - info.n_rows + rc / a.share) : info.len - 1;
                 }
             }
             // keys before this are seen by every row of the item
             const int all_see = a.causal ? min(info.len, info.len - info.n_rows + cc.rb * kRows / a.share + 1) : info.len;
 
             float acc[NB][kSteps][4], m[NB][2], l[NB][2], pm[NB][kNS][2];
-            int ev = -110;      // the exponent that the values' steps are relative to
+            int ev = -110;              // the exponent that the values' steps are relative to
+            float inv = pow2(13 + 110);
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
 #pragma unroll
@@ -450,47 +534,44 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     for (int i = 0; i < kNS; ++i) pm[n][i][c] = 0.f;
                 }
             }
-            while (cc.blk < end_blk) {
-                const int nb = min(kBlk, end_blk - cc.blk);
-                const int slot = used % a.stages;
-                ok = mbar_wait_warp(bar_a + 8 * slot, (used / a.stages) & 1, a.wait_ns, &s_abort);
-                if (!ok) break;
-                const uint32_t here = (live >> (kBlk * (issued - 1 - used))) & ((1u << kBlk) - 1u);
+            // One stage, kBlk blocks.  Masked: with blocks that are not there, or keys that some row does not see.
+            auto turn = [&](auto masked_c, uint32_t here) {
+                constexpr bool masked = decltype(masked_c)::value;
                 const uint32_t base = ring_a + slot * kStage;
                 const int key0 = cc.blk << 4;
-                const bool masked = here != (1u << kBlk) - 1u || key0 + 16 * kBlk > all_see;
                 // ---- scores
                 float s[kBlk][NB][4];
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
+                    if (masked) {
 #pragma unroll
-                    for (int n = 0; n < NB; ++n)
+                        for (int n = 0; n < NB; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[b][n][e] = -CUDART_INF_F;
-                    if (!((here >> b) & 1u)) continue;
-                    const uint32_t at = base + b * kSB;
+                            for (int e = 0; e < 4; ++e) s[b][n][e] = -CUDART_INF_F;
+                        if (!((here >> b) & 1u)) continue;
+                    }
                     uint32_t w0[kNS], w1[kNS];
-                    lds_words<kNS>(at + 16 * D + 4 * kNS * g, w0);
-                    lds_words<kNS>(at + 16 * D + 4 * kNS * (g + 8), w1);
                     uint4 w[kSteps / 4];
 #pragma unroll
-                    for (int i = 0; i < kSteps / 4; ++i) w[i] = lds128(at + (i * 32 + lane) * 16);
+                    for (int i = 0; i < kSteps / 4; ++i) w[i] = lds128(base + lane16 + b * kSB + i * 512);
+                    lds_words<kNS>(base + params + b * kSB, w0);
+                    lds_words<kNS>(base + params + b * kSB + 32 * kNS, w1);
                     float raw[NB][4], mins[NB][4];
 #pragma unroll
                     for (int i = 0; i < kNS; ++i) {
                         float d[NB][4];
-#pragma unroll
-                        for (int n = 0; n < NB; ++n)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) d[n][e] = 0.f;
 #pragma unroll
                         for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k) {
                             const uint4 v = w[k >> 2];
                             const uint32_t x = (k & 3) == 0 ? v.x : (k & 3) == 1 ? v.y : (k & 3) == 2 ? v.z : v.w;
                             const uint32_t y = x >> 8;
 #pragma unroll
-                            for (int n = 0; n < NB; ++n)
-                                mma_f16(d[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][k][0], qf[n][k][1]);
+                            for (int n = 0; n < NB; ++n) {
+                                if (k == i * (G / 16))
+                                    mma_f16_first(d[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][k][0], qf[n][k][1]);
+                                else
+                                    mma_f16(d[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][k][0], qf[n][k][1]);
+                            }
                         }
                         const float s0 = wide_cache_scale(w0[i]), s1 = wide_cache_scale(w1[i]);
                         const float m0 = wide_cache_min(w0[i]), m1 = wide_cache_min(w1[i]);
@@ -508,38 +589,33 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             s[b][n][e] = fmaf(raw[n][e], qscale[n][e & 1], mins[n][e]);
-                            if (masked && key0 + 16 * b + g + 8 * (e >> 1) > last_key[n][e & 1]) s[b][n][e] = -CUDART_INF_F;
+                            if (masked) {
+                                const int row = cc.rb * kRows + 8 * n + 2 * t + (e & 1);
+                                const int last = a.causal ? min(info.len - 1, info.len - info.n_rows + row / a.share) : info.len - 1;
+                                if (key0 + 16 * b + g + 8 * (e >> 1) > last) s[b][n][e] = -CUDART_INF_F;
+                            }
                         }
                 }
-                // ---- steps of the values: parameters of this lane's keys, the largest exponent of the stage
+                // ---- the values' parameters, and their largest step (scales are not negative: their words compare like numbers)
                 uint32_t v0[kBlk][kNS], v1[kBlk][kNS], big = 0;
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
-                    const uint32_t at = base + b * kSB + 16 * D + 64 * kNS;
-                    lds_words<kNS>(at + 4 * kNS * g, v0[b]);
-                    lds_words<kNS>(at + 4 * kNS * (g + 8), v1[b]);
-                    if (masked) {   // nothing of a position behind the end may reach a sum
-                        const bool k0 = ((here >> b) & 1u) && key0 + 16 * b + g < info.len;
-                        const bool k1 = ((here >> b) & 1u) && key0 + 16 * b + g + 8 < info.len;
-#pragma unroll
-                        for (int i = 0; i < kNS; ++i) {
-                            v0[b][i] = k0 ? v0[b][i] : 0u;
-                            v1[b][i] = k1 ? v1[b][i] : 0u;
-                        }
-                    }
+                    lds_words<kNS>(base + params + 64 * kNS + b * kSB, v0[b]);
+                    lds_words<kNS>(base + params + 96 * kNS + b * kSB, v1[b]);
 #pragma unroll
                     for (int i = 0; i < kNS; ++i) {
-                        const uint32_t x = v0[b][i] & 0xFFFFu, y = v1[b][i] & 0xFFFFu;
-                        big = max(big, x < 0x7F80u ? x : 0u);
-                        big = max(big, y < 0x7F80u ? y : 0u);
+                        if (masked) {   // nothing of a position behind the end may reach a sum
+                            const bool is = (here >> b) & 1u;
+                            v0[b][i] = is && key0 + 16 * b + g < info.len ? v0[b][i] : 0u;
+                            v1[b][i] = is && key0 + 16 * b + g + 8 < info.len ? v1[b][i] : 0u;
+                        }
+                        big = max(big, max(v0[b][i] << 16, v1[b][i] << 16));
                     }
                 }
                 big = __reduce_max_sync(0xffffffffu, big);
-                const int ev_new = max(ev, static_cast<int>(big >> 7) - 127);
-                const bool ev_up = ev_new != ev;
-                // ---- running maximum; what is summed so far is scaled down when it (or the exponent) rises
-                float alpha[NB][2];
-                bool change = ev_up;
+                // ---- running maximum; what is summed so far is scaled down when it rises, or when the steps do
+                float alpha[NB][2], mu[NB][2], top[NB][2];
+                bool change = static_cast<int>(big >> 23) - 127 > ev;
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -551,15 +627,31 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
                         change = change || mx != m[n][c];
-                        alpha[n][c] = mx == m[n][c] ? 1.f : exp2_fast(m[n][c] - mx);
-                        m[n][c] = mx;
+                        top[n][c] = mx;
+                        mu[n][c] = mx == -CUDART_INF_F ? 0.f : mx;
                     }
                 if (__any_sync(0xffffffffu, change)) {
-                    const float ev_f = ev_up ? pow2(max(-126, ev - ev_new)) : 1.f;
+                    if (big >= 0x7F800000u) {   // a value that is not finite: leave it out of the scaling
+                        big = 0;
+#pragma unroll
+                        for (int b = 0; b < kBlk; ++b)
+#pragma unroll
+                            for (int i = 0; i < kNS; ++i) {
+                                const uint32_t x = v0[b][i] << 16, y = v1[b][i] << 16;
+                                big = max(big, max(x < 0x7F800000u ? x : 0u, y < 0x7F800000u ? y : 0u));
+                            }
+                        big = __reduce_max_sync(0xffffffffu, big);
+                    }
+                    const int up = max(ev, static_cast<int>(big >> 23) - 127);
+                    const float ev_f = pow2(max(-126, ev - up));
+                    ev = up;
+                    inv = pow2(13 - ev);
 #pragma unroll
                     for (int n = 0; n < NB; ++n) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
+                            alpha[n][c] = exp2_fast(m[n][c] - mu[n][c]);
+                            m[n][c] = top[n][c];
                             l[n][c] *= alpha[n][c];
 #pragma unroll
                             for (int i = 0; i < kNS; ++i) pm[n][i][c] *= alpha[n][c];
@@ -569,26 +661,22 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 #pragma unroll
                             for (int e = 0; e < 4; ++e) acc[n][i][e] *= alpha[n][e & 1] * ev_f;
                     }
-                    ev = ev_new;
                 }
-                const float inv = pow2(13 - ev);
                 // ---- probabilities, and the values they weigh
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
-                    if (!((here >> b) & 1u)) continue;
+                    if (masked && !((here >> b) & 1u)) continue;
+                    uint4 w[kSteps / 4];
+#pragma unroll
+                    for (int i = 0; i < kSteps / 4; ++i) w[i] = lds128(base + lane16 + 8 * D + b * kSB + i * 512);
                     float p[NB][4];
 #pragma unroll
                     for (int n = 0; n < NB; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float mx = m[n][e & 1];
-                            p[n][e] = exp2_fast(s[b][n][e] - (mx == -CUDART_INF_F ? 0.f : mx));
+                            p[n][e] = exp2_fast(s[b][n][e] - mu[n][e & 1]);
                             l[n][e & 1] += p[n][e];
                         }
-                    const uint32_t at = base + b * kSB + 8 * D;
-                    uint4 w[kSteps / 4];
-#pragma unroll
-                    for (int i = 0; i < kSteps / 4; ++i) w[i] = lds128(at + (i * 32 + lane) * 16);
 #pragma unroll
                     for (int i = 0; i < kNS; ++i) {
                         const float s0 = wide_cache_scale(v0[b][i]) * inv, s1 = wide_cache_scale(v1[b][i]) * inv;
@@ -596,17 +684,21 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         uint32_t pb[NB][2];
 #pragma unroll
                         for (int n = 0; n < NB; ++n) {
-                            float x[4], y[4];
+                            float x[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 x[e] = p[n][e] * (e < 2 ? s0 : s1);
-                                y[e] = p[n][e] * (e < 2 ? m0 : m1);
-                                if (masked && s[b][n][e] == -CUDART_INF_F) x[e] = y[e] = 0.f;   // NaN steps behind the mask
+                                const float next = fmaf(p[n][e], e < 2 ? m0 : m1, pm[n][i][e & 1]);
+                                if (masked) {   // a step or minimum that is not finite, of a key this row does not see
+                                    const bool unseen = s[b][n][e] == -CUDART_INF_F;
+                                    x[e] = unseen ? 0.f : x[e];
+                                    pm[n][i][e & 1] = unseen ? pm[n][i][e & 1] : next;
+                                } else {
+                                    pm[n][i][e & 1] = next;
+                                }
                             }
                             pb[n][0] = transpose8x8(pack_f16(x[0], x[1]));
                             pb[n][1] = transpose8x8(pack_f16(x[2], x[3]));
-                            pm[n][i][0] += y[0] + y[2];
-                            pm[n][i][1] += y[1] + y[3];
                         }
 #pragma unroll
                         for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k) {
@@ -619,13 +711,38 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         }
                     }
                 }
-                __syncwarp();     // every lane has read the stage
-                ++used;
-                cc.blk += nb;
-                to_use -= nb;
-                if (to_issue > 0) issue();
+                // every lane has read the stage: its place takes the next one
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar0 + 64 + 8 * slot);
+                if (++slot == STAGES) {
+                    slot = 0;
+                    parity ^= 1u;
+                }
+            };
+            int run = (min(end_blk, all_see >> 4) - cc.blk) & -kBlk;     // blocks that every row sees whole
+            while (cc.blk < end_blk) {
+                uint32_t here = kFull;
+                while (run > 0) {
+                    ok = mbar_wait_warp(bar0 + 8 * slot, parity, a.wait_ns, &s_abort);
+                    if (!ok) break;
+                    here = here_of[warp][slot];
+                    if (here != kFull) break;
+                    turn(std::false_type{}, kFull);
+                    cc.blk += kBlk;
+                    run -= kBlk;
+                }
+                if (!ok || cc.blk >= end_blk) break;
+                if (here == kFull) {
+                    ok = mbar_wait_warp(bar0 + 8 * slot, parity, a.wait_ns, &s_abort);
+                    if (!ok) break;
+                    here = here_of[warp][slot];
+                }
+                turn(std::true_type{}, here);
+                cc.blk = min(cc.blk + kBlk, end_blk);
+                run = max(0, run - kBlk);
             }
             if (!ok) break;
+            to_use -= end_blk - first_blk;
             // ---- end of the item or of the piece: sums over the lanes, results in the values' own scale
             const float f0 = pow2(11) * pow2(ev), f1 = f0 * 0.0625f;
 #pragma unroll
@@ -661,7 +778,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     }
             } else {
                 const bool tail = to_use == 0;    // the ring is free now
-                float* dst = tail ? reinterpret_cast<float*>(ring) : a.heads + static_cast<size_t>(blockIdx.x * WARPS + warp) * slot_floats(kRows, D);
+                float* dst = tail ? reinterpret_cast<float*>(smem + kPlanSmem + warp * (STAGES * kStage)) : a.heads + static_cast<size_t>(blockIdx.x * WARPS + warp) * slot_floats(kRows, D);
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -687,17 +804,10 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     e_rb[warp][e] = cc.rb;
                 }
             }
-            if (to_use > 0) next_item<kRows>(a, plan, cc);
+            if (to_use <= 0) break;
+            next_item<kRows>(a, plan, cc);
         }
-        if (!ok) {
-            if (lane == 0) {
-                atomicExch(a.status, WIDE_ERR_TIMEOUT);
-                // copies may still be on their way into this CTA's shared memory
-                volatile int never = 0;
-                for (int i = used; i < issued; ++i) mbar_wait(bar_a + 8 * (i % a.stages), (i / a.stages) & 1, a.wait_ns, &never);
-            }
-            __syncwarp();
-        }
+        if (!ok && lane == 0) atomicExch(a.status, WIDE_ERR_TIMEOUT);
     }
     __syncthreads();
     if (s_abort) return;
@@ -742,14 +852,14 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 meta[4 * slot + 3] = e_rb[w][e];
             }
         }
-        auto piece = [&](int i) -> const float* {
-            uint32_t m = which;
-            for (; i > 0; --i) m &= m - 1;
-            const int x = __ffs(m) - 1;
-            return (x & 1) ? reinterpret_cast<const float*>(smem + kPlanSmem + static_cast<size_t>(x >> 1) * a.stages * kStage)
-                           : a.heads + static_cast<size_t>(blockIdx.x * WARPS + (x >> 1)) * slot_floats(kRows, D);
-        };
-        join<kRows, D>(a, e_seq[w][e], e_kvh[w][e], e_rb[w][e], n, piece, dst, tid, 32 * WARPS);
+        if (tid < 2 * WARPS && ((which >> tid) & 1u)) {
+            const int i = __popc(which & ((1u << tid) - 1u));
+            e_at[i] = (tid & 1) ? reinterpret_cast<const float*>(smem + kPlanSmem + static_cast<size_t>(tid >> 1) * STAGES * kStage)
+                                : a.heads + static_cast<size_t>(blockIdx.x * WARPS + (tid >> 1)) * slot_floats(kRows, D);
+        }
+        __syncthreads();
+        join<kRows, D>(a, e_seq[w][e], e_kvh[w][e], e_rb[w][e], n, [&](int i) { return e_at[i]; }, dst, weights, 0, 1);
+        __syncthreads();
         at = to;
     }
     if (tid == 0) {
@@ -762,20 +872,31 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 template <int ROWS, int D>
 __global__ void __launch_bounds__(256) attn_cache_join_kernel(const __grid_constant__ AttnArgs a, int ctas) {
     grid_dep_wait();
-    const int c = blockIdx.x;
+    __shared__ float2 weights[(kMaxCtas + 1) * ROWS];
+    __shared__ int count;
+    const int c = blockIdx.x, lane = threadIdx.x & 31;
     if (*reinterpret_cast<volatile int*>(a.status) != WIDE_OK) return;   // some CTA gave up: its pieces are not there
-    const int* meta = a.meta + c * 8 + 4;
-    if (meta[0] != 1) return;
-    int n = 1;
-    while (c + n < ctas && a.meta[(c + n) * 8] == 1) ++n;
-    if (c + n < ctas) ++n;     // the piece that ends it
-    auto piece = [&](int i) -> const float* {
+    const int4 meta = *reinterpret_cast<const int4*>(a.meta + c * 8 + 4);
+    if (meta.x != 1) return;
+    if (threadIdx.x < 32) {    // CTAs c + 1, ...: the first piece of each belongs to the item, up to the one that ends it
+        int n = 1;
+        for (int k = c + 1;; k += 32) {
+            const int st = k + lane < ctas ? a.meta[(k + lane) * 8] : 0;
+            const uint32_t stop = __ballot_sync(0xffffffffu, st != 1);
+            if (stop) {
+                const int at = __ffs(stop) - 1;
+                n += at + (__shfl_sync(0xffffffffu, st, at) == 2 ? 1 : 0);
+                break;
+            }
+            n += 32;
+        }
+        if (lane == 0) count = n;
+    }
+    __syncthreads();
+    join<ROWS, D>(a, meta.y, meta.z, meta.w, count, [&](int i) -> const float* {
         return a.parts + static_cast<size_t>(i == 0 ? 2 * c + 1 : 2 * (c + i)) * slot_floats(ROWS, D);
-    };
-    join<ROWS, D>(a, meta[1], meta[2], meta[3], n, piece, nullptr, threadIdx.x + 256 * blockIdx.y, 256 * gridDim.y);
+    }, nullptr, weights, blockIdx.y, gridDim.y);
 }
-
-constexpr int warps_of(int nb) { return nb == 1 ? 16 : 8; }
 
 struct Work {
     size_t plan, heads, parts, meta, total;
@@ -784,7 +905,7 @@ Work work_layout() {
     Work w;
     size_t at = 0;
     w.plan = at;
-    at += wide_align_up(plan_bytes(WIDE_MAX_SEQS, 8), 256);
+    at += wide_align_up(plan_bytes(WIDE_MAX_SEQS, 8, 8), 256);
     w.heads = at;
     at += wide_align_up(static_cast<size_t>(kMaxCtas) * 16 * slot_floats(8, 128) * 4, 256);
     w.parts = at;
@@ -797,29 +918,31 @@ Work work_layout() {
 
 template <int D, int G, int NB>
 int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
-    constexpr int W = warps_of(NB), kRows = 8 * NB;
+    constexpr int kRows = 8 * NB;
     constexpr int stage = kBlk * (16 * D + 128 * (D / G));
-    constexpr int room = 227 * 1024 - 4096 - kPlanSmem;   // 4 KB for the static arrays
-    constexpr int stages = room / (W * stage) > 6 ? 6 : room / (W * stage);
-    static_assert(stages >= 2 && stages * stage >= slot_floats(kRows, D) * 4, "ring");
-    a.stages = stages;
-    const int smem = kPlanSmem + W * stages * stage;
+    constexpr int room = 227 * 1024 - 5120 - kPlanSmem;   // 5 KB for the static arrays
+    // with the feeding warp 16 warps, of 128 registers or less each, which two blocks of eight query rows do not fit
+    constexpr int W = NB == 2 ? 7 : 15 * 3 * stage <= room ? 15 : 11;
+    constexpr int S = room / (W * stage) > 6 ? 6 : room / (W * stage);
+    static_assert(S >= 3 && S * stage >= slot_floats(kRows, D) * 4 && W * S <= 32 * (W + 1), "ring");
+    auto kernel = attn_cache_kernel<D, G, NB, W, S>;
+    const int smem = kPlanSmem + W * S * stage;
     const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
     const Work w = work_layout();
     a.heads = reinterpret_cast<float*>(ws + w.heads);
     a.parts = reinterpret_cast<float*>(ws + w.parts);
     a.meta = reinterpret_cast<int*>(ws + w.meta);
     a.plan = nullptr;
-    if (plan_bytes(a.q.n_seqs, a.plan_words) > kPlanSmem) {
+    if (plan_bytes(a.q.n_seqs, a.plan_words, a.words) > kPlanSmem) {
         a.plan = ws + w.plan;
         WideLaunch l(ctx, s, "attn_cache_plan");
         attn_cache_plan_kernel<kRows><<<1, 1024, 0, s>>>(a);
         WIDE_CUDA_CHECK(cudaGetLastError());
     }
-    WIDE_CUDA_CHECK(cudaFuncSetAttribute(attn_cache_kernel<D, G, NB, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    WIDE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     {
         WideLaunch l(ctx, s, "attn_cache");
-        attn_cache_kernel<D, G, NB, W><<<ctas, 32 * W, smem, s>>>(a);
+        kernel<<<ctas, 32 * (W + 1), smem, s>>>(a);
         WIDE_CUDA_CHECK(cudaGetLastError());
     }
     {
