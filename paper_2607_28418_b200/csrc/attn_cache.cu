@@ -42,8 +42,7 @@ struct AttnArgs {
     const uint32_t* mask_bits;
     float scale_log2e;
     __nv_bfloat16* o;
-    int* status;                   // device status word (timeouts); index errors go to WIDE_STATUS_INDEX
-    unsigned long long wait_ns;
+    int* status;                   // takes WIDE_ERR_BAD_INDEX
     int plan_words;                // words of a sequence's head mask
     unsigned char* plan;           // the plan in the workspace, or NULL: every CTA makes its own in shared memory
     float* heads;                  // partial results of warps whose first item began before their piece
@@ -79,10 +78,6 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t d;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
-}
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
     uint4 v;
@@ -127,7 +122,7 @@ __device__ void make_plan(const AttnArgs& a, const Plan& p, long long* part, boo
     const int s0 = min(a.q.n_seqs, tid * per), s1 = min(a.q.n_seqs, s0 + per);
     for (int s = s0; s < s1; ++s) {
         const SeqInfo i = wide_seq_info(a.q, s, a.c.page_shift);
-        if (i.bad && report) atomicExch(a.status + WIDE_STATUS_INDEX, WIDE_ERR_BAD_INDEX);
+        if (i.bad && report) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
         const bool some = i.n_rows > 0 && i.len > 0;
         const int looked = a.mask_bits && i.n_rows <= 16 ? i.n_rows : 0;
         for (int w = 0; w < a.words; ++w) {      // groups that any new row uses
@@ -205,7 +200,7 @@ __device__ __forceinline__ void enter_seq(const AttnArgs& a, Cursor& k) {
 }
 
 template <int ROWS>
-__device__ Cursor locate(const AttnArgs& a, const Plan& p, long long u) {
+__device__ __noinline__ Cursor locate(const AttnArgs& a, const Plan& p, long long u) {
     Cursor k;
     int lo = 0, hi = a.q.n_seqs - 1;   // the last sequence that starts at or before u: it holds u
     while (lo < hi) {
@@ -235,7 +230,7 @@ __device__ Cursor locate(const AttnArgs& a, const Plan& p, long long u) {
 
 // to the first block of the next item; the caller knows that there is one
 template <int ROWS>
-__device__ __forceinline__ void next_item(const AttnArgs& a, const Plan& p, Cursor& k) {
+__device__ __noinline__ void next_item(const AttnArgs& a, const Plan& p, Cursor& k) {
     k.blk = 0;
     if (++k.rb < k.n_rb) return;
     k.rb = 0;
@@ -265,54 +260,37 @@ __device__ __forceinline__ RowOut row_out(const AttnArgs& a, const SeqInfo& i, i
 
 __host__ __device__ constexpr int slot_floats(int rows, int D) { return rows * (D + 4); }   // rows of D values, then m and l of each
 
-// Joins `n` partial results of one item, the e-th at at(e): out rows, or a partial again (dst).  weights is
-// shared memory for (n + 1) * ROWS pairs; all `n_threads` threads of the CTA take part.
+// Joins `n` partial results of one item, the e-th at at(e): out rows, or a partial again (dst).  A thread takes four
+// channels of a row.  Executed once a launch, so kept short: its time is that of fetching its instructions.
 template <int ROWS, int D, typename At>
-__device__ __forceinline__ void join(const AttnArgs& a, int seq, int kvh, int rb, int n, const At& at, float* dst, float2* weights, int part,
-                                     int parts) {
-    const int tid = threadIdx.x, n_threads = blockDim.x;
-    for (int i = tid; i < n * ROWS; i += n_threads)
-        weights[i] = *reinterpret_cast<const float2*>(at(i / ROWS) + ROWS * D + 2 * (i % ROWS));
-    __syncthreads();
-    // row r: maximum, sum; each piece's weight
-    if (tid < ROWS) {
+__device__ __forceinline__ void join(const AttnArgs& a, int seq, int kvh, int rb, int n, const At& at, float* dst, int first, int step) {
+#pragma unroll 1
+    for (int i = first; i < ROWS * (D / 4); i += step) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
         float m = -CUDART_INF_F, l = 0.f;
-        for (int e = 0; e < n; ++e) m = fmaxf(m, weights[e * ROWS + tid].x);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int e = 0; e < n; ++e) m = fmaxf(m, at(e)[ROWS * D + 2 * r]);
         const float m_use = m == -CUDART_INF_F ? 0.f : m;
 #pragma unroll 4
         for (int e = 0; e < n; ++e) {
-            const float2 v = weights[e * ROWS + tid];
-            const float w = exp2_fast(v.x - m_use);
-            weights[e * ROWS + tid].x = w;
-            l = fmaf(v.y, w, l);
-        }
-        weights[n * ROWS + tid].x = l;
-        if (dst) *reinterpret_cast<float2*>(dst + ROWS * D + 2 * tid) = make_float2(m, l);
-    }
-    __syncthreads();
-    const SeqInfo info = wide_seq_info(a.q, seq, a.c.page_shift);
-    for (int i = tid + part * n_threads; i < ROWS * (D / 4); i += n_threads * parts) {
-        const int r = i / (D / 4), d = i % (D / 4) * 4;
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-        for (int e = 0; e < n; ++e) {
-            const float w = weights[e * ROWS + r].x;
-            const float4 v = *reinterpret_cast<const float4*>(at(e) + r * D + d);
-            x[0] = fmaf(v.x, w, x[0]);
-            x[1] = fmaf(v.y, w, x[1]);
-            x[2] = fmaf(v.z, w, x[2]);
-            x[3] = fmaf(v.w, w, x[3]);
+            const float* p = at(e);
+            const float w = exp2_fast(p[ROWS * D + 2 * r] - m_use);
+            const float4 v = *reinterpret_cast<const float4*>(p + r * D + d);
+            l = fmaf(p[ROWS * D + 2 * r + 1], w, l);
+            x = make_float4(fmaf(v.x, w, x.x), fmaf(v.y, w, x.y), fmaf(v.z, w, x.z), fmaf(v.w, w, x.w));
         }
         if (dst) {
-            *reinterpret_cast<float4*>(dst + r * D + d) = make_float4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<float4*>(dst + r * D + d) = x;
+            if (d == 0) *reinterpret_cast<float2*>(dst + ROWS * D + 2 * r) = make_float2(m, l);
         } else {
+            const SeqInfo info = wide_seq_info(a.q, seq, a.c.page_shift);
             const RowOut ro = row_out(a, info, kvh, rb * ROWS + r, D);
             if (!ro.o) continue;
-            const float sum = weights[n * ROWS + r].x;
+            const float inv = ro.on && l != 0.f ? 1.f / l : 0.f;
             uint2 w = make_uint2(0, 0);
-            if (ro.on && sum != 0.f) {
-                const float inv = 1.f / sum;
-                const __nv_bfloat162 b0 = __floats2bfloat162_rn(x[0] * inv, x[1] * inv), b1 = __floats2bfloat162_rn(x[2] * inv, x[3] * inv);
+            if (inv != 0.f) {
+                const __nv_bfloat162 b0 = __floats2bfloat162_rn(x.x * inv, x.y * inv), b1 = __floats2bfloat162_rn(x.z * inv, x.w * inv);
                 w = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
             }
             *reinterpret_cast<uint2*>(ro.o + d) = w;
@@ -322,32 +300,23 @@ __device__ __forceinline__ void join(const AttnArgs& a, int seq, int kvh, int rb
 
 // ------------------------------------------------------------------------------------------------ the kernel
 template <int D, int G, int NB, int WARPS, int STAGES>
-__global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int kRows = 8 * NB;
     constexpr int kNS = D / G;
     constexpr int kSteps = D / 16;              // k16 steps of a key, m16 tiles of a value
     constexpr int kSB = 16 * D + 128 * kNS;     // bytes of a block
     constexpr int kStage = kBlk * kSB;
+    constexpr int kPieces = (kSB + 511) / 512;  // 16-byte copies of a lane for a block
     constexpr uint32_t kFull = (1u << kBlk) - 1u;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ uint64_t bars[WARPS][2][8];      // per warp and stage: [0] data has arrived, [1] data has been read
-    __shared__ uint32_t here_of[WARPS][8];      // which blocks of the stage have a page
-    __shared__ long long part[WARPS + 1];
-    __shared__ int s_abort;
+    __shared__ long long part[WARPS];
     // per warp two partial results: [0] of an item that began before the piece (in global memory), [1] of the
     // piece's last item (over the ring).  state: 0 none, else 1 | begins here << 1 | ends here << 2
     __shared__ const float* e_at[WARPS];        // the pieces of one item, at most one of a warp
-    __shared__ float2 weights[(WARPS + 1) * kRows];
     __shared__ int e_state[WARPS][2], e_seq[WARPS][2], e_kvh[WARPS][2], e_rb[WARPS][2];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    if (tid < WARPS * STAGES) {
-        mbar_init(smem_u32(&bars[tid / STAGES][0][tid % STAGES]), 1);
-        mbar_init(smem_u32(&bars[tid / STAGES][1][tid % STAGES]), 1);
-    }
     if (tid < 2 * WARPS) e_state[tid >> 1][tid & 1] = 0;
-    if (tid == 0) s_abort = 0;
-    fence_barrier_init();
     // All CTAs together bring what the plan will lead to (masks, page table, queries) into L2 while it is made.
     prefetch_l2(a.mask_bits, static_cast<size_t>(a.q.rows) * a.words * 4);
     prefetch_l2(a.q.page_table, static_cast<size_t>(a.q.n_seqs) * a.q.max_pages * 4);
@@ -359,7 +328,6 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const _
     // the line of units, cut for the CTAs that are worth using (16 units each at least) and their warps
     const long long total = plan.offsets[a.q.n_seqs];
     const int ctas = static_cast<int>(min(static_cast<long long>(gridDim.x), (total + 15) / 16)), cta = blockIdx.x;
-    const int who = warp < WARPS ? warp : min(lane, WARPS - 1);    // a lane of the last warp feeds one of the others
     long long u0 = 0, u1 = 0;
     if (cta < ctas) {
         const long long share = total <= 0x7fffffffLL ? static_cast<int>(total) / ctas : total / ctas;
@@ -367,91 +335,54 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const _
         const long long c0 = share * cta + min(cta, more);
         const int n = static_cast<int>(share + (cta < more ? 1 : 0));
         const int each = n / WARPS, extra = n - each * WARPS;
-        u0 = c0 + each * who + min(who, extra);
-        u1 = u0 + each + (who < extra ? 1 : 0);
+        u0 = c0 + each * warp + min(warp, extra);
+        u1 = u0 + each + (warp < extra ? 1 : 0);
     }
-    if (warp == WARPS) {
-        // ---- the feeding warp: lane w keeps the ring of warp w full
-        int left = lane < WARPS ? static_cast<int>(u1 - u0) : 0, issued = 0;
+    if (u0 < u1) {
+        Cursor cc = locate<kRows>(a, plan, u0), ic = cc;     // used, requested
+        int to_use = static_cast<int>(u1 - u0), to_issue = to_use, slot = 0;
+        uint32_t live = 0;             // kBlk bits a stage, newest lowest: which of its blocks have a page
+        int pt_seq = -1, pt_first = 0, pt = 0;   // page numbers [pt_first, pt_first + 32) of sequence pt_seq, one a lane
         const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
-        const uint32_t bar0 = smem_u32(&bars[who][0][0]), ring_a = smem_u32(smem + kPlanSmem) + who * (STAGES * kStage);
-        Cursor ic{};
-        if (left > 0) ic = locate<kRows>(a, plan, u0);
-        int slot = 0;
-        uint32_t parity = 1;           // of the slot's previous reading
-        uint64_t since = globaltimer_ns();
-        while (__any_sync(0xffffffffu, left > 0)) {
-            const bool free_slot = left > 0 && (issued < STAGES || mbar_try_wait(bar0 + 64 + 8 * slot, parity));
-            if (!__any_sync(0xffffffffu, free_slot)) {
-                if (*reinterpret_cast<volatile int*>(&s_abort)) break;
-                if (globaltimer_ns() - since > a.wait_ns) s_abort = 1;
-                continue;
-            }
-            since = globaltimer_ns();
-            if (free_slot) {
-                const int nb = min(min(kBlk, ic.n_blk - ic.blk), left);
-                if (nb <= 0) {         // only if a length changes under the running kernel
-                    left = 0;
-                } else {
-                    const int32_t* table = a.q.page_table + static_cast<size_t>(ic.seq) * a.q.max_pages;
-                    int page[kBlk];
-#pragma unroll
-                    for (int b = 0; b < kBlk; ++b) page[b] = b < nb ? table[(ic.blk + b) >> sub_shift] : -1;
-                    uint32_t m = 0;
-#pragma unroll
-                    for (int b = 0; b < kBlk; ++b) m |= static_cast<unsigned>(page[b]) < static_cast<unsigned>(a.c.n_pages) ? 1u << b : 0u;
-                    if (m != (1u << nb) - 1u) atomicExch(a.status + WIDE_STATUS_INDEX, WIDE_ERR_BAD_INDEX);
-                    here_of[lane][slot] = m;
-                    const uint32_t bar = bar0 + 8 * slot;
-                    mbar_arrive_expect_tx(bar, __popc(m) * kSB);
-                    auto from = [&](int b) {
-                        return a.c.pages + (((static_cast<size_t>(page[b]) * a.c.n_kv_heads + ic.kvh) << sub_shift) + ((ic.blk + b) & sub_mask)) * kSB;
-                    };
-                    const uint32_t to = ring_a + slot * kStage;
-                    if (m == kFull && page[0] == page[1]) {      // neighbours within a page
-                        bulk_load(to, from(0), kStage, bar);
-                    } else {
-#pragma unroll
-                        for (int b = 0; b < kBlk; ++b)
-                            if ((m >> b) & 1u) bulk_load(to + b * kSB, from(b), kSB, bar);
-                    }
-                    if (++slot == STAGES) {
-                        slot = 0;
-                        parity ^= 1u;
-                    }
-                    ++issued;
-                    ic.blk += nb;
-                    left -= nb;
-                    if (ic.blk == ic.n_blk && left > 0) next_item<kRows>(a, plan, ic);
-                }
-            }
-            __syncwarp();
-        }
-        if (*reinterpret_cast<volatile int*>(&s_abort)) {
-            // copies may still be on their way into this CTA's shared memory
-            volatile int never = 0;
-            for (int i = max(0, issued - STAGES); i < issued; ++i) mbar_wait(bar0 + 8 * (i % STAGES), (i / STAGES) & 1, a.wait_ns, &never);
-        }
-    }
-
-    // rows that no item writes: KV heads that a sequence does not use, sequences that are left out
-    for (int s = blockIdx.x; s < a.q.n_seqs && warp < WARPS; s += gridDim.x) {
-        const SeqInfo i = wide_seq_info(a.q, s, a.c.page_shift);
-        const int per_row = a.n_q * (D / 8);
-        for (long long x = tid; x < static_cast<long long>(i.n_rows) * per_row; x += 32 * WARPS) {
-            const int r = static_cast<int>(x / per_row), v = static_cast<int>(x - static_cast<long long>(r) * per_row), h = v / (D / 8) / a.share;
-            if (!((plan.masks[s * a.plan_words + (h >> 5)] >> (h & 31)) & 1u))
-                reinterpret_cast<uint4*>(a.o + static_cast<size_t>(i.row0 + r) * a.n_q * D)[v] = make_uint4(0, 0, 0, 0);
-        }
-    }
-
-    if (warp < WARPS && u0 < u1) {
-        Cursor cc = locate<kRows>(a, plan, u0);
-        int to_use = static_cast<int>(u1 - u0), slot = 0;
-        uint32_t parity = 0;
-        bool ok = true;
-        const uint32_t bar0 = smem_u32(&bars[warp][0][0]), ring_a = smem_u32(smem + kPlanSmem) + warp * (STAGES * kStage);
+        const uint32_t ring_a = smem_u32(smem + kPlanSmem) + warp * (STAGES * kStage);
         const uint32_t lane16 = lane * 16, params = 16 * D + 4 * kNS * g;
+        // request the next stage, up to kBlk blocks of one item, into place `to` (a group of copies even where nothing is left)
+        auto issue = [&](int to) {
+            uint32_t m = 0;
+            if (to_issue > 0) {
+                const int nb = min(min(kBlk, ic.n_blk - ic.blk), to_issue);
+                const int last = (ic.blk + nb - 1) >> sub_shift;
+                if (pt_seq != ic.seq || last - pt_first >= 32 || (ic.blk >> sub_shift) < pt_first) {
+                    pt_seq = ic.seq;
+                    pt_first = ic.blk >> sub_shift;
+                    pt = pt_first + lane < a.q.max_pages ? a.q.page_table[static_cast<size_t>(ic.seq) * a.q.max_pages + pt_first + lane] : -1;
+                }
+#pragma unroll
+                for (int b = 0; b < kBlk; ++b) {
+                    if (b < nb) {
+                        const int blk = ic.blk + b;
+                        const int page = __shfl_sync(0xffffffffu, pt, (blk >> sub_shift) - pt_first);
+                        if (static_cast<unsigned>(page) < static_cast<unsigned>(a.c.n_pages)) {
+                            m |= 1u << b;
+                            const unsigned char* from = a.c.pages + lane16 +
+                                (((static_cast<size_t>(page) * a.c.n_kv_heads + ic.kvh) << sub_shift) + (blk & sub_mask)) * kSB;
+                            const uint32_t dst = ring_a + to * kStage + b * kSB + lane16;
+#pragma unroll
+                            for (int i = 0; i < kPieces; ++i)
+                                if (512 * (i + 1) <= kSB || lane16 + 512 * i < kSB) cp_async_16(dst + 512 * i, from + 512 * i);
+                        }
+                    }
+                }
+                if (m != (1u << max(nb, 0)) - 1u && lane == 0) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
+                ic.blk += nb;
+                to_issue = nb > 0 ? to_issue - nb : 0;       // nb <= 0: a length changed under the running kernel
+                if (ic.blk >= ic.n_blk && to_issue > 0) next_item<kRows>(a, plan, ic);
+            }
+            cp_async_commit();
+            live = (live << kBlk) | m;
+        };
+#pragma unroll 1
+        for (int i = 0; i < STAGES; ++i) issue(i);
 
         while (true) {
             // ---- an item, or the part of it that lies in this piece
@@ -540,62 +471,63 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const _
                 const uint32_t base = ring_a + slot * kStage;
                 const int key0 = cc.blk << 4;
                 // ---- scores
-                float s[kBlk][NB][4];
+                // (A block that is not there is computed like the others, from whatever the ring holds, and left out by
+                // selection.  The blocks take turns: eight dependent instructions on one accumulator would wait for each other.)
+                float s[kBlk][NB][4], mins[kBlk][NB][4];
+                uint4 w[kBlk][kSteps / 4];
+                uint32_t w0[kBlk][kNS], w1[kBlk][kNS];
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
-                    if (masked) {
 #pragma unroll
-                        for (int n = 0; n < NB; ++n)
+                    for (int i = 0; i < kSteps / 4; ++i) w[b][i] = lds128(base + lane16 + b * kSB + i * 512);
+                    lds_words<kNS>(base + params + b * kSB, w0[b]);
+                    lds_words<kNS>(base + params + b * kSB + 32 * kNS, w1[b]);
+                }
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) s[b][n][e] = -CUDART_INF_F;
-                        if (!((here >> b) & 1u)) continue;
-                    }
-                    uint32_t w0[kNS], w1[kNS];
-                    uint4 w[kSteps / 4];
+                for (int i = 0; i < kNS; ++i) {
+                    float d[kBlk][NB][4];
 #pragma unroll
-                    for (int i = 0; i < kSteps / 4; ++i) w[i] = lds128(base + lane16 + b * kSB + i * 512);
-                    lds_words<kNS>(base + params + b * kSB, w0);
-                    lds_words<kNS>(base + params + b * kSB + 32 * kNS, w1);
-                    float raw[NB][4], mins[NB][4];
+                    for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k)
 #pragma unroll
-                    for (int i = 0; i < kNS; ++i) {
-                        float d[NB][4];
-#pragma unroll
-                        for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k) {
-                            const uint4 v = w[k >> 2];
+                        for (int b = 0; b < kBlk; ++b) {
+                            const uint4 v = w[b][k >> 2];
                             const uint32_t x = (k & 3) == 0 ? v.x : (k & 3) == 1 ? v.y : (k & 3) == 2 ? v.z : v.w;
                             const uint32_t y = x >> 8;
 #pragma unroll
                             for (int n = 0; n < NB; ++n) {
                                 if (k == i * (G / 16))
-                                    mma_f16_first(d[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][k][0], qf[n][k][1]);
+                                    mma_f16_first(d[b][n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][k][0], qf[n][k][1]);
                                 else
-                                    mma_f16(d[n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][k][0], qf[n][k][1]);
+                                    mma_f16(d[b][n], x & 0x000F000Fu, y & 0x000F000Fu, x & 0x00F000F0u, y & 0x00F000F0u, qf[n][k][0], qf[n][k][1]);
                             }
                         }
-                        const float s0 = wide_cache_scale(w0[i]), s1 = wide_cache_scale(w1[i]);
-                        const float m0 = wide_cache_min(w0[i]), m1 = wide_cache_min(w1[i]);
+#pragma unroll
+                    for (int b = 0; b < kBlk; ++b) {
+                        const float s0 = wide_cache_scale(w0[b][i]), s1 = wide_cache_scale(w1[b][i]);
+                        const float m0 = wide_cache_min(w0[b][i]), m1 = wide_cache_min(w1[b][i]);
 #pragma unroll
                         for (int n = 0; n < NB; ++n)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const float st = e < 2 ? s0 : s1, mi = e < 2 ? m0 : m1;
-                                raw[n][e] = i == 0 ? d[n][e] * st : fmaf(d[n][e], st, raw[n][e]);
-                                mins[n][e] = i == 0 ? mi * qsum[n][i][e & 1] : fmaf(mi, qsum[n][i][e & 1], mins[n][e]);
+                                s[b][n][e] = i == 0 ? d[b][n][e] * st : fmaf(d[b][n][e], st, s[b][n][e]);
+                                mins[b][n][e] = i == 0 ? mi * qsum[n][i][e & 1] : fmaf(mi, qsum[n][i][e & 1], mins[b][n][e]);
                             }
                     }
+                }
+#pragma unroll
+                for (int b = 0; b < kBlk; ++b)
 #pragma unroll
                     for (int n = 0; n < NB; ++n)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            s[b][n][e] = fmaf(raw[n][e], qscale[n][e & 1], mins[n][e]);
+                            s[b][n][e] = fmaf(s[b][n][e], qscale[n][e & 1], mins[b][n][e]);
                             if (masked) {
                                 const int row = cc.rb * kRows + 8 * n + 2 * t + (e & 1);
                                 const int last = a.causal ? min(info.len - 1, info.len - info.n_rows + row / a.share) : info.len - 1;
-                                if (key0 + 16 * b + g + 8 * (e >> 1) > last) s[b][n][e] = -CUDART_INF_F;
+                                if (key0 + 16 * b + g + 8 * (e >> 1) > last || !((here >> b) & 1u)) s[b][n][e] = -CUDART_INF_F;
                             }
                         }
-                }
                 // ---- the values' parameters, and their largest step (scales are not negative: their words compare like numbers)
                 uint32_t v0[kBlk][kNS], v1[kBlk][kNS], big = 0;
 #pragma unroll
@@ -665,10 +597,8 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const _
                 // ---- probabilities, and the values they weigh
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
-                    if (masked && !((here >> b) & 1u)) continue;
-                    uint4 w[kSteps / 4];
 #pragma unroll
-                    for (int i = 0; i < kSteps / 4; ++i) w[i] = lds128(base + lane16 + 8 * D + b * kSB + i * 512);
+                    for (int i = 0; i < kSteps / 4; ++i) w[b][i] = lds128(base + lane16 + 8 * D + b * kSB + i * 512);
                     float p[NB][4];
 #pragma unroll
                     for (int n = 0; n < NB; ++n)
@@ -702,49 +632,52 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const _
                         }
 #pragma unroll
                         for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k) {
-                            const uint4 v = w[k >> 2];
+                            // Rows g take a whole byte, low code + 16 * high code: the rows g + 8, 16 * high code, come off
+                            // again at the end.  That saves an instruction a word.
+                            const uint4 v = w[b][k >> 2];
                             const uint32_t x = (k & 3) == 0 ? v.x : (k & 3) == 1 ? v.y : (k & 3) == 2 ? v.z : v.w;
-                            const uint32_t y = x >> 8;
+                            const uint32_t y = __byte_perm(x, 0, 0x4341);
 #pragma unroll
                             for (int n = 0; n < NB; ++n)
-                                mma_f16(acc[n][k], x & 0x000F000Fu, x & 0x00F000F0u, y & 0x000F000Fu, y & 0x00F000F0u, pb[n][0], pb[n][1]);
+                                mma_f16(acc[n][k], x & 0x00FF00FFu, x & 0x00F000F0u, y, y & 0x00F000F0u, pb[n][0], pb[n][1]);
                         }
                     }
                 }
                 // every lane has read the stage: its place takes the next one
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar0 + 64 + 8 * slot);
-                if (++slot == STAGES) {
-                    slot = 0;
-                    parity ^= 1u;
-                }
+                issue(slot);
+                slot = slot + 1 == STAGES ? 0 : slot + 1;
+            };
+            auto arrived = [&]() -> uint32_t {       // the oldest stage in flight
+                cp_async_wait<STAGES - 1>();
+                __syncwarp();
+                return (live >> (kBlk * (STAGES - 1))) & kFull;
             };
             int run = (min(end_blk, all_see >> 4) - cc.blk) & -kBlk;     // blocks that every row sees whole
             while (cc.blk < end_blk) {
-                uint32_t here = kFull;
-                while (run > 0) {
-                    ok = mbar_wait_warp(bar0 + 8 * slot, parity, a.wait_ns, &s_abort);
-                    if (!ok) break;
-                    here = here_of[warp][slot];
-                    if (here != kFull) break;
+                uint32_t here = arrived();
+                while (run > 0 && here == kFull) {
                     turn(std::false_type{}, kFull);
                     cc.blk += kBlk;
                     run -= kBlk;
+                    if (cc.blk >= end_blk) break;
+                    here = arrived();
                 }
-                if (!ok || cc.blk >= end_blk) break;
-                if (here == kFull) {
-                    ok = mbar_wait_warp(bar0 + 8 * slot, parity, a.wait_ns, &s_abort);
-                    if (!ok) break;
-                    here = here_of[warp][slot];
-                }
+                if (cc.blk >= end_blk) break;
                 turn(std::true_type{}, here);
                 cc.blk = min(cc.blk + kBlk, end_blk);
                 run = max(0, run - kBlk);
             }
-            if (!ok) break;
             to_use -= end_blk - first_blk;
             // ---- end of the item or of the piece: sums over the lanes, results in the values' own scale
             const float f0 = pow2(11) * pow2(ev), f1 = f0 * 0.0625f;
+#pragma unroll
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    acc[n][i][0] -= acc[n][i][2];
+                    acc[n][i][1] -= acc[n][i][3];
+                }
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -807,10 +740,20 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const _
             if (to_use <= 0) break;
             next_item<kRows>(a, plan, cc);
         }
-        if (!ok && lane == 0) atomicExch(a.status, WIDE_ERR_TIMEOUT);
+        cp_async_wait_all();
     }
+    // rows that no item writes: KV heads that a sequence does not use, sequences that are left out
+    for (int s = blockIdx.x; s < a.q.n_seqs; s += gridDim.x) {
+        const SeqInfo i = wide_seq_info(a.q, s, a.c.page_shift);
+        const int per_row = a.n_q * (D / 8);
+        for (long long x = tid; x < static_cast<long long>(i.n_rows) * per_row; x += 32 * WARPS) {
+            const int r = static_cast<int>(x / per_row), v = static_cast<int>(x - static_cast<long long>(r) * per_row), h = v / (D / 8) / a.share;
+            if (!((plan.masks[s * a.plan_words + (h >> 5)] >> (h & 31)) & 1u))
+                reinterpret_cast<uint4*>(a.o + static_cast<size_t>(i.row0 + r) * a.n_q * D)[v] = make_uint4(0, 0, 0, 0);
+        }
+    }
+
     __syncthreads();
-    if (s_abort) return;
 
     // ---- join the warps' pieces of each item; what is still a piece goes to the second kernel
     int* meta = a.meta + blockIdx.x * 8;
@@ -858,7 +801,7 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const _
                                 : a.heads + static_cast<size_t>(blockIdx.x * WARPS + (tid >> 1)) * slot_floats(kRows, D);
         }
         __syncthreads();
-        join<kRows, D>(a, e_seq[w][e], e_kvh[w][e], e_rb[w][e], n, [&](int i) { return e_at[i]; }, dst, weights, 0, 1);
+        join<kRows, D>(a, e_seq[w][e], e_kvh[w][e], e_rb[w][e], n, [&](int i) { return e_at[i]; }, dst, tid, 32 * WARPS);
         __syncthreads();
         at = to;
     }
@@ -869,33 +812,65 @@ __global__ void __launch_bounds__(32 * (WARPS + 1), 1) attn_cache_kernel(const _
 }
 
 // Items that more than one CTA had a piece of: block c joins the one that begins in CTA c and goes on in the next.
+// A warp takes half a row's channels (a whole row of 64): lane e reads the maximum and sum of piece e.
 template <int ROWS, int D>
 __global__ void __launch_bounds__(256) attn_cache_join_kernel(const __grid_constant__ AttnArgs a, int ctas) {
     grid_dep_wait();
-    __shared__ float2 weights[(kMaxCtas + 1) * ROWS];
-    __shared__ int count;
-    const int c = blockIdx.x, lane = threadIdx.x & 31;
-    if (*reinterpret_cast<volatile int*>(a.status) != WIDE_OK) return;   // some CTA gave up: its pieces are not there
+    const int c = blockIdx.x, lane = threadIdx.x & 31, unit = threadIdx.x >> 5;
+    // one round of loads: what does CTA c leave open, how far does it go (CTAs c + 1, ...:
+    // the first piece of each belongs to the item, up to the one that ends it)
     const int4 meta = *reinterpret_cast<const int4*>(a.meta + c * 8 + 4);
+    int st = c + 1 + lane < ctas ? a.meta[(c + 1 + lane) * 8] : 0;
     if (meta.x != 1) return;
-    if (threadIdx.x < 32) {    // CTAs c + 1, ...: the first piece of each belongs to the item, up to the one that ends it
-        int n = 1;
-        for (int k = c + 1;; k += 32) {
-            const int st = k + lane < ctas ? a.meta[(k + lane) * 8] : 0;
-            const uint32_t stop = __ballot_sync(0xffffffffu, st != 1);
-            if (stop) {
-                const int at = __ffs(stop) - 1;
-                n += at + (__shfl_sync(0xffffffffu, st, at) == 2 ? 1 : 0);
-                break;
-            }
-            n += 32;
+    int n = 1;
+    for (int k = c + 1;;) {
+        const uint32_t stop = __ballot_sync(0xffffffffu, st != 1);
+        if (stop) {
+            const int at = __ffs(stop) - 1;
+            n += at + (__shfl_sync(0xffffffffu, st, at) == 2 ? 1 : 0);
+            break;
         }
-        if (lane == 0) count = n;
+        n += 32;
+        k += 32;
+        st = k + lane < ctas ? a.meta[(k + lane) * 8] : 0;
     }
-    __syncthreads();
-    join<ROWS, D>(a, meta.y, meta.z, meta.w, count, [&](int i) -> const float* {
+    const SeqInfo info = wide_seq_info(a.q, meta.y, a.c.page_shift);
+    auto piece = [&](int i) -> const float* {
         return a.parts + static_cast<size_t>(i == 0 ? 2 * c + 1 : 2 * (c + i)) * slot_floats(ROWS, D);
-    }, nullptr, weights, blockIdx.y, gridDim.y);
+    };
+    constexpr int kHalves = D / 64;
+    for (int u = unit + 8 * blockIdx.y; u < ROWS * kHalves; u += 8 * gridDim.y) {
+        const int r = u / kHalves, d = u % kHalves * 64 + 2 * lane;
+        const RowOut ro = row_out(a, info, meta.z, meta.w * ROWS + r, D);
+        if (!ro.o) continue;
+        float m = -CUDART_INF_F, l = 0.f;
+        float2 x = make_float2(0.f, 0.f);
+        for (int e0 = 0; e0 < n; e0 += 32) {
+            const float2 ml = e0 + lane < n ? *reinterpret_cast<const float2*>(piece(e0 + lane) + ROWS * D + 2 * r) : make_float2(-CUDART_INF_F, 0.f);
+            float top = ml.x;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float m_new = fmaxf(m, top), m_use = m_new == -CUDART_INF_F ? 0.f : m_new;
+            const float old = exp2_fast(m - m_use), w = exp2_fast(ml.x - m_use);
+            float sum = ml.y * w;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            l = fmaf(l, old, sum);
+            x = make_float2(x.x * old, x.y * old);
+            m = m_new;
+            const int last = min(32, n - e0);
+#pragma unroll 8
+            for (int e = 0; e < last; ++e) {
+                const float2 v = *reinterpret_cast<const float2*>(piece(e0 + e) + r * D + d);
+                const float we = __shfl_sync(0xffffffffu, w, e);
+                x = make_float2(fmaf(v.x, we, x.x), fmaf(v.y, we, x.y));
+            }
+        }
+        const float inv = ro.on && l != 0.f ? 1.f / l : 0.f;
+        __nv_bfloat162 b = __floats2bfloat162_rn(0.f, 0.f);
+        if (inv != 0.f) b = __floats2bfloat162_rn(x.x * inv, x.y * inv);
+        *reinterpret_cast<__nv_bfloat162*>(ro.o + d) = b;
+    }
 }
 
 struct Work {
@@ -921,10 +896,10 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     constexpr int kRows = 8 * NB;
     constexpr int stage = kBlk * (16 * D + 128 * (D / G));
     constexpr int room = 227 * 1024 - 5120 - kPlanSmem;   // 5 KB for the static arrays
-    // with the feeding warp 16 warps, of 128 registers or less each, which two blocks of eight query rows do not fit
-    constexpr int W = NB == 2 ? 7 : 15 * 3 * stage <= room ? 15 : 11;
+    // 16 warps have 128 registers each, which two blocks of eight query rows do not fit
+    constexpr int W = NB == 2 ? 8 : 16 * 3 * stage <= room ? 16 : 12;
     constexpr int S = room / (W * stage) > 6 ? 6 : room / (W * stage);
-    static_assert(S >= 3 && S * stage >= slot_floats(kRows, D) * 4 && W * S <= 32 * (W + 1), "ring");
+    static_assert(S >= 3 && S * stage >= slot_floats(kRows, D) * 4, "ring");
     auto kernel = attn_cache_kernel<D, G, NB, W, S>;
     const int smem = kPlanSmem + W * S * stage;
     const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
@@ -942,7 +917,7 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     WIDE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     {
         WideLaunch l(ctx, s, "attn_cache");
-        kernel<<<ctas, 32 * (W + 1), smem, s>>>(a);
+        kernel<<<ctas, 32 * W, smem, s>>>(a);
         WIDE_CUDA_CHECK(cudaGetLastError());
     }
     {
@@ -990,8 +965,7 @@ int wide_launch_attn_cache(wide_ctx* ctx, cudaStream_t s, const wide_cache* cach
     a.mask_bits = mask_bits;
     a.scale_log2e = scale * 1.4426950408889634f;
     a.o = static_cast<__nv_bfloat16*>(o);
-    a.status = ctx->d_status;
-    a.wait_ns = ctx->wait_ns;
+    a.status = ctx->d_status + WIDE_STATUS_INDEX;
     a.plan_words = (cache->n_kv_heads + 31) / 32;
     // Rows of a sequence and KV head: `share` where a sequence has one new row, else an average (the lengths
     // are on the device).  Above eight, 16 rows share a pass over the cache.
