@@ -31,7 +31,9 @@ using namespace wptx;
 
 constexpr int kBlk = 2;            // blocks of a ring stage: 32 keys
 constexpr int kMaxCtas = 160;
-constexpr int kPlanSmem = 4096;    // bytes of shared memory for the plan of a small batch
+constexpr int kMeta = 8;           // words of meta of a partial result
+constexpr int kPlanSmem = 6144;    // bytes of shared memory for the plan of a small batch
+constexpr int kItemCost = 4;       // units that an item counts on top of its blocks: queries in, results out
 
 struct AttnArgs {
     CacheView c;
@@ -47,7 +49,7 @@ struct AttnArgs {
     unsigned char* plan;           // the plan in the workspace, or NULL: every CTA makes its own in shared memory
     float* heads;                  // partial results of warps whose first item began before their piece
     float* parts;                  // [CTA][2] partial results of CTAs
-    int* meta;                     // [CTA][2][4] {0 / 1 / 2: none, more follows, last piece; sequence, KV head, row block}
+    int* meta;                     // [CTA][2][kMeta] {0 / 1 / 2: none, more follows, last piece; first row, rows, KV head, row block}
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -98,20 +100,21 @@ __device__ __forceinline__ void prefetch_l2(const void* p, size_t bytes) {
 }
 
 // ------------------------------------------------------------------------------------------------ the plan
-// offsets[s] = units (16-key blocks of items) of the sequences before s, masks[s] = KV heads in use.
+// offsets[s] = units of the sequences before s (an item: kItemCost and its 16-key blocks), masks[s] = KV heads in use.
 struct Plan {
     long long* offsets;
-    uint32_t *masks, *groups;
+    int4* seqs;                 // first row, rows, length, row blocks; rows 0 where there is nothing to do
+    uint32_t *masks, *groups;   // groups: only on the way to the masks
 };
 __device__ __forceinline__ Plan plan_at(unsigned char* p, int n_seqs, int plan_words) {
-    uint32_t* m = reinterpret_cast<uint32_t*>(p + 8 * (n_seqs + 1));
-    return Plan{reinterpret_cast<long long*>(p), m, m + n_seqs * plan_words};
+    int4* q = reinterpret_cast<int4*>(p);
+    long long* o = reinterpret_cast<long long*>(q + n_seqs);
+    uint32_t* m = reinterpret_cast<uint32_t*>(o + n_seqs + 1);
+    return Plan{o, q, m, m + n_seqs * plan_words};
 }
 size_t plan_bytes(int n_seqs, int plan_words, int words) {
-    return 8 * static_cast<size_t>(n_seqs + 1) + 4 * static_cast<size_t>(n_seqs) * (plan_words + words);
+    return 24 * static_cast<size_t>(n_seqs) + 8 + 4 * static_cast<size_t>(n_seqs) * (plan_words + words);
 }
-
-__device__ __forceinline__ int row_blocks(int n_rows, int share, int rows_per) { return (n_rows * share + rows_per - 1) / rows_per; }
 
 // Two rounds of loads (lengths, masks; one thread a sequence), then arithmetic.  Up to 16 new rows are looked at
 // for the KV heads in use; of more rows all heads are taken.
@@ -120,38 +123,43 @@ __device__ void make_plan(const AttnArgs& a, const Plan& p, long long* part, boo
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = blockDim.x >> 5;
     const int per = (a.q.n_seqs + blockDim.x - 1) / blockDim.x;
     const int s0 = min(a.q.n_seqs, tid * per), s1 = min(a.q.n_seqs, s0 + per);
+    const bool direct = a.share == a.hpg;      // a group is the query heads of one KV head
     for (int s = s0; s < s1; ++s) {
         const SeqInfo i = wide_seq_info(a.q, s, a.c.page_shift);
         if (i.bad && report) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
         const bool some = i.n_rows > 0 && i.len > 0;
         const int looked = a.mask_bits && i.n_rows <= 16 ? i.n_rows : 0;
+        p.seqs[s] = make_int4(i.row0, i.n_rows, i.len, some ? (i.n_rows * a.share + ROWS - 1) / ROWS : 0);
+        uint32_t* out = direct ? p.masks + s * a.plan_words : p.groups + s * a.words;
         for (int w = 0; w < a.words; ++w) {      // groups that any new row uses
             uint32_t m = some && looked == 0 ? 0xffffffffu : 0u;
             if (some)
                 for (int r = 0; r < looked; ++r) m |= a.mask_bits[static_cast<size_t>(i.row0 + r) * a.words + w];
-            p.groups[s * a.words + w] = m;
+            const int left = a.c.n_kv_heads - 32 * w;
+            out[w] = direct && left < 32 ? m & ((1u << left) - 1u) : m;
         }
-        p.offsets[s] = some ? static_cast<long long>((i.len + 15) >> 4) * row_blocks(i.n_rows, a.share, ROWS) : 0;   // of one head
     }
-    __syncthreads();
-    for (int x = warp; x < a.q.n_seqs * a.plan_words; x += n_warps) {     // lanes are KV heads
-        const int s = x / a.plan_words, w = x - s * a.plan_words, h = 32 * w + lane;
-        bool any = false;
-        if (h < a.c.n_kv_heads) {
-            const int g1 = (h * a.share + a.share - 1) / a.hpg;
-            for (int g = h * a.share / a.hpg; g <= g1; ++g) any |= (p.groups[s * a.words + (g >> 5)] >> (g & 31)) & 1u;
+    if (!direct) {
+        __syncthreads();
+        for (int x = warp; x < a.q.n_seqs * a.plan_words; x += n_warps) {     // lanes are KV heads
+            const int s = x / a.plan_words, w = x - s * a.plan_words, h = 32 * w + lane;
+            bool any = false;
+            if (h < a.c.n_kv_heads) {
+                const int g1 = (h * a.share + a.share - 1) / a.hpg;
+                for (int g = h * a.share / a.hpg; g <= g1; ++g) any |= (p.groups[s * a.words + (g >> 5)] >> (g & 31)) & 1u;
+            }
+            const uint32_t m = __ballot_sync(0xffffffffu, any);
+            if (lane == 0) p.masks[x] = m;
         }
-        const uint32_t m = __ballot_sync(0xffffffffu, any);
-        if (lane == 0) p.masks[x] = m;
+        __syncthreads();
     }
-    __syncthreads();
     long long sum = 0;
     for (int s = s0; s < s1; ++s) {
         int used = 0;
         for (int w = 0; w < a.plan_words; ++w) used += __popc(p.masks[s * a.plan_words + w]);
-        const long long n = p.offsets[s] * used;
+        const int4 i = p.seqs[s];
         p.offsets[s] = sum;
-        sum += n;
+        sum += static_cast<long long>(used * i.w) * (((i.z + 15) >> 4) + kItemCost);
     }
     long long up = sum;
 #pragma unroll
@@ -177,10 +185,11 @@ __global__ void __launch_bounds__(1024) attn_cache_plan_kernel(AttnArgs a) {
     make_plan<ROWS>(a, plan_at(a.plan, a.q.n_seqs, a.plan_words), part, true);
 }
 
-// A place on the line of units: block `blk` of an item.
+// The part of an item that lies in a piece of the line: blocks [blk, end).  left: units of the piece behind it.
 struct Cursor {
     int seq, kvh, rb;      // the item
-    int blk, n_blk, n_rb;
+    int blk, end, left;
+    int n_blk, n_rb;       // blocks of an item of this sequence, row blocks of it
 };
 
 __device__ __forceinline__ int next_head(const AttnArgs& a, const Plan& p, int seq, int from) {
@@ -192,15 +201,35 @@ __device__ __forceinline__ int next_head(const AttnArgs& a, const Plan& p, int s
     return -1;
 }
 
-template <int ROWS>
-__device__ __forceinline__ void enter_seq(const AttnArgs& a, Cursor& k) {
-    const SeqInfo i = wide_seq_info(a.q, k.seq, a.c.page_shift);
-    k.n_blk = (i.len + 15) >> 4;
-    k.n_rb = row_blocks(i.n_rows, a.share, ROWS);
+// the cursor's item from unit `pos` on
+__device__ __forceinline__ void take(Cursor& k, int pos) {
+    const int to = min(k.n_blk + kItemCost, pos + k.left);
+    k.left -= to - pos;
+    k.blk = max(0, pos - kItemCost);
+    k.end = max(0, to - kItemCost);
 }
 
-template <int ROWS>
-__device__ __noinline__ Cursor locate(const AttnArgs& a, const Plan& p, long long u) {
+// to the next item of the piece that has blocks in it; the caller knows that units are left
+__device__ __forceinline__ void next_item(const AttnArgs& a, const Plan& p, Cursor& k) {
+    do {
+        if (++k.rb >= k.n_rb) {
+            k.rb = 0;
+            k.kvh = next_head(a, p, k.seq, k.kvh + 1);
+            if (k.kvh < 0) {
+                do ++k.seq;
+                while (k.seq + 1 < a.q.n_seqs && p.offsets[k.seq + 1] == p.offsets[k.seq]);
+                const int4 i = p.seqs[k.seq];
+                k.n_blk = (i.z + 15) >> 4;
+                k.n_rb = i.w;
+                k.kvh = next_head(a, p, k.seq, 0);
+            }
+        }
+        take(k, 0);
+    } while (k.blk >= k.end && k.left > 0);
+}
+
+// units [u, u + n) of the line
+__device__ __forceinline__ Cursor locate(const AttnArgs& a, const Plan& p, long long u, int n) {
     Cursor k;
     int lo = 0, hi = a.q.n_seqs - 1;   // the last sequence that starts at or before u: it holds u
     while (lo < hi) {
@@ -209,83 +238,86 @@ __device__ __noinline__ Cursor locate(const AttnArgs& a, const Plan& p, long lon
         else hi = mid - 1;
     }
     k.seq = lo;
-    enter_seq<ROWS>(a, k);
+    const int4 i = p.seqs[lo];
+    k.n_blk = (i.z + 15) >> 4;
+    k.n_rb = i.w;
+    k.left = n;
     const long long r = u - p.offsets[lo];
-    int nth;
+    const int each = k.n_blk + kItemCost;
+    int nth, pos;
     if (r <= 0x7fffffffLL) {
-        const int r32 = static_cast<int>(r), item = r32 / k.n_blk;
-        k.blk = r32 - item * k.n_blk;
-        nth = k.n_rb == 1 ? item : item / k.n_rb;
-        k.rb = item - nth * k.n_rb;
+        nth = static_cast<int>(r) / each;
+        pos = static_cast<int>(r) - nth * each;
     } else {
-        const long long item = r / k.n_blk;
-        k.blk = static_cast<int>(r - item * k.n_blk);
-        nth = static_cast<int>(item / k.n_rb);
-        k.rb = static_cast<int>(item - static_cast<long long>(nth) * k.n_rb);
+        const long long item = r / each;
+        nth = static_cast<int>(item);          // heads * row blocks: far below 2^31
+        pos = static_cast<int>(r - item * each);
+    }
+    k.rb = 0;
+    if (k.n_rb > 1) {
+        k.rb = nth % k.n_rb;
+        nth /= k.n_rb;
     }
     k.kvh = next_head(a, p, lo, 0);
     for (; nth > 0; --nth) k.kvh = next_head(a, p, lo, k.kvh + 1);
+    take(k, pos);
+    if (k.blk >= k.end && k.left > 0) next_item(a, p, k);
     return k;
 }
 
-// to the first block of the next item; the caller knows that there is one
-template <int ROWS>
-__device__ __noinline__ void next_item(const AttnArgs& a, const Plan& p, Cursor& k) {
-    k.blk = 0;
-    if (++k.rb < k.n_rb) return;
-    k.rb = 0;
-    const int h = next_head(a, p, k.seq, k.kvh + 1);
-    if (h >= 0) {
-        k.kvh = h;
-        return;
-    }
-    do ++k.seq;
-    while (k.seq + 1 < a.q.n_seqs && p.offsets[k.seq + 1] == p.offsets[k.seq]);
-    enter_seq<ROWS>(a, k);
-    k.kvh = next_head(a, p, k.seq, 0);
+// Moves a warp's cursor, kept in shared memory, to its next item: blk | end << 32.  Out of line, since it runs rarely and is
+// wanted in several places; its state in registers would cost the inner loop.
+__device__ __noinline__ long long advance(const AttnArgs* a, Plan p, Cursor* at) {
+    __syncwarp();
+    Cursor k = *at;
+    next_item(*a, p, k);
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) *at = k;
+    __syncwarp();
+    return static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(k.end)) << 32 | static_cast<unsigned>(k.blk));
 }
 
-// What the epilogues need of a row of an item.
+// What the epilogues need of a row of an item: where its output goes (nullptr: the row does not exist), whether its group is on.
 struct RowOut {
-    __nv_bfloat16* o;   // nullptr: the row does not exist
+    __nv_bfloat16* o;
     bool on;
 };
-__device__ __forceinline__ RowOut row_out(const AttnArgs& a, const SeqInfo& i, int kvh, int rr, int head_dim) {
+__device__ __forceinline__ RowOut row_out(const AttnArgs& a, int row0, int n_rows, int kvh, int rr, int head_dim) {
     RowOut r;
     const int tok = rr / a.share, h = kvh * a.share + rr - tok * a.share;
-    r.o = tok < i.n_rows ? a.o + (static_cast<size_t>(i.row0 + tok) * a.n_q + h) * head_dim : nullptr;
-    r.on = r.o && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, i.row0 + tok, h / a.hpg));
+    r.o = tok < n_rows ? a.o + (static_cast<size_t>(row0 + tok) * a.n_q + h) * head_dim : nullptr;
+    r.on = r.o && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, row0 + tok, h / a.hpg));
     return r;
 }
 
 __host__ __device__ constexpr int slot_floats(int rows, int D) { return rows * (D + 4); }   // rows of D values, then m and l of each
 
-// Joins `n` partial results of one item, the e-th at at(e): out rows, or a partial again (dst).  A thread takes four
-// channels of a row.  Executed once a launch, so kept short: its time is that of fetching its instructions.
+// Joins the partial results of one item that the bits of `which` name (piece e at at(e)): out rows, or a partial again
+// (dst).  A thread takes four channels of a row.  Runs once a launch, so it is short: its time is that of fetching its instructions.
 template <int ROWS, int D, typename At>
-__device__ __forceinline__ void join(const AttnArgs& a, int seq, int kvh, int rb, int n, const At& at, float* dst, int first, int step) {
+__device__ __forceinline__ void join(const AttnArgs& a, int row0, int n_rows, int kvh, int rb, uint32_t which, const At& at, float* dst) {
 #pragma unroll 1
-    for (int i = first; i < ROWS * (D / 4); i += step) {
+    for (int i = threadIdx.x; i < ROWS * (D / 4); i += blockDim.x) {
         const int r = i / (D / 4), d = i % (D / 4) * 4;
         float m = -CUDART_INF_F, l = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int e = 0; e < n; ++e) m = fmaxf(m, at(e)[ROWS * D + 2 * r]);
+#pragma unroll 1
+        for (uint32_t b = which; b; b &= b - 1) m = fmaxf(m, at(__ffs(b) - 1)[ROWS * D + 2 * r]);
         const float m_use = m == -CUDART_INF_F ? 0.f : m;
-#pragma unroll 4
-        for (int e = 0; e < n; ++e) {
-            const float* p = at(e);
-            const float w = exp2_fast(p[ROWS * D + 2 * r] - m_use);
+#pragma unroll 1
+        for (uint32_t b = which; b; b &= b - 1) {
+            const float* p = at(__ffs(b) - 1);
+            const float2 ml = *reinterpret_cast<const float2*>(p + ROWS * D + 2 * r);
             const float4 v = *reinterpret_cast<const float4*>(p + r * D + d);
-            l = fmaf(p[ROWS * D + 2 * r + 1], w, l);
+            const float w = exp2_fast(ml.x - m_use);
+            l = fmaf(ml.y, w, l);
             x = make_float4(fmaf(v.x, w, x.x), fmaf(v.y, w, x.y), fmaf(v.z, w, x.z), fmaf(v.w, w, x.w));
         }
         if (dst) {
             *reinterpret_cast<float4*>(dst + r * D + d) = x;
             if (d == 0) *reinterpret_cast<float2*>(dst + ROWS * D + 2 * r) = make_float2(m, l);
         } else {
-            const SeqInfo info = wide_seq_info(a.q, seq, a.c.page_shift);
-            const RowOut ro = row_out(a, info, kvh, rb * ROWS + r, D);
+            const RowOut ro = row_out(a, row0, n_rows, kvh, rb * ROWS + r, D);
             if (!ro.o) continue;
             const float inv = ro.on && l != 0.f ? 1.f / l : 0.f;
             uint2 w = make_uint2(0, 0);
@@ -312,7 +344,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
     __shared__ long long part[WARPS];
     // per warp two partial results: [0] of an item that began before the piece (in global memory), [1] of the
     // piece's last item (over the ring).  state: 0 none, else 1 | begins here << 1 | ends here << 2
-    __shared__ const float* e_at[WARPS];        // the pieces of one item, at most one of a warp
+    __shared__ Cursor cursors[WARPS][2];
     __shared__ int e_state[WARPS][2], e_seq[WARPS][2], e_kvh[WARPS][2], e_rb[WARPS][2];
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -339,33 +371,38 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
         u1 = u0 + each + (warp < extra ? 1 : 0);
     }
     if (u0 < u1) {
-        Cursor cc = locate<kRows>(a, plan, u0), ic = cc;     // used, requested
-        int to_use = static_cast<int>(u1 - u0), to_issue = to_use, slot = 0;
+        {
+            const Cursor k = locate(a, plan, u0, static_cast<int>(u1 - u0));
+            if (lane == 0) cursors[warp][0] = cursors[warp][1] = k;
+            __syncwarp();
+        }
+        Cursor &cc = cursors[warp][0], &ic = cursors[warp][1];     // used, requested
+        int blk = cc.blk, end_blk = cc.end, ic_blk = blk, ic_end = end_blk;
+        int slot = 0;
         uint32_t live = 0;             // kBlk bits a stage, newest lowest: which of its blocks have a page
-        int pt_seq = -1, pt_first = 0, pt = 0;   // page numbers [pt_first, pt_first + 32) of sequence pt_seq, one a lane
+        int pt_first = -1000000, pt = 0;         // page numbers [pt_first, pt_first + 32) of the requested sequence, one a lane
         const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
         const uint32_t ring_a = smem_u32(smem + kPlanSmem) + warp * (STAGES * kStage);
         const uint32_t lane16 = lane * 16, params = 16 * D + 4 * kNS * g;
         // request the next stage, up to kBlk blocks of one item, into place `to` (a group of copies even where nothing is left)
         auto issue = [&](int to) {
             uint32_t m = 0;
-            if (to_issue > 0) {
-                const int nb = min(min(kBlk, ic.n_blk - ic.blk), to_issue);
-                const int last = (ic.blk + nb - 1) >> sub_shift;
-                if (pt_seq != ic.seq || last - pt_first >= 32 || (ic.blk >> sub_shift) < pt_first) {
-                    pt_seq = ic.seq;
-                    pt_first = ic.blk >> sub_shift;
+            if (ic_blk < ic_end) {
+                const int nb = min(kBlk, ic_end - ic_blk);
+                const int first = ic_blk >> sub_shift, last = (ic_blk + nb - 1) >> sub_shift;
+                if (last - pt_first >= 32) {
+                    pt_first = first;
                     pt = pt_first + lane < a.q.max_pages ? a.q.page_table[static_cast<size_t>(ic.seq) * a.q.max_pages + pt_first + lane] : -1;
                 }
+                const int kvh = ic.kvh;
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
                     if (b < nb) {
-                        const int blk = ic.blk + b;
-                        const int page = __shfl_sync(0xffffffffu, pt, (blk >> sub_shift) - pt_first);
+                        const int page = __shfl_sync(0xffffffffu, pt, ((ic_blk + b) >> sub_shift) - pt_first);
                         if (static_cast<unsigned>(page) < static_cast<unsigned>(a.c.n_pages)) {
                             m |= 1u << b;
                             const unsigned char* from = a.c.pages + lane16 +
-                                (((static_cast<size_t>(page) * a.c.n_kv_heads + ic.kvh) << sub_shift) + (blk & sub_mask)) * kSB;
+                                (((static_cast<size_t>(page) * a.c.n_kv_heads + kvh) << sub_shift) + ((ic_blk + b) & sub_mask)) * kSB;
                             const uint32_t dst = ring_a + to * kStage + b * kSB + lane16;
 #pragma unroll
                             for (int i = 0; i < kPieces; ++i)
@@ -373,42 +410,49 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         }
                     }
                 }
-                if (m != (1u << max(nb, 0)) - 1u && lane == 0) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
-                ic.blk += nb;
-                to_issue = nb > 0 ? to_issue - nb : 0;       // nb <= 0: a length changed under the running kernel
-                if (ic.blk >= ic.n_blk && to_issue > 0) next_item<kRows>(a, plan, ic);
+                if (m != (1u << nb) - 1u && lane == 0) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
+                ic_blk += nb;
+                if (ic_blk >= ic_end && ic.left > 0) {
+                    const long long next = advance(&a, plan, &ic);
+                    ic_blk = static_cast<int>(next);
+                    ic_end = static_cast<int>(next >> 32);
+                    pt_first = -1000000;
+                }
             }
             cp_async_commit();
             live = (live << kBlk) | m;
         };
+        uint4 qw[NB][kSteps / 2];      // the query rows of the item at hand: 8 channels of every 32
+        auto load_queries = [&]() {
+            const int4 info = plan.seqs[cc.seq];     // first row, rows, length
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const int rr = cc.rb * kRows + 8 * n + g, tok = rr / a.share, h = cc.kvh * a.share + rr - tok * a.share;
+#pragma unroll
+                for (int i = 0; i < kSteps / 2; ++i) {
+                    qw[n][i] = make_uint4(0, 0, 0, 0);
+                    if (tok < info.y) qw[n][i] = *reinterpret_cast<const uint4*>(a.qm + (info.x + tok) * a.qs + h * D + 32 * i + 8 * t);
+                }
+            }
+        };
+        load_queries();
 #pragma unroll 1
         for (int i = 0; i < STAGES; ++i) issue(i);
 
-        while (true) {
+        while (blk < end_blk) {
             // ---- an item, or the part of it that lies in this piece
-            const SeqInfo info = wide_seq_info(a.q, cc.seq, a.c.page_shift);
-            const int first_blk = cc.blk;
-            const int end_blk = min(cc.n_blk, cc.blk + to_use);
-            if (end_blk <= first_blk) break;
+            const int first_blk = blk;
             uint32_t qf[NB][kSteps][2];
             float qsum[NB][kNS][2], qscale[NB][2];   // of this lane's score columns 2t, 2t + 1
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                const int rr = cc.rb * kRows + 8 * n + g, tok = rr / a.share, h = cc.kvh * a.share + rr - tok * a.share;
-                uint4 qw[kSteps / 2];      // 8 channels of every 32
-#pragma unroll
-                for (int i = 0; i < kSteps / 2; ++i) {
-                    qw[i] = make_uint4(0, 0, 0, 0);
-                    if (tok < info.n_rows)
-                        qw[i] = *reinterpret_cast<const uint4*>(a.qm + (info.row0 + tok) * a.qs + h * D + 32 * i + 8 * t);
-                }
                 uint32_t top = 0;
                 float sum[kNS];
 #pragma unroll
                 for (int i = 0; i < kNS; ++i) sum[i] = 0.f;
 #pragma unroll
                 for (int i = 0; i < kSteps / 2; ++i) {
-                    const uint32_t x[4] = {qw[i].x, qw[i].y, qw[i].z, qw[i].w};
+                    const uint32_t x[4] = {qw[n][i].x, qw[n][i].y, qw[n][i].z, qw[n][i].w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         top = max(top, max((x[e] << 16) & 0x7FFFFFFFu, x[e] & 0x7FFF0000u));   // orders NaN above all numbers
@@ -427,7 +471,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 const float down = pow2(-e);
 #pragma unroll
                 for (int i = 0; i < kSteps / 2; ++i) {
-                    const uint32_t x[4] = {qw[i].x, qw[i].y, qw[i].z, qw[i].w};
+                    const uint32_t x[4] = {qw[n][i].x, qw[n][i].y, qw[n][i].z, qw[n][i].w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         // words 0, 1 of step 2i: channels 0, 1 and 2, 3 (whose codes come 16 times too large); 2, 3: step 2i + 1
@@ -446,7 +490,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 }
             }
             // keys before this are seen by every row of the item
-            const int all_see = a.causal ? min(info.len, info.len - info.n_rows + cc.rb * kRows / a.share + 1) : info.len;
+            const int4 info = plan.seqs[cc.seq];
+            const int all_see = a.causal ? min(info.z, info.z - info.y + cc.rb * kRows / a.share + 1) : info.z;
 
             float acc[NB][kSteps][4], m[NB][2], l[NB][2], pm[NB][kNS][2];
             int ev = -110;              // the exponent that the values' steps are relative to
@@ -469,7 +514,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
             auto turn = [&](auto masked_c, uint32_t here) {
                 constexpr bool masked = decltype(masked_c)::value;
                 const uint32_t base = ring_a + slot * kStage;
-                const int key0 = cc.blk << 4;
+                const int key0 = blk << 4;
+                const int4 info = masked ? plan.seqs[cc.seq] : make_int4(0, 0, 0, 0);
                 // ---- scores
                 // (A block that is not there is computed like the others, from whatever the ring holds, and left out by
                 // selection.  The blocks take turns: eight dependent instructions on one accumulator would wait for each other.)
@@ -524,7 +570,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                             s[b][n][e] = fmaf(s[b][n][e], qscale[n][e & 1], mins[b][n][e]);
                             if (masked) {
                                 const int row = cc.rb * kRows + 8 * n + 2 * t + (e & 1);
-                                const int last = a.causal ? min(info.len - 1, info.len - info.n_rows + row / a.share) : info.len - 1;
+                                const int last = a.causal ? min(info.z - 1, info.z - info.y + row / a.share) : info.z - 1;
                                 if (key0 + 16 * b + g + 8 * (e >> 1) > last || !((here >> b) & 1u)) s[b][n][e] = -CUDART_INF_F;
                             }
                         }
@@ -538,8 +584,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     for (int i = 0; i < kNS; ++i) {
                         if (masked) {   // nothing of a position behind the end may reach a sum
                             const bool is = (here >> b) & 1u;
-                            v0[b][i] = is && key0 + 16 * b + g < info.len ? v0[b][i] : 0u;
-                            v1[b][i] = is && key0 + 16 * b + g + 8 < info.len ? v1[b][i] : 0u;
+                            v0[b][i] = is && key0 + 16 * b + g < info.z ? v0[b][i] : 0u;
+                            v1[b][i] = is && key0 + 16 * b + g + 8 < info.z ? v1[b][i] : 0u;
                         }
                         big = max(big, max(v0[b][i] << 16, v1[b][i] << 16));
                     }
@@ -653,22 +699,21 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 __syncwarp();
                 return (live >> (kBlk * (STAGES - 1))) & kFull;
             };
-            int run = (min(end_blk, all_see >> 4) - cc.blk) & -kBlk;     // blocks that every row sees whole
-            while (cc.blk < end_blk) {
+            int run = (min(end_blk, all_see >> 4) - blk) & -kBlk;     // blocks that every row sees whole
+            while (blk < end_blk) {
                 uint32_t here = arrived();
                 while (run > 0 && here == kFull) {
                     turn(std::false_type{}, kFull);
-                    cc.blk += kBlk;
+                    blk += kBlk;
                     run -= kBlk;
-                    if (cc.blk >= end_blk) break;
+                    if (blk >= end_blk) break;
                     here = arrived();
                 }
-                if (cc.blk >= end_blk) break;
+                if (blk >= end_blk) break;
                 turn(std::true_type{}, here);
-                cc.blk = min(cc.blk + kBlk, end_blk);
+                blk = min(blk + kBlk, end_blk);
                 run = max(0, run - kBlk);
             }
-            to_use -= end_blk - first_blk;
             // ---- end of the item or of the piece: sums over the lanes, results in the values' own scale
             const float f0 = pow2(11) * pow2(ev), f1 = f0 * 0.0625f;
 #pragma unroll
@@ -688,13 +733,13 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 #pragma unroll
                         for (int i = 0; i < kNS; ++i) pm[n][i][c] += __shfl_xor_sync(0xffffffffu, pm[n][i][c], o);
                     }
-            const bool begins = first_blk == 0, ends = end_blk == cc.n_blk;
+            const bool begins = first_blk == 0, ends = end_blk == cc.n_blk, tail = cc.left == 0;
             if (begins && ends) {
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const RowOut ro = row_out(a, info, cc.kvh, cc.rb * kRows + 8 * n + 2 * t + c, D);
+                        const RowOut ro = row_out(a, info.x, info.y, cc.kvh, cc.rb * kRows + 8 * n + 2 * t + c, D);
                         if (!ro.o) continue;
                         const float r = ro.on && l[n][c] != 0.f ? 1.f / l[n][c] : 0.f;
 #pragma unroll
@@ -710,8 +755,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         }
                     }
             } else {
-                const bool tail = to_use == 0;    // the ring is free now
-                float* dst = tail ? reinterpret_cast<float*>(smem + kPlanSmem + warp * (STAGES * kStage)) : a.heads + static_cast<size_t>(blockIdx.x * WARPS + warp) * slot_floats(kRows, D);
+                float* dst = tail ?    // the ring is free now
+                                  reinterpret_cast<float*>(smem + kPlanSmem + warp * (STAGES * kStage)) : a.heads + static_cast<size_t>(blockIdx.x * WARPS + warp) * slot_floats(kRows, D);
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -737,77 +782,64 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     e_rb[warp][e] = cc.rb;
                 }
             }
-            if (to_use <= 0) break;
-            next_item<kRows>(a, plan, cc);
+            if (tail) break;
+            const long long next = advance(&a, plan, &cc);
+            blk = static_cast<int>(next);
+            end_blk = static_cast<int>(next >> 32);
+            if (blk < end_blk) load_queries();
         }
         cp_async_wait_all();
     }
     // rows that no item writes: KV heads that a sequence does not use, sequences that are left out
     for (int s = blockIdx.x; s < a.q.n_seqs; s += gridDim.x) {
-        const SeqInfo i = wide_seq_info(a.q, s, a.c.page_shift);
+        const int4 i = plan.seqs[s];
         const int per_row = a.n_q * (D / 8);
-        for (long long x = tid; x < static_cast<long long>(i.n_rows) * per_row; x += 32 * WARPS) {
+        for (long long x = tid; x < static_cast<long long>(i.y) * per_row; x += 32 * WARPS) {
             const int r = static_cast<int>(x / per_row), v = static_cast<int>(x - static_cast<long long>(r) * per_row), h = v / (D / 8) / a.share;
             if (!((plan.masks[s * a.plan_words + (h >> 5)] >> (h & 31)) & 1u))
-                reinterpret_cast<uint4*>(a.o + static_cast<size_t>(i.row0 + r) * a.n_q * D)[v] = make_uint4(0, 0, 0, 0);
+                reinterpret_cast<uint4*>(a.o + static_cast<size_t>(i.x + r) * a.n_q * D)[v] = make_uint4(0, 0, 0, 0);
         }
     }
-
     __syncthreads();
 
     // ---- join the warps' pieces of each item; what is still a piece goes to the second kernel
-    int* meta = a.meta + blockIdx.x * 8;
-    bool out[2] = {false, false};
-    int at = 0;
-    while (at < 2 * WARPS) {
-        const int w = at >> 1, e = at & 1, st = e_state[w][e];
-        if (!st) {
-            ++at;
-            continue;
-        }
-        // the pieces that follow, up to the one that ends the item or the CTA
-        int end = st, n = 1;
-        int to = at + 1;
-        uint32_t which = 1u << at;
-        if (!(st & 4)) {
-            for (; to < 2 * WARPS; ++to) {
-                const int s2 = e_state[to >> 1][to & 1];
-                if (!s2) continue;
-                which |= 1u << to;
-                ++n;
-                end = s2;
-                if (s2 & 4) {
-                    ++to;
-                    break;
-                }
-            }
-        }
-        const bool begins = (st & 2) != 0, ends = (end & 4) != 0;
+    const int st = lane < 2 * WARPS ? e_state[lane >> 1][lane & 1] : 0;
+    const uint32_t any = __ballot_sync(0xffffffffu, st != 0), begin_bits = __ballot_sync(0xffffffffu, (st & 2) != 0),
+                   end_bits = __ballot_sync(0xffffffffu, (st & 4) != 0);
+    int* meta = a.meta + blockIdx.x * 2 * kMeta;
+    bool open[2] = {false, false};
+#pragma unroll 1
+    for (uint32_t rest = any; rest;) {
+        // the next piece and those that follow, up to the one that ends the item or the CTA
+        const int at = __ffs(rest) - 1;
+        const uint32_t stop = end_bits & rest;
+        const uint32_t which = stop ? rest & (0xffffffffu >> (32 - __ffs(stop))) : rest;
+        rest &= ~which;
+        const bool begins = (begin_bits >> at) & 1u, ends = stop != 0;
+        const int seq = e_seq[at >> 1][at & 1], kvh = e_kvh[at >> 1][at & 1], rb = e_rb[at >> 1][at & 1];
+        const int4 info = plan.seqs[seq];
         float* dst = nullptr;
         if (!(begins && ends)) {
             const int slot = begins ? 1 : 0;
-            out[slot] = true;
+            open[slot] = true;
             dst = a.parts + static_cast<size_t>(blockIdx.x * 2 + slot) * slot_floats(kRows, D);
             if (tid == 0) {
-                meta[4 * slot] = ends ? 2 : 1;
-                meta[4 * slot + 1] = e_seq[w][e];
-                meta[4 * slot + 2] = e_kvh[w][e];
-                meta[4 * slot + 3] = e_rb[w][e];
+                int* m = meta + kMeta * slot;
+                m[0] = ends ? 2 : 1;
+                m[1] = info.x;
+                m[2] = info.y;
+                m[3] = kvh;
+                m[4] = rb;
             }
         }
-        if (tid < 2 * WARPS && ((which >> tid) & 1u)) {
-            const int i = __popc(which & ((1u << tid) - 1u));
-            e_at[i] = (tid & 1) ? reinterpret_cast<const float*>(smem + kPlanSmem + static_cast<size_t>(tid >> 1) * STAGES * kStage)
-                                : a.heads + static_cast<size_t>(blockIdx.x * WARPS + (tid >> 1)) * slot_floats(kRows, D);
-        }
-        __syncthreads();
-        join<kRows, D>(a, e_seq[w][e], e_kvh[w][e], e_rb[w][e], n, [&](int i) { return e_at[i]; }, dst, tid, 32 * WARPS);
-        __syncthreads();
-        at = to;
+        join<kRows, D>(a, info.x, info.y, kvh, rb, which, [&](int x) -> const float* {
+            return (x & 1) ? reinterpret_cast<const float*>(smem + kPlanSmem + (x >> 1) * (STAGES * kStage))
+                           : a.heads + static_cast<size_t>(blockIdx.x * WARPS + (x >> 1)) * slot_floats(kRows, D);
+        }, dst);
     }
     if (tid == 0) {
-        if (!out[0]) meta[0] = 0;
-        if (!out[1]) meta[4] = 0;
+        if (!open[0]) meta[0] = 0;
+        if (!open[1]) meta[kMeta] = 0;
     }
 }
 
@@ -819,8 +851,10 @@ __global__ void __launch_bounds__(256) attn_cache_join_kernel(const __grid_const
     const int c = blockIdx.x, lane = threadIdx.x & 31, unit = threadIdx.x >> 5;
     // one round of loads: what does CTA c leave open, how far does it go (CTAs c + 1, ...:
     // the first piece of each belongs to the item, up to the one that ends it)
-    const int4 meta = *reinterpret_cast<const int4*>(a.meta + c * 8 + 4);
-    int st = c + 1 + lane < ctas ? a.meta[(c + 1 + lane) * 8] : 0;
+    const int* mine = a.meta + (2 * c + 1) * kMeta;
+    const int4 meta = *reinterpret_cast<const int4*>(mine);
+    const int rb = mine[4];
+    int st = c + 1 + lane < ctas ? a.meta[2 * (c + 1 + lane) * kMeta] : 0;
     if (meta.x != 1) return;
     int n = 1;
     for (int k = c + 1;;) {
@@ -832,16 +866,15 @@ __global__ void __launch_bounds__(256) attn_cache_join_kernel(const __grid_const
         }
         n += 32;
         k += 32;
-        st = k + lane < ctas ? a.meta[(k + lane) * 8] : 0;
+        st = k + lane < ctas ? a.meta[2 * (k + lane) * kMeta] : 0;
     }
-    const SeqInfo info = wide_seq_info(a.q, meta.y, a.c.page_shift);
     auto piece = [&](int i) -> const float* {
         return a.parts + static_cast<size_t>(i == 0 ? 2 * c + 1 : 2 * (c + i)) * slot_floats(ROWS, D);
     };
     constexpr int kHalves = D / 64;
     for (int u = unit + 8 * blockIdx.y; u < ROWS * kHalves; u += 8 * gridDim.y) {
         const int r = u / kHalves, d = u % kHalves * 64 + 2 * lane;
-        const RowOut ro = row_out(a, info, meta.z, meta.w * ROWS + r, D);
+        const RowOut ro = row_out(a, meta.y, meta.z, meta.w, rb * ROWS + r, D);
         if (!ro.o) continue;
         float m = -CUDART_INF_F, l = 0.f;
         float2 x = make_float2(0.f, 0.f);
@@ -886,7 +919,7 @@ Work work_layout() {
     w.parts = at;
     at += wide_align_up(static_cast<size_t>(kMaxCtas) * 2 * slot_floats(16, 128) * 4, 256);
     w.meta = at;
-    at += static_cast<size_t>(kMaxCtas) * 8 * 4;
+    at += static_cast<size_t>(kMaxCtas) * 2 * kMeta * 4;
     w.total = wide_align_up(at, 256);
     return w;
 }
@@ -895,7 +928,7 @@ template <int D, int G, int NB>
 int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     constexpr int kRows = 8 * NB;
     constexpr int stage = kBlk * (16 * D + 128 * (D / G));
-    constexpr int room = 227 * 1024 - 5120 - kPlanSmem;   // 5 KB for the static arrays
+    constexpr int room = 227 * 1024 - 3072 - kPlanSmem;   // 3 KB for the static arrays
     // 16 warps have 128 registers each, which two blocks of eight query rows do not fit
     constexpr int W = NB == 2 ? 8 : 16 * 3 * stage <= room ? 16 : 12;
     constexpr int S = room / (W * stage) > 6 ? 6 : room / (W * stage);
