@@ -16,113 +16,206 @@ namespace {
 
 constexpr int kWarps = 8;
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// 8 neighbouring channels as they lie in memory
+template <typename T> struct Raw8;
+template <> struct Raw8<__nv_bfloat16> {
+    uint4 v;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void clear() { v = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
     }
+    // smallest and largest of LW lanes, NaN if any is: one register holds the minimum and the negated maximum
+    template <int LW>
+    __device__ __forceinline__ void range(float& lo, float& hi) const {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+        const __nv_bfloat162 a = __hmin2_nan(__hmin2_nan(h[0], h[1]), __hmin2_nan(h[2], h[3]));
+        const __nv_bfloat162 b = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+        __nv_bfloat162 both = __halves2bfloat162(__hmin_nan(__low2bfloat16(a), __high2bfloat16(a)), __hneg(__hmax_nan(__low2bfloat16(b), __high2bfloat16(b))));
+#pragma unroll
+        for (int o = 1; o < LW; o <<= 1) {
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&both), o);
+            both = __hmin2_nan(both, *reinterpret_cast<const __nv_bfloat162*>(&other));
+        }
+        lo = __low2float(both);
+        hi = -__high2float(both);
+    }
+};
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float c;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+    return c;
 }
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float c;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+    return c;
 }
+template <> struct Raw8<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = __ldg(reinterpret_cast<const float4*>(p));
+        b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    }
+    __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+    template <int LW>
+    __device__ __forceinline__ void range(float& lo, float& hi) const {
+        lo = min_nan(min_nan(min_nan(a.x, a.y), min_nan(a.z, a.w)), min_nan(min_nan(b.x, b.y), min_nan(b.z, b.w)));
+        hi = max_nan(max_nan(max_nan(a.x, a.y), max_nan(a.z, a.w)), max_nan(max_nan(b.x, b.y), max_nan(b.z, b.w)));
+#pragma unroll
+        for (int o = 1; o < LW; o <<= 1) {
+            lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+            hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+        }
+    }
+};
 
 // sign-correct a - b - c for c near a - b: d = a - b rounded, e its exact remainder (two-sum)
-template <typename F>
-__device__ __forceinline__ F exact_gap(F a, F b, F c) {
-    const F d = a - b;
-    const F bb = d - a;
-    const F e = (a - (d - bb)) + ((-b) - bb);
+__device__ __forceinline__ double exact_gap(double a, double b, double c) {
+    const double d = a - b;
+    const double bb = d - a;
+    const double e = (a - (d - bb)) + ((-b) - bb);
     return (d - c) + e;
 }
 
-// Levels of 8 channels of a sub-group that spans LW lanes: code e in bits 4e.  Returns the parameter word.
-// The definition is exact (how many borders does x reach), so the same input always gives the same code
-// whatever the order of evaluation.  The border nearest to x is found in fp32 (2^-21 off at most, a
-// border and a half apart from the next one), and x is compared with that one exactly: (i + 1/2) s has 13
-// bits, x - m is a two-sum.  Scale: 15 c has 12 bits, so the smallest bf16 c with 15 c >= max - m is also
-// found by exact comparison.  Magnitudes at which fp32 overflows or has few bits left go through fp64.
-template <int LW>
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], uint32_t& codes) {
-    float lo = x[0], hi = x[0];
-    bool finite = fabsf(x[0]) <= 3.4028234e38f;
-#pragma unroll
-    for (int i = 1; i < 8; ++i) {
-        lo = fminf(lo, x[i]);
-        hi = fmaxf(hi, x[i]);
-        finite = finite && fabsf(x[i]) <= 3.4028234e38f;
-    }
-    int ok = finite ? 1 : 0;
-#pragma unroll
-    for (int o = 1; o < LW; o <<= 1) {
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        ok &= __shfl_xor_sync(0xffffffffu, ok, o);
-    }
-    codes = 0;
-    if (!ok) return 0x7FC07FC0u;
-    // bf16 at or below lo: towards zero for positive numbers, away from it for negative ones
+// Sub-groups that the fast way below leaves out: not finite, all channels alike, magnitudes at which fp32 overflows
+// or has few bits left, a minimum whose low bits are out of reach of the borders.  x: parameter word, y: codes.
+template <int LW, typename T>
+__device__ __noinline__ uint2 quantise8_any(Raw8<T> raw) {
+    float lo, hi, x[8];
+    raw.template range<LW>(lo, hi);
+    raw.get(x);
     lo += 0.f;   // zeros are +0
     hi += 0.f;
-    const uint32_t lb = __float_as_uint(lo);
-    const uint32_t mb = (lo < 0.f ? lb + 0xFFFFu : lb) & 0xFFFF0000u;
+    const uint32_t mb = (lo < 0.f ? __float_as_uint(lo) + 0xFFFFu : __float_as_uint(lo)) & 0xFFFF0000u;
     const float m = __uint_as_float(mb);
-    if (isinf(m)) return 0x7FC07FC0u;   // an fp32 minimum below the lowest bf16 number
-    const float kBig = 8.5070592e37f;   // 2^126
-    float s;
-    bool plain = fabsf(lo) < kBig && fabsf(hi) < kBig;
-    if (plain) {
-        const float q = (hi - m) * (1.f / 15.f) * 0.999999f;
-        uint32_t c = __float_as_uint(q) & 0xFFFF0000u;
-        if (exact_gap(hi, m, 15.f * __uint_as_float(c)) > 0.f) c += 0x10000u;
-        if (exact_gap(hi, m, 15.f * __uint_as_float(c)) > 0.f) c += 0x10000u;
-        s = __uint_as_float(c);
-        plain = s >= 1e-30f || s == 0.f;
-    }
-    if (!plain) {
-        const double q = (static_cast<double>(hi) - static_cast<double>(m)) / 15.0;
-        s = __uint_as_float((__float_as_uint(__double2float_ru(q)) + 0xFFFFu) & 0xFFFF0000u);
-    }
-    const uint32_t word = (__float_as_uint(s) >> 16) | mb;
-    if (s == 0.f) return word;
-    if (plain) {
-        const float rs = 1.f / s;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int i = min(static_cast<int>((x[e] - m) * rs), 14);
-            const float border = (static_cast<float>(i) + 0.5f) * s;
-            const uint32_t n = i + (exact_gap(x[e], m, border) >= 0.f ? 1 : 0);
-            codes |= n << (4 * e);
-        }
-    } else {
+    if (!(fabsf(m) <= 3.4e38f && hi <= 3.4028234e38f)) return make_uint2(0x7FC07FC0u, 0u);
+    const double q = (static_cast<double>(hi) - static_cast<double>(m)) / 15.0;
+    const float s = __uint_as_float((__float_as_uint(__double2float_ru(q)) + 0xFFFFu) & 0xFFFF0000u);
+    uint32_t c = 0;
 #pragma unroll 1
-        for (int i = 0; i < 15; ++i) {
-            const double border = (i + 0.5) * static_cast<double>(s);
+    for (int i = 0; i < 15 && s > 0.f; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                codes += exact_gap(static_cast<double>(x[e]), static_cast<double>(m), border) >= 0.0 ? 1u << (4 * e) : 0u;
-        }
+        for (int e = 0; e < 8; ++e)
+            c += exact_gap(static_cast<double>(x[e]), static_cast<double>(m), (i + 0.5) * static_cast<double>(s)) >= 0.0 ? 1u << (4 * e) : 0u;
+    return make_uint2((__float_as_uint(s) >> 16) | mb, c);
+}
+
+// two fp32 numbers at once
+__device__ __forceinline__ unsigned long long pair(float a, float b) {
+    unsigned long long p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+    return p;
+}
+__device__ __forceinline__ void unpair(unsigned long long p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long c;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(a), "l"(b));
+    return c;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ unsigned long long fma2_up(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long d;
+    asm("fma.rp.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+
+// Levels of 8 channels each of two tokens' sub-groups that span LW lanes: code e in bits 4e, the parameter word; false
+// where quantise8_any has to do it.
+//
+// The definition is exact (how many borders m + (i + 1/2) s does x reach), so the same input always gives the
+// same code.  What makes that cheap: for a number x and an exact y, x >= y holds iff x >= y rounded UP, and
+// y >= x iff y rounded DOWN is, and one fma rounds the exact border once.  So the level is guessed in fp32, rounded to
+// an integer by the addition of 2^23 and biased upwards by 2^-19 of itself, which leaves the right level or the one above
+// (the error is below 2^-21), and one comparison with the guess's lower border, n s + (m - s / 2), settles it.  Likewise the
+// scale, whose last level must reach the maximum.  The kernel is bound by the rate at which instructions issue, so the two
+// tokens share them: six a value.
+template <typename T>
+struct Levels {
+    float m, hi, s, mh, rs;
+    uint32_t c, mb;
+    bool fine;
+    template <int LW>
+    __device__ __forceinline__ void set(const Raw8<T>& raw) {
+        float lo;
+        raw.template range<LW>(lo, hi);
+        lo += 0.f;   // zeros are +0
+        mb = __float_as_uint(lo);
+        if (sizeof(T) == 4) mb = (lo < 0.f ? mb + 0xFFFFu : mb) & 0xFFFF0000u;   // bf16 at or below lo
+        m = __uint_as_float(mb);
+        c = __float_as_uint((hi - m) * (0.999999f / 15.f)) & 0xFFFF0000u;
+        c += __fmaf_rd(15.f, __uint_as_float(c), m) < hi ? 0x10000u : 0u;
+        c += __fmaf_rd(15.f, __uint_as_float(c), m) < hi ? 0x10000u : 0u;
+        s = __uint_as_float(c);
+        mh = fmaf(s, -0.5f, m);
+        const float kBig = 8.5070592e37f;   // 2^126
+        fine = fabsf(m) < kBig && hi < kBig && s >= 1e-30f && m - mh == 0.5f * s && fmaf(s, 0.5f, mh) == m;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rs) : "f"(s));
+        rs *= 1.0000019f;
     }
-    return word;
+};
+
+template <int LW, typename T>
+__device__ __forceinline__ void quantise_two(const Raw8<T>& r0, const Raw8<T>& r1, uint32_t& code0, uint32_t& code1, uint32_t& word0,
+                                             uint32_t& word1, bool& fine0, bool& fine1) {
+    Levels<T> a, b;
+    a.template set<LW>(r0);
+    b.template set<LW>(r1);
+    float x[8], y[8];
+    r0.get(x);
+    r1.get(y);
+    constexpr float kMagic = 8388608.f;   // 2^23: its bits plus n are those of 2^23 + n
+    const unsigned long long m2 = pair(-a.m, -b.m), rs2 = pair(a.rs, b.rs), s2 = pair(a.s, b.s), mh2 = pair(a.mh, b.mh),
+                             magic2 = pair(kMagic, kMagic), back2 = pair(-kMagic, -kMagic);
+    code0 = code1 = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const unsigned long long u = fma2(add2(pair(x[e], y[e]), m2), rs2, magic2);
+        const unsigned long long border = fma2_up(add2(u, back2), s2, mh2);
+        float u0, u1, b0, b1;
+        unpair(u, u0, u1);
+        unpair(border, b0, b1);
+        uint32_t n0 = __float_as_uint(u0), n1 = __float_as_uint(u1);
+        if (x[e] < b0) --n0;
+        if (y[e] < b1) --n1;
+        code0 = n0 * (1u << (4 * e)) + code0;
+        code1 = n1 * (1u << (4 * e)) + code1;
+    }
+    code0 -= 0xFB000000u;     // the bits of 2^23 that the eight codes left in the word
+    code1 -= 0xFB000000u;
+    word0 = (a.c >> 16) | a.mb;
+    word1 = (b.c >> 16) | b.mb;
+    fine0 = a.fine;
+    fine1 = b.fine;
 }
 
 // Which block a warp's unit is.  With row_start NULL a unit is (sequence, head); else the CTA sums the
 // sequences' block counts once and every warp finds its sequence by bisection.
 struct Unit {
-    SeqInfo info;
+    int row0, first, len;   // rows from row0 on are positions [first, len)
     int seq, block, head;
+    bool some, bad;
 };
 
-__device__ __forceinline__ int blocks_of(const SeqInfo& i) {
-    return i.n_rows > 0 && i.len > 0 ? ((i.len - 1) >> 4) - ((i.len - i.n_rows) >> 4) + 1 : 0;
+__device__ __forceinline__ int blocks_of(int n_rows, int len) {
+    return n_rows > 0 && len > 0 ? ((len - 1) >> 4) - ((len - n_rows) >> 4) + 1 : 0;
 }
 
-// offsets[s] = blocks of the sequences before s; returns the total.  All threads of the CTA.
-__device__ int scan_blocks(const SeqView& q, int page_shift, int* offsets, int* part, int* status) {
+// seqs[s] = {first row, rows, length, blocks of the sequences before s}; returns the total.  All threads of the CTA.
+__device__ int scan_blocks(const SeqView& q, int page_shift, int4* seqs, int* part, int* status) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (q.n_seqs + 32 * kWarps - 1) / (32 * kWarps);
     const int a = min(q.n_seqs, tid * per), b = min(q.n_seqs, a + per);
@@ -130,8 +223,8 @@ __device__ int scan_blocks(const SeqView& q, int page_shift, int* offsets, int* 
     for (int s = a; s < b; ++s) {
         const SeqInfo i = wide_seq_info(q, s, page_shift);
         if (i.bad && blockIdx.x == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
-        offsets[s] = sum;
-        sum += blocks_of(i);
+        seqs[s] = make_int4(i.row0, i.n_rows, i.len, sum);
+        sum += blocks_of(i.n_rows, i.len);
     }
     int up = sum;
 #pragma unroll
@@ -147,137 +240,167 @@ __device__ int scan_blocks(const SeqView& q, int page_shift, int* offsets, int* 
         if (w < warp) base += part[w];
         total += part[w];
     }
-    for (int s = a; s < b; ++s) offsets[s] += base;
+    for (int s = a; s < b; ++s) seqs[s].w += base;
     __syncthreads();
     return total;
 }
 
-__device__ __forceinline__ Unit find_unit(const SeqView& q, const CacheView& c, const int* offsets, int unit) {
+__device__ __forceinline__ Unit find_unit(const SeqView& q, const CacheView& c, const int4* seqs, int unit) {
     Unit u;
     const int i = unit / c.n_kv_heads;
     u.head = unit - i * c.n_kv_heads;
     u.seq = i;
     u.block = 0;
+    u.bad = false;
+    int n_rows;
     if (q.row_start) {
         int lo = 0, hi = q.n_seqs - 1;   // the last sequence that starts at or before block i
         while (lo < hi) {
             const int mid = (lo + hi + 1) >> 1;
-            if (offsets[mid] <= i) lo = mid;
+            if (seqs[mid].w <= i) lo = mid;
             else hi = mid - 1;
         }
+        const int4 f = seqs[lo];
         u.seq = lo;
-        u.block = i - offsets[lo];
+        u.block = i - f.w;
+        u.row0 = f.x;
+        u.len = f.z;
+        n_rows = f.y;
+    } else {
+        const SeqInfo f = wide_seq_info(q, i, c.page_shift);
+        u.row0 = f.row0;
+        u.len = f.len;
+        n_rows = f.n_rows;
+        u.bad = f.bad;
     }
-    u.info = wide_seq_info(q, u.seq, c.page_shift);
-    if (blocks_of(u.info) > 0) u.block += (u.info.len - u.info.n_rows) >> 4;
+    u.first = u.len - n_rows;
+    u.some = blocks_of(n_rows, u.len) > 0;
+    if (u.some) u.block += u.first >> 4;
     return u;
 }
 
+// A warp takes the keys or the values of a block (32 registers of loads in flight for bf16; with both, half as many
+// warps fit: 8188 tokens of 8 heads took 27 us instead).
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 3 : 2)
 cache_write_kernel(CacheView c, SeqView q, const T* __restrict__ k, const T* __restrict__ v, long long ks, long long vs,
                    int* __restrict__ status) {
     constexpr int kLT = D / 8;        // lanes of a token
     constexpr int kP = 32 / kLT;      // tokens a warp loads at once
     constexpr int kLW = G / 8;        // lanes of a sub-group
     constexpr int kNS = D / G;
-    extern __shared__ int offsets[];
+    constexpr int kRounds = 16 / kP;
+    extern __shared__ int4 seqs[];
     __shared__ int part[kWarps];
     const int lane = threadIdx.x & 31, p = lane / kLT, u8 = lane % kLT;
     const int cc = u8 >> 2, c0 = cc >> 1, c1 = cc & 1;   // 32-channel chunk of this lane's 8 channels
     int total = q.n_seqs;
-    if (q.row_start) total = scan_blocks(q, c.page_shift, offsets, part, status);
-    const long long units = static_cast<long long>(total) * c.n_kv_heads;
+    if (q.row_start) total = scan_blocks(q, c.page_shift, seqs, part, status);
+    const long long units = 2LL * total * c.n_kv_heads;
     for (long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5); unit < units;
          unit += static_cast<long long>(gridDim.x) * kWarps) {
-        const Unit w = find_unit(q, c, offsets, static_cast<int>(unit));
-        const int first = w.info.len - w.info.n_rows;
-        if (!q.row_start && w.info.bad && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
-        if (blocks_of(w.info) == 0) continue;
+        const Unit w = find_unit(q, c, seqs, static_cast<int>(unit >> 1));
+        const bool values = unit & 1;
+        if (w.bad && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
+        if (!w.some) continue;
         uint8_t* blk = wide_cache_block(c, q, w.seq, w.block << 4, w.head);
         if (!blk) {
             if (lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
             continue;
         }
         const int p0 = w.block << 4;
-        auto row_of = [&](int r) { return static_cast<long long>(w.info.row0 + (p0 + r - first)); };
-        auto is_new = [&](int r) { return p0 + r >= first && p0 + r < w.info.len; };
-        const int col = w.head * D + 8 * u8;
-        // keys: tokens g and g + 8 share words
+        const T* src = (values ? v : k) + w.head * D + 8 * u8;
+        const long long stride = values ? vs : ks;
+        // Tokens whose codes share words meet in a lane: g and g + 8 for keys; 2t, 2t + 8, 2t + 1, 2t + 9 for values, as
+        // the rounds 4 t' .. 4 t' + 3.
+        Raw8<T> raw[kRounds];
+        uint32_t here = 0;            // bit i: the token of round i is new
+        auto token = [&](int i) {
+            return values ? 2 * ((i >> 2) * kP + p) + 8 * (i & 1) + ((i >> 1) & 1) : (i >> 1) * kP + p + 8 * (i & 1);
+        };
 #pragma unroll
-        for (int it = 0; it < 8 / kP; ++it) {
-            const int g = it * kP + p;
-            uint32_t code[2];
-            bool on[2];
+        for (int i = 0; i < kRounds; ++i) {
+            const int pos = p0 + token(i);
+            raw[i].clear();
+            if (pos >= w.first && pos < w.len) {
+                raw[i].load(src + static_cast<long long>(w.row0 + (pos - w.first)) * stride);
+                here |= 1u << i;
+            }
+        }
+        uint32_t* words = reinterpret_cast<uint32_t*>(blk + 16 * D + (values ? 64 * kNS : 0));
+        uint32_t code[kRounds];
+        uint32_t odd = 0;             // rounds that need the slow way (the lanes of a sub-group agree)
+#pragma unroll
+        for (int i = 0; i < kRounds; i += 2) {
+            uint32_t word[2];
+            bool fine[2];
+            quantise_two<kLW>(raw[i], raw[i + 1], code[i], code[i + 1], word[0], word[1], fine[0], fine[1]);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int r = g + 8 * h;
-                on[h] = is_new(r);
-                float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (on[h]) load8(k + row_of(r) * ks + col, x);
-                const uint32_t word = quantise8<kLW>(x, code[h]);
-                if (on[h] && u8 % kLW == 0)
-                    reinterpret_cast<uint32_t*>(blk + 16 * D)[r * kNS + u8 / kLW] = word;
+                if (!fine[h]) odd |= 1u << (i + h);
+                if (((here >> (i + h)) & 1u) && u8 % kLW == 0) words[token(i + h) * kNS + u8 / kLW] = word[h];
             }
-            uint32_t word[2];   // channels 0..3 and 4..7 of the lane
-            uint8_t* at = blk + ((c0 * 8 + g) * 4 + (u8 & 3)) * 16 + c1 * 8;
+        }
+        odd = __reduce_or_sync(0xffffffffu, odd & here);
+        while (odd) {                 // rare: read the token again
+            const int i = __ffs(odd) - 1;
+            odd &= odd - 1;
+            Raw8<T> again;
+            again.clear();
+            const bool on = (here >> i) & 1u;
+            if (on) again.load(src + static_cast<long long>(w.row0 + (p0 + token(i) - w.first)) * stride);
+            const uint2 r = quantise8_any<kLW>(again);
 #pragma unroll
-            for (int s1 = 0; s1 < 2; ++s1) {
-                uint32_t b[2];
+            for (int j = 0; j < kRounds; ++j)
+                if (j == i) code[j] = r.y;
+            if (on && u8 % kLW == 0) words[token(i) * kNS + u8 / kLW] = r.x;
+        }
+        if (!values) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t n = (code[h] >> (16 * s1)) & 0xFFFFu;
-                    b[h] = (n & 0xFu) | ((n >> 4) & 0xF0u) | ((n << 12) & 0xF0000u) | ((n << 8) & 0xF00000u);
-                }
-                word[s1] = b[0] | (b[1] << 8);
-                if (!(on[0] && on[1])) {
+            for (int i = 0; i < kRounds; i += 2) {
+                const bool on0 = (here >> i) & 1u, on1 = (here >> i) & 2u;
+                uint32_t word[2];     // channels 0..3 and 4..7 of the lane
+                uint8_t* at = blk + ((c0 * 8 + (i >> 1) * kP + p) * 4 + (u8 & 3)) * 16 + c1 * 8;
+#pragma unroll
+                for (int s1 = 0; s1 < 2; ++s1) {
+                    uint32_t b[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        if (on[h]) {
-                            at[4 * s1 + h] = static_cast<uint8_t>(b[h]);
-                            at[4 * s1 + 2 + h] = static_cast<uint8_t>(b[h] >> 16);
+                        const uint32_t n = code[i + h] >> (16 * s1);
+                        b[h] = (n & 0xFu) | ((n >> 4) & 0xF0u) | ((n << 12) & 0xF0000u) | ((n << 8) & 0xF00000u);
+                    }
+                    word[s1] = b[0] | (b[1] << 8);
+                    if (!(on0 && on1)) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (h == 0 ? on0 : on1) {
+                                at[4 * s1 + h] = static_cast<uint8_t>(b[h]);
+                                at[4 * s1 + 2 + h] = static_cast<uint8_t>(b[h] >> 16);
+                            }
                         }
                     }
                 }
+                if (on0 && on1) *reinterpret_cast<uint2*>(at) = make_uint2(word[0], word[1]);
             }
-            if (on[0] && on[1]) *reinterpret_cast<uint2*>(at) = make_uint2(word[0], word[1]);
-        }
-        // values: tokens 2t, 2t + 8, 2t + 1, 2t + 9 share words
+        } else {
 #pragma unroll
-        for (int it = 0; it < 4 / kP || it < 1; ++it) {
-            const int t = it * kP + p;
-            uint32_t code[4];
-            bool on[4];
+            for (int i = 0; i < kRounds; i += 4) {
+                const int t = (i >> 2) * kP + p;
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const int r = 2 * t + 8 * (h & 1) + (h >> 1);
-                on[h] = is_new(r);
-                float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (on[h]) load8(v + row_of(r) * vs + col, x);
-                const uint32_t word = quantise8<kLW>(x, code[h]);
-                if (on[h] && u8 % kLW == 0)
-                    reinterpret_cast<uint32_t*>(blk + 16 * D + 64 * kNS)[r * kNS + u8 / kLW] = word;
-            }
-            const bool all = on[0] && on[1] && on[2] && on[3];
+                for (int a = 0; a < 2; ++a) {   // 4 channels each
+                    uint8_t* at = blk + 8 * D + ((c0 * 8 + 2 * (u8 & 3) + a) * 4 + t) * 16 + c1 * 8;
+                    if (((here >> i) & 15u) == 15u) {
+                        // bytes a * 2 and a * 2 + 1 of the four codes
+                        const uint32_t x = __byte_perm(code[i], code[i + 1], a == 0 ? 0x5140 : 0x7362);
+                        const uint32_t y = __byte_perm(code[i + 2], code[i + 3], a == 0 ? 0x5140 : 0x7362);
+                        *reinterpret_cast<uint2*>(at) = make_uint2(__byte_perm(x, y, 0x5410), __byte_perm(x, y, 0x7632));
+                    } else {
 #pragma unroll
-            for (int a = 0; a < 2; ++a) {   // 4 channels each
-                const int g = 2 * (u8 & 3) + a;
-                uint8_t* at = blk + 8 * D + ((c0 * 8 + g) * 4 + t) * 16 + c1 * 8;
-                if (all) {
-                    uint32_t word[2];
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        const int sh = 16 * a + 8 * m;
-                        word[m] = ((code[0] >> sh) & 0xFFu) | (((code[1] >> sh) & 0xFFu) << 8) |
-                                  (((code[2] >> sh) & 0xFFu) << 16) | (((code[3] >> sh) & 0xFFu) << 24);
-                    }
-                    *reinterpret_cast<uint2*>(at) = make_uint2(word[0], word[1]);
-                } else {
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        if (on[h]) {
-                            at[h] = static_cast<uint8_t>(code[h] >> (16 * a));
-                            at[4 + h] = static_cast<uint8_t>(code[h] >> (16 * a + 8));
+                        for (int h = 0; h < 4; ++h) {
+                            if ((here >> (i + h)) & 1u) {
+                                at[h] = static_cast<uint8_t>(code[i + h] >> (16 * a));
+                                at[4 + h] = static_cast<uint8_t>(code[i + h] >> (16 * a + 8));
+                            }
                         }
                     }
                 }
@@ -315,23 +438,22 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
                   int* __restrict__ status) {
     constexpr int kNS = D / G;
     constexpr int kC = D / 64;
-    extern __shared__ int offsets[];
+    extern __shared__ int4 seqs[];
     __shared__ int part[kWarps];
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     int total = q.n_seqs;
-    if (q.row_start) total = scan_blocks(q, c.page_shift, offsets, part, status);
+    if (q.row_start) total = scan_blocks(q, c.page_shift, seqs, part, status);
     const long long units = static_cast<long long>(total) * c.n_kv_heads;
     for (long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5); unit < units;
          unit += static_cast<long long>(gridDim.x) * kWarps) {
-        const Unit w = find_unit(q, c, offsets, static_cast<int>(unit));
-        const int first = w.info.len - w.info.n_rows;
-        if (!q.row_start && w.info.bad && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
-        if (blocks_of(w.info) == 0) continue;
+        const Unit w = find_unit(q, c, seqs, static_cast<int>(unit));
+        if (w.bad && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
+        if (!w.some) continue;
         const uint8_t* blk = wide_cache_block(c, q, w.seq, w.block << 4, w.head);
         if (!blk && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
         const int p0 = w.block << 4;
-        auto row_of = [&](int r) { return static_cast<long long>(w.info.row0 + (p0 + r - first)); };
-        auto is_new = [&](int r) { return p0 + r >= first && p0 + r < w.info.len; };
+        auto row_of = [&](int r) { return static_cast<long long>(w.row0 + (p0 + r - w.first)); };
+        auto is_new = [&](int r) { return p0 + r >= w.first && p0 + r < w.len; };
         uint4 kw[kC], vw[kC];
 #pragma unroll
         for (int i = 0; i < kC; ++i) {
@@ -383,18 +505,22 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
 
 // CTAs for the most blocks that `rows` rows of these sequences can touch: a sequence's n rows lie in at
 // most n / 16 + 2 blocks, and in at most n.
-int grid_for(const wide_ctx* ctx, const CacheView& c, const SeqView& q) {
+int grid_for(const wide_ctx* ctx, const CacheView& c, const SeqView& q, int units_per_block) {
     const long long blocks = q.row_start ? min(static_cast<long long>(q.rows), q.rows / 16 + 2LL * q.n_seqs) : q.n_seqs;
-    const long long ctas = (blocks * c.n_kv_heads + kWarps - 1) / kWarps;
+    const long long ctas = (blocks * c.n_kv_heads * units_per_block + kWarps - 1) / kWarps;
     return static_cast<int>(max(1LL, min(ctas, 8LL * ctx->sm_count)));
 }
 
 template <typename T, int D, int G>
 int launch(wide_ctx* ctx, cudaStream_t s, bool write, const CacheView& c, const SeqView& q, void* k, void* v, long long ks,
            long long vs) {
-    const int grid = grid_for(ctx, c, q);
-    const size_t smem = q.row_start ? static_cast<size_t>(q.n_seqs) * sizeof(int) : 0;
+    const int grid = grid_for(ctx, c, q, write ? 2 : 1);
+    const size_t smem = q.row_start ? static_cast<size_t>(q.n_seqs) * sizeof(int4) : 0;
     int* status = ctx->d_status + WIDE_STATUS_INDEX;
+    if (smem > 48 * 1024) {
+        const void* kernel = write ? reinterpret_cast<const void*>(cache_write_kernel<T, D, G>) : reinterpret_cast<const void*>(cache_read_kernel<T, D, G>);
+        WIDE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WIDE_MAX_SEQS * sizeof(int4)));
+    }
     WideLaunch l(ctx, s, write ? "cache_write" : "cache_read");
     if (write)
         cache_write_kernel<T, D, G><<<grid, 32 * kWarps, smem, s>>>(c, q, static_cast<const T*>(k), static_cast<const T*>(v), ks, vs, status);
