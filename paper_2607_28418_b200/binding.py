@@ -7,6 +7,7 @@ or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional
 
@@ -453,17 +454,19 @@ def wide_unpermute(ctx: Context, src_packed: torch.Tensor, meta: Dict[str, torch
 
 
 # ------------------------------------------------------------------------------ rotary positions, the 4-bit cache
+# A decode step makes these calls for a few microseconds of GPU work, so they ask torch as little as they can.
 def _rows(t: torch.Tensor, width: int, what: str):
     """Address and row stride of a [rows, width] matrix whose rows may lie apart (a slice of a fused projection)."""
-    if t.dim() != 2 or t.shape[1] != width or (t.stride(1) != 1 and width > 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] != width or stride[1] != 1:
         raise ValueError(f"{what}: expected [rows, {width}] with contiguous rows")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else max(width, t.stride(0)))
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else max(width, stride[0]))
 
 
-def _same_device(ctx: Context, *tensors: Optional[torch.Tensor]):
+def _same_device(index: int, *tensors: Optional[torch.Tensor]):
     for t in tensors:
-        if t is not None and t.device != ctx.device:
-            raise ValueError(f"expected tensors on {ctx.device}, got one on {t.device}")
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"expected tensors on cuda:{index}, got one on {t.device}")
 
 
 def _int32(t: Optional[torch.Tensor], what: str):
@@ -474,24 +477,18 @@ def _int32(t: Optional[torch.Tensor], what: str):
     return t.data_ptr()
 
 
-class _on:
-    """The context's device as the current one for the length of a call, its current stream as the stream."""
-
-    def __init__(self, ctx: Context):
-        self.ctx, self.before = ctx, None
-
-    def __enter__(self):
-        now = torch.cuda.current_device()
-        if now != self.ctx.device.index:
-            self.before = now
-            torch.cuda.set_device(self.ctx.device)
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before is not None:
-            torch.cuda.set_device(self.before)
+def _on_device(call):
+    """The context's device as the current one for the length of a call."""
+    @functools.wraps(call)
+    def wrapped(ctx, *args, **kw):
+        if torch._C._cuda_getDevice() == ctx.device.index:
+            return call(ctx, *args, **kw)
+        with torch.cuda.device(ctx.device):
+            return call(ctx, *args, **kw)
+    return wrapped
 
 
+@functools.lru_cache(maxsize=None)
 def cache_page_bytes(page_size: int, n_kv_heads: int, head_dim: int, quant_group: int) -> int:
     """Bytes of one page of the 4-bit cache (0: the shape is not supported)."""
     return int(load_library().wide_cache_page_bytes(page_size, n_kv_heads, head_dim, quant_group))
@@ -501,17 +498,20 @@ class Cache:
     """The 4-bit cache of a layer: ``pages`` is any contiguous uint8 CUDA tensor of n_pages *
     cache_page_bytes(...) bytes, first dimension n_pages (see wide_cache in include/wide.h)."""
 
+    __slots__ = ("pages", "n_kv_heads", "head_dim", "quant_group", "page_size", "struct")
+
     def __init__(self, pages: torch.Tensor, n_kv_heads: int, head_dim: int, quant_group: int = 64, page_size: int = 64):
         if pages.dtype != torch.uint8 or not pages.is_contiguous() or pages.dim() < 2:
             raise ValueError("pages: expected a contiguous uint8 tensor, one page in the first dimension")
         size = cache_page_bytes(page_size, n_kv_heads, head_dim, quant_group)
         if size == 0:
             raise WideError(ERR_UNSUPPORTED_SHAPE, "Cache")
-        if pages.numel() != pages.shape[0] * size:
-            raise ValueError(f"pages: expected {size} bytes a page, got {pages.numel() // max(1, pages.shape[0])}")
+        n_pages = pages.shape[0]
+        if pages.numel() != n_pages * size:
+            raise ValueError(f"pages: expected {size} bytes a page, got {pages.numel() // max(1, n_pages)}")
         self.pages, self.n_kv_heads, self.head_dim = pages, n_kv_heads, head_dim
         self.quant_group, self.page_size = quant_group, page_size
-        self.struct = _CacheStruct(pages.data_ptr(), pages.shape[0], page_size, n_kv_heads, head_dim, quant_group)
+        self.struct = _CacheStruct(pages.data_ptr(), n_pages, page_size, n_kv_heads, head_dim, quant_group)
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, quant_group: int = 64, page_size: int = 64, device="cuda") -> "Cache":
@@ -525,19 +525,20 @@ class Sequences:
     """Where the sequences of a call lie (see wide_seqs): page_table int32 [n_seqs, max_pages], kv_lens
     int32 [n_seqs] (the new tokens included), row_start int32 [n_seqs + 1] or None (one new row each)."""
 
+    __slots__ = ("page_table", "kv_lens", "row_start", "n_seqs", "struct")
+
     def __init__(self, page_table: torch.Tensor, kv_lens: torch.Tensor, row_start: Optional[torch.Tensor] = None):
-        if page_table.dim() != 2 or kv_lens.shape != page_table.shape[:1]:
+        shape = page_table.shape
+        if len(shape) != 2 or kv_lens.shape != shape[:1]:
             raise ValueError("expected page_table [n_seqs, max_pages] and kv_lens [n_seqs]")
-        if row_start is not None and row_start.shape != (page_table.shape[0] + 1,):
+        if row_start is not None and row_start.shape != (shape[0] + 1,):
             raise ValueError("expected row_start [n_seqs + 1]")
-        self.page_table, self.kv_lens, self.row_start = page_table, kv_lens, row_start
+        self.page_table, self.kv_lens, self.row_start, self.n_seqs = page_table, kv_lens, row_start, shape[0]
         self.struct = _SeqsStruct(_int32(page_table, "page_table"), _int32(kv_lens, "kv_lens"), _int32(row_start, "row_start"),
-                                  page_table.shape[0], page_table.shape[1])
-
-    def tensors(self):
-        return self.page_table, self.kv_lens, self.row_start
+                                  shape[0], shape[1])
 
 
+@_on_device
 def wide_rope(ctx: Context, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, inv_freq: torch.Tensor,
               axis: Optional[torch.Tensor] = None, head_dim: int = 128, interleaved: bool = False, inverse: bool = False,
               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
@@ -546,96 +547,108 @@ def wide_rope(ctx: Context, q: torch.Tensor, k: Optional[torch.Tensor], position
     follows.  q_out = q / k_out = k rotate in place.  ``inverse`` rotates back, which is the gradient."""
     if q.dim() != 2 or (k is not None and (k.dim() != 2 or k.shape[0] != q.shape[0] or k.dtype != q.dtype)):
         raise ValueError("expected q [T, n_q_heads * head_dim] and k [T, n_kv_heads * head_dim] of one dtype")
-    T, wq, wk = q.shape[0], q.shape[1], 0 if k is None else k.shape[1]
-    if wq % head_dim or wk % head_dim:
+    (T, wq), wk = q.shape, 0 if k is None else k.shape[1]
+    if head_dim <= 0 or wq % head_dim or wk % head_dim:
         raise ValueError("q and k must hold whole heads")
-    if positions.shape[-1] != T or positions.dim() > 2:
+    where = positions.shape
+    if len(where) not in (1, 2) or where[-1] != T:
         raise ValueError("expected positions [T] or [n_axes, T]")
     if inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous() or (axis is not None and axis.shape != inv_freq.shape):
         raise ValueError("expected inv_freq float64 [rot_dim / 2] and axis of its shape")
     if q_out is None:
-        q_out = torch.empty((T, wq), dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None:
-        k_out = torch.empty((T, wk), dtype=k.dtype, device=k.device)
-    for a, b in ((q, q_out), (k, k_out)):
-        if (a is None) != (b is None) or (a is not None and (a.shape != b.shape or a.dtype != b.dtype)):
-            raise ValueError("an output must have its input's shape and dtype")
-    _same_device(ctx, q, k, positions, inv_freq, axis, q_out, k_out)
+        q_out = q.new_empty((T, wq))
+    elif q_out.shape != q.shape or q_out.dtype != q.dtype:
+        raise ValueError("q_out: expected q's shape and dtype")
+    if k is None:
+        if k_out is not None:
+            raise ValueError("k_out without k")
+    elif k_out is None:
+        k_out = k.new_empty((T, wk))
+    elif k_out.shape != k.shape or k_out.dtype != k.dtype:
+        raise ValueError("k_out: expected k's shape and dtype")
+    index = ctx.device.index
+    _same_device(index, q, k, positions, inv_freq, axis, q_out, k_out)
     (qp, qs), (qo, oqs) = _rows(q, wq, "q"), _rows(q_out, wq, "q_out")
     (kp, ks), (ko, oks) = ((None, 0), (None, 0)) if k is None else (_rows(k, wk, "k"), _rows(k_out, wk, "k_out"))
     flags = (FLAG_ROPE_INTERLEAVED if interleaved else 0) | (FLAG_ROPE_INVERSE if inverse else 0)
+    pos, ax = _int32(positions, "positions"), _int32(axis, "axis")
     if T == 0:
         return q_out, k_out
-    with _on(ctx) as stream:
-        rc = ctx.lib.wide_rope(ctx.handle, stream, qp, kp, _dtype_code(q), T, wq // head_dim, wk // head_dim, head_dim,
-                               2 * inv_freq.numel(), qs, ks, _int32(positions, "positions"),
-                               positions.shape[0] if positions.dim() == 2 else 1, inv_freq.data_ptr(), _int32(axis, "axis"), qo, ko,
-                               oqs, oks, flags)
-    _check(rc, "wide_rope")
+    rc = ctx.lib.wide_rope(ctx.handle, torch._C._cuda_getCurrentRawStream(index), qp, kp, _dtype_code(q), T, wq // head_dim,
+                           wk // head_dim, head_dim, 2 * inv_freq.numel(), qs, ks, pos, where[0] if len(where) == 2 else 1,
+                           inv_freq.data_ptr(), ax, qo, ko, oqs, oks, flags)
+    if rc != OK:
+        raise WideError(rc, "wide_rope")
     return q_out, k_out
 
 
-def wide_cache_write(ctx: Context, cache: Cache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor):
-    """Quantise and store the new rows k, v [rows, n_kv_heads * head_dim] (bf16 or fp32)."""
+def _move(ctx: Context, what: str, call, cache: Cache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor):
     if k.dtype != v.dtype or k.shape != v.shape:
         raise ValueError("k and v must have one shape and dtype")
-    _same_device(ctx, cache.pages, k, v, *seqs.tensors())
+    index = ctx.device.index
+    _same_device(index, cache.pages, k, v, seqs.page_table, seqs.kv_lens, seqs.row_start)
     width = cache.n_kv_heads * cache.head_dim
     (kp, ks), (vp, vs) = _rows(k, width, "k"), _rows(v, width, "v")
-    if k.shape[0] == 0 or seqs.struct.n_seqs == 0:
+    rows = k.shape[0]
+    if rows == 0 or seqs.n_seqs == 0:
         return
-    with _on(ctx) as stream:
-        rc = ctx.lib.wide_cache_write(ctx.handle, stream, ctypes.byref(cache.struct), ctypes.byref(seqs.struct), kp, vp,
-                                      _dtype_code(k), k.shape[0], ks, vs)
-    _check(rc, "wide_cache_write")
+    rc = call(ctx.handle, torch._C._cuda_getCurrentRawStream(index), ctypes.byref(cache.struct), ctypes.byref(seqs.struct), kp, vp,
+              _dtype_code(k), rows, ks, vs)
+    if rc != OK:
+        raise WideError(rc, what)
 
 
+@_on_device
+def wide_cache_write(ctx: Context, cache: Cache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor):
+    """Quantise and store the new rows k, v [rows, n_kv_heads * head_dim] (bf16 or fp32)."""
+    _move(ctx, "wide_cache_write", ctx.lib.wide_cache_write, cache, seqs, k, v)
+
+
+@_on_device
 def wide_cache_read(ctx: Context, cache: Cache, seqs: Sequences, rows: int, dtype: torch.dtype = torch.bfloat16,
                     k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
     """The values the cache holds for the sequences' new rows: returns (k, v) [rows, n_kv_heads * head_dim].
     Rows of no sequence are not written."""
     width = cache.n_kv_heads * cache.head_dim
     if k is None:
-        k = torch.empty((rows, width), dtype=dtype, device=cache.pages.device)
+        k = cache.pages.new_empty((rows, width), dtype=dtype)
     if v is None:
-        v = torch.empty((rows, width), dtype=dtype, device=cache.pages.device)
-    if k.dtype != v.dtype or k.shape[0] != rows or v.shape[0] != rows:
-        raise ValueError("k and v must have `rows` rows and one dtype")
-    _same_device(ctx, cache.pages, k, v, *seqs.tensors())
-    (kp, ks), (vp, vs) = _rows(k, width, "k"), _rows(v, width, "v")
-    if rows == 0 or seqs.struct.n_seqs == 0:
-        return k, v
-    with _on(ctx) as stream:
-        rc = ctx.lib.wide_cache_read(ctx.handle, stream, ctypes.byref(cache.struct), ctypes.byref(seqs.struct), kp, vp,
-                                     _dtype_code(k), rows, ks, vs)
-    _check(rc, "wide_cache_read")
+        v = cache.pages.new_empty((rows, width), dtype=dtype)
+    if k.shape[0] != rows:
+        raise ValueError("k and v must have `rows` rows")
+    _move(ctx, "wide_cache_read", ctx.lib.wide_cache_read, cache, seqs, k, v)
     return k, v
 
 
+@_on_device
 def wide_attn_cache(ctx: Context, q: torch.Tensor, cache: Cache, seqs: Sequences, n_q_heads: int, heads_per_group: int,
                     mask_bits: Optional[torch.Tensor] = None, causal: bool = True, scale: float = 0.0,
                     o: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Masked attention of the new rows q [rows, n_q_heads * head_dim] bf16 over the cache.  ``workspace``
     (uint8, attn_cache_workspace_bytes) replaces the context's own scratch, which calls on one stream share."""
-    rows, D = q.shape[0], cache.head_dim
+    width = n_q_heads * cache.head_dim
+    qp, qs = _rows(q, width, "q")
+    rows = q.shape[0]
     if o is None:
-        o = torch.empty((rows, n_q_heads * D), dtype=q.dtype, device=q.device)
-    if o.shape != (rows, n_q_heads * D) or o.dtype != q.dtype or not o.is_contiguous():
+        o = q.new_empty((rows, width))
+    elif o.shape != q.shape or o.dtype != q.dtype or not o.is_contiguous():
         raise ValueError("o: expected a contiguous tensor of q's shape and dtype")
     if mask_bits is not None and mask_bits.shape != (rows, (n_q_heads // max(1, heads_per_group) + 31) // 32):
         raise ValueError("mask_bits: expected [rows, ceil(n_groups / 32)]")
-    qp, qs = _rows(q, n_q_heads * D, "q")
-    ws = workspace
-    if ws is None:
-        ws = ctx.workspace(attn_cache_workspace_bytes(rows, n_q_heads, cache.n_kv_heads, D), slot=2)
-    _same_device(ctx, q, cache.pages, o, mask_bits, ws, *seqs.tensors())
-    if rows == 0 or seqs.struct.n_seqs == 0:
+    if workspace is None:      # one size serves every call, so this one stays where it is (captured graphs hold its address)
+        workspace = ctx._ws.get(2)
+        if workspace is None:
+            workspace = ctx.workspace(attn_cache_workspace_bytes(rows, n_q_heads, cache.n_kv_heads, cache.head_dim), slot=2)
+    index = ctx.device.index
+    _same_device(index, q, cache.pages, o, mask_bits, workspace, seqs.page_table, seqs.kv_lens, seqs.row_start)
+    bits = _int32(mask_bits, "mask_bits")
+    if rows == 0 or seqs.n_seqs == 0:
         return o
-    with _on(ctx) as stream:
-        rc = ctx.lib.wide_attn_cache(ctx.handle, stream, ctypes.byref(cache.struct), ctypes.byref(seqs.struct), qp, _dtype_code(q), rows,
-                                     qs, n_q_heads, heads_per_group, _int32(mask_bits, "mask_bits"), 1 if causal else 0, float(scale),
-                                     o.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(), 0)
-    _check(rc, "wide_attn_cache")
+    rc = ctx.lib.wide_attn_cache(ctx.handle, torch._C._cuda_getCurrentRawStream(index), ctypes.byref(cache.struct),
+                                 ctypes.byref(seqs.struct), qp, _dtype_code(q), rows, qs, n_q_heads, heads_per_group, bits,
+                                 1 if causal else 0, float(scale), o.data_ptr(), workspace.data_ptr(), workspace.nbytes, 0)
+    if rc != OK:
+        raise WideError(rc, "wide_attn_cache")
     return o
 
 

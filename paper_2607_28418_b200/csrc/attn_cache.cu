@@ -20,6 +20,7 @@
 //     CTA, then (at most two per CTA) by a second small kernel.  The order of joining is fixed.
 #include <math_constants.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "cache.cuh"
@@ -996,13 +997,21 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
         attn_cache_plan_kernel<kRows><<<1, 1024, 0, s>>>(a, ctas);
         WIDE_CUDA_CHECK(cudaGetLastError());
     }
-    WIDE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    // once a device; threads that come here together all set the same
+    static std::atomic<unsigned> set{0};
+    const unsigned bit = ctx->device < 32 ? 1u << ctx->device : 0u;
+    if (!(set.load(std::memory_order_relaxed) & bit) || !bit) {
+        WIDE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        set.fetch_or(bit, std::memory_order_relaxed);
+    }
     {
         WideLaunch l(ctx, s, "attn_cache");
         kernel<<<ctas, 32 * W, smem, s>>>(a);
         WIDE_CUDA_CHECK(cudaGetLastError());
     }
-    {
+    // Nothing to join where the plan is certain to give every item a CTA of its own (make_plan; rows / kRows + n_seqs row blocks at most).
+    const long long items = static_cast<long long>(a.c.n_kv_heads) * (static_cast<long long>(a.q.rows) * a.share / kRows + a.q.n_seqs);
+    if (items > ctas || (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) > kItemAlone) {
         WideLaunch l(ctx, s, "attn_cache_join");
         const dim3 grid(ctas, 2);
         if (ctx->prof) attn_cache_join_kernel<kRows, D><<<grid, 256, 0, s>>>(a, ctas);
