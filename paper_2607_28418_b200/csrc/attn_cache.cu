@@ -210,6 +210,8 @@ __device__ void make_plan(const AttnArgs& a, const Plan& p, long long* part, int
 template <int ROWS>
 __global__ void __launch_bounds__(1024) attn_cache_plan_kernel(AttnArgs a, int ctas) {
     __shared__ long long part[32];
+    grid_dep_launch();
+    grid_dep_wait();
     make_plan<ROWS>(a, plan_at(a.plan, a.q.n_seqs, a.plan_words), part, ctas, true);
 }
 
@@ -327,14 +329,16 @@ __host__ __device__ constexpr int slot_floats(int rows, int D) { return rows * (
 // (dst).  A thread takes four channels of a row.  Runs once a launch, so it is short: its time is that of fetching its instructions.
 template <int ROWS, int D, typename At>
 __device__ __forceinline__ void join(const AttnArgs& a, int row0, int n_rows, int kvh, int rb, uint32_t which, const At& at, float* dst) {
+    // two neighbouring threads share an element, each takes every other group of pieces
+    const int odd = threadIdx.x & 1;
 #pragma unroll 1
-    for (int i = threadIdx.x; i < ROWS * (D / 4); i += blockDim.x) {
+    for (int i = threadIdx.x >> 1; i < ROWS * (D / 4); i += blockDim.x >> 1) {      // a multiple of 16 elements: whole warps go on together
         const int r = i / (D / 4), d = i % (D / 4) * 4;
         float m = -CUDART_INF_F, l = 0.f;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
         // four pieces at a time, so that their loads overlap
 #pragma unroll 1
-        for (uint32_t b = which; b;) {
+        for (uint32_t b = which & (odd ? 0xF0F0F0F0u : 0x0F0F0F0Fu); b;) {
             float2 ml[4];
             float4 v[4];
             float top = m;
@@ -362,6 +366,17 @@ __device__ __forceinline__ void join(const AttnArgs& a, int row0, int n_rows, in
                 x = make_float4(fmaf(v[e].x, w, x.x), fmaf(v[e].y, w, x.y), fmaf(v[e].z, w, x.z), fmaf(v[e].w, w, x.w));
             }
         }
+        __syncwarp();
+        const float other = __shfl_xor_sync(0xffffffffu, m, 1), top = fmaxf(m, other), w = exp2_fast(m - (top == -CUDART_INF_F ? 0.f : top));
+        m = top;
+        l *= w;
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        x = make_float4(x.x * w, x.y * w, x.z * w, x.w * w);
+        x.x += __shfl_xor_sync(0xffffffffu, x.x, 1);
+        x.y += __shfl_xor_sync(0xffffffffu, x.y, 1);
+        x.z += __shfl_xor_sync(0xffffffffu, x.z, 1);
+        x.w += __shfl_xor_sync(0xffffffffu, x.w, 1);
+        if (odd) continue;
         if (dst) {
             *reinterpret_cast<float4*>(dst + r * D + d) = x;
             if (d == 0) *reinterpret_cast<float2*>(dst + ROWS * D + 2 * r) = make_float2(m, l);
@@ -398,6 +413,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     if (tid < 2 * WARPS) e_state[tid >> 1][tid & 1] = 0;
+    grid_dep_launch();     // the joining kernel may take its place as soon as CTAs end; it waits for all of them
+    grid_dep_wait();
     // All CTAs together bring what the plan will lead to (masks, page table, queries) into L2 while it is made.
     prefetch_l2(a.mask_bits, static_cast<size_t>(a.q.rows) * a.words * 4);
     prefetch_l2(a.q.page_table, static_cast<size_t>(a.q.n_seqs) * a.q.max_pages * 4);
@@ -485,9 +502,10 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 }
             }
         };
+        // The queries and the first stage go first: were all stages asked for at once, the first would arrive with the last.
         load_queries();
-#pragma unroll 1
-        for (int i = 0; i < STAGES; ++i) issue(i);
+        issue(0);
+        int primed = 1;
 
         while (blk < end_blk) {
             // ---- an item, or the part of it that lies in this piece
@@ -539,6 +557,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         qsum[n][i][c] = __shfl_sync(0xffffffffu, finite ? sum[i] * a.scale_log2e : CUDART_NAN_F, src);
                 }
             }
+#pragma unroll 1
+            for (; primed < STAGES; ++primed) issue(primed);
             // keys before this are seen by every row of the item
             const int4 info = plan.seqs[cc.seq];
             const int all_see = a.causal ? min(info.z, info.z - info.y + cc.rb * kRows / a.share + 1) : info.z;
@@ -929,7 +949,13 @@ __global__ void __launch_bounds__(256) attn_cache_join_kernel(const __grid_const
         float m = -CUDART_INF_F, l = 0.f;
         float2 x = make_float2(0.f, 0.f);
         for (int e0 = 0; e0 < n; e0 += 32) {
-            const float2 ml = e0 + lane < n ? *reinterpret_cast<const float2*>(piece(e0 + lane) + ROWS * D + 2 * r) : make_float2(-CUDART_INF_F, 0.f);
+            // all pieces' values are asked for together with their maxima and sums
+            const int last = min(32, n - e0);
+            const float2 ml = lane < last ? *reinterpret_cast<const float2*>(piece(e0 + lane) + ROWS * D + 2 * r) : make_float2(-CUDART_INF_F, 0.f);
+            float2 v[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+                v[e] = e < last ? *reinterpret_cast<const float2*>(piece(e0 + e) + r * D + d) : make_float2(0.f, 0.f);
             float top = ml.x;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -941,12 +967,10 @@ __global__ void __launch_bounds__(256) attn_cache_join_kernel(const __grid_const
             l = fmaf(l, old, sum);
             x = make_float2(x.x * old, x.y * old);
             m = m_new;
-            const int last = min(32, n - e0);
-#pragma unroll 8
-            for (int e = 0; e < last; ++e) {
-                const float2 v = *reinterpret_cast<const float2*>(piece(e0 + e) + r * D + d);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
                 const float we = __shfl_sync(0xffffffffu, w, e);
-                x = make_float2(fmaf(v.x, we, x.x), fmaf(v.y, we, x.y));
+                x = make_float2(fmaf(v[e].x, we, x.x), fmaf(v[e].y, we, x.y));
             }
         }
         const float inv = ro.on && l != 0.f ? 1.f / l : 0.f;
@@ -1006,7 +1030,8 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     }
     {
         WideLaunch l(ctx, s, "attn_cache");
-        kernel<<<ctas, 32 * W, smem, s>>>(a);
+        if (ctx->prof) kernel<<<ctas, 32 * W, smem, s>>>(a);
+        else WIDE_CUDA_CHECK(wide_launch_dependent(kernel, dim3(ctas), dim3(32 * W), smem, s, a));
         WIDE_CUDA_CHECK(cudaGetLastError());
     }
     // Nothing to join where the plan is certain to give every item a CTA of its own (make_plan; rows / kRows + n_seqs row blocks at most).

@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = 64;
-constexpr int kMaxTile = 4;      // tokens of a CTA
+constexpr int kMaxTile = 4;      // tokens of a CTA (16384 tokens of 80 heads, bf16: 133 us with 1, 119 with 2, 113 with 4, 117 with 8)
 
 template <typename T> struct Vec8;   // 8 channels as the memory holds them
 template <> struct Vec8<__nv_bfloat16> {
@@ -77,6 +77,32 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
     __shared__ __align__(16) float2 cs[kMaxTile][kMaxPairs];
     const int pairs = a.rot / 2, tid = threadIdx.x;
     const int t0 = blockIdx.x * a.tile, nt = min(a.tile, a.tokens - t0);
+    // A unit is 8 pairs of one head: two 8-channel pieces, rot / 2 apart or neighbours.  A thread has the same pairs of
+    // every (kThreads / kUnits)-th head of the tile's tokens in turn.
+    constexpr int kUnits = D / 16, kStep = kThreads / kUnits;
+    const int heads = a.n_q + a.n_kv, j = tid % kUnits;
+    const bool turned = 16 * j < a.rot;
+    const int lo = (turned && !a.interleaved) ? 8 * j : 16 * j;
+    const int hi = (turned && !a.interleaved) ? 8 * j + pairs : 16 * j + 8;
+    int t = 0, head = tid / kUnits;
+    auto wrap = [&]() {
+        while (head >= heads) {
+            head -= heads;
+            ++t;
+        }
+    };
+    auto from = [&]() {
+        const long long row = t0 + t;
+        return head < a.n_q ? static_cast<const T*>(a.q) + row * a.qs + head * D : static_cast<const T*>(a.k) + row * a.ks + (head - a.n_q) * D;
+    };
+    wrap();
+    // the first unit is on its way while the angles are worked out, each later one while its predecessor turns
+    Vec8<T> u, w;
+    if (t < nt) {
+        const T* src = from();
+        u.load(src + lo);
+        w.load(src + hi);
+    }
     if (tid < pairs) {
         double f = a.inv_freq[tid] * 0.15915494309189533577;   // 1 / (2 pi)
         f -= floor(f);
@@ -84,11 +110,11 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
     }
     __syncthreads();
     for (int i = tid; i < nt * pairs; i += kThreads) {
-        const int t = i / pairs, p = i - t * pairs;
+        const int tt = i / pairs, p = i - tt * pairs;
         const int ax = a.axis ? a.axis[p] : 0;
         float2 v = make_float2(1.f, 0.f);
         if (static_cast<unsigned>(ax) < static_cast<unsigned>(a.n_axes)) {
-            const long long pos = a.positions[static_cast<size_t>(ax) * a.tokens + t0 + t];
+            const long long pos = a.positions[static_cast<size_t>(ax) * a.tokens + t0 + tt];
             const unsigned long long phase = static_cast<unsigned long long>(pos) * turn[p];
             const float half_turns = static_cast<float>(static_cast<int>(phase >> 32)) * 4.656612873077393e-10f;   // 2^-31
             sincospif(half_turns, &v.y, &v.x);
@@ -96,35 +122,28 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
         } else {
             atomicExch(a.status, WIDE_ERR_BAD_INDEX);
         }
-        cs[t][p] = v;
+        cs[tt][p] = v;
     }
     __syncthreads();
-    // a unit is 8 pairs of one head: two 8-channel pieces, rot / 2 apart or neighbours
-    constexpr int kUnits = D / 16;
-    const int heads = a.n_q + a.n_kv, per_token = heads * kUnits;
-    for (int i = tid; i < nt * per_token; i += kThreads) {
-        const int t = i / per_token, r = i - t * per_token;
-        const int head = r / kUnits, j = r % kUnits;
-        const bool is_q = head < a.n_q;
-        const long long row = t0 + t;
-        const T* src = is_q ? static_cast<const T*>(a.q) + row * a.qs + head * D
-                            : static_cast<const T*>(a.k) + row * a.ks + (head - a.n_q) * D;
-        T* dst = is_q ? static_cast<T*>(a.q_out) + row * a.oqs + head * D
-                      : static_cast<T*>(a.k_out) + row * a.oks + (head - a.n_q) * D;
-        const bool turned = 16 * j < a.rot;
-        const int lo = (turned && !a.interleaved) ? 8 * j : 16 * j;
-        const int hi = (turned && !a.interleaved) ? 8 * j + pairs : 16 * j + 8;
-        Vec8<T> u, w;
-        u.load(src + lo);
-        w.load(src + hi);
+    while (t < nt) {
+        T* dst = (head < a.n_q ? static_cast<T*>(a.q_out) + (t0 + t) * a.oqs + head * D : static_cast<T*>(a.k_out) + (t0 + t) * a.oks + (head - a.n_q) * D);
+        const int tt = t;
+        Vec8<T> x8 = u, y8 = w;
+        head += kStep;
+        wrap();
+        if (t < nt) {
+            const T* src = from();
+            u.load(src + lo);
+            w.load(src + hi);
+        }
         if (turned) {
             float x[8], y[8];
-            u.get(x);
-            w.get(y);
+            x8.get(x);
+            y8.get(y);
             float2 c[8];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float4 two = *reinterpret_cast<const float4*>(&cs[t][8 * j + 2 * e]);
+                const float4 two = *reinterpret_cast<const float4*>(&cs[tt][8 * j + 2 * e]);
                 c[2 * e] = make_float2(two.x, two.y);
                 c[2 * e + 1] = make_float2(two.z, two.w);
             }
@@ -145,11 +164,11 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
                     y[e] = p * c[e].y + s * c[e].x;
                 }
             }
-            u.set(x);
-            w.set(y);
+            x8.set(x);
+            y8.set(y);
         }
-        u.store(dst + lo);
-        w.store(dst + hi);
+        x8.store(dst + lo);
+        y8.store(dst + hi);
     }
 }
 
