@@ -530,7 +530,7 @@ WIDE_API int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cach
  *   scale: multiplies the logits (<= 0 selects 1/sqrt(head_dim))
  *   workspace: wide_attn_cache_workspace_bytes(...) bytes; needs no initial value and keeps nothing,
  *       but two calls that can overlap on the GPU need one each
- * Built for few new rows a sequence (decoding, verifying drafted tokens): up to 16 query rows share one pass
+ * Built for few new rows a sequence (decoding, verifying drafted tokens): up to 24 query rows share one pass
  * over a KV head, more take several passes.  A long prefill reads the cache back
  * (wide_cache_read) and runs wide_attn.
  * Results do not depend on the other sequences of the batch beyond fp32 rounding, and are the same bit for bit in every run.

@@ -43,6 +43,7 @@ struct AttnArgs {
     const __nv_bfloat16* qm;
     long long qs;
     int n_q, share, hpg, words, causal;
+    unsigned by_share;             // 2^32 / share rounded up (0: share is 1): n / share = n * by_share >> 32 for n below 2^32 / share
     const uint32_t* mask_bits;
     float scale_log2e;
     __nv_bfloat16* o;
@@ -310,87 +311,87 @@ __device__ __noinline__ long long advance(const AttnArgs* a, Plan p, Cursor* at)
     return static_cast<long long>(static_cast<unsigned long long>(static_cast<unsigned>(k.end)) << 32 | static_cast<unsigned>(k.blk));
 }
 
-// What the epilogues need of a row of an item: where its output goes (nullptr: the row does not exist), whether its group is on.
+// Row block `rb` of a KV head: its rows are (new token, query head of the KV head) pairs, token by token.  Row rr of the
+// block is token `tok` of the sequence, query head `sub` of the KV head.
+struct Row {
+    int tok, sub;
+};
+struct RowBlock {
+    int tok0, rem;     // of the block's first row
+};
+__device__ __forceinline__ RowBlock row_block(const AttnArgs& a, int first) {
+    RowBlock b;
+    b.tok0 = first / a.share;
+    b.rem = first - b.tok0 * a.share;
+    return b;
+}
+__device__ __forceinline__ Row row_of(const AttnArgs& a, const RowBlock& b, int rr) {
+    const unsigned n = b.rem + rr, t = a.by_share ? __umulhi(n, a.by_share) : n;
+    return Row{b.tok0 + static_cast<int>(t), static_cast<int>(n - t * a.share)};
+}
+
+// What the epilogues need of a row: where its output goes (nullptr: the row does not exist), whether its group is on.
 struct RowOut {
     __nv_bfloat16* o;
     bool on;
 };
-__device__ __forceinline__ RowOut row_out(const AttnArgs& a, int row0, int n_rows, int kvh, int rr, int head_dim) {
+__device__ __forceinline__ RowOut row_out(const AttnArgs& a, int row0, int n_rows, int kvh, const Row& w, int head_dim) {
     RowOut r;
-    const int tok = rr / a.share, h = kvh * a.share + rr - tok * a.share;
-    r.o = tok < n_rows ? a.o + (static_cast<size_t>(row0 + tok) * a.n_q + h) * head_dim : nullptr;
-    r.on = r.o && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, row0 + tok, h / a.hpg));
+    const int h = kvh * a.share + w.sub;
+    r.o = w.tok < n_rows ? a.o + (static_cast<size_t>(row0 + w.tok) * a.n_q + h) * head_dim : nullptr;
+    r.on = r.o && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, row0 + w.tok, h / a.hpg));
     return r;
 }
 
 __host__ __device__ constexpr int slot_floats(int rows, int D) { return rows * (D + 4); }   // rows of D values, then m and l of each
 
-// Joins the partial results of one item that the bits of `which` name (piece e at at(e)): out rows, or a partial again
-// (dst).  A thread takes four channels of a row.  Runs once a launch, so it is short: its time is that of fetching its instructions.
+// Four channels (from d on) of row r of the partial results of one item that the bits of `which` name (piece e at at(e)): an
+// output row, or a row of a partial result again (dst).
 template <int ROWS, int D, typename At>
-__device__ __forceinline__ void join(const AttnArgs& a, int row0, int n_rows, int kvh, int rb, uint32_t which, const At& at, float* dst) {
-    // two neighbouring threads share an element, each takes every other group of pieces
-    const int odd = threadIdx.x & 1;
+__device__ __forceinline__ void join_four(int r, int d, uint32_t which, const At& at, float* dst, const RowOut& ro) {
+    float m = -CUDART_INF_F, l = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    // four pieces at a time, so that their loads overlap
 #pragma unroll 1
-    for (int i = threadIdx.x >> 1; i < ROWS * (D / 4); i += blockDim.x >> 1) {      // a multiple of 16 elements: whole warps go on together
-        const int r = i / (D / 4), d = i % (D / 4) * 4;
-        float m = -CUDART_INF_F, l = 0.f;
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        // four pieces at a time, so that their loads overlap
-#pragma unroll 1
-        for (uint32_t b = which & (odd ? 0xF0F0F0F0u : 0x0F0F0F0Fu); b;) {
-            float2 ml[4];
-            float4 v[4];
-            float top = m;
+    for (uint32_t b = which; b;) {
+        float2 ml[4];
+        float4 v[4];
+        float top = m;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                ml[e] = make_float2(-CUDART_INF_F, 0.f);
-                v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (b) {
-                    const float* p = at(__ffs(b) - 1);
-                    ml[e] = *reinterpret_cast<const float2*>(p + ROWS * D + 2 * r);
-                    v[e] = *reinterpret_cast<const float4*>(p + r * D + d);
-                }
-                b &= b - 1;
+        for (int e = 0; e < 4; ++e) {
+            ml[e] = make_float2(-CUDART_INF_F, 0.f);
+            v[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (b) {
+                const float* p = at(__ffs(b) - 1);
+                ml[e] = *reinterpret_cast<const float2*>(p + ROWS * D + 2 * r);
+                v[e] = *reinterpret_cast<const float4*>(p + r * D + d);
             }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = fmaxf(top, ml[e].x);
-            const float use = top == -CUDART_INF_F ? 0.f : top, old = exp2_fast(m - use);
-            l *= old;
-            x = make_float4(x.x * old, x.y * old, x.z * old, x.w * old);
-            m = top;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float w = exp2_fast(ml[e].x - use);
-                l = fmaf(ml[e].y, w, l);
-                x = make_float4(fmaf(v[e].x, w, x.x), fmaf(v[e].y, w, x.y), fmaf(v[e].z, w, x.z), fmaf(v[e].w, w, x.w));
-            }
+            b &= b - 1;
         }
-        __syncwarp();
-        const float other = __shfl_xor_sync(0xffffffffu, m, 1), top = fmaxf(m, other), w = exp2_fast(m - (top == -CUDART_INF_F ? 0.f : top));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, ml[e].x);
+        const float use = top == -CUDART_INF_F ? 0.f : top, old = exp2_fast(m - use);
+        l *= old;
+        x = make_float4(x.x * old, x.y * old, x.z * old, x.w * old);
         m = top;
-        l *= w;
-        l += __shfl_xor_sync(0xffffffffu, l, 1);
-        x = make_float4(x.x * w, x.y * w, x.z * w, x.w * w);
-        x.x += __shfl_xor_sync(0xffffffffu, x.x, 1);
-        x.y += __shfl_xor_sync(0xffffffffu, x.y, 1);
-        x.z += __shfl_xor_sync(0xffffffffu, x.z, 1);
-        x.w += __shfl_xor_sync(0xffffffffu, x.w, 1);
-        if (odd) continue;
-        if (dst) {
-            *reinterpret_cast<float4*>(dst + r * D + d) = x;
-            if (d == 0) *reinterpret_cast<float2*>(dst + ROWS * D + 2 * r) = make_float2(m, l);
-        } else {
-            const RowOut ro = row_out(a, row0, n_rows, kvh, rb * ROWS + r, D);
-            if (!ro.o) continue;
-            const float inv = ro.on && l != 0.f ? 1.f / l : 0.f;
-            uint2 w = make_uint2(0, 0);
-            if (inv != 0.f) {
-                const __nv_bfloat162 b0 = __floats2bfloat162_rn(x.x * inv, x.y * inv), b1 = __floats2bfloat162_rn(x.z * inv, x.w * inv);
-                w = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
-            }
-            *reinterpret_cast<uint2*>(ro.o + d) = w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float w = exp2_fast(ml[e].x - use);
+            l = fmaf(ml[e].y, w, l);
+            x = make_float4(fmaf(v[e].x, w, x.x), fmaf(v[e].y, w, x.y), fmaf(v[e].z, w, x.z), fmaf(v[e].w, w, x.w));
         }
+    }
+    if (dst) {
+        *reinterpret_cast<float4*>(dst + r * D + d) = x;
+        if (d == 0) *reinterpret_cast<float2*>(dst + ROWS * D + 2 * r) = make_float2(m, l);
+    } else if (ro.o) {
+        const float inv = ro.on && l != 0.f ? 1.f / l : 0.f;
+        uint2 w = make_uint2(0, 0);
+        if (inv != 0.f) {
+            const __nv_bfloat162 b0 = __floats2bfloat162_rn(x.x * inv, x.y * inv), b1 = __floats2bfloat162_rn(x.z * inv, x.w * inv);
+            w = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
+        }
+        *reinterpret_cast<uint2*>(ro.o + d) = w;
     }
 }
 
@@ -492,13 +493,15 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
         uint4 qw[NB][kSteps / 2];      // the query rows of the item at hand: 8 channels of every 32
         auto load_queries = [&]() {
             const int4 info = plan.seqs[cc.seq];     // first row, rows, length
+            const RowBlock rows = row_block(a, cc.rb * kRows);
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
-                const int rr = cc.rb * kRows + 8 * n + g, tok = rr / a.share, h = cc.kvh * a.share + rr - tok * a.share;
+                const Row w = row_of(a, rows, 8 * n + g);
+                const __nv_bfloat16* from = a.qm + (info.x + w.tok) * a.qs + (cc.kvh * a.share + w.sub) * D + 8 * t;
 #pragma unroll
                 for (int i = 0; i < kSteps / 2; ++i) {
                     qw[n][i] = make_uint4(0, 0, 0, 0);
-                    if (tok < info.y) qw[n][i] = *reinterpret_cast<const uint4*>(a.qm + (info.x + tok) * a.qs + h * D + 32 * i + 8 * t);
+                    if (w.tok < info.y) qw[n][i] = *reinterpret_cast<const uint4*>(from + 32 * i);
                 }
             }
         };
@@ -586,16 +589,15 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 const uint32_t base = ring_a + slot * kStage;
                 const int key0 = blk << 4;
                 const int4 info = masked ? plan.seqs[cc.seq] : make_int4(0, 0, 0, 0);
+                const RowBlock rows = masked ? row_block(a, cc.rb * kRows) : RowBlock{0, 0};
                 // ---- scores
                 // (A block that is not there is computed like the others, from whatever the ring holds, and left out by
                 // selection.  The blocks take turns: eight dependent instructions on one accumulator would wait for each other.)
                 float s[kBlk][NB][4], mins[kBlk][NB][4];
-                uint4 w[kBlk][kSteps / 4];
+                uint4 w[kBlk];         // 64 channels of a block's codes
                 uint32_t w0[kBlk][kNS], w1[kBlk][kNS];
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
-#pragma unroll
-                    for (int i = 0; i < kSteps / 4; ++i) w[b][i] = lds128(base + lane16 + b * kSB + i * 512);
                     lds_words<kNS>(base + params + b * kSB, w0[b]);
                     lds_words<kNS>(base + params + b * kSB + 32 * kNS, w1[b]);
                 }
@@ -606,7 +608,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k)
 #pragma unroll
                         for (int b = 0; b < kBlk; ++b) {
-                            const uint4 v = w[b][k >> 2];
+                            if ((k & 3) == 0) w[b] = lds128(base + lane16 + b * kSB + (k >> 2) * 512);
+                            const uint4 v = w[b];
                             const uint32_t x = (k & 3) == 0 ? v.x : (k & 3) == 1 ? v.y : (k & 3) == 2 ? v.z : v.w;
                             const uint32_t y = x >> 8;
 #pragma unroll
@@ -639,8 +642,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         for (int e = 0; e < 4; ++e) {
                             s[b][n][e] = fmaf(s[b][n][e], qscale[n][e & 1], mins[b][n][e]);
                             if (masked) {
-                                const int row = cc.rb * kRows + 8 * n + 2 * t + (e & 1);
-                                const int last = a.causal ? min(info.z - 1, info.z - info.y + row / a.share) : info.z - 1;
+                                const int last = a.causal ? min(info.z - 1, info.z - info.y + row_of(a, rows, 8 * n + 2 * t + (e & 1)).tok) : info.z - 1;
                                 if (key0 + 16 * b + g + 8 * (e >> 1) > last || !((here >> b) & 1u)) s[b][n][e] = -CUDART_INF_F;
                             }
                         }
@@ -713,8 +715,6 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 // ---- probabilities, and the values they weigh
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
-#pragma unroll
-                    for (int i = 0; i < kSteps / 4; ++i) w[b][i] = lds128(base + lane16 + 8 * D + b * kSB + i * 512);
                     float p[NB][4];
 #pragma unroll
                     for (int n = 0; n < NB; ++n)
@@ -750,7 +750,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k) {
                             // Rows g take a whole byte, low code + 16 * high code: the rows g + 8, 16 * high code, come off
                             // again at the end.  That saves an instruction a word.
-                            const uint4 v = w[b][k >> 2];
+                            if ((k & 3) == 0) w[b] = lds128(base + lane16 + 8 * D + b * kSB + (k >> 2) * 512);
+                            const uint4 v = w[b];
                             const uint32_t x = (k & 3) == 0 ? v.x : (k & 3) == 1 ? v.y : (k & 3) == 2 ? v.z : v.w;
                             const uint32_t y = __byte_perm(x, 0, 0x4341);
 #pragma unroll
@@ -805,11 +806,12 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     }
             const bool begins = first_blk == 0, ends = end_blk == cc.n_blk, tail = cc.left == 0;
             if (begins && ends) {
+                const RowBlock rows = row_block(a, cc.rb * kRows);
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const RowOut ro = row_out(a, info.x, info.y, cc.kvh, cc.rb * kRows + 8 * n + 2 * t + c, D);
+                        const RowOut ro = row_out(a, info.x, info.y, cc.kvh, row_of(a, rows, 8 * n + 2 * t + c), D);
                         if (!ro.o) continue;
                         const float r = ro.on && l[n][c] != 0.f ? 1.f / l[n][c] : 0.f;
 #pragma unroll
@@ -878,6 +880,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                    end_bits = __ballot_sync(0xffffffffu, (st & 4) != 0);
     int* meta = a.meta + blockIdx.x * 2 * kMeta;
     bool open[2] = {false, false};
+    int mine = tid;    // the runs' elements go to the threads in turn
 #pragma unroll 1
     for (uint32_t rest = any; rest;) {
         // the next piece and those that follow, up to the one that ends the item or the CTA
@@ -902,10 +905,18 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 m[4] = rb;
             }
         }
-        join<kRows, D>(a, info.x, info.y, kvh, rb, which, [&](int x) -> const float* {
-            return (x & 1) ? reinterpret_cast<const float*>(smem + kPlanSmem + (x >> 1) * (STAGES * kStage))
-                           : a.heads + static_cast<size_t>(blockIdx.x * WARPS + (x >> 1)) * slot_floats(kRows, D);
-        }, dst);
+        const RowBlock rows = row_block(a, rb * kRows);
+        constexpr int kElements = kRows * (D / 4);
+#pragma unroll 1
+        for (; mine < kElements; mine += 32 * WARPS) {
+            const int r = mine / (D / 4), d = mine % (D / 4) * 4;
+            const RowOut ro = dst ? RowOut{nullptr, false} : row_out(a, info.x, info.y, kvh, row_of(a, rows, r), D);
+            join_four<kRows, D>(r, d, which, [&](int x) -> const float* {
+                return (x & 1) ? reinterpret_cast<const float*>(smem + kPlanSmem + (x >> 1) * (STAGES * kStage))
+                               : a.heads + static_cast<size_t>(blockIdx.x * WARPS + (x >> 1)) * slot_floats(kRows, D);
+            }, dst, ro);
+        }
+        mine -= kElements;
     }
     if (tid == 0) {
         if (!open[0]) meta[0] = 0;
@@ -942,9 +953,10 @@ __global__ void __launch_bounds__(256) attn_cache_join_kernel(const __grid_const
         return a.parts + static_cast<size_t>(i == 0 ? 2 * c + 1 : 2 * (c + i)) * slot_floats(ROWS, D);
     };
     constexpr int kHalves = D / 64;
+    const RowBlock rows = row_block(a, rb * ROWS);
     for (int u = unit + 8 * blockIdx.y; u < ROWS * kHalves; u += 8 * gridDim.y) {
         const int r = u / kHalves, d = u % kHalves * 64 + 2 * lane;
-        const RowOut ro = row_out(a, meta.y, meta.z, meta.w, rb * ROWS + r, D);
+        const RowOut ro = row_out(a, meta.y, meta.z, meta.w, row_of(a, rows, r), D);
         if (!ro.o) continue;
         float m = -CUDART_INF_F, l = 0.f;
         float2 x = make_float2(0.f, 0.f);
@@ -989,9 +1001,9 @@ Work work_layout() {
     w.plan = at;
     at += wide_align_up(plan_bytes(WIDE_MAX_SEQS, 8, 8), 256);
     w.heads = at;
-    at += wide_align_up(static_cast<size_t>(kMaxCtas) * 16 * slot_floats(8, 128) * 4, 256);
+    at += wide_align_up(static_cast<size_t>(kMaxCtas) * 8 * slot_floats(24, 128) * 4, 256);       // 8 warps of 24 rows: more than 16 of 8
     w.parts = at;
-    at += wide_align_up(static_cast<size_t>(kMaxCtas) * 2 * slot_floats(16, 128) * 4, 256);
+    at += wide_align_up(static_cast<size_t>(kMaxCtas) * 2 * slot_floats(24, 128) * 4, 256);
     w.meta = at;
     at += static_cast<size_t>(kMaxCtas) * 2 * kMeta * 4;
     w.total = wide_align_up(at, 256);
@@ -1003,8 +1015,8 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     constexpr int kRows = 8 * NB;
     constexpr int stage = kBlk * (16 * D + 128 * (D / G));
     constexpr int room = 227 * 1024 - 3072 - kPlanSmem;   // 3 KB for the static arrays
-    // 16 warps have 128 registers each, which two blocks of eight query rows do not fit
-    constexpr int W = NB == 2 ? 8 : 16 * 3 * stage <= room ? 16 : 12;
+    // 16 warps have 128 registers each, which two and three blocks of eight query rows do not fit
+    constexpr int W = NB > 1 ? 8 : 16 * 3 * stage <= room ? 16 : 12;
     constexpr int S = room / (W * stage) > 6 ? 6 : room / (W * stage);
     static_assert(S >= 3 && S * stage >= slot_floats(kRows, D) * 4, "ring");
     auto kernel = attn_cache_kernel<D, G, NB, W, S>;
@@ -1075,6 +1087,7 @@ int wide_launch_attn_cache(wide_ctx* ctx, cudaStream_t s, const wide_cache* cach
     a.qs = qs;
     a.n_q = n_q;
     a.share = n_q / cache->n_kv_heads;
+    a.by_share = a.share > 1 ? static_cast<unsigned>(((1ull << 32) + a.share - 1) / a.share) : 0u;
     a.hpg = hpg;
     a.words = (n_q / hpg + 31) / 32;
     a.causal = causal;
@@ -1084,8 +1097,9 @@ int wide_launch_attn_cache(wide_ctx* ctx, cudaStream_t s, const wide_cache* cach
     a.status = ctx->d_status + WIDE_STATUS_INDEX;
     a.plan_words = (cache->n_kv_heads + 31) / 32;
     // Rows of a sequence and KV head: `share` where a sequence has one new row, else an average (the lengths
-    // are on the device).  Above eight, 16 rows share a pass over the cache.
+    // are on the device).  Above eight, 16 rows share a pass over the cache, above 16, 24.
     const long long rows_per_head = seqs->row_start ? static_cast<long long>(rows) * a.share / seqs->n_seqs : a.share;
     if (rows_per_head <= 8) return launch_shape<1>(ctx, s, a, cache->head_dim, cache->quant_group, static_cast<unsigned char*>(ws));
+    if (rows_per_head > 16) return launch_shape<3>(ctx, s, a, cache->head_dim, cache->quant_group, static_cast<unsigned char*>(ws));
     return launch_shape<2>(ctx, s, a, cache->head_dim, cache->quant_group, static_cast<unsigned char*>(ws));
 }
