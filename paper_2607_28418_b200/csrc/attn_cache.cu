@@ -31,6 +31,8 @@ namespace {
 using namespace wptx;
 
 constexpr int kBlk = 2;            // blocks of a ring stage: 32 keys
+constexpr float kSlack = 8.f;       // the reference of a softmax may stay this far (in powers of two) below its running maximum
+constexpr int kUp = 5;             // steps enter fp16 as 2^kUp .. 2^(kUp + 1) at most: 2^(kUp + 1 + kSlack) is far below 65504
 constexpr int kMaxCtas = 160;
 constexpr int kMeta = 8;           // words of meta of a partial result
 constexpr int kPlanSmem = 6144;    // bytes of shared memory for the plan of a small batch
@@ -42,6 +44,7 @@ struct AttnArgs {
     SeqView q;
     const __nv_bfloat16* qm;
     long long qs;
+    unsigned page_bytes;
     int n_q, share, hpg, words, causal;
     unsigned by_share;             // 2^32 / share rounded up (0: share is 1): n / share = n * by_share >> 32 for n below 2^32 / share
     const uint32_t* mask_bits;
@@ -448,6 +451,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
         int blk = cc.blk, end_blk = cc.end, ic_blk = blk, ic_end = end_blk;
         int slot = 0;
         uint32_t live = 0;             // kBlk bits a stage, newest lowest: which of its blocks have a page
+        const unsigned char* head_at = nullptr;  // block 0 of page 0 of the requested KV head, this lane's part
         int pt_first = -1000000, pt = 0;         // page numbers [pt_first, pt_first + 32) of the requested sequence, one a lane
         const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
         const uint32_t ring_a = smem_u32(smem + kPlanSmem) + warp * (STAGES * kStage);
@@ -461,20 +465,20 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 if (last - pt_first >= 32) {
                     pt_first = first;
                     pt = pt_first + lane < a.q.max_pages ? a.q.page_table[static_cast<size_t>(ic.seq) * a.q.max_pages + pt_first + lane] : -1;
+                    head_at = a.c.pages + static_cast<size_t>(static_cast<unsigned>(ic.kvh) << sub_shift) * kSB + lane16;
                 }
-                const int kvh = ic.kvh;
+                const uint32_t dst = ring_a + to * kStage + lane16;
+                int page = __shfl_sync(0xffffffffu, pt, first - pt_first);
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
                     if (b < nb) {
-                        const int page = __shfl_sync(0xffffffffu, pt, ((ic_blk + b) >> sub_shift) - pt_first);
+                        if (b > 0 && last != first) page = __shfl_sync(0xffffffffu, pt, last - pt_first);
                         if (static_cast<unsigned>(page) < static_cast<unsigned>(a.c.n_pages)) {
                             m |= 1u << b;
-                            const unsigned char* from = a.c.pages + lane16 +
-                                (((static_cast<size_t>(page) * a.c.n_kv_heads + kvh) << sub_shift) + ((ic_blk + b) & sub_mask)) * kSB;
-                            const uint32_t dst = ring_a + to * kStage + b * kSB + lane16;
+                            const unsigned char* from = head_at + static_cast<size_t>(page) * a.page_bytes + ((ic_blk + b) & sub_mask) * kSB;
 #pragma unroll
                             for (int i = 0; i < kPieces; ++i)
-                                if (512 * (i + 1) <= kSB || lane16 + 512 * i < kSB) cp_async_16(dst + 512 * i, from + 512 * i);
+                                if (512 * (i + 1) <= kSB || lane16 + 512 * i < kSB) cp_async_16(dst + b * kSB + 512 * i, from + 512 * i);
                         }
                     }
                 }
@@ -568,7 +572,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 
             float acc[NB][kSteps][4], m[NB][2], l[NB][2], pm[NB][kNS][2];
             int ev = -110;              // the exponent that the values' steps are relative to
-            float inv = pow2(13 + 110);
+            float inv = pow2(kUp + 110);
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
 #pragma unroll
@@ -663,22 +667,23 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     }
                 }
                 big = __reduce_max_sync(0xffffffffu, big);
-                // ---- running maximum; what is summed so far is scaled down when it rises, or when the steps do
-                float alpha[NB][2], mu[NB][2], top[NB][2];
+                // ---- the reference m that probabilities are taken relative to.  It follows the running maximum only when that has
+                // risen by more than kSlack, and the steps' exponent only upwards: then what is summed so far is scaled down.
+                // (Following every rise, four in ten stages of a decoding batch would scale.)
+                float mu[NB][2], top[NB][2];
                 bool change = static_cast<int>(big >> 23) - 127 > ev;
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float mx = m[n][c];
+                        float mx = fmaxf(s[0][n][c], s[0][n][c + 2]);
 #pragma unroll
-                        for (int b = 0; b < kBlk; ++b) mx = fmaxf(mx, fmaxf(s[b][n][c], s[b][n][c + 2]));
+                        for (int b = 1; b < kBlk; ++b) mx = fmaxf(mx, fmaxf(s[b][n][c], s[b][n][c + 2]));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        change = change || mx != m[n][c];
                         top[n][c] = mx;
-                        mu[n][c] = mx == -CUDART_INF_F ? 0.f : mx;
+                        change = change || mx > m[n][c] + kSlack;
                     }
                 if (__any_sync(0xffffffffu, change)) {
                     if (big >= 0x7F800000u) {   // a value that is not finite: leave it out of the scaling
@@ -695,23 +700,29 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     const int up = max(ev, static_cast<int>(big >> 23) - 127);
                     const float ev_f = pow2(max(-126, ev - up));
                     ev = up;
-                    inv = pow2(13 - ev);
+                    inv = pow2(kUp - ev);
 #pragma unroll
                     for (int n = 0; n < NB; ++n) {
+                        float alpha[2];
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            alpha[n][c] = exp2_fast(m[n][c] - mu[n][c]);
-                            m[n][c] = top[n][c];
-                            l[n][c] *= alpha[n][c];
+                            const float now = fmaxf(m[n][c], top[n][c]);
+                            alpha[c] = exp2_fast(m[n][c] - (now == -CUDART_INF_F ? 0.f : now));
+                            m[n][c] = now;
+                            l[n][c] *= alpha[c];
 #pragma unroll
-                            for (int i = 0; i < kNS; ++i) pm[n][i][c] *= alpha[n][c];
+                            for (int i = 0; i < kNS; ++i) pm[n][i][c] *= alpha[c];
                         }
 #pragma unroll
                         for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[n][i][e] *= alpha[n][e & 1] * ev_f;
+                            for (int e = 0; e < 4; ++e) acc[n][i][e] *= alpha[e & 1] * ev_f;
                     }
                 }
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) mu[n][c] = m[n][c] == -CUDART_INF_F ? 0.f : m[n][c];
                 // ---- probabilities, and the values they weigh
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
@@ -786,13 +797,15 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 run = max(0, run - kBlk);
             }
             // ---- end of the item or of the piece: sums over the lanes, results in the values' own scale
-            const float f0 = pow2(11) * pow2(ev), f1 = f0 * 0.0625f;
+            const float f = pow2(ev);
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
-                    acc[n][i][0] -= acc[n][i][2];
-                    acc[n][i][1] -= acc[n][i][3];
+                    acc[n][i][0] = (acc[n][i][0] - acc[n][i][2]) * pow2(24 - kUp);
+                    acc[n][i][1] = (acc[n][i][1] - acc[n][i][3]) * pow2(24 - kUp);
+                    acc[n][i][2] *= pow2(20 - kUp);
+                    acc[n][i][3] *= pow2(20 - kUp);
                 }
 #pragma unroll
             for (int n = 0; n < NB; ++n)
@@ -819,8 +832,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                             const float add = pm[n][32 * i / G][c];
                             uint2 w = make_uint2(0, 0);
                             if (r != 0.f) {
-                                const __nv_bfloat162 b0 = __floats2bfloat162_rn(fmaf(acc[n][2 * i][c], f0, add) * r, fmaf(acc[n][2 * i][c + 2], f1, add) * r);
-                                const __nv_bfloat162 b1 = __floats2bfloat162_rn(fmaf(acc[n][2 * i + 1][c], f0, add) * r, fmaf(acc[n][2 * i + 1][c + 2], f1, add) * r);
+                                const __nv_bfloat162 b0 = __floats2bfloat162_rn(fmaf(acc[n][2 * i][c], f, add) * r, fmaf(acc[n][2 * i][c + 2], f, add) * r);
+                                const __nv_bfloat162 b1 = __floats2bfloat162_rn(fmaf(acc[n][2 * i + 1][c], f, add) * r, fmaf(acc[n][2 * i + 1][c + 2], f, add) * r);
                                 w = make_uint2(*reinterpret_cast<const uint32_t*>(&b0), *reinterpret_cast<const uint32_t*>(&b1));
                             }
                             *reinterpret_cast<uint2*>(ro.o + 32 * i + 4 * g) = w;
@@ -838,8 +851,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         for (int i = 0; i < kSteps / 2; ++i) {
                             const float add = pm[n][32 * i / G][c];
                             *reinterpret_cast<float4*>(dst + r * D + 32 * i + 4 * g) =
-                                make_float4(fmaf(acc[n][2 * i][c], f0, add), fmaf(acc[n][2 * i][c + 2], f1, add),
-                                            fmaf(acc[n][2 * i + 1][c], f0, add), fmaf(acc[n][2 * i + 1][c + 2], f1, add));
+                                make_float4(fmaf(acc[n][2 * i][c], f, add), fmaf(acc[n][2 * i][c + 2], f, add),
+                                            fmaf(acc[n][2 * i + 1][c], f, add), fmaf(acc[n][2 * i + 1][c + 2], f, add));
                         }
                         if (g == 0) {
                             dst[kRows * D + 2 * r] = m[n][c];
@@ -1083,6 +1096,7 @@ int wide_launch_attn_cache(wide_ctx* ctx, cudaStream_t s, const wide_cache* cach
     AttnArgs a{};
     a.c = wide_cache_view(cache);
     a.q = wide_seq_view(seqs, rows);
+    a.page_bytes = static_cast<unsigned>(a.c.block_bytes) * static_cast<unsigned>(cache->n_kv_heads) << (a.c.page_shift - 4);
     a.qm = static_cast<const __nv_bfloat16*>(q);
     a.qs = qs;
     a.n_q = n_q;
