@@ -1043,8 +1043,7 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     if (plan_bytes(a.q.n_seqs, a.plan_words, a.words) > kPlanSmem) {
         a.plan = ws + w.plan;
         WideLaunch l(ctx, s, "attn_cache_plan");
-        attn_cache_plan_kernel<kRows><<<1, 1024, 0, s>>>(a, ctas);
-        WIDE_CUDA_CHECK(cudaGetLastError());
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_cache_plan_kernel<kRows>, dim3(1), dim3(1024), 0, s, a, ctas));
     }
     // once a device; threads that come here together all set the same
     static std::atomic<unsigned> set{0};
@@ -1055,18 +1054,13 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     }
     {
         WideLaunch l(ctx, s, "attn_cache");
-        if (ctx->prof) kernel<<<ctas, 32 * W, smem, s>>>(a);
-        else WIDE_CUDA_CHECK(wide_launch_dependent(kernel, dim3(ctas), dim3(32 * W), smem, s, a));
-        WIDE_CUDA_CHECK(cudaGetLastError());
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, kernel, dim3(ctas), dim3(32 * W), smem, s, a));
     }
     // Nothing to join where the plan is certain to give every item a CTA of its own (make_plan; rows / kRows + n_seqs row blocks at most).
     const long long items = static_cast<long long>(a.c.n_kv_heads) * (static_cast<long long>(a.q.rows) * a.share / kRows + a.q.n_seqs);
     if (items > ctas || (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) > kItemAlone) {
         WideLaunch l(ctx, s, "attn_cache_join");
-        const dim3 grid(ctas, 2);
-        if (ctx->prof) attn_cache_join_kernel<kRows, D><<<grid, 256, 0, s>>>(a, ctas);
-        else WIDE_CUDA_CHECK(wide_launch_dependent(attn_cache_join_kernel<kRows, D>, grid, dim3(256), 0, s, a, ctas));
-        WIDE_CUDA_CHECK(cudaGetLastError());
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_cache_join_kernel<kRows, D>, dim3(ctas, 2), dim3(256), 0, s, a, ctas));
     }
     return WIDE_OK;
 }

@@ -56,6 +56,15 @@ inline cudaError_t wide_launch_dependent(void (*kernel)(KArgs...), dim3 grid, di
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
+// Launch of a kernel that calls grid_dep_wait() before it touches memory: dependent, or the ordinary way while kernels are timed.
+template <typename... KArgs, typename... Args>
+inline cudaError_t wide_launch_after(const wide_ctx* ctx, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                                     Args&&... args) {
+    if (!ctx->prof) return wide_launch_dependent(kernel, grid, block, smem, s, static_cast<Args&&>(args)...);
+    kernel<<<grid, block, smem, s>>>(static_cast<KArgs>(args)...);
+    return cudaGetLastError();
+}
+
 // Counts one kernel launch and, when profiling is on, brackets it with a pair of CUDA events on
 // the launching stream.  Usage: { WideLaunch l(ctx, s, "name"); kernel<<<..., s>>>(...); }
 struct WideLaunch {

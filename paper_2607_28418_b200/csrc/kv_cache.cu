@@ -295,6 +295,7 @@ cache_write_kernel(CacheView c, SeqView q, const T* __restrict__ k, const T* __r
     const int lane = threadIdx.x & 31, p = lane / kLT, u8 = lane % kLT;
     const int cc = u8 >> 2, c0 = cc >> 1, c1 = cc & 1;   // 32-channel chunk of this lane's 8 channels
     int total = q.n_seqs;
+    wptx::grid_dep_wait();
     if (q.row_start) total = scan_blocks(q, c.page_shift, seqs, part, status);
     const long long units = 2LL * total * c.n_kv_heads;
     for (long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5); unit < units;
@@ -431,9 +432,10 @@ __device__ __forceinline__ void store_values(float* p, const float (&x)[4]) {
 }
 
 // The reverse: a lane takes the words that a lane of wide_attn_cache would (one 16-byte piece per 64
-// channels), which hold 8 neighbouring channels of two keys and 4 of four values.
+// channels), which hold 8 neighbouring channels of two keys and 4 of four values.  A warp's next block is on its way while
+// it writes one out.
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(32 * kWarps)
+__global__ void __launch_bounds__(32 * kWarps, 3)
 cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, long long ks, long long vs,
                   int* __restrict__ status) {
     constexpr int kNS = D / G;
@@ -442,38 +444,62 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
     __shared__ int part[kWarps];
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     int total = q.n_seqs;
+    wptx::grid_dep_wait();
     if (q.row_start) total = scan_blocks(q, c.page_shift, seqs, part, status);
-    const long long units = static_cast<long long>(total) * c.n_kv_heads;
-    for (long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5); unit < units;
-         unit += static_cast<long long>(gridDim.x) * kWarps) {
-        const Unit w = find_unit(q, c, seqs, static_cast<int>(unit));
-        if (w.bad && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
-        if (!w.some) continue;
-        const uint8_t* blk = wide_cache_block(c, q, w.seq, w.block << 4, w.head);
+    const long long units = static_cast<long long>(total) * c.n_kv_heads, step = static_cast<long long>(gridDim.x) * kWarps;
+    struct Block {
+        Unit w;
+        bool some;
+        uint4 kw[kC], vw[kC];
+        uint32_t kp[2][kNS], vp[4][kNS];
+    };
+    auto fetch = [&](long long unit, Block& b) {
+        b.some = false;
+        if (unit >= units) return;
+        b.w = find_unit(q, c, seqs, static_cast<int>(unit));
+        if (b.w.bad && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
+        b.some = b.w.some;
+        if (!b.some) return;
+        const uint8_t* blk = wide_cache_block(c, q, b.w.seq, b.w.block << 4, b.w.head);
         if (!blk && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
+        const uint32_t* kp = reinterpret_cast<const uint32_t*>(blk + 16 * D);
+        const uint32_t* vp = reinterpret_cast<const uint32_t*>(blk + 16 * D + 64 * kNS);
+#pragma unroll
+        for (int i = 0; i < kC; ++i) {
+            b.kw[i] = b.vw[i] = make_uint4(0, 0, 0, 0);
+            if (blk) {
+                b.kw[i] = *reinterpret_cast<const uint4*>(blk + (i * 32 + lane) * 16);
+                b.vw[i] = *reinterpret_cast<const uint4*>(blk + 8 * D + (i * 32 + lane) * 16);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kNS; ++i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) b.kp[h][i] = blk ? kp[(g + 8 * h) * kNS + i] : 0u;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) b.vp[h][i] = blk ? vp[(2 * t + 8 * (h & 1) + (h >> 1)) * kNS + i] : 0u;
+        }
+    };
+    long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    Block now, next;
+    fetch(unit, now);
+    for (; unit < units; unit += step, now = next) {
+        fetch(unit + step, next);
+        if (!now.some) continue;
+        const Unit& w = now.w;
         const int p0 = w.block << 4;
         auto row_of = [&](int r) { return static_cast<long long>(w.row0 + (p0 + r - w.first)); };
         auto is_new = [&](int r) { return p0 + r >= w.first && p0 + r < w.len; };
-        uint4 kw[kC], vw[kC];
-#pragma unroll
-        for (int i = 0; i < kC; ++i) {
-            kw[i] = vw[i] = make_uint4(0, 0, 0, 0);
-            if (blk) {
-                kw[i] = *reinterpret_cast<const uint4*>(blk + (i * 32 + lane) * 16);
-                vw[i] = *reinterpret_cast<const uint4*>(blk + 8 * D + (i * 32 + lane) * 16);
-            }
-        }
-        const uint32_t* kp = reinterpret_cast<const uint32_t*>(blk + 16 * D);
-        const uint32_t* vp = reinterpret_cast<const uint32_t*>(blk + 16 * D + 64 * kNS);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r = g + 8 * h;
             if (!is_new(r)) continue;
+            T* to = k + row_of(r) * ks + w.head * D + 8 * t;
 #pragma unroll
             for (int cc = 0; cc < D / 32; ++cc) {
-                const uint32_t w0 = (cc & 1) ? kw[cc >> 1].z : kw[cc >> 1].x, w1 = (cc & 1) ? kw[cc >> 1].w : kw[cc >> 1].y;
-                const uint32_t pw = blk ? kp[r * kNS + cc * 32 / G] : 0u;
-                const float s = wide_cache_scale(pw), m = wide_cache_min(pw);
+                const uint4 four = now.kw[cc >> 1];
+                const uint32_t w0 = (cc & 1) ? four.z : four.x, w1 = (cc & 1) ? four.w : four.y;
+                const float s = wide_cache_scale(now.kp[h][cc * 32 / G]), m = wide_cache_min(now.kp[h][cc * 32 / G]);
                 float x[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -481,23 +507,24 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
                     const int shift = 8 * h + 16 * (e & 1) + 4 * ((e >> 1) & 1);
                     x[e] = fmaf(s, static_cast<float>((word >> shift) & 15u), m);
                 }
-                store_values(k + row_of(r) * ks + w.head * D + 32 * cc + 8 * t, x);
+                store_values(to + 32 * cc, x);
             }
         }
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
             const int r = 2 * t + 8 * (h & 1) + (h >> 1);
             if (!is_new(r)) continue;
+            T* to = v + row_of(r) * vs + w.head * D + 4 * g;
 #pragma unroll
             for (int cc = 0; cc < D / 32; ++cc) {
-                const uint32_t w0 = (cc & 1) ? vw[cc >> 1].z : vw[cc >> 1].x, w1 = (cc & 1) ? vw[cc >> 1].w : vw[cc >> 1].y;
-                const uint32_t pw = blk ? vp[r * kNS + cc * 32 / G] : 0u;
-                const float s = wide_cache_scale(pw), m = wide_cache_min(pw);
+                const uint4 four = now.vw[cc >> 1];
+                const uint32_t w0 = (cc & 1) ? four.z : four.x, w1 = (cc & 1) ? four.w : four.y;
+                const float s = wide_cache_scale(now.vp[h][cc * 32 / G]), m = wide_cache_min(now.vp[h][cc * 32 / G]);
                 float x[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     x[e] = fmaf(s, static_cast<float>(((e < 2 ? w0 : w1) >> (8 * h + 4 * (e & 1))) & 15u), m);
-                store_values(v + row_of(r) * vs + w.head * D + 32 * cc + 4 * g, x);
+                store_values(to + 32 * cc, x);
             }
         }
     }
@@ -505,16 +532,16 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
 
 // CTAs for the most blocks that `rows` rows of these sequences can touch: a sequence's n rows lie in at
 // most n / 16 + 2 blocks, and in at most n.
-int grid_for(const wide_ctx* ctx, const CacheView& c, const SeqView& q, int units_per_block) {
+int grid_for(const wide_ctx* ctx, const CacheView& c, const SeqView& q, int units_per_block, int per_sm) {
     const long long blocks = q.row_start ? min(static_cast<long long>(q.rows), q.rows / 16 + 2LL * q.n_seqs) : q.n_seqs;
     const long long ctas = (blocks * c.n_kv_heads * units_per_block + kWarps - 1) / kWarps;
-    return static_cast<int>(max(1LL, min(ctas, 8LL * ctx->sm_count)));
+    return static_cast<int>(max(1LL, min(ctas, static_cast<long long>(per_sm) * ctx->sm_count)));
 }
 
 template <typename T, int D, int G>
 int launch(wide_ctx* ctx, cudaStream_t s, bool write, const CacheView& c, const SeqView& q, void* k, void* v, long long ks,
            long long vs) {
-    const int grid = grid_for(ctx, c, q, write ? 2 : 1);
+    const int grid = grid_for(ctx, c, q, write ? 2 : 1, write ? 8 : 3);
     const size_t smem = q.row_start ? static_cast<size_t>(q.n_seqs) * sizeof(int4) : 0;
     int* status = ctx->d_status + WIDE_STATUS_INDEX;
     if (smem > 48 * 1024) {
@@ -523,10 +550,12 @@ int launch(wide_ctx* ctx, cudaStream_t s, bool write, const CacheView& c, const 
     }
     WideLaunch l(ctx, s, write ? "cache_write" : "cache_read");
     if (write)
-        cache_write_kernel<T, D, G><<<grid, 32 * kWarps, smem, s>>>(c, q, static_cast<const T*>(k), static_cast<const T*>(v), ks, vs, status);
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, cache_write_kernel<T, D, G>, dim3(grid), dim3(32 * kWarps), smem, s, c, q,
+                                          static_cast<const T*>(k), static_cast<const T*>(v), ks, vs, status));
     else
-        cache_read_kernel<T, D, G><<<grid, 32 * kWarps, smem, s>>>(c, q, static_cast<T*>(k), static_cast<T*>(v), ks, vs, status);
-    return cudaGetLastError() == cudaSuccess ? WIDE_OK : WIDE_ERR_CUDA;
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, cache_read_kernel<T, D, G>, dim3(grid), dim3(32 * kWarps), smem, s, c, q, static_cast<T*>(k),
+                                          static_cast<T*>(v), ks, vs, status));
+    return WIDE_OK;
 }
 
 template <typename T>

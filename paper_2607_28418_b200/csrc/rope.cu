@@ -96,6 +96,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
         return head < a.n_q ? static_cast<const T*>(a.q) + row * a.qs + head * D : static_cast<const T*>(a.k) + row * a.ks + (head - a.n_q) * D;
     };
     wrap();
+    wptx::grid_dep_wait();
     // the first unit is on its way while the angles are worked out, each later one while its predecessor turns
     Vec8<T> u, w;
     if (t < nt) {
@@ -190,11 +191,11 @@ int wide_launch_rope(wide_ctx* ctx, cudaStream_t s, const void* q, const void* k
     const int grid = (tokens + a.tile - 1) / a.tile;
     WideLaunch l(ctx, s, "rope");
     if (dtype == WIDE_F32) {
-        if (head_dim == 128) rope_kernel<float, 128><<<grid, kThreads, 0, s>>>(a);
-        else rope_kernel<float, 64><<<grid, kThreads, 0, s>>>(a);
+        if (head_dim == 128) WIDE_CUDA_CHECK(wide_launch_after(ctx, rope_kernel<float, 128>, dim3(grid), dim3(kThreads), 0, s, a));
+        else WIDE_CUDA_CHECK(wide_launch_after(ctx, rope_kernel<float, 64>, dim3(grid), dim3(kThreads), 0, s, a));
     } else {
-        if (head_dim == 128) rope_kernel<__nv_bfloat16, 128><<<grid, kThreads, 0, s>>>(a);
-        else rope_kernel<__nv_bfloat16, 64><<<grid, kThreads, 0, s>>>(a);
+        if (head_dim == 128) WIDE_CUDA_CHECK(wide_launch_after(ctx, rope_kernel<__nv_bfloat16, 128>, dim3(grid), dim3(kThreads), 0, s, a));
+        else WIDE_CUDA_CHECK(wide_launch_after(ctx, rope_kernel<__nv_bfloat16, 64>, dim3(grid), dim3(kThreads), 0, s, a));
     }
-    return cudaGetLastError() == cudaSuccess ? WIDE_OK : WIDE_ERR_CUDA;
+    return WIDE_OK;
 }
