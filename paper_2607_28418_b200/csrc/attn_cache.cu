@@ -31,6 +31,10 @@ namespace {
 using namespace wptx;
 
 constexpr int kBlk = 2;            // blocks of a ring stage: 32 keys
+// -8 and -8 * 16 as the codes' subnormal fp16 numbers, twice: values are summed as m + 8 s + s (n - 8), so that sums of many values of
+// either sign stay near zero.  (Summed as m + s n, the fp32 sums of 16384 evenly weighed values lost a digit to cancellation.)  The
+// - 8 is the same for all channels of a sub-group, so it has one accumulator, which joins the others every fourth stage, before they grow.
+constexpr uint32_t kEight = 0x00080008u, kEightHigh = 0x80808080u;
 constexpr float kSlack = 8.f;       // the reference of a softmax may stay this far (in powers of two) below its running maximum
 constexpr int kUp = 5;             // steps enter fp16 as 2^kUp .. 2^(kUp + 1) at most: 2^(kUp + 1 + kSlack) is far below 65504
 constexpr int kMaxCtas = 160;
@@ -406,6 +410,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
     constexpr int kSteps = D / 16;              // k16 steps of a key, m16 tiles of a value
     constexpr int kSB = 16 * D + 128 * kNS;     // bytes of a block
     constexpr int kStage = kBlk * kSB;
+    constexpr bool kDirect = G == 32;           // two tiles a sub-group: - 8 goes into their accumulators at once
     constexpr int kPieces = (kSB + 511) / 512;  // 16-byte copies of a lane for a block
     constexpr uint32_t kFull = (1u << kBlk) - 1u;
     extern __shared__ __align__(128) unsigned char smem[];
@@ -571,6 +576,23 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
             const int all_see = a.causal ? min(info.z, info.z - info.y + cc.rb * kRows / a.share + 1) : info.z;
 
             float acc[NB][kSteps][4], m[NB][2], l[NB][2], pm[NB][kNS][2];
+            constexpr int kMid = kDirect ? 1 : kNS;
+            float mid[NB][kMid][4];     // -8 sum p s (and -8 * 17, as the rows g are summed), not yet in acc
+            int turns = 0;
+            auto settle = [&]() {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[n][i][e] += mid[n][16 * i / G % kMid][e];
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int i = 0; i < kMid; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) mid[n][i][e] = 0.f;
+            };
             int ev = -110;              // the exponent that the values' steps are relative to
             float inv = pow2(kUp + 110);
 #pragma unroll
@@ -579,6 +601,10 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 for (int i = 0; i < kSteps; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[n][i][e] = 0.f;
+#pragma unroll
+                for (int i = 0; i < kMid; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mid[n][i][e] = 0.f;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     m[n][c] = -CUDART_INF_F;
@@ -717,6 +743,10 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         for (int i = 0; i < kSteps; ++i)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) acc[n][i][e] *= alpha[e & 1] * ev_f;
+#pragma unroll
+                        for (int i = 0; i < kMid && !kDirect; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) mid[n][i][e] *= alpha[e & 1] * ev_f;
                     }
                 }
 #pragma unroll
@@ -737,7 +767,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 #pragma unroll
                     for (int i = 0; i < kNS; ++i) {
                         const float s0 = wide_cache_scale(v0[b][i]) * inv, s1 = wide_cache_scale(v1[b][i]) * inv;
-                        const float m0 = wide_cache_min(v0[b][i]), m1 = wide_cache_min(v1[b][i]);
+                        const float m0 = fmaf(wide_cache_scale(v0[b][i]), 8.f, wide_cache_min(v0[b][i]));
+                        const float m1 = fmaf(wide_cache_scale(v1[b][i]), 8.f, wide_cache_min(v1[b][i]));
                         uint32_t pb[NB][2];
 #pragma unroll
                         for (int n = 0; n < NB; ++n) {
@@ -758,6 +789,9 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                             pb[n][1] = transpose8x8(pack_f16(x[2], x[3]));
                         }
 #pragma unroll
+                        for (int n = 0; n < NB && !kDirect; ++n)
+                            mma_f16(mid[n][i], kEight + kEightHigh, kEightHigh, kEight + kEightHigh, kEightHigh, pb[n][0], pb[n][1]);
+#pragma unroll
                         for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k) {
                             // Rows g take a whole byte, low code + 16 * high code: the rows g + 8, 16 * high code, come off
                             // again at the end.  That saves an instruction a word.
@@ -767,10 +801,15 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                             const uint32_t y = __byte_perm(x, 0, 0x4341);
 #pragma unroll
                             for (int n = 0; n < NB; ++n)
+                            {
                                 mma_f16(acc[n][k], x & 0x00FF00FFu, x & 0x00F000F0u, y, y & 0x00F000F0u, pb[n][0], pb[n][1]);
+                                if (kDirect)
+                                    mma_f16(acc[n][k], kEight + kEightHigh, kEightHigh, kEight + kEightHigh, kEightHigh, pb[n][0], pb[n][1]);
+                            }
                         }
                     }
                 }
+                if (!kDirect && (++turns & 3) == 0) settle();
                 // every lane has read the stage: its place takes the next one
                 __syncwarp();
                 issue(slot);
@@ -797,6 +836,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                 run = max(0, run - kBlk);
             }
             // ---- end of the item or of the piece: sums over the lanes, results in the values' own scale
+            if (!kDirect) settle();
             const float f = pow2(ev);
 #pragma unroll
             for (int n = 0; n < NB; ++n)
