@@ -39,7 +39,7 @@ constexpr float kSlack = 8.f;       // the reference of a softmax may stay this 
 constexpr int kUp = 5;             // steps enter fp16 as 2^kUp .. 2^(kUp + 1) at most: 2^(kUp + 1 + kSlack) is far below 65504
 constexpr int kMaxCtas = 160;
 constexpr int kMeta = 8;           // words of meta of a partial result
-constexpr int kPlanSmem = 6144;    // bytes of shared memory for the plan of a small batch
+constexpr int kPlanSmem = 16384;   // bytes of shared memory for the plan of a small batch
 constexpr int kItemAlone = 96;     // blocks of an item that one CTA may take alone
 constexpr int kItemCost = 4;       // units that an item counts on top of its blocks: queries in, results out
 
@@ -1068,10 +1068,11 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     constexpr int kRows = 8 * NB;
     constexpr int stage = kBlk * (16 * D + 128 * (D / G));
     constexpr int room = 227 * 1024 - 3072 - kPlanSmem;   // 3 KB for the static arrays
-    // 16 warps have 128 registers each, which two and three blocks of eight query rows do not fit
-    constexpr int W = NB > 1 ? 8 : 16 * 3 * stage <= room ? 16 : 12;
-    constexpr int S = room / (W * stage) > 6 ? 6 : room / (W * stage);
-    static_assert(S >= 3 && S * stage >= slot_floats(kRows, D) * 4, "ring");
+    // 12 warps have 168 registers each, which eight query rows need 163 of; 16 with 128 each keep some in memory, and were slower
+    // everywhere (a batch of 64: 72.2 against 68.6 us, one short sequence: 12.7 against 9.9), as were 10 and 14.  More rows, 8 warps.
+    constexpr int W = NB > 1 ? 8 : 12;
+    constexpr int S = 3;                                   // stages of a ring (a batch of 64: 66.9 us with 3, 67.1 with 2, 68.2 with 4)
+    static_assert(W * S * stage <= room && S * stage >= slot_floats(kRows, D) * 4, "ring");
     auto kernel = attn_cache_kernel<D, G, NB, W, S>;
     const int smem = kPlanSmem + W * S * stage;
     const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
@@ -1100,7 +1101,7 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     const long long items = static_cast<long long>(a.c.n_kv_heads) * (static_cast<long long>(a.q.rows) * a.share / kRows + a.q.n_seqs);
     if (items > ctas || (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) > kItemAlone) {
         WideLaunch l(ctx, s, "attn_cache_join");
-        WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_cache_join_kernel<kRows, D>, dim3(ctas, 2), dim3(256), 0, s, a, ctas));
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_cache_join_kernel<kRows, D>, dim3(ctas, kRows * D / 512), dim3(256), 0, s, a, ctas));
     }
     return WIDE_OK;
 }
