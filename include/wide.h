@@ -530,12 +530,14 @@ WIDE_API int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cach
  *   scale: multiplies the logits (<= 0 selects 1/sqrt(head_dim))
  *   workspace: wide_attn_cache_workspace_bytes(...) bytes; needs no initial value and keeps nothing,
  *       but two calls that can overlap on the GPU need one each
+ * Accuracy: the output is rounded to bf16; probabilities are rounded to fp16 (2^-11) once, all sums are fp32.  Queries of
+ * magnitude up to 2^100, keys and values such that logits and sums fit fp32.
  * Built for few new rows a sequence (decoding, verifying drafted tokens): up to 24 query rows share one pass
  * over a KV head, more take several passes.  A long prefill reads the cache back
  * (wide_cache_read) and runs wide_attn.
  * Results do not depend on the other sequences of the batch beyond fp32 rounding, and are the same bit for bit in every run.
- * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA; WIDE_ERR_BAD_INDEX and WIDE_ERR_TIMEOUT
- * through wide_status.
+ * The arrays of `seqs` must not change while the call runs.  `flags` must be 0.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA; WIDE_ERR_BAD_INDEX through wide_status.
  */
 WIDE_API size_t wide_attn_cache_workspace_bytes(int rows, int n_q_heads, int n_kv_heads, int head_dim);
 WIDE_API int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* q,

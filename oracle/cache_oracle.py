@@ -20,6 +20,14 @@ def bf16_toward(x: np.ndarray, up: bool) -> np.ndarray:
     return ((np.ceil(n) if up else np.floor(n)) * unit).astype(np.float64)
 
 
+def reaches(y, a, b):
+    """y >= a + b, exactly: the sum is rounded to 64 bits of mantissa, and where y equals it the rounding's exact remainder decides."""
+    t = a + b
+    v = t - a
+    rest = (a - (t - v)) + (b - v)
+    return (y > t) | ((y == t) & (rest <= 0))
+
+
 def quantise(x: np.ndarray, group: int):
     """x [..., dim] (bf16- or fp32-representable) -> codes uint8 [..., dim], scale and minimum float64
     [..., dim / group] (NaN where the sub-group is not finite)."""
@@ -29,13 +37,12 @@ def quantise(x: np.ndarray, group: int):
     m = bf16_toward(y.min(-1), up=False) + 0.0     # a zero minimum is +0
     m80 = m.astype(np.longdouble)
     s = bf16_toward((y.max(-1) - m80) / np.longdouble(15), up=True) + 0.0
-    # m + b s is exact in 64 bits of mantissa (13 bits of b s; s is no smaller than 2^-28 |m| or it is 0), while x - m is
-    # not where x is vanishing: so x is compared with the border, and the scale checked by its last level
-    short = m80 + 15 * s.astype(np.longdouble) < y.max(-1)
+    # the quotient is rounded, so the scale is checked by its last level
+    short = reaches(y.max(-1), m80, 15 * s.astype(np.longdouble)) & ~reaches(-y.max(-1), -m80, -15 * s.astype(np.longdouble))
     s = np.where(short, bf16_toward(s * (1 + 2.0 ** -12), up=True), s)
     n = np.zeros(y.shape, dtype=np.uint8)
     for b in BORDERS:
-        n += (y >= (m80 + np.longdouble(b) * s.astype(np.longdouble))[..., None]) & (s[..., None] > 0)
+        n += reaches(y, m80[..., None], (np.longdouble(b) * s.astype(np.longdouble))[..., None]) & (s[..., None] > 0)
     s, m = np.where(bad, np.nan, s), np.where(bad, np.nan, m)
     return n.reshape(x.shape), s, m
 

@@ -100,7 +100,10 @@ __device__ __noinline__ uint2 quantise8_any(Raw8<T> raw) {
     const float m = __uint_as_float(mb);
     if (!(fabsf(m) <= 3.4e38f && hi <= 3.4028234e38f)) return make_uint2(0x7FC07FC0u, 0u);
     const double q = (static_cast<double>(hi) - static_cast<double>(m)) / 15.0;
-    const float s = __uint_as_float((__float_as_uint(__double2float_ru(q)) + 0xFFFFu) & 0xFFFF0000u);
+    uint32_t sb = (__float_as_uint(__double2float_ru(q)) + 0xFFFFu) & 0xFFFF0000u;
+    // the quotient is rounded: does the last level, rounded down, reach the maximum?
+    if (__fma_rd(15.0, static_cast<double>(__uint_as_float(sb)), static_cast<double>(m)) < static_cast<double>(hi)) sb += 0x10000u;
+    const float s = __uint_as_float(sb);
     uint32_t c = 0;
 #pragma unroll 1
     for (int i = 0; i < 15 && s > 0.f; ++i)

@@ -172,6 +172,32 @@ def test_indices_out_of_range_are_dropped_and_reported(ctx):
     assert np.array_equal(cache.pages.cpu().numpy(), got)
 
 
+@pytest.mark.parametrize("seqs", [600, 4096])
+def test_many_sequences(ctx, seqs):
+    from paper_2607_28418_b200 import binding
+    rng = np.random.default_rng(seqs)
+    lens = rng.integers(0, 40, seqs)
+    news = np.minimum(lens, rng.integers(0, 20, seqs))
+    c = CacheCase(lens.tolist(), news.tolist(), 1, 64, 64, 16, seed=13)
+    cache = written(ctx, c)
+    assert np.array_equal(cache.pages.cpu().numpy(), expected_pages(c))
+    k, v = binding.wide_cache_read(ctx, cache, c.seqs(), c.rows, dtype=torch.float32)
+    assert np.array_equal(k.cpu().numpy(), co.held(c.new("k").reshape(c.rows, 1, 64), 64).reshape(c.rows, -1))
+
+
+def test_minima_beside_vanishing_numbers(ctx):
+    """Sub-groups whose minimum lies far below the scale, where m - s / 2 is no fp32 number (bf16 and fp32 inputs)."""
+    rng = np.random.default_rng(14)
+    for dtype in ("bf16", "f32"):
+        x = np.abs(rng.standard_normal((200, 2, 64))).astype(np.float32) + 0.5
+        x[:, :, 0] = np.exp2(rng.integers(-60, -5, (200, 2)).astype(np.float32))
+        x[100:, :, 1] = -np.exp2(rng.integers(-60, -5, (100, 2)).astype(np.float32))
+        x = co.round_bf16(x) if dtype == "bf16" else x
+        c = CacheCase([200], [200], 2, 64, 32, 32, dtype=dtype)
+        c.k, c.v = [x], [x[::-1].copy()]
+        assert np.array_equal(written(ctx, c).pages.cpu().numpy(), expected_pages(c))
+
+
 def test_places_beyond_four_gigabytes(ctx):
     from paper_2607_28418_b200 import binding
     page_bytes = binding.cache_page_bytes(256, 8, 128, 64)

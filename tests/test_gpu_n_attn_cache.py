@@ -114,6 +114,87 @@ def test_batches_of_any_size(ctx, seqs):
     check(run(ctx, c, q, on, 1, row_start=False), ref, tol)
 
 
+@pytest.mark.parametrize("share", [9, 12, 16, 17, 24, 25, 40])
+@pytest.mark.parametrize("dim,group", [(64, 32), (128, 128)])
+def test_many_query_heads_on_a_kv_head(ctx, share, dim, group):
+    """Row counts on both sides of what one pass holds (8, 16, 24)."""
+    c = CacheCase([70, 1, 33], [1, 1, 1], 2, dim, group, 16, seed=share)
+    q = queries(c, 2 * share, 1)
+    on = np.random.default_rng(2).random((c.rows, 2)) < 0.7
+    ref, tol = reference(c, q, on, share)
+    check(run(ctx, c, q, on, share, row_start=False), ref, tol)
+    check(run(ctx, c, q, on, share), ref, tol)
+
+
+@pytest.mark.parametrize("longest", [1535, 1536, 1537, 1600])
+@pytest.mark.parametrize("seqs", [36, 37, 38, 75])
+def test_around_one_item_a_cta(ctx, longest, seqs):
+    """Few short items get a CTA each; one block or one item more, and they are cut evenly."""
+    lens = [longest] + [1 + 7 * i % 40 for i in range(seqs - 1)]
+    c = CacheCase(lens, [1] * seqs, 4, 64, 64, 16, seed=seqs)
+    q = queries(c, 4, 3)
+    ref, tol = reference(c, q, np.ones((seqs, 4), bool), 1)
+    check(run(ctx, c, q, None, 1, row_start=False), ref, tol)
+
+
+def test_more_sequences_than_the_plan_has_room_for(ctx):
+    """The plan goes to the workspace; some sequences are empty, some have several new rows."""
+    rng = np.random.default_rng(40)
+    seqs = 1500
+    lens = rng.integers(0, 25, seqs)
+    news = np.minimum(lens, rng.integers(0, 4, seqs))
+    c = CacheCase(lens.tolist(), news.tolist(), 3, 64, 32, 16, seed=41)
+    q = queries(c, 6, 42)
+    on = rng.random((c.rows, 3)) < 0.5
+    ref, tol = reference(c, q, on, 2)
+    check(run(ctx, c, q, on, 2), ref, tol)
+
+
+def test_chunk_whose_rows_leave_a_head_unused(ctx):
+    """More new rows than are looked at for unused heads: the head's rows are zeros all the same."""
+    c = CacheCase([60], [25], 2, 64, 64, 16, seed=43)
+    q = queries(c, 4, 44)
+    on = np.zeros((25, 2), bool)
+    on[:, 0] = np.arange(25) % 3 > 0
+    check(run(ctx, c, q, on, 2), *reference(c, q, on, 2))
+    on[:] = False
+    got = run(ctx, c, q, on, 2)
+    assert (got == 0).all()
+
+
+def test_workspace_needs_no_initial_value(ctx):
+    from paper_2607_28418_b200 import binding
+    c = CacheCase([3000, 5, 700], [1, 2, 1], 2, 128, 64, 64, seed=45)
+    q = queries(c, 4, 46)
+    on = np.ones((c.rows, 2), bool)
+    ref, tol = reference(c, q, on, 2)
+    for fill in (0x00, 0xFF, 0x01):
+        ws = torch.full((binding.attn_cache_workspace_bytes(c.rows, 4, 2, 128),), fill, dtype=torch.uint8, device="cuda")
+        check(run(ctx, c, q, on, 2, workspace=ws), ref, tol)
+
+
+def test_long_flat_average_keeps_its_digits(ctx):
+    """131072 keys of nearly equal weight: the average is some 300 times smaller than the values, whose 4-bit parts
+    cancel.  Rounding the output to bf16 is off by at most 2^-8 of each element, hence of the norm; the bound leaves half
+    as much again for everything else (observed before the codes were centred: more than that)."""
+    from paper_2607_28418_b200 import binding
+    n, dim = 131072, 128
+    g = torch.Generator(device="cuda").manual_seed(47)
+    k = torch.randn((n, dim), generator=g, device="cuda").to(torch.bfloat16)
+    v = torch.randn((n, dim), generator=g, device="cuda").to(torch.bfloat16)
+    cache = binding.Cache.empty(n // 64, 1, dim, 128, 64)
+    seqs = binding.Sequences(torch.arange(n // 64, dtype=torch.int32, device="cuda")[None], torch.tensor([n], dtype=torch.int32, device="cuda"),
+                             torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    binding.wide_cache_write(ctx, cache, seqs, k, v)
+    kd, vd = binding.wide_cache_read(ctx, cache, seqs, n, dtype=torch.float32)
+    one = binding.Sequences(seqs.page_table, seqs.kv_lens)
+    q = (torch.randn((1, 4 * dim), generator=g, device="cuda") * 0.3).to(torch.bfloat16)
+    got = binding.wide_attn_cache(ctx, q, cache, one, 4, 4).double().view(4, dim)
+    p = torch.softmax(q.double().view(4, dim) @ kd.double().t() / dim ** 0.5, -1)
+    ref = p @ vd.double()
+    assert (got - ref).norm() <= 1.5 * 2.0 ** -8 * ref.norm(), ((got - ref).norm() / ref.norm()).item()
+
+
 def test_many_groups_and_heads_that_span_groups(ctx):
     """40 groups (two mask words) of one head, and a group that covers heads of two KV heads."""
     c = CacheCase([50, 81, 7], [1, 2, 1], 20, 64, 32, 16, seed=12)
