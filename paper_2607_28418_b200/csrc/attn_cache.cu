@@ -351,7 +351,8 @@ struct RowOut {
 __device__ __forceinline__ RowOut row_out(const AttnArgs& a, int row0, int n_rows, int kvh, const Row& w, int head_dim) {
     RowOut r;
     const int h = kvh * a.share + w.sub;
-    r.o = w.tok < n_rows ? a.o + (static_cast<size_t>(row0 + w.tok) * a.n_q + h) * head_dim : nullptr;
+    // (the comparison with all rows: what the second kernel is told comes from the workspace, which another call may be using by mistake)
+    r.o = w.tok < n_rows && static_cast<unsigned>(row0 + w.tok) < static_cast<unsigned>(a.q.rows) ? a.o + (static_cast<size_t>(row0 + w.tok) * a.n_q + h) * head_dim : nullptr;
     r.on = r.o && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, row0 + w.tok, h / a.hpg));
     return r;
 }
@@ -995,7 +996,7 @@ __global__ void __launch_bounds__(256) attn_cache_join_kernel(const __grid_const
     const int4 meta = *reinterpret_cast<const int4*>(mine);
     const int rb = mine[4];
     int st = c + 1 + lane < ctas ? a.meta[2 * (c + 1 + lane) * kMeta] : 0;
-    if (meta.x != 1) return;
+    if (meta.x != 1 || static_cast<unsigned>(meta.w) >= static_cast<unsigned>(a.c.n_kv_heads)) return;
     int n = 1;
     for (int k = c + 1;;) {
         const uint32_t stop = __ballot_sync(0xffffffffu, st != 1);

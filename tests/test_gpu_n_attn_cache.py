@@ -176,7 +176,7 @@ def test_workspace_needs_no_initial_value(ctx):
 def test_long_flat_average_keeps_its_digits(ctx):
     """131072 keys of nearly equal weight: the average is some 300 times smaller than the values, whose 4-bit parts
     cancel.  Rounding the output to bf16 is off by at most 2^-8 of each element, hence of the norm; the bound leaves half
-    as much again for everything else (observed before the codes were centred: more than that)."""
+    as much again for everything else."""
     from paper_2607_28418_b200 import binding
     n, dim = 131072, 128
     g = torch.Generator(device="cuda").manual_seed(47)
