@@ -283,9 +283,10 @@ __device__ __forceinline__ Unit find_unit(const SeqView& q, const CacheView& c, 
 }
 
 // A warp takes the keys or the values of a block (32 registers of loads in flight for bf16; with both, half as many
-// warps fit: 8188 tokens of 8 heads took 27 us instead).
+// warps fit: the write of 8188 tokens of 8 heads took 27 us instead).  Four CTAs an SM for the 16-bit types: those tokens
+// written and read back take 28.5 us, with three 30.0, with five (fewer loads in flight) 30.9.
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 3 : 2)
+__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 4 : 2)
 cache_write_kernel(CacheView c, SeqView q, const T* __restrict__ k, const T* __restrict__ v, long long ks, long long vs,
                    int* __restrict__ status) {
     constexpr int kLT = D / 8;        // lanes of a token
