@@ -483,12 +483,13 @@ typedef struct wide_cache {
  * Rows that belong to no sequence are neither read nor written.
  *
  * All three arrays are on the device and are checked there.  A sequence whose length is outside
- * [0, max_pages * page_size], or that has more new rows than positions, or whose rows are not a range
+ * [0, max_pages * page_size] or above 2^31 - 16, or that has more new rows than positions, or whose rows are not a range
  * within [0, rows], is left out (wide_attn_cache: its rows, if they are a range, become zero).  A page number outside
  * [0, n_pages) holds no tokens: writes to it are dropped, reads from it give zeros, attention does
  * not see its keys.  Each of these sets WIDE_ERR_BAD_INDEX in the context's status (wide_status).
  * Pages may be shared by sequences that read them.  No position may be written twice in one call
- * (two sequences with new tokens on one shared page, or overlapping row ranges): what it then holds is not defined.
+ * (two sequences with new tokens at one place of a shared page): what it then holds is not defined.  Row ranges must not
+ * overlap: calls on ranges that do may do nothing (and set WIDE_ERR_BAD_INDEX), or leave any of their rows and positions undefined.
  */
 typedef struct wide_seqs {
     const int32_t* page_table; /* [n_seqs, max_pages] */
@@ -508,7 +509,7 @@ WIDE_API size_t wide_cache_page_bytes(int page_size, int n_kv_heads, int head_di
  *   k, v [rows, n_kv_heads * head_dim] bf16 or fp32, rows k_stride / v_stride elements apart
  * wide_cache_read -- the same rows out of the cache, m + s n in fp32 (one rounding), then rounded to the output type; with
  * row_start = the running sum of kv_lens that is the whole cache of the sequences, as wide_attn reads it.
- *   k_out, v_out as k, v
+ *   k_out, v_out as k, v; they must not overlap
  * Rows and pointers 16-byte aligned.  One launch, no workspace.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA; WIDE_ERR_BAD_INDEX through wide_status.
  */
@@ -525,7 +526,7 @@ WIDE_API int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cach
  *     o[i, h, :] = sum_j softmax_j(scale * q[i, h, :] . k[j, h_kv, :]) v[j, h_kv, :],   h_kv = h / (n_q_heads / n_kv_heads)
  * Pairs (row, h) whose routing group h / heads_per_group is off in mask_bits, and rows that see no key,
  * give exact zeros; the cache of a KV head that no new row of a sequence uses is not read (sequences of up to 16 new rows).
- *   q   [rows, n_q_heads * head_dim] bf16, rows q_stride elements apart;  o [rows, n_q_heads * head_dim] bf16, contiguous
+ *   q   [rows, n_q_heads * head_dim] bf16, rows q_stride elements apart;  o [rows, n_q_heads * head_dim] bf16, contiguous, no overlap with q
  *   mask_bits [rows, W], n_groups = n_q_heads / heads_per_group <= WIDE_MAX_GROUPS; NULL: all groups on
  *   scale: multiplies the logits (<= 0 selects 1/sqrt(head_dim))
  *   workspace: wide_attn_cache_workspace_bytes(...) bytes; needs no initial value and keeps nothing,

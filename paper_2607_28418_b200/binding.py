@@ -460,7 +460,7 @@ def _rows(t: torch.Tensor, width: int, what: str):
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or shape[1] != width or stride[1] != 1:
         raise ValueError(f"{what}: expected [rows, {width}] with contiguous rows")
-    return t.data_ptr(), (stride[0] if shape[0] > 1 else max(width, stride[0]))
+    return t.data_ptr(), (stride[0] if shape[0] > 1 else width)     # one row may claim any stride
 
 
 def _same_device(index: int, *tensors: Optional[torch.Tensor]):

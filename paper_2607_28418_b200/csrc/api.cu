@@ -74,7 +74,7 @@ int cache_move(wide_ctx* ctx, void* stream, bool write, const wide_cache* cache,
     const long long width = static_cast<long long>(cache->n_kv_heads) * cache->head_dim;
     if ((rc = check_rows(k, ks, width, wide_elem_bytes(dtype))) != WIDE_OK) return rc;
     if ((rc = check_rows(v, vs, width, wide_elem_bytes(dtype))) != WIDE_OK) return rc;
-    if (!on_device(ctx)) return WIDE_ERR_INVALID_ARG;
+    if ((!write && k == v) || !on_device(ctx)) return WIDE_ERR_INVALID_ARG;
     if (rows == 0 || seqs->n_seqs == 0) return WIDE_OK;
     return wide_launch_cache_move(ctx, static_cast<cudaStream_t>(stream), write, cache, seqs, k, v, dtype, rows, ks, vs);
 }
@@ -545,7 +545,7 @@ int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cache, const 
     if (!wide_aligned16(o) || !wide_aligned16(workspace)) return WIDE_ERR_ALIGNMENT;
     if (!workspace || workspace_bytes < wide_attn_cache_workspace(rows, n_q_heads, cache->n_kv_heads, cache->head_dim))
         return WIDE_ERR_WORKSPACE;
-    if (!on_device(ctx)) return WIDE_ERR_INVALID_ARG;
+    if (q == o || !on_device(ctx)) return WIDE_ERR_INVALID_ARG;
     if (rows == 0 || seqs->n_seqs == 0) return WIDE_OK;
     if (!(scale > 0.f)) scale = 1.0f / sqrtf(static_cast<float>(cache->head_dim));
     return wide_launch_attn_cache(ctx, static_cast<cudaStream_t>(stream), cache, seqs, q, rows, q_stride, n_q_heads,

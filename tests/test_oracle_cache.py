@@ -163,6 +163,12 @@ def test_bad_matrices_are_refused(lib):
     assert attn(ws=None) == -4 and attn(size=16) == -4
 
 
+def test_outputs_on_top_of_inputs_are_refused(lib):
+    c, s = ctypes.byref(_cache()), ctypes.byref(_seqs())
+    assert lib.wide_cache_read(FAKE, None, c, s, P, P, 0, 8, 256, 256) == -1
+    assert lib.wide_attn_cache(FAKE, None, c, s, P, 0, 8, 1024, 8, 4, P, 1, 0.0, P, P, 1 << 30, 0) == -1
+
+
 def test_bad_rope_is_refused(lib):
     def rope(q=P, k=P, dtype=0, tokens=4, hq=2, hk=1, dim=128, rot=128, qs=256, ks=128, pos=P, axes=1, inv=P, axis=None, qo=P, ko=P,
              oqs=256, oks=128):
