@@ -217,35 +217,47 @@ __device__ __forceinline__ int blocks_of(int n_rows, int len) {
     return n_rows > 0 && len > 0 ? ((len - 1) >> 4) - ((len - n_rows) >> 4) + 1 : 0;
 }
 
+// The most blocks that `rows` rows of these sequences can touch: a sequence's n rows lie in at most n / 16 + 2 blocks, and in
+// at most n.
+__host__ __device__ __forceinline__ int most_blocks(const SeqView& q) {
+    const int a = q.rows, b = q.rows / 16 + 2 * q.n_seqs;
+    return q.row_start ? (a < b ? a : b) : q.n_seqs;
+}
+
 // seqs[s] = {first row, rows, length, blocks of the sequences before s}; returns the total.  All threads of the CTA.
-__device__ int scan_blocks(const SeqView& q, int page_shift, int4* seqs, int* part, int* status) {
+// More blocks than there can be: row ranges that overlap.  None is taken then (their number need not fit an int).
+__device__ int scan_blocks(const SeqView& q, int page_shift, int4* seqs, long long* part, int* status) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (q.n_seqs + 32 * kWarps - 1) / (32 * kWarps);
     const int a = min(q.n_seqs, tid * per), b = min(q.n_seqs, a + per);
-    int sum = 0;
+    long long sum = 0;
     for (int s = a; s < b; ++s) {
         const SeqInfo i = wide_seq_info(q, s, page_shift);
         if (i.bad && blockIdx.x == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
-        seqs[s] = make_int4(i.row0, i.n_rows, i.len, sum);
+        seqs[s] = make_int4(i.row0, i.n_rows, i.len, static_cast<int>(sum));
         sum += blocks_of(i.n_rows, i.len);
     }
-    int up = sum;
+    long long up = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, up, o);
+        const long long v = __shfl_up_sync(0xffffffffu, up, o);
         if (lane >= o) up += v;
     }
     if (lane == 31) part[warp] = up;
     __syncthreads();
-    int base = up - sum, total = 0;
+    long long base = up - sum, total = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
         if (w < warp) base += part[w];
         total += part[w];
     }
-    for (int s = a; s < b; ++s) seqs[s].w += base;
+    for (int s = a; s < b; ++s) seqs[s].w += static_cast<int>(base);
     __syncthreads();
-    return total;
+    if (total > most_blocks(q)) {
+        if (blockIdx.x == 0 && tid == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
+        total = 0;
+    }
+    return static_cast<int>(total);
 }
 
 __device__ __forceinline__ Unit find_unit(const SeqView& q, const CacheView& c, const int4* seqs, int unit) {
@@ -295,7 +307,7 @@ cache_write_kernel(CacheView c, SeqView q, const T* __restrict__ k, const T* __r
     constexpr int kNS = D / G;
     constexpr int kRounds = 16 / kP;
     extern __shared__ int4 seqs[];
-    __shared__ int part[kWarps];
+    __shared__ long long part[kWarps];
     const int lane = threadIdx.x & 31, p = lane / kLT, u8 = lane % kLT;
     const int cc = u8 >> 2, c0 = cc >> 1, c1 = cc & 1;   // 32-channel chunk of this lane's 8 channels
     int total = q.n_seqs;
@@ -445,7 +457,7 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
     constexpr int kNS = D / G;
     constexpr int kC = D / 64;
     extern __shared__ int4 seqs[];
-    __shared__ int part[kWarps];
+    __shared__ long long part[kWarps];
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     int total = q.n_seqs;
     wptx::grid_dep_wait();
@@ -534,11 +546,9 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
     }
 }
 
-// CTAs for the most blocks that `rows` rows of these sequences can touch: a sequence's n rows lie in at
-// most n / 16 + 2 blocks, and in at most n.
+// CTAs for the most blocks that there can be
 int grid_for(const wide_ctx* ctx, const CacheView& c, const SeqView& q, int units_per_block, int per_sm) {
-    const long long blocks = q.row_start ? min(static_cast<long long>(q.rows), q.rows / 16 + 2LL * q.n_seqs) : q.n_seqs;
-    const long long ctas = (blocks * c.n_kv_heads * units_per_block + kWarps - 1) / kWarps;
+    const long long ctas = (static_cast<long long>(most_blocks(q)) * c.n_kv_heads * units_per_block + kWarps - 1) / kWarps;
     return static_cast<int>(max(1LL, min(ctas, static_cast<long long>(per_sm) * ctx->sm_count)));
 }
 

@@ -172,6 +172,25 @@ def test_indices_out_of_range_are_dropped_and_reported(ctx):
     assert np.array_equal(cache.pages.cpu().numpy(), got)
 
 
+def test_row_ranges_that_overlap_many_times_are_dropped_and_reported(ctx):
+    """More blocks than the rows could touch: the sum of the ranges need not fit anything, so the call does nothing."""
+    from paper_2607_28418_b200 import binding
+    n = 64
+    c = CacheCase([48] * n, [1] * n, 2, 64, 64, 16, seed=33)
+    rows = 48
+    start = torch.tensor([rows * (s & 1) for s in range(n + 1)], dtype=torch.int32, device="cuda")
+    seqs = binding.Sequences(torch.from_numpy(c.table).cuda(), torch.full((n,), 48, dtype=torch.int32, device="cuda"), start)
+    x = torch.ones((rows, 128), dtype=torch.bfloat16, device="cuda")
+    cache = c.cache(c.garbage.copy())
+    binding.wide_cache_write(ctx, cache, seqs, x, x)
+    assert ctx.status() == binding.ERR_BAD_INDEX
+    assert np.array_equal(cache.pages.cpu().numpy(), c.garbage)
+    k, v = torch.full((rows, 128), 9.0, device="cuda"), torch.full((rows, 128), 9.0, device="cuda")
+    binding.wide_cache_read(ctx, cache, seqs, rows, k=k, v=v)
+    assert ctx.status() == binding.ERR_BAD_INDEX
+    assert (k == 9).all() and (v == 9).all()
+
+
 @pytest.mark.parametrize("seqs", [600, 4096])
 def test_many_sequences(ctx, seqs):
     from paper_2607_28418_b200 import binding
