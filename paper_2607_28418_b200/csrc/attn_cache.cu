@@ -1074,7 +1074,7 @@ template <int D, int G, int NB>
 int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     constexpr int kRows = 8 * NB;
     constexpr int stage = kBlk * (16 * D + 128 * (D / G));
-    constexpr int room = 227 * 1024 - 3072 - kPlanSmem;   // 3 KB for the static arrays
+    constexpr int room = (227 - 3) * 1024 - kPlanSmem;   // 3 KB for the static arrays
     // 12 warps have 168 registers each, which eight query rows need 163 of; 16 with 128 each keep some in memory, and were slower
     // everywhere (a batch of 64: 72.2 against 68.6 us, one short sequence: 12.7 against 9.9), as were 10 and 14.  More rows, 8 warps.
     constexpr int W = NB > 1 ? 8 : 12;

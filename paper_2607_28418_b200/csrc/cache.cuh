@@ -3,6 +3,8 @@
 
 #include "internal.h"
 
+constexpr int WIDE_MAX_LEN = 0x7ffffff0;   // of a sequence: rounded up to whole blocks it stays an int
+
 struct CacheView {
     uint8_t* pages;
     int n_pages, page_shift, n_kv_heads;   // page_size = 1 << page_shift
@@ -33,7 +35,7 @@ __device__ __forceinline__ SeqInfo wide_seq_info(const SeqView& q, int s, int pa
     }
     const bool rows_ok = a >= 0 && b >= a && b <= q.rows;
     const int len = q.kv_lens[s];
-    const bool len_ok = len >= 0 && static_cast<long long>(len) <= (static_cast<long long>(q.max_pages) << page_shift) &&
+    const bool len_ok = len >= 0 && len <= WIDE_MAX_LEN && static_cast<long long>(len) <= (static_cast<long long>(q.max_pages) << page_shift) &&
                         (!rows_ok || len >= b - a);
     i.row0 = a;
     i.n_rows = rows_ok ? b - a : 0;

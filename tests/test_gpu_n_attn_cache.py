@@ -297,6 +297,28 @@ def test_strided_queries_and_rows_behind_the_last_sequence(ctx):
     assert (o[c.rows:] == 5).all()
 
 
+def test_lengths_at_the_end_of_the_integers(ctx):
+    """A length that cannot be rounded up to whole blocks is left out and reported; its row is zero, its neighbour's is not."""
+    from paper_2607_28418_b200 import binding
+    c = CacheCase([40, 200], [1, 1], 2, 64, 64, 256, seed=35)
+    q = queries(c, 4, 36)
+    table = torch.full((2, 1 << 23), int(c.table[0, 0]), dtype=torch.int32, device="cuda")    # 2^31 positions
+    table[1, 0] = int(c.table[1, 0])
+    seqs = binding.Sequences(table, torch.tensor([2 ** 31 - 1, 200], dtype=torch.int32, device="cuda"))
+    ref, tol = reference(c, q, np.ones((2, 2), bool), 2)
+    ref[0], tol[0] = 0, 0
+    cache = c.cache(c.full_pages())
+    o = torch.full((2, 256), 5.0, dtype=torch.bfloat16, device="cuda")
+    binding.wide_attn_cache(ctx, to_device(q.reshape(2, -1)), cache, seqs, 4, 2, o=o)
+    assert ctx.status() == binding.ERR_BAD_INDEX
+    check(o, ref, tol)
+    before = cache.pages.cpu().numpy()
+    one = torch.ones((2, 128), dtype=torch.bfloat16, device="cuda")
+    binding.wide_cache_write(ctx, cache, binding.Sequences(table[:1], seqs.kv_lens[:1]), one[:1], one[:1])
+    assert ctx.status() == binding.ERR_BAD_INDEX
+    assert np.array_equal(cache.pages.cpu().numpy(), before)
+
+
 def test_indices_out_of_range(ctx):
     """Keys on pages that are none are seen by nobody; sequences with a bad length give zeros; all is reported."""
     from paper_2607_28418_b200 import binding
