@@ -91,6 +91,8 @@ struct WideLaunch {
     } while (0)
 
 static inline bool wide_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// rows that 32-byte accesses can walk
+static inline bool wide_rows32(const void* p, long long row_bytes) { return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(row_bytes)) & 31u) == 0; }
 static inline size_t wide_align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 static inline int wide_elem_bytes(int dtype) { return dtype == WIDE_BF16 ? 2 : 4; }
 

@@ -127,6 +127,25 @@ def test_rows_of_a_fused_projection_and_rows_behind_the_last_sequence(ctx):
     assert np.array_equal(out[:c.rows, width:2 * width].float().cpu().numpy(), ref)
 
 
+@pytest.mark.parametrize("offset,extra", [(0, 0), (4, 0), (0, 4), (4, 4), (8, 8)])
+def test_f32_rows_at_every_16_bytes(ctx, offset, extra):
+    """Rows on 16-byte but not on 32-byte boundaries are the same values, and nothing beside them is touched."""
+    from paper_2607_28418_b200 import binding
+    c = CacheCase([50, 20], [9, 20], 2, 64, 32, 16, seed=8, dtype="f32")
+    flat = torch.full((offset + c.rows * (256 + extra) + 8,), 7.0, device="cuda")
+    both = flat[offset:offset + c.rows * (256 + extra)].view(c.rows, 256 + extra)
+    k, v = both[:, :128], both[:, 128:256]
+    k.copy_(to_device(c.new("k"), "f32"))
+    v.copy_(to_device(c.new("v"), "f32"))
+    cache = c.cache(c.garbage.copy())
+    binding.wide_cache_write(ctx, cache, c.seqs(), k, v)
+    assert np.array_equal(cache.pages.cpu().numpy(), expected_pages(c))
+    binding.wide_cache_read(ctx, cache, c.seqs(), c.rows, k=k, v=v)
+    for got, which in ((k, "k"), (v, "v")):
+        assert np.array_equal(got.cpu().numpy(), co.held(c.new(which).reshape(c.rows, 2, 64), 32).reshape(c.rows, -1).astype(np.float32))
+    assert (both[:, 256:] == 7).all() and (flat[:offset] == 7).all() and (flat[-8:] == 7).all()
+
+
 def test_indices_out_of_range_are_dropped_and_reported(ctx):
     from paper_2607_28418_b200 import binding
     c = CacheCase([40, 40, 40, 40, 40], [40, 40, 40, 40, 40], 2, 64, 64, 16, seed=9)

@@ -53,6 +53,25 @@ def test_against_the_oracle(ctx, dim, rot, interleaved, axes, dtype, T):
             assert (err <= tolerance(ref, x, dtype)).all(), err.max()
 
 
+@pytest.mark.parametrize("offset,extra", [(0, 0), (4, 0), (0, 4), (4, 4), (8, 8)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_f32_rows_at_every_16_bytes(ctx, offset, extra, interleaved):
+    """Rows on 16-byte but not on 32-byte boundaries, rotated in place: the same bits, and nothing beside them is touched."""
+    from paper_2607_28418_b200 import binding
+    T, heads, dim = 21, 3, 64
+    x = to_device(inputs(T, heads, dim, 7, "f32").reshape(T, -1), "f32")
+    dev = (torch.arange(T, dtype=torch.int32, device="cuda") * 11,
+           torch.tensor([10000.0 ** (-2 * i / 48) for i in range(24)], dtype=torch.float64, device="cuda"))
+    ref, _ = binding.wide_rope(ctx, x, None, *dev, head_dim=dim, interleaved=interleaved)
+    flat = torch.full((offset + T * (192 + extra) + 8,), 7.0, device="cuda")
+    rows = flat[offset:offset + T * (192 + extra)].view(T, 192 + extra)
+    q = rows[:, :192]
+    q.copy_(x)
+    binding.wide_rope(ctx, q, None, *dev, head_dim=dim, interleaved=interleaved, q_out=q)
+    assert torch.equal(q, ref)
+    assert (rows[:, 192:] == 7).all() and (flat[:offset] == 7).all() and (flat[-8:] == 7).all()
+
+
 def test_far_and_negative_positions(ctx):
     from paper_2607_28418_b200 import binding
     pos = np.array([[0, 1, -1, 999999, 2 ** 31 - 1, -2 ** 31, 16777217, 12345678]], dtype=np.int32)
