@@ -488,8 +488,8 @@ typedef struct wide_cache {
  * [0, n_pages) holds no tokens: writes to it are dropped, reads from it give zeros, attention does
  * not see its keys.  Each of these sets WIDE_ERR_BAD_INDEX in the context's status (wide_status).
  * Pages may be shared by sequences that read them.  No position may be written twice in one call
- * (two sequences with new tokens at one place of a shared page): what it then holds is not defined.  Row ranges must not
- * overlap: calls on ranges that do may do nothing (and set WIDE_ERR_BAD_INDEX), or leave any of their rows and positions undefined.
+ * (two sequences with new tokens at one place of a shared page): what it then holds is not defined.  row_start must ascend:
+ * where it does not, WIDE_ERR_BAD_INDEX is set and any of the call's rows, and positions of its sequences, may be left out.
  */
 typedef struct wide_seqs {
     const int32_t* page_table; /* [n_seqs, max_pages] */

@@ -14,7 +14,7 @@
 
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4;           // of a CTA (8 start and end in larger steps: 8188 tokens written and read back 28.7 us, with four 27.5)
 
 // 8 neighbouring channels as they lie in memory
 template <typename T> struct Raw8;
@@ -205,8 +205,11 @@ __device__ __forceinline__ void quantise_two(const Raw8<T>& r0, const Raw8<T>& r
     fine1 = b.fine;
 }
 
-// Which block a warp's unit is.  With row_start NULL a unit is (sequence, head); else the CTA sums the
-// sequences' block counts once and every warp finds its sequence by bisection.
+// Which block a warp's unit is.  With row_start NULL it belongs to sequence unit / heads.  Else sequence s has the slots from
+// slot_of(row_start[s], s) on: room for the most blocks that its n rows can touch, n of them or, where that is less for
+// all sequences together, n / 16 + 2.  Slots that it does not need stay empty; so no sequence has to know the blocks of those
+// before it, and a warp finds its own by a 32-way search.  (Summing the blocks of all sequences in every CTA, 4096 sequences of one
+// row and 8 heads took 59 us to read instead of 32, 64 of five rows 3.6 instead of 3.1.)
 struct Unit {
     int row0, first, len;   // rows from row0 on are positions [first, len)
     int seq, block, head;
@@ -217,88 +220,56 @@ __device__ __forceinline__ int blocks_of(int n_rows, int len) {
     return n_rows > 0 && len > 0 ? ((len - 1) >> 4) - ((len - n_rows) >> 4) + 1 : 0;
 }
 
-// The most blocks that `rows` rows of these sequences can touch: a sequence's n rows lie in at most n / 16 + 2 blocks, and in
-// at most n.
-__host__ __device__ __forceinline__ int most_blocks(const SeqView& q) {
-    const int a = q.rows, b = q.rows / 16 + 2 * q.n_seqs;
-    return q.row_start ? (a < b ? a : b) : q.n_seqs;
+__host__ __device__ __forceinline__ bool slot_a_row(const SeqView& q) { return q.rows <= q.rows / 16 + 2 * q.n_seqs; }
+__host__ __device__ __forceinline__ int slots_of(const SeqView& q) {
+    return !q.row_start ? q.n_seqs : slot_a_row(q) ? q.rows : q.rows / 16 + 2 * q.n_seqs;
 }
+__device__ __forceinline__ int slot_of(int row, int s, bool a_row) { return a_row ? row : (row >> 4) + 2 * s; }
 
-// seqs[s] = {first row, rows, length, blocks of the sequences before s}; returns the total.  All threads of the CTA.
-// More blocks than there can be: row ranges that overlap.  None is taken then (their number need not fit an int).
-__device__ int scan_blocks(const SeqView& q, int page_shift, int4* seqs, long long* part, int* status) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (q.n_seqs + 32 * kWarps - 1) / (32 * kWarps);
-    const int a = min(q.n_seqs, tid * per), b = min(q.n_seqs, a + per);
-    long long sum = 0;
-    for (int s = a; s < b; ++s) {
-        const SeqInfo i = wide_seq_info(q, s, page_shift);
-        if (i.bad && blockIdx.x == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
-        seqs[s] = make_int4(i.row0, i.n_rows, i.len, static_cast<int>(sum));
-        sum += blocks_of(i.n_rows, i.len);
-    }
-    long long up = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, up, o);
-        if (lane >= o) up += v;
-    }
-    if (lane == 31) part[warp] = up;
-    __syncthreads();
-    long long base = up - sum, total = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) base += part[w];
-        total += part[w];
-    }
-    for (int s = a; s < b; ++s) seqs[s].w += static_cast<int>(base);
-    __syncthreads();
-    if (total > most_blocks(q)) {
-        if (blockIdx.x == 0 && tid == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
-        total = 0;
-    }
-    return static_cast<int>(total);
-}
-
-__device__ __forceinline__ Unit find_unit(const SeqView& q, const CacheView& c, const int4* seqs, int unit) {
+// The whole warp.  Whatever row_start holds, the block found lies within its sequence.
+__device__ __forceinline__ Unit find_unit(const SeqView& q, const CacheView& c, int unit) {
     Unit u;
-    const int i = unit / c.n_kv_heads;
+    const int i = unit / c.n_kv_heads, lane = threadIdx.x & 31;
     u.head = unit - i * c.n_kv_heads;
     u.seq = i;
-    u.block = 0;
-    u.bad = false;
-    int n_rows;
+    long long nth = 0;
     if (q.row_start) {
-        int lo = 0, hi = q.n_seqs - 1;   // the last sequence that starts at or before block i
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (seqs[mid].w <= i) lo = mid;
-            else hi = mid - 1;
+        const bool a_row = slot_a_row(q);
+        int lo = 0, at = 0;               // the last sequence whose slots begin at or before i, and where they do
+        for (int n = q.n_seqs; n > 0;) {
+            const int stride = (n + 31) >> 5, s = lo + lane * stride;
+            const int first = lane * stride < n ? slot_of(q.row_start[s], s, a_row) : 0;
+            const uint32_t before = __ballot_sync(0xffffffffu, lane * stride < n && first <= i);
+            const int k = before ? 31 - __clz(before) : 0;
+            at = __shfl_sync(0xffffffffu, first, k);
+            lo += k * stride;
+            n = stride > 1 ? min(stride, n - k * stride) : 0;
         }
-        const int4 f = seqs[lo];
         u.seq = lo;
-        u.block = i - f.w;
-        u.row0 = f.x;
-        u.len = f.z;
-        n_rows = f.y;
-    } else {
-        const SeqInfo f = wide_seq_info(q, i, c.page_shift);
-        u.row0 = f.row0;
-        u.len = f.len;
-        n_rows = f.n_rows;
-        u.bad = f.bad;
+        nth = static_cast<long long>(i) - at;
     }
-    u.first = u.len - n_rows;
-    u.some = blocks_of(n_rows, u.len) > 0;
-    if (u.some) u.block += u.first >> 4;
+    const SeqInfo f = wide_seq_info(q, u.seq, c.page_shift);
+    u.row0 = f.row0;
+    u.len = f.len;
+    u.bad = f.bad;
+    u.first = u.len - f.n_rows;
+    u.some = nth >= 0 && nth < blocks_of(f.n_rows, u.len);
+    u.block = u.some ? (u.first >> 4) + static_cast<int>(nth) : 0;
     return u;
 }
 
+// sequences that no unit leads to are checked too
+__device__ __forceinline__ void report_bad(const SeqView& q, int page_shift, int* status) {
+    if (q.row_start)
+        for (int s = blockIdx.x * blockDim.x + threadIdx.x; s < q.n_seqs; s += gridDim.x * blockDim.x)
+            if (wide_seq_info(q, s, page_shift).bad) atomicExch(status, WIDE_ERR_BAD_INDEX);
+}
+
 // A warp takes the keys or the values of a block (32 registers of loads in flight for bf16; with both, half as many
-// warps fit: the write of 8188 tokens of 8 heads took 27 us instead).  Four CTAs an SM for the 16-bit types: those tokens
-// written and read back take 28.5 us, with three 30.0, with five (fewer loads in flight) 30.9.
+// warps fit: the write of 8188 tokens of 8 heads took 27 us instead).  32 warps an SM for the 16-bit types: those tokens
+// written and read back take 28.5 us, with 24 30.0, with 40 (fewer loads in flight) 30.9, all in CTAs of eight warps.
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 4 : 2)
+__global__ void __launch_bounds__(32 * kWarps, sizeof(T) == 2 ? 8 : 4)
 cache_write_kernel(CacheView c, SeqView q, const T* __restrict__ k, const T* __restrict__ v, long long ks, long long vs,
                    int* __restrict__ status) {
     constexpr int kLT = D / 8;        // lanes of a token
@@ -306,17 +277,14 @@ cache_write_kernel(CacheView c, SeqView q, const T* __restrict__ k, const T* __r
     constexpr int kLW = G / 8;        // lanes of a sub-group
     constexpr int kNS = D / G;
     constexpr int kRounds = 16 / kP;
-    extern __shared__ int4 seqs[];
-    __shared__ long long part[kWarps];
     const int lane = threadIdx.x & 31, p = lane / kLT, u8 = lane % kLT;
     const int cc = u8 >> 2, c0 = cc >> 1, c1 = cc & 1;   // 32-channel chunk of this lane's 8 channels
-    int total = q.n_seqs;
+    const int total = slots_of(q);
     wptx::grid_dep_wait();
-    if (q.row_start) total = scan_blocks(q, c.page_shift, seqs, part, status);
     const long long units = 2LL * total * c.n_kv_heads;
     for (long long unit = static_cast<long long>(blockIdx.x) * kWarps + (threadIdx.x >> 5); unit < units;
          unit += static_cast<long long>(gridDim.x) * kWarps) {
-        const Unit w = find_unit(q, c, seqs, static_cast<int>(unit >> 1));
+        const Unit w = find_unit(q, c, static_cast<int>(unit >> 1));
         const bool values = unit & 1;
         if (w.bad && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
         if (!w.some) continue;
@@ -346,9 +314,14 @@ cache_write_kernel(CacheView c, SeqView q, const T* __restrict__ k, const T* __r
         }
         uint32_t* words = reinterpret_cast<uint32_t*>(blk + 16 * D + (values ? 64 * kNS : 0));
         uint32_t code[kRounds];
+        // Rounds without a new token are left out: one row a sequence, 8 heads, 1024 sequences: 18 us instead of 29.5 (64: 3.7, 4.9);
+        // 8188 tokens in full blocks pay 0.3 of 27 us.
+        const uint32_t rounds = __reduce_or_sync(0xffffffffu, here);
         uint32_t odd = 0;             // rounds that need the slow way (the lanes of a sub-group agree)
 #pragma unroll
         for (int i = 0; i < kRounds; i += 2) {
+            code[i] = code[i + 1] = 0;
+            if (!((rounds >> i) & 3u)) continue;
             uint32_t word[2];
             bool fine[2];
             quantise_two<kLW>(raw[i], raw[i + 1], code[i], code[i + 1], word[0], word[1], fine[0], fine[1]);
@@ -424,6 +397,7 @@ cache_write_kernel(CacheView c, SeqView q, const T* __restrict__ k, const T* __r
             }
         }
     }
+    report_bad(q, c.page_shift, status);
 }
 
 __device__ __forceinline__ void store_values(__nv_bfloat16* p, const float (&x)[8], bool) {
@@ -455,20 +429,17 @@ __device__ __forceinline__ void store_values(float* p, const float (&x)[4]) {
 // The reverse: a lane takes the words that a lane of wide_attn_cache would (one 16-byte piece per 64
 // channels), which hold 8 neighbouring channels of two keys and 4 of four values.  A warp's next block is on its way while
 // it writes one out.  wide: rows of k allow 32-byte stores (fp32: two 16-byte stores leave half of every 32-byte sector to the
-// second; 5356 tokens of 40 heads of 64 take 26 us with one, 27.6 with two).  Keys and values in warps of their own, four or
-// more CTAs an SM, whole rows a store: no faster.
+// second; 5356 tokens of 40 heads of 64 take 26 us with one, 27.6 with two).  Keys and values in warps of their own, more than
+// 24 warps an SM, whole rows a store: no faster.
 template <typename T, int D, int G>
-__global__ void __launch_bounds__(32 * kWarps, 3)
+__global__ void __launch_bounds__(32 * kWarps, 6)
 cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, long long ks, long long vs, bool wide,
                   int* __restrict__ status) {
     constexpr int kNS = D / G;
     constexpr int kC = D / 64;
-    extern __shared__ int4 seqs[];
-    __shared__ long long part[kWarps];
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    int total = q.n_seqs;
+    const int total = slots_of(q);
     wptx::grid_dep_wait();
-    if (q.row_start) total = scan_blocks(q, c.page_shift, seqs, part, status);
     const long long units = static_cast<long long>(total) * c.n_kv_heads, step = static_cast<long long>(gridDim.x) * kWarps;
     struct Block {
         Unit w;
@@ -479,7 +450,7 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
     auto fetch = [&](long long unit, Block& b) {
         b.some = false;
         if (unit >= units) return;
-        b.w = find_unit(q, c, seqs, static_cast<int>(unit));
+        b.w = find_unit(q, c, static_cast<int>(unit));
         if (b.w.bad && lane == 0) atomicExch(status, WIDE_ERR_BAD_INDEX);
         b.some = b.w.some;
         if (!b.some) return;
@@ -551,30 +522,30 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
             }
         }
     }
+    report_bad(q, c.page_shift, status);
 }
 
-// CTAs for the most blocks that there can be
-int grid_for(const wide_ctx* ctx, const CacheView& c, const SeqView& q, int units_per_block, int per_sm) {
-    const long long ctas = (static_cast<long long>(most_blocks(q)) * c.n_kv_heads * units_per_block + kWarps - 1) / kWarps;
-    return static_cast<int>(max(1LL, min(ctas, static_cast<long long>(per_sm) * ctx->sm_count)));
+// CTAs for the slots.  Writing: twice what is resident, if there is so much.  Reading: what is resident,
+// so that a warp asks for its next block ahead; but three times that where there is so much, since later CTAs then even out
+// what the first ones finish unevenly (8 heads of 128 read into bf16, resident / three times: 8192 tokens 9.5 / 10.8 us, 16384
+// 17.6 / 18.0, 24576 25.7 / 24.5, 65536 68.6 / 63.0).
+int grid_for(const wide_ctx* ctx, const CacheView& c, const SeqView& q, bool write) {
+    const long long units = static_cast<long long>(slots_of(q)) * c.n_kv_heads * (write ? 2 : 1);
+    const long long ctas = (units + kWarps - 1) / kWarps, sms = ctx->sm_count;
+    return static_cast<int>(max(1LL, min(ctas, write ? 16 * sms : ctas > 18 * sms ? 18 * sms : 6 * sms)));
 }
 
 template <typename T, int D, int G>
 int launch(wide_ctx* ctx, cudaStream_t s, bool write, const CacheView& c, const SeqView& q, void* k, void* v, long long ks,
            long long vs) {
-    const int grid = grid_for(ctx, c, q, write ? 2 : 1, write ? 8 : 3);
-    const size_t smem = q.row_start ? static_cast<size_t>(q.n_seqs) * sizeof(int4) : 0;
+    const int grid = grid_for(ctx, c, q, write);
     int* status = ctx->d_status + WIDE_STATUS_INDEX;
-    if (smem > 48 * 1024) {
-        const void* kernel = write ? reinterpret_cast<const void*>(cache_write_kernel<T, D, G>) : reinterpret_cast<const void*>(cache_read_kernel<T, D, G>);
-        WIDE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WIDE_MAX_SEQS * sizeof(int4)));
-    }
     WideLaunch l(ctx, s, write ? "cache_write" : "cache_read");
     if (write)
-        WIDE_CUDA_CHECK(wide_launch_after(ctx, cache_write_kernel<T, D, G>, dim3(grid), dim3(32 * kWarps), smem, s, c, q,
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, cache_write_kernel<T, D, G>, dim3(grid), dim3(32 * kWarps), 0, s, c, q,
                                           static_cast<const T*>(k), static_cast<const T*>(v), ks, vs, status));
     else
-        WIDE_CUDA_CHECK(wide_launch_after(ctx, cache_read_kernel<T, D, G>, dim3(grid), dim3(32 * kWarps), smem, s, c, q, static_cast<T*>(k),
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, cache_read_kernel<T, D, G>, dim3(grid), dim3(32 * kWarps), 0, s, c, q, static_cast<T*>(k),
                                           static_cast<T*>(v), ks, vs, wide_rows32(k, ks * static_cast<long long>(sizeof(T))), status));
     return WIDE_OK;
 }

@@ -191,23 +191,52 @@ def test_indices_out_of_range_are_dropped_and_reported(ctx):
     assert np.array_equal(cache.pages.cpu().numpy(), got)
 
 
-def test_row_ranges_that_overlap_many_times_are_dropped_and_reported(ctx):
-    """More blocks than the rows could touch: the sum of the ranges need not fit anything, so the call does nothing."""
+@pytest.mark.parametrize("rows", [48, 640])
+def test_row_start_that_does_not_ascend_is_reported(ctx, rows):
+    """Which rows are then left out is open, but nothing that is not theirs is touched."""
     from paper_2607_28418_b200 import binding
     n = 64
     c = CacheCase([48] * n, [1] * n, 2, 64, 64, 16, seed=33)
-    rows = 48
-    start = torch.tensor([rows * (s & 1) for s in range(n + 1)], dtype=torch.int32, device="cuda")
-    seqs = binding.Sequences(torch.from_numpy(c.table).cuda(), torch.full((n,), 48, dtype=torch.int32, device="cuda"), start)
-    x = torch.ones((rows, 128), dtype=torch.bfloat16, device="cuda")
-    cache = c.cache(c.garbage.copy())
-    binding.wide_cache_write(ctx, cache, seqs, x, x)
-    assert ctx.status() == binding.ERR_BAD_INDEX
-    assert np.array_equal(cache.pages.cpu().numpy(), c.garbage)
-    k, v = torch.full((rows, 128), 9.0, device="cuda"), torch.full((rows, 128), 9.0, device="cuda")
+    x = torch.ones((rows + 8, 128), dtype=torch.bfloat16, device="cuda")
+    for start in ([48 * (s & 1) for s in range(n + 1)], [rows - 10 * s for s in range(n + 1)], [-5] + [2 ** 31 - 1] * n, [-2 ** 31] * n + [rows]):
+        seqs = binding.Sequences(torch.from_numpy(c.table).cuda(), torch.full((n,), 48, dtype=torch.int32, device="cuda"),
+                                 torch.tensor(start, dtype=torch.int32, device="cuda"))
+        cache = c.cache(c.garbage.copy())
+        binding.wide_cache_write(ctx, cache, seqs, x[:rows], x[:rows])
+        assert ctx.status() == binding.ERR_BAD_INDEX
+        got = cache.pages.cpu().numpy()
+        spare = np.setdiff1d(np.arange(c.n_pages), c.table.ravel())
+        assert len(spare) and np.array_equal(got[spare], c.garbage[spare])
+        k, v = torch.full((rows + 8, 128), 9.0, device="cuda"), torch.full((rows + 8, 128), 9.0, device="cuda")
+        binding.wide_cache_read(ctx, cache, seqs, rows, k=k[:rows], v=v[:rows])
+        assert ctx.status() == binding.ERR_BAD_INDEX
+        assert (k[rows:] == 9).all() and (v[rows:] == 9).all()
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 64, 65, 1023, 1025, 2100])
+@pytest.mark.parametrize("most", [1, 3, 40])
+def test_every_sequence_is_found(ctx, n, most):
+    """Sequences of no, few and many new rows (and rows before the first and behind the last): written and read back are all
+    of theirs and only those."""
+    from paper_2607_28418_b200 import binding
+    rng = np.random.default_rng(1000 * n + most)
+    news = rng.integers(0, most + 1, n)
+    lens = news + rng.integers(0, 40, n)
+    start = 7 + np.concatenate([[0], np.cumsum(news)])
+    rows, pages = int(start[-1]) + 9, 5                      # five pages of 16 for up to 79 positions
+    table = rng.permutation(pages * n).astype(np.int32).reshape(n, pages)
+    cache = binding.Cache(torch.zeros((pages * n, binding.cache_page_bytes(16, 1, 64, 64)), dtype=torch.uint8, device="cuda"), 1, 64, 64, 16)
+    seqs = binding.Sequences(*(torch.from_numpy(a.astype(np.int32)).cuda() for a in (table, lens, start)))
+    x = torch.arange(1, rows + 1, dtype=torch.float32, device="cuda")[:, None].expand(rows, 64).contiguous()
+    binding.wide_cache_write(ctx, cache, seqs, x, -x)
+    k, v = torch.full((rows, 64), 0.5, device="cuda"), torch.full((rows, 64), 0.5, device="cuda")
     binding.wide_cache_read(ctx, cache, seqs, rows, k=k, v=v)
-    assert ctx.status() == binding.ERR_BAD_INDEX
-    assert (k == 9).all() and (v == 9).all()
+    assert ctx.status() == 0
+    # channels all alike are held as their bf16 floor and a step up to it: within half a step, 2^-7 of the value / 15, of x
+    own = slice(7, rows - 9)
+    assert ((k - x).abs()[own] <= 2.0 ** -7 * x[own]).all() and ((v + x).abs()[own] <= 2.0 ** -7 * x[own]).all()
+    for y in (k, v):
+        assert (y[:7] == 0.5).all() and (y[rows - 9:] == 0.5).all()
 
 
 @pytest.mark.parametrize("seqs", [600, 4096])
