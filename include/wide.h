@@ -531,8 +531,10 @@ WIDE_API int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cach
  *   scale: multiplies the logits (<= 0 selects 1/sqrt(head_dim))
  *   workspace: wide_attn_cache_workspace_bytes(...) bytes; needs no initial value and keeps nothing,
  *       but two calls that can overlap on the GPU need one each
- * Accuracy: the output is rounded to bf16; probabilities are rounded to fp16 (2^-11) once, all sums are fp32.  Queries of
- * magnitude up to 2^100, keys and values such that logits and sums fit fp32.
+ * Accuracy: the output is rounded to bf16; a probability times the step of a value's sub-group is rounded to fp16 once (2^-11 of
+ * itself, or 2^-27 of the largest such product of the row and sub-group: values that a row gives no weight cost it no digits), all
+ * sums are fp32, probabilities 2^126 times smaller than the largest are zero.  A query number is rounded to 2^-34 of the largest of
+ * its row and head (bf16 numbers down to 2^-25 of it are exact).  Queries of magnitude up to 2^100, keys and values such that logits and sums fit fp32.
  * Built for few new rows a sequence (decoding, verifying drafted tokens): up to 24 query rows share one pass
  * over a KV head, more take several passes.  A long prefill reads the cache back
  * (wide_cache_read) and runs wide_attn.

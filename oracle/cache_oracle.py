@@ -144,5 +144,60 @@ def attention_tolerance(ref: np.ndarray, q: np.ndarray, k: np.ndarray, v: np.nda
     return 2.0 ** -8 * np.abs(ref) + 4 * 2.0 ** -11 * vmax + 2 * vmax * 4 * (dim + 16) * 2.0 ** -23 * logits
 
 
+def attention_with_bound(q: np.ndarray, k: np.ndarray, v: np.ndarray, group: int, on: np.ndarray, heads_per_group: int, causal: bool = True,
+                         scale: float = 0.0, lost=(), blocks: int = 2):
+    """`attention` of one sequence whose cache was written from k and v [L, heads, dim], with a bound for every output element that
+    counts only what the row itself weighs: (o, bound) [n, n_q_heads, dim].  `blocks`: 16-key blocks that one warp takes at most.
+    With the natural logits z, p = exp(z - max z) and l = sum p, a value m + s c (code c) and an output o, wide_attn_cache may be off by
+      - the output's rounding to bf16: 2^-8 |o|
+      - weighed steps p s in fp16: half a unit, 2^-11 of each, or 2^-27 of the row's and sub-group's largest where that is more (its
+        product is 2^2 at least and the smallest fp16 numbers are 2^-24 apart), never more than p s itself; each times |c - 8|
+      - fp32 sums of p s (c - 8): the tensor core adds at most c + 16 c' + 8 * 17 < 400 times p s (c' the code that shares the byte)
+        to a sum and is off by 2^-22 of it at most each time; a block is two such additions, and eight fp32 ones join the parts
+      - fp32 sums of p (m + 8 s): every lane adds two keys a block, then five lanes and the parts are joined; 2^-24 each
+      - logits: sum_d q (s c + m) is added by the tensor core in dim / 16 <= 8 steps (2^-22 each), the sum of the queries beside the
+        minimum in 34 (2^-24 each), and six roundings join them: below 48 * 2^-23 of sum_d |q| (s c + |m|) times scale
+      - exponentials: 2^-22 of their own and of the joining, 2^-24 of the argument: with the logits' part each p is off by a share eps, and o by
+        sum p eps |v - o| / l.
+    The sum is rounded up by 2 % for products of these."""
+    n, hq, dim = q.shape
+    L, hkv, _ = k.shape
+    scale = scale if scale > 0 else dim ** -0.5
+    out, bound = np.zeros((n, hq, dim)), np.zeros((n, hq, dim))
+    if L == 0:
+        return out, bound
+
+    def parts(x):
+        c, s, m = quantise(x, group)
+        return c.astype(np.float64), *(np.repeat(y.astype(np.float64), group, -1) for y in (s, m))
+    kc, ks, km = parts(k)
+    vc, vs, vm = parts(v)
+    kh, vh = km + ks * kc, vm + vs * vc
+    ka = np.abs(km) + ks * kc
+    live = np.ones(L, dtype=bool)
+    live[list(lost)] = False
+    for i in range(n):
+        see = live & (np.arange(L) <= (L - n + i if causal else L - 1))
+        if not see.any():
+            continue
+        for h in range(hq):
+            if not on[i, h // heads_per_group]:
+                continue
+            a = h // (hq // hkv)
+            x = q[i, h].astype(np.float64)
+            z = kh[see, a] @ x * scale
+            eps = 48 * 2.0 ** -23 * (ka[see, a] @ np.abs(x)) * scale + 2.0 ** -20 + 2.0 ** -23 * (z.max() - z)
+            p = np.exp(z - z.max())
+            l, s, c, m, y = p.sum(), vs[see, a], vc[see, a], vm[see, a], vh[see, a]
+            o = p @ y / l
+            w = p[:, None] * s
+            step = np.minimum(w, np.maximum(2.0 ** -11 * w, 2.0 ** -27 * w.max(0)))
+            off = 2.0 ** -8 * np.abs(o) + (step * np.abs(c - 8)).sum(0) / l
+            off += (2 * blocks + 2) * 2.0 ** -22 * 400 * w.sum(0) / l + (2 * blocks + 40) * 2.0 ** -24 * (p @ np.abs(m + 8 * s)) / l
+            off += (p * eps) @ np.abs(y - o) / l
+            out[i, h], bound[i, h] = o, 1.02 * off
+    return out, bound
+
+
 def round_bf16(x: np.ndarray) -> np.ndarray:
     return synth.round_to_bf16(np.asarray(x, dtype=np.float32))

@@ -11,8 +11,9 @@
 //     so nothing is padded but the queries.  (With at most 24 rows there is no shape here for the 64-row tcgen05 instructions, and
 //     their operands would have to be unpacked into shared memory first.)
 //   - Queries enter as fp16 times a power of two of their own (exact for bf16 numbers within 2^-25 of the
-//     row's largest), probabilities as fp16 (2^-11) times the step of the value relative to a running
-//     power of two, so that neither can leave fp16's range.  Scores, sums and outputs are fp32.
+//     row's largest).  Probabilities enter as fp16 (2^-11) times the step of the value times a power of two of the query
+//     row and sub-group, which follows the largest of these weighed steps so far: what a row does not weigh, however large it is,
+//     costs the rest no digits, and neither can leave fp16's range.  Scores, sums and outputs are fp32.
 //   - 16-key blocks are the unit of work.  All blocks of all (sequence, KV head in use, 8 * NB query
 //     rows) items form one line that is cut into equal pieces for CTAs and warps, so uneven sequences load
 //     the SMs evenly.  A warp streams its piece through a ring of its own in shared memory (16-byte asynchronous
@@ -41,8 +42,13 @@ constexpr int kBlk = 2;            // blocks of a ring stage: 32 keys
 // either sign stay near zero.  (Summed as m + s n, the fp32 sums of 16384 evenly weighed values lost a digit to cancellation.)  The
 // - 8 is the same for all channels of a sub-group, so it has one accumulator, which joins the others every fourth stage, before they grow.
 constexpr uint32_t kEight = 0x00080008u, kEightHigh = 0x80808080u;
-constexpr float kSlack = 8.f;       // the reference of a softmax may stay this far (in powers of two) below its running maximum
-constexpr int kUp = 5;             // steps enter fp16 as 2^kUp .. 2^(kUp + 1) at most: 2^(kUp + 1 + kSlack) is far below 65504
+// Weighed steps, probability times step, enter fp16 times 2^e: with every new e the largest of the row and sub-group becomes
+// 2^kUp .. 2^(kUp + 1), so that one 2^26 times smaller still is no zero.  Until a step times 2^e passes kMostStep or a logit the
+// reference by more than kSlack powers of two, e and the reference of the softmax stay: 2^kSlack * kMostStep is below 65504.
+constexpr float kSlack = 8.f;
+constexpr int kUp = 2;
+constexpr float kMostStep = 128.f;
+constexpr int kMostExp = 120;      // of e: 2^(kMostExp + kSlack) is an fp32 number
 constexpr int kMaxCtas = 160;
 constexpr int kMeta = 8;           // words of meta of a partial result
 constexpr int kPlanSmem = 16384;   // bytes of shared memory for the plan of a small batch
@@ -582,7 +588,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
             const int4 info = plan.seqs[cc.seq];
             const int all_see = a.causal ? min(info.z, info.z - info.y + cc.rb * kRows / a.share + 1) : info.z;
 
-            float acc[NB][kSteps][4], m[NB][2], l[NB][2], pm[NB][kNS][2];
+            float acc[NB][kSteps][4], m[NB][2];
+            unsigned long long l[NB], pm[NB][kNS];    // pairs of the columns
             constexpr int kMid = kDirect ? 1 : kNS;
             float mid[NB][kMid][4];     // -8 sum p s (and -8 * 17, as the rows g are summed), not yet in acc
             int turns = 0;
@@ -600,8 +607,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 #pragma unroll
                         for (int e = 0; e < 4; ++e) mid[n][i][e] = 0.f;
             };
-            int ev = -110;              // the exponent that the values' steps are relative to
-            float inv = pow2(kUp + 110);
+            uint32_t up[NB][kNS];       // 2^e of the score columns 2t and 2t + 1, as two bf16 numbers
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
 #pragma unroll
@@ -613,12 +619,11 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
 #pragma unroll
                     for (int e = 0; e < 4; ++e) mid[n][i][e] = 0.f;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    m[n][c] = -CUDART_INF_F;
-                    l[n][c] = 0.f;
+                for (int i = 0; i < kNS; ++i) up[n][i] = (127u + kMostExp) * 0x00800080u;
 #pragma unroll
-                    for (int i = 0; i < kNS; ++i) pm[n][i][c] = 0.f;
-                }
+                for (int i = 0; i < kNS; ++i) pm[n][i] = 0;
+                l[n] = 0;
+                m[n][0] = m[n][1] = -CUDART_INF_F;
             }
             // One stage, kBlk blocks.  Masked: with blocks that are not there, or keys that some row does not see.
             auto turn = [&](auto masked_c, uint32_t here) {
@@ -683,8 +688,8 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                                 if (key0 + 16 * b + g + 8 * (e >> 1) > last || !((here >> b) & 1u)) s[b][n][e] = -CUDART_INF_F;
                             }
                         }
-                // ---- the values' parameters, and their largest step (scales are not negative: their words compare like numbers)
-                uint32_t v0[kBlk][kNS], v1[kBlk][kNS], big = 0;
+                // ---- the values' parameters
+                uint32_t v0[kBlk][kNS], v1[kBlk][kNS];
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
                     lds_words<kNS>(base + params + 64 * kNS + b * kSB, v0[b]);
@@ -696,15 +701,22 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                             v0[b][i] = is && key0 + 16 * b + g < info.z ? v0[b][i] : 0u;
                             v1[b][i] = is && key0 + 16 * b + g + 8 < info.z ? v1[b][i] : 0u;
                         }
-                        big = max(big, max(v0[b][i] << 16, v1[b][i] << 16));
                     }
                 }
-                big = __reduce_max_sync(0xffffffffu, big);
-                // ---- the reference m that probabilities are taken relative to.  It follows the running maximum only when that has
-                // risen by more than kSlack, and the steps' exponent only upwards: then what is summed so far is scaled down.
-                // (Following every rise, four in ten stages of a decoding batch would scale.)
+                // ---- the reference m that probabilities are taken relative to, and e.  They are set anew only when the running maximum has
+                // risen by more than kSlack, or a step (of any key: probabilities are not known here) is too large for its e; then
+                // what is summed so far is scaled.  (Following every rise, four in ten stages of a decoding batch would scale.)
                 float mu[NB][2], top[NB][2];
-                bool change = static_cast<int>(big >> 23) - 127 > ev;
+                bool change = false;
+#pragma unroll
+                for (int i = 0; i < kNS; ++i) {
+                    uint32_t step = 0, e = up[0][i];   // scales are not negative: their words compare like numbers
+#pragma unroll
+                    for (int b = 0; b < kBlk; ++b) step = max(step, max(v0[b][i] << 16, v1[b][i] << 16));
+#pragma unroll
+                    for (int n = 1; n < NB; ++n) e = __vmaxu2(e, up[n][i]);
+                    change = change || !(__uint_as_float(step) * fmaxf(__uint_as_float(e << 16), __uint_as_float(e & 0xFFFF0000u)) <= kMostStep);   // (also where a step is NaN)
+                }
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -719,81 +731,96 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         change = change || mx > m[n][c] + kSlack;
                     }
                 if (__any_sync(0xffffffffu, change)) {
-                    if (big >= 0x7F800000u) {   // a value that is not finite: leave it out of the scaling
-                        big = 0;
-#pragma unroll
-                        for (int b = 0; b < kBlk; ++b)
-#pragma unroll
-                            for (int i = 0; i < kNS; ++i) {
-                                const uint32_t x = v0[b][i] << 16, y = v1[b][i] << 16;
-                                big = max(big, max(x < 0x7F800000u ? x : 0u, y < 0x7F800000u ? y : 0u));
-                            }
-                        big = __reduce_max_sync(0xffffffffu, big);
-                    }
-                    const int up = max(ev, static_cast<int>(big >> 23) - 127);
-                    const float ev_f = pow2(max(-126, ev - up));
-                    ev = up;
-                    inv = pow2(kUp - ev);
 #pragma unroll
                     for (int n = 0; n < NB; ++n) {
-                        float alpha[2];
+                        float alpha[2], ref[2];
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const float now = fmaxf(m[n][c], top[n][c]);
-                            alpha[c] = exp2_fast(m[n][c] - (now == -CUDART_INF_F ? 0.f : now));
+                            ref[c] = now == -CUDART_INF_F ? 0.f : now;
+                            alpha[c] = exp2_fast(m[n][c] - ref[c]);
                             m[n][c] = now;
-                            l[n][c] *= alpha[c];
-#pragma unroll
-                            for (int i = 0; i < kNS; ++i) pm[n][i][c] *= alpha[c];
                         }
+                        l[n] = mul2(l[n], pair(alpha[0], alpha[1]));
 #pragma unroll
-                        for (int i = 0; i < kSteps; ++i)
+                        for (int i = 0; i < kNS; ++i) pm[n][i] = mul2(pm[n][i], pair(alpha[0], alpha[1]));
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[n][i][e] *= alpha[e & 1] * ev_f;
+                        for (int i = 0; i < kNS; ++i) {
+                            float w[2] = {0.f, 0.f};   // the stage's largest weighed step (fmaxf passes NaN over)
 #pragma unroll
-                        for (int i = 0; i < kMid && !kDirect; ++i)
+                            for (int b = 0; b < kBlk; ++b)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) mid[n][i][e] *= alpha[e & 1] * ev_f;
+                                for (int e = 0; e < 4; ++e)
+                                    w[e & 1] = fmaxf(w[e & 1], exp2_fast(s[b][n][e] - ref[e & 1]) * wide_cache_scale(e < 2 ? v0[b][i] : v1[b][i]));
+                            uint32_t both = __byte_perm(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x7632);   // only their exponents count
+                            both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 4));
+                            both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 8));
+                            both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 16));
+                            uint32_t next[2];
+                            float by[2];               // alpha * 2^(new e - old e), below 2
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                constexpr uint32_t kTurn = (254u + kUp) << 23;     // less the bits of 2^x: the bits of 2^(kUp - x)
+                                const uint32_t old = c ? up[n][i] & 0xFFFF0000u : up[n][i] << 16;
+                                const float before = alpha[c] * __uint_as_float(kTurn - old);    // the largest so far was that at least
+                                const float most = fmaxf(__uint_as_float(c ? both & 0xFFFF0000u : both << 16), before);
+                                next[c] = min(kTurn - (__float_as_uint(most) & 0x7F800000u), (127u + kMostExp) << 23);
+                                by[c] = before * (__uint_as_float(next[c]) * (1.f / (1 << kUp)));
+                            }
+                            up[n][i] = __byte_perm(next[0], next[1], 0x7632);
+#pragma unroll
+                            for (int k = i * (G / 16); k < (i + 1) * (G / 16); ++k)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) acc[n][k][e] *= by[e & 1];
+                            if (!kDirect) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) mid[n][i % kMid][e] *= by[e & 1];
+                            }
+                        }
                     }
                 }
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int c = 0; c < 2; ++c) mu[n][c] = m[n][c] == -CUDART_INF_F ? 0.f : m[n][c];
-                // ---- probabilities, and the values they weigh
+                // ---- probabilities, and the values they weigh (both score columns of a lane at once)
 #pragma unroll
                 for (int b = 0; b < kBlk; ++b) {
-                    float p[NB][4];
+                    unsigned long long p[NB][2];      // of keys g and g + 8
 #pragma unroll
                     for (int n = 0; n < NB; ++n)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            p[n][e] = exp2_fast(s[b][n][e] - mu[n][e & 1]);
-                            l[n][e & 1] += p[n][e];
+                        for (int h = 0; h < 2; ++h) {
+                            p[n][h] = pair(exp2_fast(s[b][n][2 * h] - mu[n][0]), exp2_fast(s[b][n][2 * h + 1] - mu[n][1]));
+                            l[n] = add2(l[n], p[n][h]);
                         }
 #pragma unroll
                     for (int i = 0; i < kNS; ++i) {
-                        const float s0 = wide_cache_scale(v0[b][i]) * inv, s1 = wide_cache_scale(v1[b][i]) * inv;
-                        const float m0 = fmaf(wide_cache_scale(v0[b][i]), 8.f, wide_cache_min(v0[b][i]));
-                        const float m1 = fmaf(wide_cache_scale(v1[b][i]), 8.f, wide_cache_min(v1[b][i]));
                         uint32_t pb[NB][2];
 #pragma unroll
-                        for (int n = 0; n < NB; ++n) {
-                            float x[4];
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t word = h ? v1[b][i] : v0[b][i];
+                            const float st = wide_cache_scale(word), mi = fmaf(st, 8.f, wide_cache_min(word));
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                x[e] = p[n][e] * (e < 2 ? s0 : s1);
-                                const float next = fmaf(p[n][e], e < 2 ? m0 : m1, pm[n][i][e & 1]);
+                            for (int n = 0; n < NB; ++n) {
+                                // in this order nothing overflows
+                                const unsigned long long x = mul2(mul2(p[n][h], pair(__uint_as_float(up[n][i] << 16), __uint_as_float(up[n][i] & 0xFFFF0000u))), pair(st, st));
+                                const unsigned long long next = fma2(p[n][h], pair(mi, mi), pm[n][i]);
+                                float x0, x1;
+                                unpair(x, x0, x1);
                                 if (masked) {   // a step or minimum that is not finite, of a key this row does not see
-                                    const bool unseen = s[b][n][e] == -CUDART_INF_F;
-                                    x[e] = unseen ? 0.f : x[e];
-                                    pm[n][i][e & 1] = unseen ? pm[n][i][e & 1] : next;
+                                    float n0, n1, o0, o1;
+                                    unpair(next, n0, n1);
+                                    unpair(pm[n][i], o0, o1);
+                                    const bool u0 = s[b][n][2 * h] == -CUDART_INF_F, u1 = s[b][n][2 * h + 1] == -CUDART_INF_F;
+                                    x0 = u0 ? 0.f : x0;
+                                    x1 = u1 ? 0.f : x1;
+                                    pm[n][i] = pair(u0 ? o0 : n0, u1 ? o1 : n1);
                                 } else {
-                                    pm[n][i][e & 1] = next;
+                                    pm[n][i] = next;
                                 }
+                                pb[n][h] = transpose8x8(pack_f16(x0, x1));
                             }
-                            pb[n][0] = transpose8x8(pack_f16(x[0], x[1]));
-                            pb[n][1] = transpose8x8(pack_f16(x[2], x[3]));
                         }
 #pragma unroll
                         for (int n = 0; n < NB && !kDirect; ++n)
@@ -844,26 +871,31 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
             }
             // ---- end of the item or of the piece: sums over the lanes, results in the values' own scale
             if (!kDirect) settle();
-            const float f = pow2(ev);
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int i = 0; i < kSteps; ++i) {
-                    acc[n][i][0] = (acc[n][i][0] - acc[n][i][2]) * pow2(24 - kUp);
-                    acc[n][i][1] = (acc[n][i][1] - acc[n][i][3]) * pow2(24 - kUp);
-                    acc[n][i][2] *= pow2(20 - kUp);
-                    acc[n][i][3] *= pow2(20 - kUp);
+                    acc[n][i][0] = (acc[n][i][0] - acc[n][i][2]) * pow2(24);
+                    acc[n][i][1] = (acc[n][i][1] - acc[n][i][3]) * pow2(24);
+                    acc[n][i][2] *= pow2(20);
+                    acc[n][i][3] *= pow2(20);
                 }
+            auto down = [&](int n, int i, int c) { return pow2(127 - static_cast<int>((up[n][i] >> (16 * c + 7)) & 255u)); };   // 2^-e
+            float ls[NB][2], pms[NB][kNS][2];
 #pragma unroll
-            for (int n = 0; n < NB; ++n)
+            for (int n = 0; n < NB; ++n) {
+                unpair(l[n], ls[n][0], ls[n][1]);
+#pragma unroll
+                for (int i = 0; i < kNS; ++i) unpair(pm[n][i], pms[n][i][0], pms[n][i][1]);
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) {
-                        l[n][c] += __shfl_xor_sync(0xffffffffu, l[n][c], o);
+                        ls[n][c] += __shfl_xor_sync(0xffffffffu, ls[n][c], o);
 #pragma unroll
-                        for (int i = 0; i < kNS; ++i) pm[n][i][c] += __shfl_xor_sync(0xffffffffu, pm[n][i][c], o);
+                        for (int i = 0; i < kNS; ++i) pms[n][i][c] += __shfl_xor_sync(0xffffffffu, pms[n][i][c], o);
                     }
+            }
             const bool begins = first_blk == 0, ends = end_blk == cc.n_blk, tail = cc.left == 0;
             if (begins && ends) {
                 const RowBlock rows = row_block(a, cc.rb * kRows);
@@ -873,10 +905,10 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                     for (int c = 0; c < 2; ++c) {
                         const RowOut ro = row_out(a, info.x, info.y, cc.kvh, row_of(a, rows, 8 * n + 2 * t + c), D);
                         if (!ro.o) continue;
-                        const float r = ro.on && l[n][c] != 0.f ? 1.f / l[n][c] : 0.f;
+                        const float r = ro.on && ls[n][c] != 0.f ? 1.f / ls[n][c] : 0.f;
 #pragma unroll
                         for (int i = 0; i < kSteps / 2; ++i) {
-                            const float add = pm[n][32 * i / G][c];
+                            const float add = pms[n][32 * i / G][c], f = down(n, 32 * i / G, c);
                             uint2 w = make_uint2(0, 0);
                             if (r != 0.f) {
                                 const __nv_bfloat162 b0 = __floats2bfloat162_rn(fmaf(acc[n][2 * i][c], f, add) * r, fmaf(acc[n][2 * i][c + 2], f, add) * r);
@@ -896,14 +928,14 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
                         const int r = 8 * n + 2 * t + c;
 #pragma unroll
                         for (int i = 0; i < kSteps / 2; ++i) {
-                            const float add = pm[n][32 * i / G][c];
+                            const float add = pms[n][32 * i / G][c], f = down(n, 32 * i / G, c);
                             *reinterpret_cast<float4*>(dst + r * D + 32 * i + 4 * g) =
                                 make_float4(fmaf(acc[n][2 * i][c], f, add), fmaf(acc[n][2 * i][c + 2], f, add),
                                             fmaf(acc[n][2 * i + 1][c], f, add), fmaf(acc[n][2 * i + 1][c + 2], f, add));
                         }
                         if (g == 0) {
                             dst[kRows * D + 2 * r] = m[n][c];
-                            dst[kRows * D + 2 * r + 1] = l[n][c];
+                            dst[kRows * D + 2 * r + 1] = ls[n][c];
                         }
                     }
                 const int e = tail ? 1 : 0;

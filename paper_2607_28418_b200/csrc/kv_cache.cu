@@ -14,6 +14,11 @@
 
 namespace {
 
+using wptx::add2;
+using wptx::fma2;
+using wptx::pair;
+using wptx::unpair;
+
 constexpr int kWarps = 4;           // of a CTA (8 start and end in larger steps: 8188 tokens written and read back 28.7 us, with four 27.5)
 
 // 8 neighbouring channels as they lie in memory
@@ -113,23 +118,7 @@ __device__ __noinline__ uint2 quantise8_any(Raw8<T> raw) {
     return make_uint2((__float_as_uint(s) >> 16) | mb, c);
 }
 
-// two fp32 numbers at once
-__device__ __forceinline__ unsigned long long pair(float a, float b) {
-    unsigned long long p;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
-    return p;
-}
-__device__ __forceinline__ void unpair(unsigned long long p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
-__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
-    unsigned long long c;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(a), "l"(b));
-    return c;
-}
-__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
-    unsigned long long d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
+// two fp32 numbers at once, rounded up
 __device__ __forceinline__ unsigned long long fma2_up(unsigned long long a, unsigned long long b, unsigned long long c) {
     unsigned long long d;
     asm("fma.rp.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
