@@ -115,7 +115,8 @@ WIDE_API int wide_destroy(wide_ctx* ctx);
 
 /* Synchronise `stream`, read the device status word into *status (WIDE_OK, WIDE_ERR_TIMEOUT, or
  * WIDE_ERR_BAD_INDEX from the calls on a cache, see wide_seqs) and clear it; after a timeout the
- * context's internal buffers are reset.  WIDE_ERR_BAD_INDEX holds nothing up: later calls run as usual.
+ * context's internal buffers are reset.  WIDE_ERR_BAD_INDEX holds nothing up: later calls run as usual. Where
+ * both are due, the timeout comes first and the bad index with the next call.
  * The only call that blocks the host.
  * After a device-side wait has expired the context's counters and accumulators are in an
  * undefined state: until wide_status has been called, every decode-path call on the context

@@ -226,17 +226,19 @@ int wide_destroy(wide_ctx* ctx) {
 int wide_status(wide_ctx* ctx, void* stream, int* status) {
     if (!ctx || !status) return WIDE_ERR_INVALID_ARG;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    int v = 0, index = 0;
-    WIDE_CUDA_CHECK(cudaMemcpyAsync(&v, ctx->d_status, sizeof(int), cudaMemcpyDeviceToHost, s));
-    WIDE_CUDA_CHECK(cudaMemcpyAsync(&index, ctx->d_status + WIDE_STATUS_INDEX, sizeof(int), cudaMemcpyDeviceToHost, s));
-    WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_status, 0, sizeof(int), s));
-    WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_status + WIDE_STATUS_INDEX, 0, sizeof(int), s));
+    int words[WIDE_STATUS_INDEX + 1] = {};
+    WIDE_CUDA_CHECK(cudaMemcpyAsync(words, ctx->d_status, sizeof(words), cudaMemcpyDeviceToHost, s));
     WIDE_CUDA_CHECK(cudaStreamSynchronize(s));
+    const int v = words[0], index = words[WIDE_STATUS_INDEX];
+    // only what is reported is cleared: a bad index beside an expired wait waits for the next call
     if (v != WIDE_OK) {
         // a kernel gave up half-way: restore the invariants later calls rely on
-        WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_status, 0, 16 * sizeof(int), s));
+        WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_status, 0, WIDE_STATUS_INDEX * sizeof(int), s));
         WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->decode_acc, 0, ctx->decode_acc_floats * sizeof(float), s));
         WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_tickets, 0, 2048 * sizeof(unsigned), s));
+        WIDE_CUDA_CHECK(cudaStreamSynchronize(s));
+    } else if (index != WIDE_OK) {
+        WIDE_CUDA_CHECK(cudaMemsetAsync(ctx->d_status + WIDE_STATUS_INDEX, 0, sizeof(int), s));
         WIDE_CUDA_CHECK(cudaStreamSynchronize(s));
     }
     *status = v != WIDE_OK ? v : index;
