@@ -439,7 +439,7 @@ WIDE_API int wide_qproj(wide_ctx* ctx, void* stream, const void* x, const void* 
  * The angle is reduced exactly (64-bit fixed point, in turns), so far positions lose nothing; the
  * rotation is fp32, rounded once.
  * Needs head_dim in {64, 128}, rot_dim % 16 == 0, rot_dim <= head_dim, n_axes <= 8, and every pointer
- * to q, k and every row of them 16-byte aligned.
+ * to q, k and every row of them 16-byte aligned.  Other flags than the two above are refused.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA.
  */
 WIDE_API int wide_rope(wide_ctx* ctx, void* stream, const void* q, const void* k, int dtype, int tokens, int n_q_heads,

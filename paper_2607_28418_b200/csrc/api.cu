@@ -496,6 +496,7 @@ int wide_rope(wide_ctx* ctx, void* stream, const void* q, const void* k, int dty
     if (!ctx || !q || !q_out || !positions || !inv_freq || !valid_dtype(dtype)) return WIDE_ERR_INVALID_ARG;
     if (tokens < 0 || n_q_heads <= 0 || n_kv_heads < 0 || head_dim <= 0 || rot_dim <= 0 || n_axes <= 0) return WIDE_ERR_INVALID_ARG;
     if ((n_kv_heads > 0) != (k != nullptr) || (k != nullptr) != (k_out != nullptr)) return WIDE_ERR_INVALID_ARG;
+    if (flags & ~(WIDE_FLAG_ROPE_INTERLEAVED | WIDE_FLAG_ROPE_INVERSE)) return WIDE_ERR_INVALID_ARG;
     if ((head_dim != 64 && head_dim != 128) || rot_dim % 16 != 0 || rot_dim > head_dim || n_axes > 8 || n_q_heads > 4096 ||
         n_kv_heads > 4096 || tokens > (1 << 27))
         return WIDE_ERR_UNSUPPORTED_SHAPE;
