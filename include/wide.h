@@ -511,7 +511,7 @@ WIDE_API size_t wide_cache_page_bytes(int page_size, int n_kv_heads, int head_di
  * wide_cache_read -- the same rows out of the cache, m + s n in fp32 (one rounding), then rounded to the output type; with
  * row_start = the running sum of kv_lens that is the whole cache of the sequences, as wide_attn reads it.
  *   k_out, v_out as k, v; they must not overlap
- * Rows and pointers 16-byte aligned.  One launch, no workspace.
+ * Rows and pointers 16-byte aligned.  (rows / 16 + 2 n_seqs) * n_kv_heads must stay below 2^31.  One launch, no workspace.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA; WIDE_ERR_BAD_INDEX through wide_status.
  */
 WIDE_API int wide_cache_write(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* k,
@@ -540,7 +540,7 @@ WIDE_API int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cach
  * over a KV head, more take several passes.  A long prefill reads the cache back
  * (wide_cache_read) and runs wide_attn.
  * Results do not depend on the other sequences of the batch beyond fp32 rounding, and are the same bit for bit in every run.
- * The arrays of `seqs` must not change while the call runs.  `flags` must be 0.
+ * rows * n_q_heads <= 2^30.  The arrays of `seqs` must not change while the call runs.  `flags` must be 0.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA; WIDE_ERR_BAD_INDEX through wide_status.
  */
 WIDE_API size_t wide_attn_cache_workspace_bytes(int rows, int n_q_heads, int n_kv_heads, int head_dim);

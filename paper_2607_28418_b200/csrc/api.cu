@@ -1,4 +1,6 @@
 // C ABI of libwide: argument validation, workspace sizing and dispatch.  See include/wide.h.
+#include <algorithm>
+#include <climits>
 #include <cstdio>
 #include <new>
 
@@ -71,6 +73,9 @@ int cache_move(wide_ctx* ctx, void* stream, bool write, const wide_cache* cache,
     if (!k || !v || !valid_dtype(dtype)) return WIDE_ERR_INVALID_ARG;
     int rc = check_cache(ctx, cache, seqs, rows);
     if (rc != WIDE_OK) return rc;
+    // the kernels number (block, head) pairs with an int
+    const long long blocks = seqs->row_start ? std::min<long long>(rows, rows / 16 + 2LL * seqs->n_seqs) : seqs->n_seqs;
+    if (blocks * cache->n_kv_heads > INT_MAX) return WIDE_ERR_UNSUPPORTED_SHAPE;
     const long long width = static_cast<long long>(cache->n_kv_heads) * cache->head_dim;
     if ((rc = check_rows(k, ks, width, wide_elem_bytes(dtype))) != WIDE_OK) return rc;
     if ((rc = check_rows(v, vs, width, wide_elem_bytes(dtype))) != WIDE_OK) return rc;
@@ -543,7 +548,9 @@ int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cache, const 
     int rc = check_cache(ctx, cache, seqs, rows);
     if (rc != WIDE_OK) return rc;
     if (n_q_heads % cache->n_kv_heads != 0) return WIDE_ERR_INVALID_ARG;
-    if (dtype != WIDE_BF16 || n_q_heads / heads_per_group > WIDE_MAX_GROUPS || n_q_heads > 4096) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    if (dtype != WIDE_BF16 || n_q_heads / heads_per_group > WIDE_MAX_GROUPS || n_q_heads > 4096 ||
+        static_cast<long long>(rows) * n_q_heads > (1 << 30))     // rows of all heads are counted with an int
+        return WIDE_ERR_UNSUPPORTED_SHAPE;
     if ((rc = check_rows(q, q_stride, static_cast<long long>(n_q_heads) * cache->head_dim, 2)) != WIDE_OK) return rc;
     if (!wide_aligned16(o) || !wide_aligned16(workspace)) return WIDE_ERR_ALIGNMENT;
     if (!workspace || workspace_bytes < wide_attn_cache_workspace(rows, n_q_heads, cache->n_kv_heads, cache->head_dim))

@@ -454,8 +454,10 @@ __global__ void __launch_bounds__(32 * WARPS, 1) attn_cache_kernel(const __grid_
         const long long share = total <= 0x7fffffffLL ? static_cast<int>(total) / ctas : total / ctas;
         const int more = static_cast<int>(total - share * ctas);
         const long long c0 = share * cta + min(cta, more);
-        const int n = static_cast<int>(share + (cta < more ? 1 : 0));
-        const int each = n / WARPS, extra = n - each * WARPS;
+        const long long n = share + (cta < more ? 1 : 0);
+        // (a warp's own units fit an int: 2^31 of them would take it minutes)
+        const long long each = n <= 0x7fffffffLL ? static_cast<int>(n) / WARPS : n / WARPS;
+        const int extra = static_cast<int>(n - each * WARPS);
         u0 = c0 + each * warp + min(warp, extra);
         u1 = u0 + each + (warp < extra ? 1 : 0);
     }
