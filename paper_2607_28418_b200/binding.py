@@ -494,7 +494,23 @@ def cache_page_bytes(page_size: int, n_kv_heads: int, head_dim: int, quant_group
     return int(load_library().wide_cache_page_bytes(page_size, n_kv_heads, head_dim, quant_group))
 
 
-class Cache:
+class _Fixed:
+    """A handle whose C structure holds the addresses of its tensors: the tensors' contents may change, the tensors may not."""
+
+    __slots__ = ()
+
+    def _set(self, *values):
+        for name, value in zip(self.__slots__, values):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed: change the tensor in place, or make another {type(self).__name__}")
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{type(self).__name__}.{name} is fixed")
+
+
+class Cache(_Fixed):
     """The 4-bit cache of a layer: ``pages`` is any contiguous uint8 CUDA tensor of n_pages *
     cache_page_bytes(...) bytes, first dimension n_pages (see wide_cache in include/wide.h)."""
 
@@ -509,9 +525,8 @@ class Cache:
         n_pages = pages.shape[0]
         if pages.numel() != n_pages * size:
             raise ValueError(f"pages: expected {size} bytes a page, got {pages.numel() // max(1, n_pages)}")
-        self.pages, self.n_kv_heads, self.head_dim = pages, n_kv_heads, head_dim
-        self.quant_group, self.page_size = quant_group, page_size
-        self.struct = _CacheStruct(pages.data_ptr(), n_pages, page_size, n_kv_heads, head_dim, quant_group)
+        self._set(pages, n_kv_heads, head_dim, quant_group, page_size,
+                  _CacheStruct(pages.data_ptr(), n_pages, page_size, n_kv_heads, head_dim, quant_group))
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, quant_group: int = 64, page_size: int = 64, device="cuda") -> "Cache":
@@ -521,9 +536,10 @@ class Cache:
         return cls(torch.empty((n_pages, size), dtype=torch.uint8, device=device), n_kv_heads, head_dim, quant_group, page_size)
 
 
-class Sequences:
+class Sequences(_Fixed):
     """Where the sequences of a call lie (see wide_seqs): page_table int32 [n_seqs, max_pages], kv_lens
-    int32 [n_seqs] (the new tokens included), row_start int32 [n_seqs + 1] or None (one new row each)."""
+    int32 [n_seqs] (the new tokens included), row_start int32 [n_seqs + 1] or None (one new row each).  The tensors' contents may
+    change between calls, the tensors themselves may not."""
 
     __slots__ = ("page_table", "kv_lens", "row_start", "n_seqs", "struct")
 
@@ -533,9 +549,8 @@ class Sequences:
             raise ValueError("expected page_table [n_seqs, max_pages] and kv_lens [n_seqs]")
         if row_start is not None and row_start.shape != (shape[0] + 1,):
             raise ValueError("expected row_start [n_seqs + 1]")
-        self.page_table, self.kv_lens, self.row_start, self.n_seqs = page_table, kv_lens, row_start, shape[0]
-        self.struct = _SeqsStruct(_int32(page_table, "page_table"), _int32(kv_lens, "kv_lens"), _int32(row_start, "row_start"),
-                                  shape[0], shape[1])
+        self._set(page_table, kv_lens, row_start, shape[0],
+                  _SeqsStruct(_int32(page_table, "page_table"), _int32(kv_lens, "kv_lens"), _int32(row_start, "row_start"), shape[0], shape[1]))
 
 
 @_on_device
