@@ -539,7 +539,9 @@ WIDE_API int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cach
  * Built for few new rows a sequence (decoding, verifying drafted tokens): up to 24 query rows share one pass
  * over a KV head, more take several passes.  A long prefill reads the cache back
  * (wide_cache_read) and runs wide_attn.
- * Results do not depend on the other sequences of the batch beyond fp32 rounding, and are the same bit for bit in every run.
+ * The other sequences of a batch decide where the work is cut and how many rows share a pass, hence in which order a sequence's sums
+ * are made and against which power of two its probabilities are rounded: its results differ with them by no more than the accuracy above.
+ * The same call gives the same bits in every run.
  * rows * n_q_heads <= 2^30.  The arrays of `seqs` must not change while the call runs.  `flags` must be 0.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA; WIDE_ERR_BAD_INDEX through wide_status.
  */
