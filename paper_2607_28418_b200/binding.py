@@ -640,7 +640,8 @@ def wide_attn_cache(ctx: Context, q: torch.Tensor, cache: Cache, seqs: Sequences
                     mask_bits: Optional[torch.Tensor] = None, causal: bool = True, scale: float = 0.0,
                     o: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Masked attention of the new rows q [rows, n_q_heads * head_dim] bf16 over the cache.  ``workspace``
-    (uint8, attn_cache_workspace_bytes) replaces the context's own scratch, which calls on one stream share."""
+    (uint8, attn_cache_workspace_bytes) replaces the context's own scratch, which calls on one stream share.  Rows that belong to no
+    sequence, or to a row range that is none, are not written: without ``o`` they hold what the allocation held before."""
     width = n_q_heads * cache.head_dim
     qp, qs = _rows(q, width, "q")
     rows = q.shape[0]

@@ -21,10 +21,11 @@
 //   - A warp that covered an item writes its output; pieces of items are joined first within the
 //     CTA, then (at most two per CTA) by a second small kernel.  The order of joining is fixed.
 //
-// Measured (device time of a call): 64 sequences of up to 16384 tokens, half of 8 KV heads, 284 MB: 66.9 us, 4.2 TB/s, 0.65 of the copy
-// rate.  Of these about 55 are the streaming loop, where issue slots (550 a stage, a quarter of them control) and HBM are near balance:
-// without the compute the same copies take 58.  The rest is start and end: 3 us until the plan is made, 4 more until the first keys are
-// there, 2 to join the warps, 3 for the second kernel; with one sequence of 32768 tokens (38 MB, 21.2 us) they are most of the time.
+// Measured (device time of a call): 64 sequences of up to 16384 tokens, half of 8 KV heads, 284 MB: 67.5 us, 4.2 TB/s, 0.64 of the copy
+// rate.  Of these about 55 are the streaming loop (530 instructions a stage, a quarter of them control).  Over the whole kernel issue
+// slots are busy 54 %, DRAM 51 %, the tensor pipe 27 %, so none of them is the bound: warps wait for their own results (1.6 cycles an
+// instruction) and for each other's issue.  The rest is start and end: 3 us until the plan is made, 4 more until the first keys are
+// there, 2 to join the warps, 3 for the second kernel; with one sequence of 32768 tokens (38 MB, 21.3 us) they are most of the time.
 #include <math_constants.h>
 
 #include <atomic>
@@ -1109,8 +1110,10 @@ int launch(wide_ctx* ctx, cudaStream_t s, AttnArgs a, unsigned char* ws) {
     constexpr int kRows = 8 * NB;
     constexpr int stage = kBlk * (16 * D + 128 * (D / G));
     constexpr int room = (227 - 3) * 1024 - kPlanSmem;   // 3 KB for the static arrays
-    // 12 warps have 168 registers each, which eight query rows need 163 of; 16 with 128 each keep some in memory, and were slower
-    // everywhere (a batch of 64: 72.2 against 68.6 us, one short sequence: 12.7 against 9.9), as were 10 and 14.  More rows, 8 warps.
+    // 12 warps have 168 registers each, which eight query rows need 132 to 168 of; 16 with 128 each keep some in memory, and were slower
+    // everywhere (a batch of 64: 72.2 against 68.6 us, one short sequence: 12.7 against 9.9), as were 10 and 14.  More rows, 8 warps of 255.
+    // Spilled a thread (bytes stored) for heads of 128: 8 rows 112 with sub-groups of 32, none with 64 and 128; 16 rows 272, 232, 184 (sub-groups
+    // of 32, 64, 128); 24 rows 1404, 1088, 624.  For heads of 64: 24 rows with sub-groups of 32, 72; none else.
     constexpr int W = NB > 1 ? 8 : 12;
     constexpr int S = 3;                                   // stages of a ring (a batch of 64: 66.9 us with 3, 67.1 with 2, 68.2 with 4)
     static_assert(W * S * stage <= room && S * stage >= slot_floats(kRows, D) * 4, "ring");
@@ -1186,8 +1189,10 @@ int wide_launch_attn_cache(wide_ctx* ctx, cudaStream_t s, const wide_cache* cach
     a.o = static_cast<__nv_bfloat16*>(o);
     a.status = ctx->d_status + WIDE_STATUS_INDEX;
     a.plan_words = (cache->n_kv_heads + 31) / 32;
-    // Rows of a sequence and KV head: `share` where a sequence has one new row, else an average (the lengths
-    // are on the device).  Above eight, 16 rows share a pass over the cache, above 16, 24.
+    // Rows of a sequence and KV head: `share` where a sequence has one new row, else an average over all sequences, those
+    // without new rows among them (the lengths are on the device).  Above eight, 16 rows share a pass over the cache, above 16, 24.
+    // An average fits batches of like sequences.  Five rows of four heads of 128 (20 a KV head) on 8192 tokens, sub-groups of 64 / 128, cold:
+    // alone one pass of 24 rows, 39 / 33 us; beside 63 idle sequences three of 8, 27 / 25 us, since the 24-row kernel spills.
     const long long rows_per_head = seqs->row_start ? static_cast<long long>(rows) * a.share / seqs->n_seqs : a.share;
     if (rows_per_head <= 8) return launch_shape<1>(ctx, s, a, cache->head_dim, cache->quant_group, static_cast<unsigned char*>(ws));
     if (rows_per_head > 16) return launch_shape<3>(ctx, s, a, cache->head_dim, cache->quant_group, static_cast<unsigned char*>(ws));

@@ -514,7 +514,7 @@ cache_read_kernel(CacheView c, SeqView q, T* __restrict__ k, T* __restrict__ v, 
     report_bad(q, c.page_shift, status);
 }
 
-// CTAs for the slots.  Writing: twice what is resident, if there is so much.  Reading: what is resident,
+// CTAs for the slots.  Writing: twice what is resident of 16-bit types (four times of fp32), if there is so much.  Reading: what is resident,
 // so that a warp asks for its next block ahead; but three times that where there is so much, since later CTAs then even out
 // what the first ones finish unevenly (8 heads of 128 read into bf16, resident / three times: 8192 tokens 9.5 / 10.8 us, 16384
 // 17.6 / 18.0, 24576 25.7 / 24.5, 65536 68.6 / 63.0).
