@@ -49,7 +49,8 @@ constexpr uint32_t kEight = 0x00080008u, kEightHigh = 0x80808080u;
 constexpr float kSlack = 8.f;
 constexpr int kUp = 2;
 constexpr float kMostStep = 128.f;
-constexpr int kMostExp = 120;      // of e: 2^(kMostExp + kSlack) is an fp32 number
+constexpr int kMostExp = 118;      // of e, which stays there while steps are zero: a probability of 2^kSlack times 2^e is an fp32 number
+static_assert(kMostExp + kSlack < 127.f && kSlack <= 8.f && kMostStep <= 128.f, "weighed steps leave their types");
 constexpr int kMaxCtas = 160;
 constexpr int kMeta = 8;           // words of meta of a partial result
 constexpr int kPlanSmem = 16384;   // bytes of shared memory for the plan of a small batch

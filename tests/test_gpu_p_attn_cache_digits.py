@@ -127,3 +127,24 @@ def test_vanishing_and_constant_values(ctx):
     on = np.ones((3, 1), bool)
     ref, bound = reference(c, q, on, 4)
     check(run(ctx, c, q, on, 4), ref, bound + 2.0 ** -130)     # 8 units of the smallest bf16 number, where outputs are that small
+
+
+@pytest.mark.parametrize("dim,group", SHAPES)
+@pytest.mark.parametrize("rise", [7.0, 8.0, 9.0])
+def test_constant_values_under_rising_logits(ctx, dim, group, rise):
+    """Steps of zero give the power of two nothing to follow, and logits rise by up to 2^8 without a new reference: their product must
+    stay a number.  All channels of a key are alike (0 or `rise`) and queries are a single 1, so with this scale logits are whole powers."""
+    scale = float(np.float32(np.log(2)))
+    assert np.float32(scale) * np.float32(1.4426950408889634) == 1
+    c = CacheCase([1536, 1536, 700], [1, 1, 1], 1, dim, group, 16, seed=11)
+    rng = np.random.default_rng(12)
+    for s, n in enumerate(c.lens):
+        high = np.repeat(rng.random(-(-n // 16)) < 0.15, 16)[:n]
+        c.k[s][:] = np.where(high, np.float32(rise), np.float32(0))[:, None, None]
+        c.v[s][:] = co.round_bf16(rng.standard_normal((n, 1, 1)))
+    q = np.zeros((3, 4, dim), np.float32)
+    q[:, :, 5] = 1
+    on = np.ones((3, 1), bool)
+    parts = [co.attention_with_bound(q[s:s + 1], c.k[s], c.v[s], group, on[s:s + 1], 4, True, scale, blocks=13) for s in range(3)]
+    ref, bound = (np.concatenate(x) for x in zip(*parts))
+    check(run(ctx, c, q, on, 4, scale=scale), ref, bound)
