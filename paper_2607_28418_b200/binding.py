@@ -498,23 +498,29 @@ class _Fixed:
     """A handle whose C structure holds the addresses of its tensors: the tensors' contents may change, the tensors may not."""
 
     __slots__ = ()
-
-    def _set(self, *values):
-        for name, value in zip(self.__slots__, values):
-            object.__setattr__(self, name, value)
+    _fixed = ()
 
     def __setattr__(self, name, value):
-        raise AttributeError(f"{type(self).__name__}.{name} is fixed: change the tensor in place, or make another {type(self).__name__}")
+        if name in self._fixed:
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed: change the tensor in place, or make another {type(self).__name__}")
+        object.__setattr__(self, name, value)
 
     def __delattr__(self, name):
-        raise AttributeError(f"{type(self).__name__}.{name} is fixed")
+        if name in self._fixed:
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed")
+        object.__delattr__(self, name)
+
+    def __setstate__(self, state):      # a copy: its attributes and its slots
+        for part in state:
+            for name, value in (part or {}).items():
+                object.__setattr__(self, name, value)
 
 
 class Cache(_Fixed):
     """The 4-bit cache of a layer: ``pages`` is any contiguous uint8 CUDA tensor of n_pages *
     cache_page_bytes(...) bytes, first dimension n_pages (see wide_cache in include/wide.h)."""
 
-    __slots__ = ("pages", "n_kv_heads", "head_dim", "quant_group", "page_size", "struct")
+    __slots__ = _fixed = ("pages", "n_kv_heads", "head_dim", "quant_group", "page_size", "struct")
 
     def __init__(self, pages: torch.Tensor, n_kv_heads: int, head_dim: int, quant_group: int = 64, page_size: int = 64):
         if pages.dtype != torch.uint8 or not pages.is_contiguous() or pages.dim() < 2:
@@ -525,8 +531,13 @@ class Cache(_Fixed):
         n_pages = pages.shape[0]
         if pages.numel() != n_pages * size:
             raise ValueError(f"pages: expected {size} bytes a page, got {pages.numel() // max(1, n_pages)}")
-        self._set(pages, n_kv_heads, head_dim, quant_group, page_size,
-                  _CacheStruct(pages.data_ptr(), n_pages, page_size, n_kv_heads, head_dim, quant_group))
+        put = object.__setattr__
+        put(self, "pages", pages)
+        put(self, "n_kv_heads", n_kv_heads)
+        put(self, "head_dim", head_dim)
+        put(self, "quant_group", quant_group)
+        put(self, "page_size", page_size)
+        put(self, "struct", _CacheStruct(pages.data_ptr(), n_pages, page_size, n_kv_heads, head_dim, quant_group))
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, quant_group: int = 64, page_size: int = 64, device="cuda") -> "Cache":
@@ -541,7 +552,7 @@ class Sequences(_Fixed):
     int32 [n_seqs] (the new tokens included), row_start int32 [n_seqs + 1] or None (one new row each).  The tensors' contents may
     change between calls, the tensors themselves may not."""
 
-    __slots__ = ("page_table", "kv_lens", "row_start", "n_seqs", "struct")
+    __slots__ = _fixed = ("page_table", "kv_lens", "row_start", "n_seqs", "struct")
 
     def __init__(self, page_table: torch.Tensor, kv_lens: torch.Tensor, row_start: Optional[torch.Tensor] = None):
         shape = page_table.shape
@@ -549,8 +560,12 @@ class Sequences(_Fixed):
             raise ValueError("expected page_table [n_seqs, max_pages] and kv_lens [n_seqs]")
         if row_start is not None and row_start.shape != (shape[0] + 1,):
             raise ValueError("expected row_start [n_seqs + 1]")
-        self._set(page_table, kv_lens, row_start, shape[0],
-                  _SeqsStruct(_int32(page_table, "page_table"), _int32(kv_lens, "kv_lens"), _int32(row_start, "row_start"), shape[0], shape[1]))
+        put = object.__setattr__
+        put(self, "page_table", page_table)
+        put(self, "kv_lens", kv_lens)
+        put(self, "row_start", row_start)
+        put(self, "n_seqs", shape[0])
+        put(self, "struct", _SeqsStruct(_int32(page_table, "page_table"), _int32(kv_lens, "kv_lens"), _int32(row_start, "row_start"), shape[0], shape[1]))
 
 
 @_on_device

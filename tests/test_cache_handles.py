@@ -38,3 +38,33 @@ def test_cache_refuses_another_tensor(name):
         setattr(cache, name, getattr(cache, name))
     with pytest.raises(AttributeError):
         delattr(cache, name)
+
+
+def test_they_can_be_derived_from_and_copied():
+    """A program's own handle may add what it likes, with or without slots of its own."""
+    import copy
+
+    from paper_2607_28418_b200 import binding
+
+    class Batch(binding.Sequences):
+        pass
+
+    class Layer(binding.Cache):
+        __slots__ = ("index",)
+    b = Batch(torch.zeros((2, 4), dtype=torch.int32), torch.ones(2, dtype=torch.int32))
+    b.names = ["a", "b"]
+    b.names = ["c"]
+    del b.names
+    assert b.kv_lens.tolist() == [1, 1] and b.row_start is None and b.struct.n_seqs == 2
+    layer = Layer.empty(3, 2, 64, 64, 16, device="cpu")
+    layer.index = 7
+    assert layer.index == 7 and layer.page_size == 16 and layer.struct.n_pages == 3
+    b.names = ["a"]
+    for one, name in ((b, "names"), (layer, "index")):
+        two = copy.copy(one)
+        setattr(two, name, None)
+        assert getattr(one, name) is not None and two.struct is one.struct
+    assert copy.copy(layer).pages is layer.pages and copy.copy(b).kv_lens is b.kv_lens
+    for one, name in ((b, "kv_lens"), (layer, "pages")):
+        with pytest.raises(AttributeError):
+            setattr(one, name, getattr(one, name))
