@@ -12,6 +12,7 @@
  * and what serving puts between the projections and the attention (no counterpart in the paper):
  *   wide_rope         rotary positions of the queries and keys, one or several position axes
  *   wide_cache_write  keys and values of new tokens into a paged 4-bit cache; wide_cache_read: back
+ *   wide_cache_append wide_rope and wide_cache_write in one launch
  *   wide_attn_cache   head-group-masked causal attention of a batch of sequences over that cache
  *
  * General rules
@@ -45,7 +46,7 @@
 extern "C" {
 #endif
 
-#define WIDE_VERSION 113
+#define WIDE_VERSION 114
 
 #if defined(__GNUC__)
 #define WIDE_API __attribute__((visibility("default")))
@@ -518,6 +519,24 @@ WIDE_API int wide_cache_write(wide_ctx* ctx, void* stream, const wide_cache* cac
                               const void* v, int dtype, int rows, long long k_stride, long long v_stride);
 WIDE_API int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, void* k_out,
                              void* v_out, int dtype, int rows, long long k_stride, long long v_stride);
+
+/*
+ * wide_cache_append -- rotary positions of the new rows' queries and keys, and the rotated keys and the values into the cache: the same
+ * bits as wide_rope followed by wide_cache_write, in one launch and without the rotated keys in memory.
+ *   q [rows, n_q_heads * head_dim] -> q_out, k, v [rows, n_kv_heads * head_dim]: dtype bf16 or fp32, rows *_stride elements apart (slices
+ *       of a fused projection); q and q_out NULL with n_q_heads 0.  q_out may be q (equal strides); it must not overlap k, v or another part of q
+ *   positions int32 [n_axes, rows], inv_freq fp64 [rot_dim / 2], axis int32 [rot_dim / 2] or NULL, WIDE_FLAG_ROPE_INTERLEAVED: as for
+ *       wide_rope (drafted tokens that are alternatives have one position).  WIDE_FLAG_ROPE_INVERSE is refused
+ * A rotated key is rounded to dtype before its levels are found, as it would be on its way through memory.  Rows of no sequence, or of a
+ * sequence that is left out, are neither read nor written, queries among them; a missing page drops keys and values only.
+ * Needs rot_dim % 16 == 0, rot_dim <= head_dim, n_axes <= 8, n_q_heads <= 4096, rows and pointers 16-byte aligned, sizes as for
+ * wide_cache_write.  No workspace.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA; WIDE_ERR_BAD_INDEX through wide_status.
+ */
+WIDE_API int wide_cache_append(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* q, const void* k,
+                               const void* v, int dtype, int rows, int n_q_heads, int rot_dim, long long q_stride, long long k_stride,
+                               long long v_stride, const int32_t* positions, int n_axes, const double* inv_freq, const int32_t* axis,
+                               void* q_out, long long o_q_stride, unsigned flags);
 
 /*
  * wide_attn_cache -- Eq. 1 under the head-group mask over the 4-bit cache, a batch of sequences in one call.

@@ -39,7 +39,7 @@ EXPORTS = ["wide_create", "wide_destroy", "wide_status", "wide_set_wait_limit_ns
            "wide_ffn",
            "wide_oproj", "wide_attn", "wide_qproj", "wide_unpermute",
            "wide_rope", "wide_cache_page_bytes", "wide_cache_write", "wide_cache_read", "wide_attn_cache_workspace_bytes",
-           "wide_attn_cache"]
+           "wide_attn_cache", "wide_cache_append"]
 
 _c_void_p, _c_int, _c_size_t, _c_uint = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint
 _c_ll = ctypes.c_longlong
@@ -118,6 +118,7 @@ def load_library() -> ctypes.CDLL:
     lib.wide_cache_page_bytes.restype = _c_size_t
     for fn in (lib.wide_cache_write, lib.wide_cache_read):
         fn.argtypes = [_c_void_p] * 6 + [_c_int] * 2 + [_c_ll] * 2
+    lib.wide_cache_append.argtypes = [_c_void_p] * 7 + [_c_int] * 4 + [_c_ll] * 3 + [_c_void_p, _c_int] + [_c_void_p] * 3 + [_c_ll, _c_uint]
     lib.wide_attn_cache_workspace_bytes.argtypes = [_c_int] * 4
     lib.wide_attn_cache_workspace_bytes.restype = _c_size_t
     lib.wide_attn_cache.argtypes = [_c_void_p] * 5 + [_c_int, _c_int, _c_ll, _c_int, _c_int, _c_void_p, _c_int,
@@ -458,7 +459,7 @@ def wide_unpermute(ctx: Context, src_packed: torch.Tensor, meta: Dict[str, torch
 def _rows(t: torch.Tensor, width: int, what: str):
     """Address and row stride of a [rows, width] matrix whose rows may lie apart (a slice of a fused projection)."""
     shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or shape[1] != width or stride[1] != 1:
+    if len(shape) != 2 or shape[1] != width or (stride[1] != 1 and shape[0] > 0):
         raise ValueError(f"{what}: expected [rows, {width}] with contiguous rows")
     return t.data_ptr(), (stride[0] if shape[0] > 1 else width)     # one row may claim any stride
 
@@ -648,6 +649,49 @@ def wide_cache_read(ctx: Context, cache: Cache, seqs: Sequences, rows: int, dtyp
         raise ValueError("k and v must have `rows` rows")
     _move(ctx, "wide_cache_read", ctx.lib.wide_cache_read, cache, seqs, k, v)
     return k, v
+
+
+@_on_device
+def wide_cache_append(ctx: Context, cache: Cache, seqs: Sequences, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                      positions: torch.Tensor, inv_freq: torch.Tensor, axis: Optional[torch.Tensor] = None, interleaved: bool = False,
+                      q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """wide_rope of the new rows' queries and keys and wide_cache_write of the rotated keys and of the values, in one launch with the
+    same bits: returns the rotated queries.  q [rows, n_q_heads * head_dim] or None, k, v [rows, n_kv_heads * head_dim], bf16 or
+    fp32, rows may lie apart (slices of a fused projection); positions, inv_freq, axis as for wide_rope.  q_out = q rotates in
+    place.  Rows that belong to no sequence are left as they were: without ``q_out`` they hold what the allocation held before."""
+    rows, dim = k.shape[0], cache.head_dim
+    if k.dtype != v.dtype or k.shape != v.shape or (q is not None and (q.dim() != 2 or q.shape[0] != rows or q.dtype != k.dtype or q.shape[1] % dim)):
+        raise ValueError("expected k, v [rows, n_kv_heads * head_dim] and q [rows, n_q_heads * head_dim] of one dtype")
+    where = positions.shape
+    if len(where) not in (1, 2) or where[-1] != rows:
+        raise ValueError("expected positions [rows] or [n_axes, rows]")
+    if inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous() or (axis is not None and axis.shape != inv_freq.shape):
+        raise ValueError("expected inv_freq float64 [rot_dim / 2] and axis of its shape")
+    width = cache.n_kv_heads * dim
+    (kp, ks), (vp, vs) = _rows(k, width, "k"), _rows(v, width, "v")
+    qp = qo = None
+    wq = qs = oqs = 0
+    if q is not None:
+        wq = q.shape[1]
+        if q_out is None:
+            q_out = q.new_empty((rows, wq))
+        elif q_out.shape != q.shape or q_out.dtype != q.dtype:
+            raise ValueError("q_out: expected q's shape and dtype")
+        (qp, qs), (qo, oqs) = _rows(q, wq, "q"), _rows(q_out, wq, "q_out")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    index = ctx.device.index
+    _same_device(index, cache.pages, q, k, v, q_out, positions, inv_freq, axis, seqs.page_table, seqs.kv_lens, seqs.row_start)
+    pos, ax = _int32(positions, "positions"), _int32(axis, "axis")
+    if rows == 0 or seqs.n_seqs == 0:
+        return q_out
+    rc = ctx.lib.wide_cache_append(ctx.handle, torch._C._cuda_getCurrentRawStream(index), ctypes.byref(cache.struct), ctypes.byref(seqs.struct),
+                                   qp, kp, vp, _dtype_code(k), rows, wq // dim, 2 * inv_freq.numel(), qs, ks, vs, pos,
+                                   where[0] if len(where) == 2 else 1, inv_freq.data_ptr(), ax, qo, oqs,
+                                   FLAG_ROPE_INTERLEAVED if interleaved else 0)
+    if rc != OK:
+        raise WideError(rc, "wide_cache_append")
+    return q_out
 
 
 @_on_device

@@ -68,14 +68,18 @@ int check_cache(const wide_ctx* ctx, const wide_cache* c, const wide_seqs* q, in
     return wide_aligned16(c->pages) ? WIDE_OK : WIDE_ERR_ALIGNMENT;
 }
 
+// the kernels number (block, head) pairs with an int
+bool blocks_countable(const wide_cache* cache, const wide_seqs* seqs, int rows) {
+    const long long blocks = seqs->row_start ? std::min<long long>(rows, rows / 16 + 2LL * seqs->n_seqs) : seqs->n_seqs;
+    return blocks * cache->n_kv_heads <= INT_MAX;
+}
+
 int cache_move(wide_ctx* ctx, void* stream, bool write, const wide_cache* cache, const wide_seqs* seqs, void* k, void* v,
                int dtype, int rows, long long ks, long long vs) {
     if (!k || !v || !valid_dtype(dtype)) return WIDE_ERR_INVALID_ARG;
     int rc = check_cache(ctx, cache, seqs, rows);
     if (rc != WIDE_OK) return rc;
-    // the kernels number (block, head) pairs with an int
-    const long long blocks = seqs->row_start ? std::min<long long>(rows, rows / 16 + 2LL * seqs->n_seqs) : seqs->n_seqs;
-    if (blocks * cache->n_kv_heads > INT_MAX) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    if (!blocks_countable(cache, seqs, rows)) return WIDE_ERR_UNSUPPORTED_SHAPE;
     const long long width = static_cast<long long>(cache->n_kv_heads) * cache->head_dim;
     if ((rc = check_rows(k, ks, width, wide_elem_bytes(dtype))) != WIDE_OK) return rc;
     if ((rc = check_rows(v, vs, width, wide_elem_bytes(dtype))) != WIDE_OK) return rc;
@@ -533,6 +537,31 @@ int wide_cache_write(wide_ctx* ctx, void* stream, const wide_cache* cache, const
 int wide_cache_read(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, void* k_out, void* v_out,
                     int dtype, int rows, long long k_stride, long long v_stride) {
     return cache_move(ctx, stream, false, cache, seqs, k_out, v_out, dtype, rows, k_stride, v_stride);
+}
+
+int wide_cache_append(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* q, const void* k,
+                      const void* v, int dtype, int rows, int n_q_heads, int rot_dim, long long q_stride, long long k_stride,
+                      long long v_stride, const int32_t* positions, int n_axes, const double* inv_freq, const int32_t* axis,
+                      void* q_out, long long o_q_stride, unsigned flags) {
+    if (!k || !v || !positions || !inv_freq || !valid_dtype(dtype) || n_q_heads < 0 || rot_dim <= 0 || n_axes <= 0) return WIDE_ERR_INVALID_ARG;
+    if ((n_q_heads > 0) != (q != nullptr) || (q != nullptr) != (q_out != nullptr) || (flags & ~WIDE_FLAG_ROPE_INTERLEAVED)) return WIDE_ERR_INVALID_ARG;
+    int rc = check_cache(ctx, cache, seqs, rows);
+    if (rc != WIDE_OK) return rc;
+    if (rot_dim % 16 != 0 || rot_dim > cache->head_dim || n_axes > 8 || n_q_heads > 4096 || !blocks_countable(cache, seqs, rows))
+        return WIDE_ERR_UNSUPPORTED_SHAPE;
+    if (q && ((q == q_out && q_stride != o_q_stride) || q_out == k || q_out == v)) return WIDE_ERR_INVALID_ARG;
+    const int elem = wide_elem_bytes(dtype);
+    const long long width = static_cast<long long>(cache->n_kv_heads) * cache->head_dim, q_width = static_cast<long long>(n_q_heads) * cache->head_dim;
+    if ((rc = check_rows(k, k_stride, width, elem)) != WIDE_OK) return rc;
+    if ((rc = check_rows(v, v_stride, width, elem)) != WIDE_OK) return rc;
+    if (q) {
+        if ((rc = check_rows(q, q_stride, q_width, elem)) != WIDE_OK) return rc;
+        if ((rc = check_rows(q_out, o_q_stride, q_width, elem)) != WIDE_OK) return rc;
+    }
+    if (!on_device(ctx)) return WIDE_ERR_INVALID_ARG;
+    if (rows == 0 || seqs->n_seqs == 0) return WIDE_OK;
+    return wide_launch_cache_append(ctx, static_cast<cudaStream_t>(stream), cache, seqs, q, k, v, dtype, rows, n_q_heads, rot_dim, q_stride,
+                                    k_stride, v_stride, positions, n_axes, inv_freq, axis, q_out, o_q_stride, flags);
 }
 
 size_t wide_attn_cache_workspace_bytes(int rows, int n_q_heads, int n_kv_heads, int head_dim) {

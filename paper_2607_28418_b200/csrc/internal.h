@@ -238,6 +238,11 @@ int wide_launch_rope(wide_ctx* ctx, cudaStream_t s, const void* q, const void* k
 // The 4-bit cache: rows in (write) or out (csrc/kv_cache.cu), attention over it (csrc/attn_cache.cu).
 int wide_launch_cache_move(wide_ctx* ctx, cudaStream_t s, bool write, const wide_cache* cache, const wide_seqs* seqs, void* k,
                            void* v, int dtype, int rows, long long ks, long long vs);
+// Queries and keys rotated, keys and values into the cache (csrc/cache_append.cu).
+int wide_launch_cache_append(wide_ctx* ctx, cudaStream_t s, const wide_cache* cache, const wide_seqs* seqs, const void* q, const void* k,
+                             const void* v, int dtype, int rows, int n_q, int rot, long long qs, long long ks, long long vs,
+                             const int32_t* positions, int n_axes, const double* inv_freq, const int32_t* axis, void* q_out,
+                             long long oqs, unsigned flags);
 size_t wide_attn_cache_workspace(int rows, int n_q, int n_kv, int head_dim);
 int wide_launch_attn_cache(wide_ctx* ctx, cudaStream_t s, const wide_cache* cache, const wide_seqs* seqs, const void* q,
                            int rows, long long qs, int n_q, int hpg, const uint32_t* mask_bits, int causal, float scale,

@@ -9,65 +9,13 @@
 // frequency), and only the reduced angle, in half turns, is rounded to fp32 for sincospif.
 #include "internal.h"
 #include "ptx.cuh"
+#include "rope.cuh"
 
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = 64;
 constexpr int kMaxTile = 4;      // tokens of a CTA (16384 tokens of 80 heads, bf16: 133 us with 1, 119 with 2, 113 with 4, 117 with 8)
-
-template <typename T> struct Vec8;   // 8 channels as the memory holds them
-template <> struct Vec8<__nv_bfloat16> {
-    uint4 v;
-    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool) { v = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void store(__nv_bfloat16* p, bool) const { *reinterpret_cast<uint4*>(p) = v; }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
-    }
-    __device__ __forceinline__ void set(const float (&x)[8]) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&b);
-        }
-        v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-};
-template <> struct Vec8<float> {
-    float4 a, b;
-    // in two halves, neighbouring lanes would leave each other's half of every 32-byte sector to a second access
-    // (4099 tokens of 40 heads in fp32: 33.8 us in halves, 29.0 whole)
-    __device__ __forceinline__ void load(const float* p, bool wide) {
-        if (wide) {
-            wptx::ld_global_256(p, a, b);
-        } else {
-            a = reinterpret_cast<const float4*>(p)[0];
-            b = reinterpret_cast<const float4*>(p)[1];
-        }
-    }
-    __device__ __forceinline__ void store(float* p, bool wide) const {
-        if (wide) {
-            wptx::st_global_256(p, a, b);
-        } else {
-            reinterpret_cast<float4*>(p)[0] = a;
-            reinterpret_cast<float4*>(p)[1] = b;
-        }
-    }
-    __device__ __forceinline__ void get(float (&x)[8]) const {
-        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-    }
-    __device__ __forceinline__ void set(const float (&x)[8]) {
-        a = make_float4(x[0], x[1], x[2], x[3]);
-        b = make_float4(x[4], x[5], x[6], x[7]);
-    }
-};
 
 struct RopeArgs {
     const void *q, *k;
@@ -115,21 +63,14 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
         u.load(src + lo, a.wide);
         w.load(src + hi, a.wide);
     }
-    if (tid < pairs) {
-        double f = a.inv_freq[tid] * 0.15915494309189533577;   // 1 / (2 pi)
-        f -= floor(f);
-        turn[tid] = static_cast<unsigned long long>(f * 18446744073709551616.0);
-    }
+    if (tid < pairs) turn[tid] = wide_rope_turn(a.inv_freq[tid]);
     __syncthreads();
     for (int i = tid; i < nt * pairs; i += kThreads) {
         const int tt = i / pairs, p = i - tt * pairs;
         const int ax = a.axis ? a.axis[p] : 0;
         float2 v = make_float2(1.f, 0.f);
         if (static_cast<unsigned>(ax) < static_cast<unsigned>(a.n_axes)) {
-            const long long pos = a.positions[static_cast<size_t>(ax) * a.tokens + t0 + tt];
-            const unsigned long long phase = static_cast<unsigned long long>(pos) * turn[p];
-            const float half_turns = static_cast<float>(static_cast<int>(phase >> 32)) * 4.656612873077393e-10f;   // 2^-31
-            sincospif(half_turns, &v.y, &v.x);
+            v = wide_rope_angle(a.positions[static_cast<size_t>(ax) * a.tokens + t0 + tt], turn[p]);
             if (a.inverse) v.y = -v.y;
         } else {
             atomicExch(a.status, WIDE_ERR_BAD_INDEX);
@@ -163,17 +104,17 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float p = x[2 * e], s = x[2 * e + 1], p2 = y[2 * e], s2 = y[2 * e + 1];
-                    x[2 * e] = p * c[e].x - s * c[e].y;
-                    x[2 * e + 1] = p * c[e].y + s * c[e].x;
-                    y[2 * e] = p2 * c[4 + e].x - s2 * c[4 + e].y;
-                    y[2 * e + 1] = p2 * c[4 + e].y + s2 * c[4 + e].x;
+                    x[2 * e] = wide_rope_low(p, s, c[e]);
+                    x[2 * e + 1] = wide_rope_high(p, s, c[e]);
+                    y[2 * e] = wide_rope_low(p2, s2, c[4 + e]);
+                    y[2 * e + 1] = wide_rope_high(p2, s2, c[4 + e]);
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float p = x[e], s = y[e];
-                    x[e] = p * c[e].x - s * c[e].y;
-                    y[e] = p * c[e].y + s * c[e].x;
+                    x[e] = wide_rope_low(p, s, c[e]);
+                    y[e] = wide_rope_high(p, s, c[e]);
                 }
             }
             x8.set(x);
