@@ -9,6 +9,7 @@
  *   wide_attn       head-group-masked causal attention            (Eq. 1; Algorithm 4: prefill and decode forms)
  *   wide_qproj      routed query projection, GEMM-MN              (Eq. 1 under the mask; Algorithm 2)
  *   wide_unpermute  the scatter epilogue as a standalone step     (Algorithm 2, epilogue)
+ *   wide_linear     the dense products of a routed layer (keys, values, head), with bias, activation and residual
  * and what serving puts between the projections and the attention (no counterpart in the paper):
  *   wide_rope         rotary positions of the queries and keys, one or several position axes
  *   wide_cache_write  keys and values of new tokens into a paged 4-bit cache; wide_cache_read: back
@@ -419,6 +420,28 @@ WIDE_API int wide_attn(wide_ctx* ctx, void* stream, const void* q, const void* k
 WIDE_API int wide_qproj(wide_ctx* ctx, void* stream, const void* x, const void* w, int dtype, int tokens,
                int hidden, int n_out, int group, const int32_t* perm, const int32_t* counts, void* y,
                unsigned flags);
+
+/* activations of wide_linear */
+#define WIDE_ACT_NONE 0
+#define WIDE_ACT_SILU 1      /* v / (1 + exp(-v)) */
+#define WIDE_ACT_GELU 2      /* v (1 + erf(v / sqrt 2)) / 2 */
+#define WIDE_ACT_GELU_TANH 3 /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2 */
+
+/*
+ * wide_linear -- the dense linear layer (no routing: keys, values and the output head are dense for every token), with its epilogue:
+ *     y[t, n] = act(sum_i x[t, i] w[n, i] + bias[n]) + residual[t, n]
+ *   x [tokens, k] bf16, rows x_stride elements apart;  w [n, k] bf16;  bias [n] bf16 or NULL
+ *   y [tokens, n] of out_dtype (bf16 or fp32), residual the same type or NULL, rows y_stride / residual_stride elements apart.
+ *       residual may be y (equal strides); y must not overlap anything else that is read
+ * Sums, bias, activation and residual are fp32, rounded once to out_dtype.  From one token to any number.  The same call gives the
+ * same bits in every run.
+ * Needs k % 8 == 0; x, y, residual and their rows 16-byte aligned, w and bias too.  n may be anything (columns from n on are not
+ * written).  No workspace.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA; a bounded device wait that expires sets WIDE_ERR_TIMEOUT (wide_status).
+ */
+WIDE_API int wide_linear(wide_ctx* ctx, void* stream, const void* x, int dtype, int tokens, int k, long long x_stride, const void* w, int n,
+                         const void* bias, int activation, const void* residual, long long residual_stride, void* y, int out_dtype,
+                         long long y_stride, unsigned flags);
 
 /* flags for wide_rope */
 #define WIDE_FLAG_ROPE_INTERLEAVED 256u /* pair i = channels (2i, 2i + 1); default (i, i + rot_dim / 2) */

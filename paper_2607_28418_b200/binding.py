@@ -24,6 +24,7 @@ FLAG_NONE, FLAG_SIMT, FLAG_FORCE_PREFILL, FLAG_FORCE_DECODE, FLAG_INPUT_MASKED =
 FLAG_KAXIS_GROUP, FLAG_KAXIS_OWNER, FLAG_REDUCE_BF16 = 16, 32, 64
 FLAG_DECODE_TC = 128
 FLAG_ROPE_INTERLEAVED, FLAG_ROPE_INVERSE = 256, 512
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
 DECODE_MAX_TOKENS = 64
 DECODE_GEMV_MAX_TOKENS = 2
 MAX_GROUPS = 256
@@ -39,7 +40,7 @@ EXPORTS = ["wide_create", "wide_destroy", "wide_status", "wide_set_wait_limit_ns
            "wide_ffn",
            "wide_oproj", "wide_attn", "wide_qproj", "wide_unpermute",
            "wide_rope", "wide_cache_page_bytes", "wide_cache_write", "wide_cache_read", "wide_attn_cache_workspace_bytes",
-           "wide_attn_cache", "wide_cache_append"]
+           "wide_attn_cache", "wide_cache_append", "wide_linear"]
 
 _c_void_p, _c_int, _c_size_t, _c_uint = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint
 _c_ll = ctypes.c_longlong
@@ -114,6 +115,8 @@ def load_library() -> ctypes.CDLL:
     lib.wide_unpermute.argtypes = [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_int,
                                    _c_int, _c_int, _c_int, _c_void_p]
     lib.wide_rope.argtypes = [_c_void_p] * 4 + [_c_int] * 6 + [_c_ll] * 2 + [_c_void_p, _c_int] + [_c_void_p] * 4 + [_c_ll] * 2 + [_c_uint]
+    lib.wide_linear.argtypes = ([_c_void_p] * 3 + [_c_int] * 3 + [_c_ll, _c_void_p, _c_int, _c_void_p, _c_int, _c_void_p, _c_ll, _c_void_p, _c_int,
+                                                                  _c_ll, _c_uint])
     lib.wide_cache_page_bytes.argtypes = [_c_int] * 4
     lib.wide_cache_page_bytes.restype = _c_size_t
     for fn in (lib.wide_cache_write, lib.wide_cache_read):
@@ -611,6 +614,58 @@ def wide_rope(ctx: Context, q: torch.Tensor, k: Optional[torch.Tensor], position
     if rc != OK:
         raise WideError(rc, "wide_rope")
     return q_out, k_out
+
+
+@_on_device
+def wide_linear(ctx: Context, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: str = "none",
+                residual: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y = act(x w^T + bias) + residual.  x [T, k], w [n, k], bias [n] bf16; y and residual [T, n] bf16 or fp32; rows of x, y and
+    residual may lie apart.  activation: "none", "silu", "gelu" or "gelu_tanh".  y = residual adds in place.  A y that is made here has rows
+    that start on 16-byte borders: for other n it is a view of a wider tensor."""
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation: expected one of {', '.join(ACTIVATIONS)}")
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or x.dtype != w.dtype:
+        raise ValueError("expected x [T, k] and w [n, k] of one dtype")
+    (T, k), n = x.shape, w.shape[0]
+    if bias is not None and (bias.shape != (n,) or bias.dtype != x.dtype or not bias.is_contiguous()):
+        raise ValueError("bias: expected a contiguous [n] tensor of x's dtype")
+    if not w.is_contiguous():
+        raise ValueError("w: expected a contiguous tensor")
+    if y is None:
+        out_dtype = out_dtype or (residual.dtype if residual is not None else x.dtype)
+        per = 4 if out_dtype == torch.float32 else 8
+        wide = (n + per - 1) // per * per
+        y = x.new_empty((T, wide), dtype=out_dtype)
+        if wide != n:
+            y = y[:, :n]
+    elif y.shape != (T, n) or (out_dtype is not None and y.dtype != out_dtype):
+        raise ValueError("y: expected [T, n] of out_dtype")
+    if residual is not None and (residual.shape != (T, n) or residual.dtype != y.dtype):
+        raise ValueError("residual: expected [T, n] of y's dtype")
+    index = ctx.device.index
+    _same_device(index, x, w, bias, residual, y)
+    dtype, out = _dtype_code(x), _dtype_code(y)
+    if T == 0:
+        return y
+    (xp, xs), (yp, ys) = _matrix(x, "x"), _matrix(y, "y")
+    rp, rs = (None, 0) if residual is None else _matrix(residual, "residual")
+    rc = ctx.lib.wide_linear(ctx.handle, torch._C._cuda_getCurrentRawStream(index), xp, dtype, T, k, xs, w.data_ptr(), n,
+                             None if bias is None else bias.data_ptr(), ACTIVATIONS[activation], rp, rs, yp, out, ys, 0)
+    if rc != OK:
+        raise WideError(rc, "wide_linear")
+    return y
+
+
+def _matrix(t: torch.Tensor, what: str):
+    """Address and row stride of a matrix whose rows may lie apart; a single row or column claims the stride that the call's checks allow."""
+    (rows, width), (stride, step) = t.shape, t.stride()
+    if step != 1 and width > 1:
+        raise ValueError(f"{what}: expected contiguous rows")
+    if rows == 1:
+        per = 16 // t.element_size()
+        stride = (width + per - 1) // per * per
+    return t.data_ptr(), stride
 
 
 def _move(ctx: Context, what: str, call, cache: Cache, seqs: Sequences, k: torch.Tensor, v: torch.Tensor):

@@ -498,6 +498,27 @@ int wide_qproj(wide_ctx* ctx, void* stream, const void* x, const void* w, int dt
                                     counts, y);
 }
 
+int wide_linear(wide_ctx* ctx, void* stream, const void* x, int dtype, int tokens, int k, long long x_stride, const void* w, int n,
+                const void* bias, int activation, const void* residual, long long residual_stride, void* y, int out_dtype,
+                long long y_stride, unsigned flags) {
+    if (!ctx || !x || !w || !y || !valid_dtype(dtype) || !valid_dtype(out_dtype) || flags != 0) return WIDE_ERR_INVALID_ARG;
+    if (tokens < 0 || k <= 0 || n <= 0 || activation < WIDE_ACT_NONE || activation > WIDE_ACT_GELU_TANH) return WIDE_ERR_INVALID_ARG;
+    if (y == x || y == w || y == bias || (residual == y && residual_stride != y_stride)) return WIDE_ERR_INVALID_ARG;
+    if (dtype != WIDE_BF16 || k % 8 != 0 || tokens > (1 << 27) || n > (1 << 27) || k > (1 << 27)) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    int rc;
+    const int elem = wide_elem_bytes(out_dtype);
+    if ((rc = check_rows(x, x_stride, k, 2)) != WIDE_OK) return rc;
+    if ((rc = check_rows(y, y_stride, n, elem)) != WIDE_OK) return rc;
+    if (residual && (rc = check_rows(residual, residual_stride, n, elem)) != WIDE_OK) return rc;
+    if (!wide_aligned16(w) || !wide_aligned16(bias)) return WIDE_ERR_ALIGNMENT;
+    if (x_stride >= (1LL << 38)) return WIDE_ERR_UNSUPPORTED_SHAPE;     // a tensor map's stride has 40 bits
+    if (!on_device(ctx)) return WIDE_ERR_INVALID_ARG;
+    if (!ctx->encode_tiled) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    if (tokens == 0) return WIDE_OK;
+    return wide_launch_linear(ctx, static_cast<cudaStream_t>(stream), x, tokens, k, x_stride, w, n, bias, activation, residual, residual_stride, y,
+                              out_dtype, y_stride);
+}
+
 int wide_rope(wide_ctx* ctx, void* stream, const void* q, const void* k, int dtype, int tokens, int n_q_heads, int n_kv_heads,
               int head_dim, int rot_dim, long long q_stride, long long k_stride, const int32_t* positions, int n_axes,
               const double* inv_freq, const int32_t* axis, void* q_out, void* k_out, long long o_q_stride,

@@ -229,6 +229,10 @@ int wide_launch_attn_decode(wide_ctx* ctx, cudaStream_t s, const void* q, const 
                             const uint32_t* mask_bits, int Tq, int Tk, int Hq, int Hkv, int head_dim, int hpg,
                             int causal, float scale, void* o, unsigned flags);
 
+// Dense linear layer with its epilogue (csrc/linear.cu).
+int wide_launch_linear(wide_ctx* ctx, cudaStream_t s, const void* x, int T, int K, long long xs, const void* w, int N, const void* bias, int act,
+                       const void* residual, long long rs, void* y, int out_dtype, long long ys);
+
 // Rotary positions (csrc/rope.cu).
 int wide_launch_rope(wide_ctx* ctx, cudaStream_t s, const void* q, const void* k, int dtype, int tokens, int n_q, int n_kv,
                      int head_dim, int rot, long long qs, long long ks, const int32_t* positions, int n_axes,

@@ -1,0 +1,309 @@
+// Dense linear layer with its epilogue (wide_linear):  y[t, n] = act(sum_k x[t, k] w[n, k] + bias[n]) + residual[t, n].
+//
+// Weights are the 128-row operand of the tensor cores, tokens the other: D [128 output channels (TMEM lanes)][tokens (columns)] in fp32,
+// so that a single token costs no more than the weights' bytes.  An epilogue warp has 32 channels of all the tile's tokens; it turns
+// them round through its own part of shared memory, so that rows of y are read and written in runs of 64 or 128 bytes.
+//
+// Few tokens: the weights' bytes bound it, and N / 128 tiles are fewer than SMs.  A cluster of CTAs shares a tile: each takes a part
+// of K, and each joins the parts of some of the tokens over distributed shared memory, in the order of K, so results do not
+// depend on timing.
+#include <cuda.h>
+
+#include <atomic>
+
+#include "internal.h"
+#include "ptx.cuh"
+
+namespace {
+
+using namespace wptx;
+
+constexpr int kM = 128;                 // output channels of a tile
+constexpr int kBK = 64;                 // bf16 numbers of a 128-byte swizzle row
+constexpr int kABytes = kM * kBK * 2;
+constexpr int kThreads = 192;           // TMA, MMA, four epilogue warps
+
+struct LinearArgs {
+    int T, N, nk;                       // nk: steps of kBK
+    int tiles_n, split;
+    const __nv_bfloat16* bias;
+    const void* residual;
+    void* y;
+    long long rs, ys;                   // row strides in elements
+    int act, out_f32;
+    int stream_weights;                 // one tile of tokens: weights are read once
+    int* status;
+    unsigned long long wait_ns;
+};
+
+__device__ __forceinline__ float activate(float v, int act) {
+    switch (act) {
+        case WIDE_ACT_SILU: return __fdividef(v, 1.f + __expf(-v));
+        case WIDE_ACT_GELU: return 0.5f * v * erfcf(-0.70710678118654752f * v);
+        case WIDE_ACT_GELU_TANH: {        // 0.5 v (1 + tanh u) = v / (1 + exp(-2 u))
+            const float u = 0.79788456080286536f * fmaf(0.044715f * v * v, v, v);
+            return __fdividef(v, 1.f + __expf(-2.f * u));
+        }
+        default: return v;
+    }
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// the address in CTA `rank` of the cluster that `addr` is in this one
+__device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float4 ld_cluster(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+
+// four neighbouring outputs of a row from channel f on
+__device__ __forceinline__ void finish(const LinearArgs& a, long long t, int f, float4 v, const float (&bias)[4]) {
+    float x[4] = {activate(v.x + bias[0], a.act), activate(v.y + bias[1], a.act), activate(v.z + bias[2], a.act), activate(v.w + bias[3], a.act)};
+    const int n = min(4, a.N - f);
+    if (a.out_f32) {
+        float* y = static_cast<float*>(a.y) + t * a.ys + f;
+        const float* r = static_cast<const float*>(a.residual) + t * a.rs + f;
+        if (n == 4) {
+            if (a.residual) {
+                const float4 z = *reinterpret_cast<const float4*>(r);
+                x[0] += z.x, x[1] += z.y, x[2] += z.z, x[3] += z.w;
+            }
+            *reinterpret_cast<float4*>(y) = make_float4(x[0], x[1], x[2], x[3]);
+        } else {
+            for (int e = 0; e < n; ++e) y[e] = x[e] + (a.residual ? r[e] : 0.f);
+        }
+    } else {
+        __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + t * a.ys + f;
+        const __nv_bfloat16* r = static_cast<const __nv_bfloat16*>(a.residual) + t * a.rs + f;
+        if (n == 4) {
+            if (a.residual) {
+                const uint2 z = *reinterpret_cast<const uint2*>(r);
+                x[0] += __uint_as_float(z.x << 16), x[1] += __uint_as_float(z.x & 0xFFFF0000u);
+                x[2] += __uint_as_float(z.y << 16), x[3] += __uint_as_float(z.y & 0xFFFF0000u);
+            }
+            const __nv_bfloat162 p = __floats2bfloat162_rn(x[0], x[1]), q = __floats2bfloat162_rn(x[2], x[3]);
+            *reinterpret_cast<uint2*>(y) = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
+        } else {
+            for (int e = 0; e < n; ++e) y[e] = __float2bfloat16_rn(x[e] + (a.residual ? __bfloat162float(r[e]) : 0.f));
+        }
+    }
+}
+
+template <int NT>
+struct Small {
+    static constexpr int kStages = 6, kStage = kABytes + NT * kBK * 2, kSmem = kStages * kStage + 1024;
+};
+
+// One tile of 128 channels and NT tokens a cluster.
+template <int NT>
+__global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
+                                                          const __grid_constant__ LinearArgs a) {
+    constexpr int kStages = Small<NT>::kStages, kStage = Small<NT>::kStage;
+    constexpr uint32_t kCols = NT < 32 ? 32 : NT;
+    static_assert(kStages * kStage >= NT * kM * 4, "the parts of a tile take the place of the stages");
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 1];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_word;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t full = smem_u32(bars), empty = smem_u32(bars + kStages), done = smem_u32(bars + 2 * kStages);
+    volatile int* abort_flag = &abort_word;
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        mbar_init(done, 1);
+        abort_word = 0;
+        fence_barrier_init();
+        prefetch_tmap(&tm_w);
+        prefetch_tmap(&tm_x);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&tmem_slot), kCols);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    const int rank = a.split > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const int tile = blockIdx.x / a.split, tile_n = tile % a.tiles_n, tile_t = tile / a.tiles_n;
+    const int k0 = static_cast<int>(static_cast<long long>(a.nk) * rank / a.split), k1 = static_cast<int>(static_cast<long long>(a.nk) * (rank + 1) / a.split);
+    grid_dep_launch();
+    grid_dep_wait();
+
+    if (warp == 0) {
+        if (lane == 0) {
+            const uint64_t once = l2_policy_evict_first();
+            for (int k = k0; k < k1; ++k) {
+                const int i = k - k0, s = i % kStages;
+                if (!mbar_wait(empty + 8 * s, ((i / kStages) & 1) ^ 1u, a.wait_ns, abort_flag)) break;
+                mbar_arrive_expect_tx(full + 8 * s, kStage);
+                const uint32_t at = smem_u32(base + s * kStage);
+                if (a.stream_weights) tma_load_2d_hint(at, &tm_w, k * kBK, tile_n * kM, full + 8 * s, once);
+                else tma_load_2d(at, &tm_w, k * kBK, tile_n * kM, full + 8 * s);
+                tma_load_2d(at + kABytes, &tm_x, k * kBK, tile_t * NT, full + 8 * s);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            bool ok = true;
+            for (int k = k0; k < k1 && ok; ++k) {
+                const int i = k - k0, s = i % kStages;
+                ok = mbar_wait(full + 8 * s, (i / kStages) & 1, a.wait_ns, abort_flag);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint32_t at = smem_u32(base + s * kStage);
+                const uint64_t wd = umma_desc_sw128(at), xd = umma_desc_sw128(at + kABytes);
+#pragma unroll
+                for (int e = 0; e < kBK / 16; ++e) umma_bf16(tmem, wd + 2 * e, xd + 2 * e, umma_idesc_bf16(kM, NT), (i | e) ? 1u : 0u);
+                umma_commit(empty + 8 * s);
+            }
+            if (ok) umma_commit(done);
+        }
+    }
+    __syncwarp();
+    // ---- epilogue: warps 2..5, of the TMEM lanes that a warp's number gives it
+    const int quarter = warp & 3;
+    float* parts = reinterpret_cast<float*>(base);      // [token][128]: every stage has been read when `done` completes
+    bool ok = true;
+    if (warp >= 2) {
+        ok = mbar_wait_warp(done, 0, a.wait_ns, abort_flag);
+        if (!ok && lane == 0) atomicExch(a.status, WIDE_ERR_TIMEOUT);
+        tc_fence_after_sync();
+        if (ok) {
+#pragma unroll 1
+            for (int c = 0; c < NT; c += 16) {
+                uint32_t r[16];
+                tmem_ld_32x16(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c, r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) parts[(c + e) * kM + quarter * 32 + lane] = __uint_as_float(r[e]);
+            }
+        }
+        __syncwarp();
+    }
+    if (a.split > 1) {
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (warp >= 2 && ok) {
+        const int t0 = NT * rank / a.split, t1 = NT * (rank + 1) / a.split;      // the tokens that this CTA joins
+        const int f = tile_n * kM + quarter * 32 + (lane & 7) * 4;
+        float bias[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bias[e] = a.bias && f + e < a.N ? __bfloat162float(a.bias[f + e]) : 0.f;
+        const uint32_t mine = smem_u32(parts) + (quarter * 32 + (lane & 7) * 4) * 4;
+        if (f < a.N) {
+            for (int t = t0 + (lane >> 3); t < t1 && tile_t * NT + t < a.T; t += 4) {
+                float4 v;
+                if (a.split == 1) {
+                    v = *reinterpret_cast<const float4*>(parts + t * kM + quarter * 32 + (lane & 7) * 4);
+                } else {
+                    v = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int p = 0; p < a.split; ++p) {
+                        const float4 z = ld_cluster(map_rank(mine + t * kM * 4, p));
+                        v = make_float4(v.x + z.x, v.y + z.y, v.z + z.z, v.w + z.w);
+                    }
+                }
+                finish(a, static_cast<long long>(tile_t) * NT + t, f, v, bias);
+            }
+        }
+    }
+    if (a.split > 1) {       // no CTA leaves while its part may be read
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (*abort_flag && tid == 0)
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);   // copies in flight land before the shared memory is given up
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 1) tmem_dealloc(tmem, kCols);
+}
+
+// bf16 rows `stride` bytes apart, box [rows, 64 columns], 128-byte swizzle
+bool make_map(const wide_ctx* ctx, CUtensorMap* map, const void* base, long long rows, long long cols, long long stride, uint32_t box_rows) {
+    typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)}, strides[1] = {static_cast<cuuint64_t>(stride)};
+    const cuuint32_t box[2] = {kBK, box_rows}, each[2] = {1, 1};
+    return reinterpret_cast<Encode>(ctx->encode_tiled)(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, each,
+                                                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Once a device and kernel; threads that come here together all set the same.
+template <typename K>
+bool allow_smem(const wide_ctx* ctx, K kernel, int bytes, std::atomic<unsigned>& set) {
+    const unsigned bit = ctx->device < 32 ? 1u << ctx->device : 0u;
+    if (bit && (set.load(std::memory_order_relaxed) & bit)) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    set.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+
+template <int NT>
+int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long xs, const void* w, int K) {
+    CUtensorMap tm_w, tm_x;
+    if (!make_map(ctx, &tm_w, w, a.N, K, 2LL * K, kM) || !make_map(ctx, &tm_x, x, a.T, K, 2 * xs, NT)) return WIDE_ERR_CUDA;
+    static std::atomic<unsigned> set{0};
+    if (!allow_smem(ctx, linear_kernel<NT>, Small<NT>::kSmem, set)) return WIDE_ERR_CUDA;
+    const long long tiles = static_cast<long long>(a.tiles_n) * ((a.T + NT - 1) / NT);
+    a.stream_weights = a.T <= NT;
+    a.split = 1;
+    while (a.split < 8 && tiles * a.split < ctx->sm_count && a.nk / (2 * a.split) >= 4) a.split *= 2;
+    if (tiles * a.split > 0x7fffffffLL) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Small<NT>::kSmem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = a.split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = ctx->prof ? 1 : 2;
+    WideLaunch l(ctx, s, "linear");
+    WIDE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, linear_kernel<NT>, tm_w, tm_x, a));
+    return WIDE_OK;
+}
+
+}  // namespace
+
+int wide_launch_linear(wide_ctx* ctx, cudaStream_t s, const void* x, int T, int K, long long xs, const void* w, int N, const void* bias, int act,
+                       const void* residual, long long rs, void* y, int out_dtype, long long ys) {
+    LinearArgs a{};
+    a.T = T;
+    a.N = N;
+    a.nk = (K + kBK - 1) / kBK;
+    a.tiles_n = (N + kM - 1) / kM;
+    a.bias = static_cast<const __nv_bfloat16*>(bias);
+    a.residual = residual;
+    a.y = y;
+    a.rs = rs;
+    a.ys = ys;
+    a.act = act;
+    a.out_f32 = out_dtype == WIDE_F32;
+    a.status = ctx->d_status;
+    a.wait_ns = ctx->wait_ns;
+    if (T <= 16) return launch<16>(ctx, s, a, x, xs, w, K);
+    if (T <= 32) return launch<32>(ctx, s, a, x, xs, w, K);
+    if (T <= 64) return launch<64>(ctx, s, a, x, xs, w, K);
+    return launch<128>(ctx, s, a, x, xs, w, K);
+}
