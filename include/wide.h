@@ -15,6 +15,7 @@
  *   wide_cache_write  keys and values of new tokens into a paged 4-bit cache; wide_cache_read: back
  *   wide_cache_append wide_rope and wide_cache_write in one launch
  *   wide_attn_cache   head-group-masked causal attention of a batch of sequences over that cache
+ *   wide_attn_tree    the same for trees of drafted tokens, each of which sees its own ancestors
  *
  * General rules
  *   - Every data pointer is a DEVICE pointer owned by the caller; the library never
@@ -592,6 +593,32 @@ WIDE_API int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cach
                              int dtype, int rows, long long q_stride, int n_q_heads, int heads_per_group,
                              const uint32_t* mask_bits, int causal, float scale, void* o, void* workspace,
                              size_t workspace_bytes, unsigned flags);
+
+/*
+ * wide_attn_tree -- wide_attn_cache for trees of drafted tokens: a step that verifies several continuations at once.
+ * The new rows of a sequence (their keys and values already written, at its last positions) are the nodes of a tree, or of any other
+ * relation: row i of a sequence with n new rows and length L sees all positions j < L - n, and position L - n + j iff bit j % 32 of
+ * tree_bits[row, j / 32] is 1 (its ancestors and, where the caller sets its own bit, itself):
+ *     o[i, h, :] = sum_j softmax_j(scale * q[i, h, :] . k[j, h_kv, :]) v[j, h_kv, :] over the positions that it sees
+ * with the keys and values that wide_cache_read returns in bf16.  Pairs whose routing group is off, and rows that see no key, give
+ * exact zeros; an infinity or a NaN in a new position reaches the rows that see it and no other.
+ *   tree_bits uint32 [rows, tree_words], 1 <= tree_words <= 8.  A sequence with more than 32 * tree_words new rows is left out (its rows
+ *       become zero) and sets WIDE_ERR_BAD_INDEX
+ *   q, o, mask_bits, scale, flags, rows of no sequence, bad places: as for wide_attn_cache
+ *   workspace: wide_attn_tree_workspace_bytes() bytes; needs no initial value and keeps nothing, but two calls that can overlap on the GPU
+ *       need one each
+ * After the accepted path is known its keys and values are written again at the positions they have in the answer
+ * (wide_cache_write with the rows picked) and the length is set back.
+ * Accuracy: probabilities are rounded to bf16 (2^-8 of themselves), sums are fp32, the output is rounded to bf16.  Keys, values and
+ * queries of magnitude up to 2^100 such that logits and sums fit fp32.  The same call gives the same bits in every run.
+ * Built for 16 query rows a KV head and more (up to 128 share a pass over the cache); fewer are served, wide_attn_cache
+ * is quicker for a single row.  rows * n_q_heads <= 2^30.
+ * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA; WIDE_ERR_BAD_INDEX and WIDE_ERR_TIMEOUT through wide_status.
+ */
+WIDE_API size_t wide_attn_tree_workspace_bytes(void);
+WIDE_API int wide_attn_tree(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* q, int dtype, int rows,
+                            long long q_stride, int n_q_heads, int heads_per_group, const uint32_t* mask_bits, const uint32_t* tree_bits,
+                            int tree_words, float scale, void* o, void* workspace, size_t workspace_bytes, unsigned flags);
 
 /*
  * wide_unpermute -- scatter epilogue of Algorithm 2 as its own call: packed-sorted rows back to

@@ -40,7 +40,7 @@ EXPORTS = ["wide_create", "wide_destroy", "wide_status", "wide_set_wait_limit_ns
            "wide_ffn",
            "wide_oproj", "wide_attn", "wide_qproj", "wide_unpermute",
            "wide_rope", "wide_cache_page_bytes", "wide_cache_write", "wide_cache_read", "wide_attn_cache_workspace_bytes",
-           "wide_attn_cache", "wide_cache_append", "wide_linear"]
+           "wide_attn_cache", "wide_cache_append", "wide_linear", "wide_attn_tree_workspace_bytes", "wide_attn_tree"]
 
 _c_void_p, _c_int, _c_size_t, _c_uint = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint
 _c_ll = ctypes.c_longlong
@@ -126,9 +126,14 @@ def load_library() -> ctypes.CDLL:
     lib.wide_attn_cache_workspace_bytes.restype = _c_size_t
     lib.wide_attn_cache.argtypes = [_c_void_p] * 5 + [_c_int, _c_int, _c_ll, _c_int, _c_int, _c_void_p, _c_int,
                                                       ctypes.c_float, _c_void_p, _c_void_p, _c_size_t, _c_uint]
+    lib.wide_attn_tree_workspace_bytes.argtypes = []
+    lib.wide_attn_tree_workspace_bytes.restype = _c_size_t
+    lib.wide_attn_tree.argtypes = [_c_void_p] * 5 + [_c_int, _c_int, _c_ll, _c_int, _c_int, _c_void_p, _c_void_p, _c_int, ctypes.c_float,
+                                                     _c_void_p, _c_void_p, _c_size_t, _c_uint]
     for name in EXPORTS:
         if name not in ("wide_strerror", "wide_workspace_bytes", "wide_route_pair_prepared_bytes",
-                        "wide_route_pair_norm_workspace_bytes", "wide_cache_page_bytes", "wide_attn_cache_workspace_bytes"):
+                        "wide_route_pair_norm_workspace_bytes", "wide_cache_page_bytes", "wide_attn_cache_workspace_bytes",
+                        "wide_attn_tree_workspace_bytes"):
             getattr(lib, name).restype = _c_int
     _lib = lib
     return lib
@@ -784,3 +789,58 @@ def wide_attn_cache(ctx: Context, q: torch.Tensor, cache: Cache, seqs: Sequences
 
 def attn_cache_workspace_bytes(rows: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
     return int(load_library().wide_attn_cache_workspace_bytes(rows, n_q_heads, n_kv_heads, head_dim))
+
+
+@_on_device
+def wide_attn_tree(ctx: Context, q: torch.Tensor, cache: Cache, seqs: Sequences, n_q_heads: int, heads_per_group: int,
+                   tree_bits: torch.Tensor, mask_bits: Optional[torch.Tensor] = None, scale: float = 0.0, o: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """wide_attn_cache for trees of drafted tokens: row i of a sequence sees its prefix and, of the sequence's new rows, those whose bits
+    tree_bits int32 [rows, ceil(most new rows / 32)] names (``tree_ancestors`` makes them of parents).  ``workspace`` (uint8,
+    attn_tree_workspace_bytes) replaces the context's own scratch.  Rows that belong to no sequence are not written."""
+    width = n_q_heads * cache.head_dim
+    qp, qs = _rows(q, width, "q")
+    rows = q.shape[0]
+    if o is None:
+        o = q.new_empty((rows, width))
+    elif o.shape != q.shape or o.dtype != q.dtype or not o.is_contiguous():
+        raise ValueError("o: expected a contiguous tensor of q's shape and dtype")
+    if mask_bits is not None and mask_bits.shape != (rows, (n_q_heads // max(1, heads_per_group) + 31) // 32):
+        raise ValueError("mask_bits: expected [rows, ceil(n_groups / 32)]")
+    if tree_bits.dim() != 2 or tree_bits.shape[0] != rows:
+        raise ValueError("tree_bits: expected [rows, words]")
+    if workspace is None:      # one size serves every call, so this one stays where it is (captured graphs hold its address)
+        workspace = ctx._ws.get(3)
+        if workspace is None:
+            workspace = ctx.workspace(attn_tree_workspace_bytes(), slot=3)
+    index = ctx.device.index
+    _same_device(index, q, cache.pages, o, mask_bits, tree_bits, workspace, seqs.page_table, seqs.kv_lens, seqs.row_start)
+    bits, tree = _int32(mask_bits, "mask_bits"), _int32(tree_bits, "tree_bits")
+    if rows == 0 or seqs.n_seqs == 0:
+        return o
+    rc = ctx.lib.wide_attn_tree(ctx.handle, torch._C._cuda_getCurrentRawStream(index), ctypes.byref(cache.struct),
+                                ctypes.byref(seqs.struct), qp, _dtype_code(q), rows, qs, n_q_heads, heads_per_group, bits, tree,
+                                tree_bits.shape[1], float(scale), o.data_ptr(), workspace.data_ptr(), workspace.nbytes, 0)
+    if rc != OK:
+        raise WideError(rc, "wide_attn_tree")
+    return o
+
+
+def attn_tree_workspace_bytes() -> int:
+    return int(load_library().wide_attn_tree_workspace_bytes())
+
+
+def tree_ancestors(parents, words: Optional[int] = None):
+    """Host helper: the rows of tree_bits (int32 [n, words], a CPU tensor) of a sequence whose new row i hangs on new row parents[i] < i,
+    or on the prefix (-1): the bits of its ancestors and its own."""
+    n = len(parents)
+    words = words or max(1, (n + 31) // 32)
+    if n > 32 * words:
+        raise ValueError(f"{n} rows do not fit {words} words")
+    bits = []
+    for i, p in enumerate(parents):
+        if not -1 <= p < i:
+            raise ValueError(f"parents[{i}] = {p}: expected -1 or an earlier row")
+        bits.append((bits[p] if p >= 0 else 0) | 1 << i)
+    wrap = lambda w: w - (1 << 32) if w >= 1 << 31 else w  # noqa: E731
+    return torch.tensor([[wrap(b >> (32 * w) & 0xFFFFFFFF) for w in range(words)] for b in bits], dtype=torch.int32).reshape(n, words)

@@ -22,7 +22,7 @@ OBJ = os.path.join(PKG, "build")
 LIB = os.path.join(PKG, "libwide.so")
 
 SOURCES = ["api.cu", "route.cu", "reorder.cu", "ffn_simt.cu", "prefill_tc.cu", "gemmk_group.cu", "decode_tc.cu", "decode_gemv.cu", "attn_tc.cu", "attn_decode.cu", "linear.cu", "rope.cu", "kv_cache.cu", "cache_append.cu",
-           "attn_cache.cu", "selftest.cu"]
+           "attn_cache.cu", "attn_tree.cu", "selftest.cu"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",

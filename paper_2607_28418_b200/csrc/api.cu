@@ -88,6 +88,21 @@ int cache_move(wide_ctx* ctx, void* stream, bool write, const wide_cache* cache,
     return wide_launch_cache_move(ctx, static_cast<cudaStream_t>(stream), write, cache, seqs, k, v, dtype, rows, ks, vs);
 }
 
+// what the attentions over a cache ask of their arguments
+int check_attn(const wide_ctx* ctx, const wide_cache* cache, const wide_seqs* seqs, const void* q, int dtype, int rows, long long q_stride,
+               int n_q_heads, int heads_per_group, const void* o, const void* workspace, unsigned flags) {
+    if (!q || !o || !valid_dtype(dtype) || n_q_heads <= 0 || heads_per_group <= 0 || n_q_heads % heads_per_group != 0 || flags != 0)
+        return WIDE_ERR_INVALID_ARG;
+    int rc = check_cache(ctx, cache, seqs, rows);
+    if (rc != WIDE_OK) return rc;
+    if (n_q_heads % cache->n_kv_heads != 0) return WIDE_ERR_INVALID_ARG;
+    if (dtype != WIDE_BF16 || n_q_heads / heads_per_group > WIDE_MAX_GROUPS || n_q_heads > 4096 ||
+        static_cast<long long>(rows) * n_q_heads > (1 << 30))     // rows of all heads are counted with an int
+        return WIDE_ERR_UNSUPPORTED_SHAPE;
+    if ((rc = check_rows(q, q_stride, static_cast<long long>(n_q_heads) * cache->head_dim, 2)) != WIDE_OK) return rc;
+    return wide_aligned16(o) && wide_aligned16(workspace) ? WIDE_OK : WIDE_ERR_ALIGNMENT;
+}
+
 }  // namespace
 
 extern "C" {
@@ -593,16 +608,8 @@ size_t wide_attn_cache_workspace_bytes(int rows, int n_q_heads, int n_kv_heads, 
 int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* q, int dtype,
                     int rows, long long q_stride, int n_q_heads, int heads_per_group, const uint32_t* mask_bits, int causal,
                     float scale, void* o, void* workspace, size_t workspace_bytes, unsigned flags) {
-    if (!q || !o || !valid_dtype(dtype) || n_q_heads <= 0 || heads_per_group <= 0 || n_q_heads % heads_per_group != 0 || flags != 0)
-        return WIDE_ERR_INVALID_ARG;
-    int rc = check_cache(ctx, cache, seqs, rows);
+    const int rc = check_attn(ctx, cache, seqs, q, dtype, rows, q_stride, n_q_heads, heads_per_group, o, workspace, flags);
     if (rc != WIDE_OK) return rc;
-    if (n_q_heads % cache->n_kv_heads != 0) return WIDE_ERR_INVALID_ARG;
-    if (dtype != WIDE_BF16 || n_q_heads / heads_per_group > WIDE_MAX_GROUPS || n_q_heads > 4096 ||
-        static_cast<long long>(rows) * n_q_heads > (1 << 30))     // rows of all heads are counted with an int
-        return WIDE_ERR_UNSUPPORTED_SHAPE;
-    if ((rc = check_rows(q, q_stride, static_cast<long long>(n_q_heads) * cache->head_dim, 2)) != WIDE_OK) return rc;
-    if (!wide_aligned16(o) || !wide_aligned16(workspace)) return WIDE_ERR_ALIGNMENT;
     if (!workspace || workspace_bytes < wide_attn_cache_workspace(rows, n_q_heads, cache->n_kv_heads, cache->head_dim))
         return WIDE_ERR_WORKSPACE;
     if (q == o || !on_device(ctx)) return WIDE_ERR_INVALID_ARG;
@@ -610,6 +617,23 @@ int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cache, const 
     if (!(scale > 0.f)) scale = 1.0f / sqrtf(static_cast<float>(cache->head_dim));
     return wide_launch_attn_cache(ctx, static_cast<cudaStream_t>(stream), cache, seqs, q, rows, q_stride, n_q_heads,
                                   heads_per_group, mask_bits, causal ? 1 : 0, scale, o, workspace);
+}
+
+size_t wide_attn_tree_workspace_bytes(void) { return wide_attn_tree_workspace(); }
+
+int wide_attn_tree(wide_ctx* ctx, void* stream, const wide_cache* cache, const wide_seqs* seqs, const void* q, int dtype, int rows,
+                   long long q_stride, int n_q_heads, int heads_per_group, const uint32_t* mask_bits, const uint32_t* tree_bits,
+                   int tree_words, float scale, void* o, void* workspace, size_t workspace_bytes, unsigned flags) {
+    if (!tree_bits || tree_words <= 0) return WIDE_ERR_INVALID_ARG;
+    const int rc = check_attn(ctx, cache, seqs, q, dtype, rows, q_stride, n_q_heads, heads_per_group, o, workspace, flags);
+    if (rc != WIDE_OK) return rc;
+    if (tree_words > 8) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    if (!workspace || workspace_bytes < wide_attn_tree_workspace()) return WIDE_ERR_WORKSPACE;
+    if (q == o || !on_device(ctx)) return WIDE_ERR_INVALID_ARG;
+    if (rows == 0 || seqs->n_seqs == 0) return WIDE_OK;
+    if (!(scale > 0.f)) scale = 1.0f / sqrtf(static_cast<float>(cache->head_dim));
+    return wide_launch_attn_tree(ctx, static_cast<cudaStream_t>(stream), cache, seqs, q, rows, q_stride, n_q_heads, heads_per_group, mask_bits,
+                                 tree_bits, tree_words, scale, o, workspace);
 }
 
 int wide_unpermute(wide_ctx* ctx, void* stream, const void* src_packed, const int32_t* perm,

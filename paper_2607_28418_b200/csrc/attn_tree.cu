@@ -1,0 +1,742 @@
+// Attention of trees of drafted tokens over the 4-bit paged cache (wide_attn_tree): every new row sees the prefix of its sequence and, of the
+// new tokens, those that its bits name.
+//
+// A tree of 8 to 64 tokens and 4 query heads a KV head has 32 to 256 query rows that share every key, many more than the 8 to 24 that
+// wide_attn_cache keeps in registers, so here the codes become bf16 tiles in shared memory once and the products run on
+// tcgen05, 64 or 128 query rows a pass.  Keys are the 128-row operand, so what a tile costs follows the rows there are:
+//     S^T [128 keys (TMEM lanes)][rows]      = K [128 x D]   Q^T
+//     P^T = exp2(S^T scale - ref)              a thread has one key; written to shared memory as [key][row]
+//     O^T [D channels (lanes)][rows]        += V^T [D x 128] P^T   (V as unpacked, [key][channel], is the MN-major operand)
+// The reference `ref` of a row is raised (and its O rescaled in TMEM) only when a logit passes it by 2^kSlack; the sum over keys stays
+// in the threads and is made once an item.
+//
+// Roles: a warp that walks the items and brings 16-key blocks by bulk copies, eight warps that unpack them, eight that make P and
+// the outputs (four a group, the groups take turns of 16 rows), one thread for each of the two products.  K is unpacked for the next tile
+// while the softmax has this one.  Unpacking takes 3.75 instructions for two values: a code n in the low bits of the bf16 number 128
+// is 128 + n; taking 128 off is exact, and one fma rounds m + s n once, as wide_cache_read does.  With the fragment order in which
+// the codes lie, keys go out as 16-byte rows and values through transposing 8x8 stores; O's channels come out permuted within 32.
+//
+// Items are cut into equal pieces for the CTAs and joined as in wide_attn_cache (attn_plan.cuh).
+#include <atomic>
+
+#include "cache.cuh"
+
+namespace {
+
+constexpr int kItemAlone = 96;     // blocks of an item that one CTA may take alone
+constexpr int kItemCost = 8;       // units that an item counts on top of its blocks: queries in, results out
+
+}  // namespace
+
+#include "attn_plan.cuh"
+
+namespace {
+
+constexpr int kTile = 8;            // blocks of a tile: 128 keys
+constexpr int kKeys = 16 * kTile;
+constexpr int kMostRing = 3;        // tiles of codes on their way
+constexpr int kDescs = 8;           // tiles that are known: the ring's, and at most three behind it whose softmax is not done
+constexpr int kUnpackWarps = 8, kSoftWarps = 8;
+constexpr int kLoadWarp = 16, kScoreWarp = 17, kValueWarp = 18, kWarps = 20;   // (whole groups of four warps)
+constexpr float kSlack = 8.f;
+constexpr int kHalf = 16384;        // bytes of [128 keys][64 channels or rows]
+
+struct TreeArgs : AttnArgs {
+    const uint32_t* tree;
+    int tree_words;
+    int* timeout;                   // takes WIDE_ERR_TIMEOUT
+    unsigned long long wait_ns;
+};
+
+struct Tile {                       // what the roles are told of a tile
+    int blk, nb;                    // first block, blocks
+    uint32_t present;               // bit b: block b has a page
+    int first, last;                // of the item's part in this CTA
+    int masked;                     // not all rows see all 128 keys
+    int seq, kvh, rb, row0, n_rows, len;
+    int begins, ends;               // whether the part has the item's first, last block
+    int final;                      // the CTA's last tile
+};
+
+struct alignas(16) Shared {
+    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full, pv_done, meet[2];
+    uint32_t tmem;
+    int abort;
+    Cursor start;
+    Tile tiles[kDescs];
+    alignas(16) float ref[2][128];              // of a row, twice: the one in use and the next
+    float most[4][128];             // of a row, per warp of a group: the largest logit; at the end the sum of P
+    alignas(16) int flag[2][2][4];              // [tile parity][group][warp]: a logit passed its reference
+    uint32_t odd[2][kKeys];         // sub-groups of a new token's values that are not finite (their values are 0 in the tile)
+    uint32_t spoilt[128];           // rows that see such a sub-group
+};
+
+template <int D, int G, int NB>
+struct Layout {
+    static constexpr int kRows = 64 * NB, kNS = D / G, kSB = 16 * D + 128 * kNS, kStage = kTile * kSB, kBlocks = D / 64;
+    static constexpr int kTileBytes = kBlocks * kHalf;                 // of unpacked keys, or values
+    static constexpr int kRing = D == 128 && NB == 2 && G == 32 ? 2 : kMostRing;     // (no room for three)
+    static constexpr int kQ = 0, kK = kQ + kBlocks * kRows * 128, kV = kK + kTileBytes, kP = kV + 2 * kTileBytes, kCodes = kP + NB * kHalf,
+                         kPlan = kCodes + kRing * kStage;
+    static constexpr int kPlanRoom = 227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512 < 16384
+                                         ? (227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512) / 256 * 256 : 16384;
+    static constexpr int kSmem = kPlan + kPlanRoom + 1024;
+    static constexpr uint32_t kCols = NB == 1 ? 256 : 512, kO = 2 * kRows;
+    static_assert(kPlanRoom >= 1024 && kSmem + sizeof(Shared) <= 227 * 1024, "shared memory");
+};
+
+// MN-major operand in the 128-byte swizzle: rows of 64 elements, one per step of K; blocks of 64 elements `lbo` bytes apart
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t lbo) {
+    return umma_desc_sw128(addr & ~0u) & ~(static_cast<uint64_t>(0x3FFF) << 16) | static_cast<uint64_t>(lbo >> 4) << 16;
+}
+__host__ __device__ constexpr uint32_t idesc(int n, bool mn_major) { return umma_idesc_bf16(128, n) | (mn_major ? (1u << 15) | (1u << 16) : 0u); }
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void store_transposed(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+__device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
+__device__ __forceinline__ uint32_t as_word(__nv_bfloat162 b) { return *reinterpret_cast<const uint32_t*>(&b); }
+// m + s n of the two codes in bits 0..3 and 16..19 of w
+__device__ __forceinline__ uint32_t unpack_two(uint32_t w, uint32_t s, uint32_t m) {
+    const uint32_t high = (w & 0x000F000Fu) | 0x43004300u;       // 128 + n
+    return as_word(__hfma2(__hsub2(as_bf162(high), as_bf162(0x43004300u)), as_bf162(s), as_bf162(m)));
+}
+__device__ __forceinline__ bool not_finite(uint32_t word) { return (word & 0x7F80u) == 0x7F80u || (word & 0x7F800000u) == 0x7F800000u; }
+
+// order of fp32 numbers as that of integers, NaN aside
+__device__ __forceinline__ int ordered(float x) {
+    const int b = __float_as_int(x);
+    return b ^ ((b >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ float unordered(int b) { return __int_as_float(b ^ ((b >> 31) & 0x7fffffff)); }
+
+template <int D, int G, int NB>
+__global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_constant__ TreeArgs a) {
+    using L = Layout<D, G, NB>;
+    constexpr int kRows = L::kRows, kNS = L::kNS, kSB = L::kSB, kRing = L::kRing;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Shared sh;
+    __shared__ long long part[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t sm = smem_u32(base);
+    volatile int* abort_flag = &sh.abort;
+    auto bar = [&](const uint64_t& b) { return smem_u32(&b); };
+    if (tid == 0) {
+        for (int i = 0; i < kRing; ++i) {
+            mbar_init(bar(sh.ring_full[i]), 1);
+            mbar_init(bar(sh.ring_empty[i]), kUnpackWarps);
+        }
+        mbar_init(bar(sh.k_full), kUnpackWarps);
+        mbar_init(bar(sh.k_free), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(sh.v_full[i]), kUnpackWarps);
+            mbar_init(bar(sh.v_free[i]), 1);
+            mbar_init(bar(sh.s_full[i]), 1);
+            mbar_init(bar(sh.s_free[i]), kSoftWarps);
+            mbar_init(bar(sh.meet[i]), 4);
+        }
+        mbar_init(bar(sh.p_full), kSoftWarps);
+        mbar_init(bar(sh.pv_done), 1);
+        sh.abort = 0;
+        fence_barrier_init();
+    }
+    if (tid < 128) sh.spoilt[tid] = 0;
+    grid_dep_wait();
+    // (Tensor memory is taken after the kernel before has ended and before the next may come: no two wait for each other's.)
+    if (warp == kScoreWarp) {
+        tmem_alloc(smem_u32(&sh.tmem), L::kCols);
+        tmem_relinquish();
+    }
+    prefetch_l2(a.mask_bits, static_cast<size_t>(a.q.rows) * a.words * 4);
+    prefetch_l2(a.tree, static_cast<size_t>(a.q.rows) * a.tree_words * 4);
+    prefetch_l2(a.q.page_table, static_cast<size_t>(a.q.n_seqs) * a.q.max_pages * 4);
+    prefetch_l2(a.qm, (static_cast<size_t>(a.q.rows - 1) * a.qs + a.n_q * D) * 2);
+    const Plan plan = plan_at(a.plan ? a.plan : base + L::kPlan, a.q.n_seqs, a.plan_words);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    grid_dep_launch();     // the joining kernel may take its place as soon as CTAs end; it waits for all of them
+    if (!a.plan) make_plan<kRows>(a, plan, part, gridDim.x, blockIdx.x == 0);
+    const uint32_t tmem = sh.tmem;
+
+    const long long total = plan.offsets[a.q.n_seqs];
+    const int same = *plan.same, cta = blockIdx.x;
+    // a tile's worth of units a CTA at least
+    const int ctas = same ? static_cast<int>(total) / same : static_cast<int>(min(static_cast<long long>(gridDim.x), (total + kTile - 1) / kTile));
+    long long u0 = 0, u1 = 0;
+    if (cta < ctas) {
+        const long long share = total / ctas;
+        const int more = static_cast<int>(total - share * ctas);
+        u0 = share * cta + min(cta, more);
+        u1 = u0 + share + (cta < more ? 1 : 0);
+    }
+    int* meta = a.meta + cta * 2 * kMeta;
+    float* parts = a.parts + static_cast<size_t>(cta) * 2 * slot_floats(kRows, D);
+
+    if (u0 < u1) {         // (uniform in the CTA)
+        if (warp == kLoadWarp) {
+            const Cursor k = locate(a, plan, u0, static_cast<int>(min(u1 - u0, 0x7fffffffLL)));
+            if (lane == 0) sh.start = k;
+        }
+        __syncthreads();
+    }
+    int open = 0;          // which of the two partial results this CTA leaves; of the loading warp
+    if (u0 < u1 && sh.start.blk < sh.start.end) {
+        if (warp < kUnpackWarps) {
+            // ------------------------------------------------------------------------ codes to bf16 tiles
+            const int kr = ((lane >> 2) & 1) * 4 + (lane >> 3), kc = lane & 3;     // key (and key + 8), 8-channel piece: no bank twice in a store
+            const int g = lane >> 2, t = lane & 3;
+            bool ok = true;
+            for (int n = 0;; ++n) {
+                const int st = n % kRing;
+                if (!(ok = mbar_wait_warp(bar(sh.ring_full[st]), (n / kRing) & 1, a.wait_ns, abort_flag))) break;
+                const Tile& d = sh.tiles[n % kDescs];
+                const bool here = warp < d.nb && ((d.present >> warp) & 1u);
+                const int key0 = (d.blk + warp) * 16;                               // of this warp's block
+                const uint32_t codes = sm + L::kCodes + st * L::kStage + warp * kSB, words = codes + 16 * D;
+                // the scores of the tile before have been made: K, and Q at the end of an item, may change
+                if (n > 0 && !(ok = mbar_wait_warp(bar(sh.k_free), (n - 1) & 1, a.wait_ns, abort_flag))) break;
+                if (d.first) {
+                    const RowBlock rows = row_block(a, d.rb * kRows);
+                    constexpr int kChunks = kRows * D / 8;                          // of 16 bytes
+#pragma unroll 4
+                    for (int i = tid; i < kChunks; i += 32 * kUnpackWarps) {
+                        const int r = i / (D / 8), c = i % (D / 8);
+                        const Row w = row_of(a, rows, r);
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (w.tok < d.n_rows)
+                            v = *reinterpret_cast<const uint4*>(a.qm + static_cast<long long>(d.row0 + w.tok) * a.qs + (d.kvh * a.share + w.sub) * D + 8 * c);
+                        sts128(sm + L::kQ + (c >> 3) * (kRows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), v.x, v.y, v.z, v.w);
+                    }
+                }
+                if (here) {
+                    uint32_t s0[kNS], s1[kNS];
+                    lds_words<kNS>(words + kr * kNS * 4, s0);
+                    lds_words<kNS>(words + (kr + 8) * kNS * 4, s1);
+                    uint32_t m0[kNS], m1[kNS];
+#pragma unroll
+                    for (int i = 0; i < kNS; ++i) {
+                        m0[i] = __byte_perm(s0[i], 0, 0x3232), s0[i] = __byte_perm(s0[i], 0, 0x1010);
+                        m1[i] = __byte_perm(s1[i], 0, 0x3232), s1[i] = __byte_perm(s1[i], 0, 0x1010);
+                    }
+                    const uint32_t row = sm + L::kK + (warp * 16 + kr) * 128;
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) {
+                        const uint4 v = lds128(codes + c * 512 + (kr * 4 + kc) * 16);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {                               // channels 64 c + 32 h + 8 kc ..
+                            const int i = (64 * c + 32 * h) / G;
+                            const uint32_t x = h ? v.z : v.x, y = h ? v.w : v.y;
+                            const uint32_t at = row + c * kHalf + (((4 * h + kc) ^ kr) << 4);
+                            sts128(at, unpack_two(x, s0[i], m0[i]), unpack_two(x >> 4, s0[i], m0[i]), unpack_two(y, s0[i], m0[i]), unpack_two(y >> 4, s0[i], m0[i]));
+                            sts128(at + 8 * 128, unpack_two(x >> 8, s1[i], m1[i]), unpack_two(x >> 12, s1[i], m1[i]), unpack_two(y >> 8, s1[i], m1[i]),
+                                   unpack_two(y >> 12, s1[i], m1[i]));
+                        }
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sh.k_full));
+                // ---- values
+                if (n >= 2 && !(ok = mbar_wait_warp(bar(sh.v_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
+                {
+                    uint32_t p[4][kNS];                                             // tokens 2t, 2t + 1, 2t + 8, 2t + 9
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 2 * t + 8 * (e >> 1) + (e & 1);
+                        lds_words<kNS>(words + 64 * kNS + r * kNS * 4, p[e]);
+                        if (d.masked) {
+                            const bool is = here && key0 + r < d.len, young = key0 + r >= d.len - d.n_rows;
+                            uint32_t bad = 0;
+#pragma unroll
+                            for (int i = 0; i < kNS; ++i) {
+                                if (!is) p[e][i] = 0;
+                                if (young && not_finite(p[e][i])) {
+                                    p[e][i] = 0;
+                                    bad |= 1u << i;
+                                }
+                            }
+                            if (g == 0) sh.odd[n & 1][warp * 16 + r] = bad;
+                        }
+                    }
+                    uint32_t s0[kNS], m0[kNS], s1[kNS], m1[kNS];
+#pragma unroll
+                    for (int i = 0; i < kNS; ++i) {
+                        s0[i] = __byte_perm(p[0][i], p[1][i], 0x5410), m0[i] = __byte_perm(p[0][i], p[1][i], 0x7632);
+                        s1[i] = __byte_perm(p[2][i], p[3][i], 0x5410), m1[i] = __byte_perm(p[2][i], p[3][i], 0x7632);
+                    }
+                    const int token = (lane & 7) + 8 * (lane >> 4);                 // whose row this lane's address is, and which nibble
+                    const uint32_t row = sm + L::kV + (n & 1) * L::kTileBytes + (warp * 16 + token) * 128;
+#pragma unroll
+                    for (int c = 0; c < D / 64; ++c) {
+                        const uint4 v = lds128(codes + 8 * D + c * 512 + lane * 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {                               // channels 64 c + 32 (e / 2) + 4 g + 2 (e % 2) ..
+                            const int i = (64 * c + 32 * (e >> 1)) / G;
+                            const uint32_t x = e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
+                            const int piece = (e >> 1) * 4 + 2 * (e & 1) + ((lane >> 3) & 1);
+                            store_transposed(row + c * kHalf + ((piece ^ (token & 7)) << 4), unpack_two(x, s0[i], m0[i]), unpack_two(x >> 4, s0[i], m0[i]),
+                                             unpack_two(x >> 8, s1[i], m1[i]), unpack_two(x >> 12, s1[i], m1[i]));
+                        }
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(sh.v_full[n & 1]));
+                }
+                if (d.final) break;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sh.ring_empty[st]));     // (the tile's description may go with it)
+            }
+            if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
+        } else if (warp < kUnpackWarps + kSoftWarps) {
+            // ------------------------------------------------------------------------ softmax, outputs
+            const int group = (warp - kUnpackWarps) >> 2, quarter = warp & 3;
+            const int key = quarter * 32 + lane;                                    // of a tile
+            const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+            constexpr int kChunks = NB * 2;                                         // of 16 rows, of this group: group, group + 2, ..
+            float l[kChunks][16];
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) l[i][e] = 0.f;
+            int use = 0, meets = 0;
+            bool ok = true;
+            auto meet = [&]() {             // the four warps of the group
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sh.meet[group]));
+                return mbar_wait_warp(bar(sh.meet[group]), meets++ & 1, a.wait_ns, abort_flag);
+            };
+            for (int n = 0;; ++n) {
+                if (!(ok = mbar_wait_warp(bar(sh.s_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                tc_fence_after_sync();
+                const Tile& d = sh.tiles[n % kDescs];
+                const int n_rows = min(kRows, d.n_rows * a.share - d.rb * kRows);   // query rows of the item
+                const uint32_t scores = tmem + lanes + (n & 1) * kRows;
+                const bool masked = d.masked;
+                const RowBlock rows = row_block(a, d.rb * kRows);
+                const int pos = d.blk * 16 + key, node = pos - (d.len - d.n_rows);
+                const bool is = (key >> 4) < d.nb && ((d.present >> (key >> 4)) & 1u) && pos < d.len;
+                // bit e: row 16 c + e sees this thread's key
+                auto sees = [&](int c) -> uint32_t {
+                    uint32_t m = 0;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int tok = row_of(a, rows, 16 * c + e).tok;
+                        bool s = is && tok < d.n_rows;
+                        if (s && node >= 0)
+                            s = node < 32 * a.tree_words && ((a.tree[static_cast<size_t>(d.row0 + tok) * a.tree_words + (node >> 5)] >> (node & 31)) & 1u);
+                        m |= s ? 1u << e : 0u;
+                    }
+                    return m;
+                };
+                uint32_t seen[kChunks];
+                bool change = d.first;
+                // ---- does a logit pass its reference?
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i) {
+                    const int c = group + 2 * i;
+                    seen[i] = 0xffffu;
+                    if (16 * c >= n_rows) continue;
+                    if (masked) seen[i] = sees(c);
+                    if (d.first) continue;
+                    uint32_t s[16];
+                    tmem_ld_32x16(scores + 16 * c, s);
+                    tmem_ld_wait();
+                    float most = -CUDART_INF_F;
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 r = *reinterpret_cast<const float4*>(&sh.ref[use][16 * c + e]);
+                        const float rr[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) {
+                            const float x = fmaf(__uint_as_float(s[e + f]), a.scale_log2e, -(rr[f] == -CUDART_INF_F ? -1e38f : rr[f]));
+                            most = fmaxf(most, (seen[i] >> (e + f)) & 1u ? x : -CUDART_INF_F);
+                        }
+                    }
+                    change = change || most > kSlack;
+                }
+                change = __any_sync(0xffffffffu, change);
+                if (lane == 0) sh.flag[n & 1][group][quarter] = change;
+                if (!(ok = meet())) break;
+                const int4 flags = *reinterpret_cast<const int4*>(sh.flag[n & 1][group]);
+                if (flags.x | flags.y | flags.z | flags.w) {
+                    // ---- new references: the largest logits so far; what is summed is scaled
+#pragma unroll
+                    for (int i = 0; i < kChunks; ++i) {
+                        const int c = group + 2 * i;
+                        if (16 * c >= n_rows) continue;
+                        uint32_t s[16];
+                        tmem_ld_32x16(scores + 16 * c, s);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float x = __uint_as_float(s[e]) * a.scale_log2e;
+                            const int top = __reduce_max_sync(0xffffffffu, ordered((seen[i] >> e) & 1u && x == x ? x : -CUDART_INF_F));
+                            if (lane == e) sh.most[quarter][16 * c + e] = unordered(top);
+                        }
+                    }
+                    if (!(ok = meet())) break;
+                    // O holds the tiles up to the one before
+                    if (n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done), (n - 1) & 1, a.wait_ns, abort_flag))) break;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int i = 0; i < kChunks; ++i) {
+                        const int c = group + 2 * i;
+                        if (16 * c >= n_rows) continue;
+                        float alpha = 1.f;          // of row 16 c + lane % 16
+                        {
+                            const int r = 16 * c + (lane & 15);
+                            const float old = d.first ? -CUDART_INF_F : sh.ref[use][r];
+                            const float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])), old);
+                            alpha = now == -CUDART_INF_F ? 1.f : exp2_fast(old - now);
+                            if (lane < 16) sh.ref[use ^ 1][r] = now;     // every warp of the group writes the same
+                        }
+                        uint32_t o[16];
+                        if (!d.first) {
+                            tmem_ld_32x16(tmem + lanes + L::kO + 16 * c, o);
+                            tmem_ld_wait();
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const float f = __shfl_sync(0xffffffffu, alpha, e);
+                            l[i][e] *= f;
+                            if (!d.first) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        }
+                        if (!d.first) tmem_st_32x16(tmem + lanes + L::kO + 16 * c, o);
+                    }
+                    tmem_st_wait();
+                    __syncwarp();
+                    use ^= 1;
+                }
+                // ---- P; the product of the tile before has read its own
+                if (n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done), (n - 1) & 1, a.wait_ns, abort_flag))) break;
+                if (masked) {          // values that are not finite, of keys that some row may not see
+                    if (!(ok = mbar_wait_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                }
+                const uint32_t bad = masked ? sh.odd[n & 1][key] : 0u;
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i) {
+                    const int c = group + 2 * i;
+                    if (16 * c >= n_rows) continue;
+                    uint32_t s[16], p[8];
+                    tmem_ld_32x16(scores + 16 * c, s);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 r = *reinterpret_cast<const float4*>(&sh.ref[use][16 * c + e]);
+                        const float rr[4] = {r.x, r.y, r.z, r.w};
+                        float x[4];
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) {
+                            x[f] = exp2_fast(fmaf(__uint_as_float(s[e + f]), a.scale_log2e, rr[f] == -CUDART_INF_F ? 0.f : -rr[f]));
+                            if (masked && !((seen[i] >> (e + f)) & 1u)) x[f] = 0.f;
+                            l[i][e + f] += x[f];
+                        }
+                        p[e / 2] = as_word(__floats2bfloat162_rn(x[0], x[1]));
+                        p[e / 2 + 1] = as_word(__floats2bfloat162_rn(x[2], x[3]));
+                    }
+                    const uint32_t row = sm + L::kP + (c >> 2) * kHalf + key * 128;
+                    sts128(row + (((2 * c) & 7) ^ (key & 7)) * 16, p[0], p[1], p[2], p[3]);
+                    sts128(row + (((2 * c + 1) & 7) ^ (key & 7)) * 16, p[4], p[5], p[6], p[7]);
+                    if (bad)
+                        for (int e = 0; e < 16; ++e)
+                            if ((seen[i] >> e) & 1u) atomicOr(&sh.spoilt[16 * c + e], bad);
+                }
+                fence_proxy_async_smem();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(bar(sh.s_free[n & 1]));
+                    mbar_arrive(bar(sh.p_full));
+                }
+                if (!d.last) continue;          // (the CTA's last tile is the last of its part)
+                // ---- end of the item or of the piece
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i) {
+                    const int c = group + 2 * i;
+                    if (16 * c >= n_rows) continue;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float x = l[i][e];
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+                        if (lane == e) sh.most[quarter][16 * c + e] = x;
+                        l[i][e] = 0.f;
+                    }
+                }
+                if (!(ok = meet())) break;
+                if (!(ok = mbar_wait_warp(bar(sh.pv_done), n & 1, a.wait_ns, abort_flag))) break;
+                tc_fence_after_sync();
+                // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j
+                const int at = quarter * 32 + lane, channel = (at & ~31) + 4 * (lane & 7) + (lane >> 3);
+                const bool whole = d.begins && d.ends;
+                float* dst = parts + (d.begins ? slot_floats(kRows, D) : 0);
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i) {
+                    const int c = group + 2 * i;
+                    if (16 * c >= n_rows) continue;
+                    uint32_t o[16];
+                    tmem_ld_32x16(tmem + lanes + L::kO + 16 * c, o);
+                    tmem_ld_wait();
+                    if (at >= D) continue;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int r = 16 * c + e;
+                        const float sum = (sh.most[0][r] + sh.most[1][r]) + (sh.most[2][r] + sh.most[3][r]);
+                        float x = __uint_as_float(o[e]);
+                        if ((sh.spoilt[r] >> (channel / G)) & 1u) x = CUDART_NAN_F;
+                        if (whole) {
+                            const RowOut ro = row_out(a, d.row0, d.n_rows, d.kvh, row_of(a, rows, r), D);
+                            if (ro.o) ro.o[channel] = __float2bfloat16_rn(ro.on && sum != 0.f ? x / sum : 0.f);
+                        } else if (r < n_rows) {
+                            dst[r * D + channel] = x;
+                            if (at == 0) *reinterpret_cast<float2*>(dst + kRows * D + 2 * r) = make_float2(sh.ref[use][r], sum);
+                        }
+                    }
+                }
+                if (!(ok = meet())) break;          // all have read sums and spoilt rows
+                for (int r = quarter * 32 + lane; r < kRows; r += 128)
+                    if (((r >> 4) & 1) == group) sh.spoilt[r] = 0;
+                tc_fence_before_sync();
+                if (d.final) break;
+            }
+            if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
+        } else if (warp == kLoadWarp) {
+            // ------------------------------------------------------------------------ items, codes
+            Cursor k = sh.start;
+            const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
+            bool ok = true, first = true;
+            int first_blk = k.blk, pt_first = -1000000, pt = -1, pt_next = -1;
+            for (int n = 0;; ++n) {
+                const int st = n % kRing, nb = min(kTile, k.end - k.blk), from = k.blk >> sub_shift, to = (k.blk + nb - 1) >> sub_shift;
+                // page numbers: 32 at hand, the next 32 on their way
+                auto pages_from = [&](int p) { return p + lane < a.q.max_pages ? a.q.page_table[static_cast<size_t>(k.seq) * a.q.max_pages + p + lane] : -1; };
+                if (from < pt_first || to >= pt_first + 64) {
+                    pt_first = from;
+                    pt = pages_from(pt_first);
+                    pt_next = pages_from(pt_first + 32);
+                } else if (from >= pt_first + 32) {
+                    pt_first += 32;
+                    pt = pt_next;
+                    pt_next = pages_from(pt_first + 32);
+                }
+                const int want = ((k.blk + min(lane, nb - 1)) >> sub_shift) - pt_first;
+                int page = __shfl_sync(0xffffffffu, pt, want & 31);
+                if (to >= pt_first + 32) {
+                    const int far = __shfl_sync(0xffffffffu, pt_next, want & 31);
+                    if (want >= 32) page = far;
+                }
+                const bool there = lane < nb && static_cast<unsigned>(page) < static_cast<unsigned>(a.c.n_pages);
+                const uint32_t present = __ballot_sync(0xffffffffu, there);
+                const int4 info = plan.seqs[k.seq];
+                Cursor next = k;            // what comes behind this tile
+                next.blk += nb;
+                const bool last = next.blk >= next.end, begins = first_blk == 0, ends = k.end == k.n_blk;
+                if (last && next.left > 0) next_item(a, plan, next);
+                const bool final = last && next.blk >= next.end;
+                if (n >= kRing && !(ok = mbar_wait_warp(bar(sh.ring_empty[st]), ((n / kRing) & 1) ^ 1, a.wait_ns, abort_flag))) break;
+                if (lane == 0) {
+                    if (present != (1u << nb) - 1u) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
+                    Tile& d = sh.tiles[n % kDescs];
+                    d.blk = k.blk, d.nb = nb, d.present = present, d.first = first, d.last = last;
+                    d.masked = present != (1u << kTile) - 1u || (k.blk + nb) * 16 > info.z - info.y;
+                    d.seq = k.seq, d.kvh = k.kvh, d.rb = k.rb, d.row0 = info.x, d.n_rows = info.y, d.len = info.z;
+                    d.begins = begins, d.ends = ends, d.final = final;
+                    mbar_arrive_expect_tx(bar(sh.ring_full[st]), __popc(present) * kSB);
+                }
+                __syncwarp();
+                if (there)
+                    bulk_load(sm + L::kCodes + st * L::kStage + lane * kSB,
+                              a.c.pages + static_cast<size_t>(page) * a.page_bytes + ((static_cast<size_t>(k.kvh) << sub_shift) + ((k.blk + lane) & sub_mask)) * kSB, kSB,
+                              bar(sh.ring_full[st]));
+                if (last && !(begins && ends)) {
+                    int* m = meta + (begins ? kMeta : 0);
+                    if (lane == 0) {
+                        m[0] = ends ? 2 : 1;
+                        m[1] = info.x;
+                        m[2] = info.y;
+                        m[3] = k.kvh;
+                        m[4] = k.rb;
+                    }
+                    open |= begins ? 2 : 1;
+                }
+                if (final) break;
+                first = last;
+                if (last) {
+                    if (next.seq != k.seq) pt_first = -1000000;
+                    first_blk = next.blk;
+                }
+                k = next;
+            }
+            if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
+        } else if (warp == kScoreWarp) {
+            // ------------------------------------------------------------------------ S^T = K Q^T
+            if (lane == 0) {
+                bool ok = true;
+                for (int n = 0;; ++n) {
+                    if (!(ok = mbar_wait(bar(sh.k_full), n & 1, a.wait_ns, abort_flag))) break;
+                    if (n >= 2 && !(ok = mbar_wait(bar(sh.s_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
+                    tc_fence_after_sync();
+                    const uint64_t kd = umma_desc_sw128(sm + L::kK), qd = umma_desc_sw128(sm + L::kQ);
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+                        umma_bf16(tmem + (n & 1) * kRows, kd + (i / 4) * (kHalf >> 4) + 2 * (i % 4), qd + (i / 4) * (kRows * 128 >> 4) + 2 * (i % 4), idesc(kRows, false),
+                                  i > 0 ? 1u : 0u);
+                    umma_commit(bar(sh.k_free));
+                    umma_commit(bar(sh.s_full[n & 1]));
+                    if (sh.tiles[n % kDescs].final) break;
+                }
+                if (!ok) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
+            }
+        } else if (warp == kValueWarp) {
+            // ------------------------------------------------------------------------ O^T += V^T P^T
+            if (lane == 0) {
+                bool ok = true;
+                for (int n = 0;; ++n) {
+                    if (!(ok = mbar_wait(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                    if (!(ok = mbar_wait(bar(sh.p_full), n & 1, a.wait_ns, abort_flag))) break;
+                    tc_fence_after_sync();
+                    // (heads of 64: the upper 64 lanes take whatever lies behind the tile, and nobody reads them)
+                    const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf), pd = desc_mn(sm + L::kP, kHalf);
+                    const bool first = sh.tiles[n % kDescs].first, final = sh.tiles[n % kDescs].final;
+#pragma unroll
+                    for (int i = 0; i < kKeys / 16; ++i) umma_bf16(tmem + L::kO, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(kRows, true), first && i == 0 ? 0u : 1u);
+                    umma_commit(bar(sh.v_free[n & 1]));
+                    umma_commit(bar(sh.pv_done));
+                    if (final) break;
+                }
+                if (!ok) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
+            }
+        }
+        __syncwarp();
+    }
+    if (warp == kLoadWarp && lane == 0) {
+        if (!(open & 1)) meta[0] = 0;
+        if (!(open & 2)) meta[kMeta] = 0;
+    }
+    // rows that no item writes: KV heads that a sequence does not use, sequences that are left out
+    for (int s = cta; s < a.q.n_seqs; s += gridDim.x) {
+        const int4 i = plan.seqs[s];
+        const int per_row = a.n_q * (D / 8);
+        for (long long x = tid; x < static_cast<long long>(i.y) * per_row; x += 32 * kWarps) {
+            const int r = static_cast<int>(x / per_row), v = static_cast<int>(x - static_cast<long long>(r) * per_row), h = v / (D / 8) / a.share;
+            if (!((plan.masks[s * a.plan_words + (h >> 5)] >> (h & 31)) & 1u))
+                reinterpret_cast<uint4*>(a.o + static_cast<size_t>(i.x + r) * a.n_q * D)[v] = make_uint4(0, 0, 0, 0);
+        }
+    }
+    if (*abort_flag && tid == 0)
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);   // copies in flight land before the shared memory is given up
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == kScoreWarp) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem, L::kCols);
+    }
+}
+
+struct Work {
+    size_t plan, parts, meta, total;
+};
+Work work_layout() {
+    Work w;
+    size_t at = 0;
+    w.plan = at;
+    at += wide_align_up(plan_bytes(WIDE_MAX_SEQS, 8, 8), 256);
+    w.parts = at;
+    at += wide_align_up(static_cast<size_t>(kMaxCtas) * 2 * slot_floats(128, 128) * 4, 256);
+    w.meta = at;
+    at += static_cast<size_t>(kMaxCtas) * 2 * kMeta * 4;
+    w.total = wide_align_up(at, 256);
+    return w;
+}
+
+template <int D, int G, int NB>
+int launch(wide_ctx* ctx, cudaStream_t s, TreeArgs a, unsigned char* ws) {
+    using L = Layout<D, G, NB>;
+    auto kernel = attn_tree_kernel<D, G, NB>;
+    const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
+    const Work w = work_layout();
+    a.heads = nullptr;
+    a.parts = reinterpret_cast<float*>(ws + w.parts);
+    a.meta = reinterpret_cast<int*>(ws + w.meta);
+    a.plan = nullptr;
+    if (plan_bytes(a.q.n_seqs, a.plan_words, a.words) > static_cast<size_t>(L::kPlanRoom)) {
+        a.plan = ws + w.plan;
+        WideLaunch l(ctx, s, "attn_tree_plan");
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_cache_plan_kernel<L::kRows>, dim3(1), dim3(1024), 0, s, a, ctas));
+    }
+    // once a device; threads that come here together all set the same
+    static std::atomic<unsigned> set{0};
+    const unsigned bit = ctx->device < 32 ? 1u << ctx->device : 0u;
+    if (!(set.load(std::memory_order_relaxed) & bit) || !bit) {
+        WIDE_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kSmem));
+        set.fetch_or(bit, std::memory_order_relaxed);
+    }
+    {
+        WideLaunch l(ctx, s, "attn_tree");
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, kernel, dim3(ctas), dim3(32 * kWarps), L::kSmem, s, a));
+    }
+    // Nothing to join where the plan is certain to give every item a CTA of its own (make_plan).
+    const long long items = static_cast<long long>(a.c.n_kv_heads) * (static_cast<long long>(a.q.rows) * a.share / L::kRows + a.q.n_seqs);
+    if (items > ctas || (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) > kItemAlone) {
+        WideLaunch l(ctx, s, "attn_tree_join");
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_cache_join_kernel<L::kRows, D>, dim3(ctas, L::kRows * D / 512), dim3(256), 0, s, a, ctas));
+    }
+    return WIDE_OK;
+}
+
+template <int NB>
+int launch_shape(wide_ctx* ctx, cudaStream_t s, const TreeArgs& a, int D, int G, unsigned char* ws) {
+    if (D == 128) {
+        if (G == 128) return launch<128, 128, NB>(ctx, s, a, ws);
+        if (G == 64) return launch<128, 64, NB>(ctx, s, a, ws);
+        return launch<128, 32, NB>(ctx, s, a, ws);
+    }
+    if (G == 64) return launch<64, 64, NB>(ctx, s, a, ws);
+    return launch<64, 32, NB>(ctx, s, a, ws);
+}
+
+}  // namespace
+
+size_t wide_attn_tree_workspace() { return work_layout().total; }
+
+int wide_launch_attn_tree(wide_ctx* ctx, cudaStream_t s, const wide_cache* cache, const wide_seqs* seqs, const void* q, int rows,
+                          long long qs, int n_q, int hpg, const uint32_t* mask_bits, const uint32_t* tree_bits, int tree_words, float scale,
+                          void* o, void* ws) {
+    TreeArgs a{};
+    a.c = wide_cache_view(cache);
+    a.q = wide_seq_view(seqs, rows);
+    a.page_bytes = static_cast<unsigned>(a.c.block_bytes) * static_cast<unsigned>(cache->n_kv_heads) << (a.c.page_shift - 4);
+    a.qm = static_cast<const __nv_bfloat16*>(q);
+    a.qs = qs;
+    a.n_q = n_q;
+    a.share = n_q / cache->n_kv_heads;
+    a.by_share = a.share > 1 ? static_cast<unsigned>(((1ull << 32) + a.share - 1) / a.share) : 0u;
+    a.hpg = hpg;
+    a.words = (n_q / hpg + 31) / 32;
+    a.most_rows = 32 * tree_words;
+    a.mask_bits = mask_bits;
+    a.tree = tree_bits;
+    a.tree_words = tree_words;
+    a.scale_log2e = scale * 1.4426950408889634f;
+    a.o = static_cast<__nv_bfloat16*>(o);
+    a.status = ctx->d_status + WIDE_STATUS_INDEX;
+    a.timeout = ctx->d_status;
+    a.wait_ns = ctx->wait_ns;
+    a.plan_words = (cache->n_kv_heads + 31) / 32;
+    // Query rows of a sequence and KV head, on average (the lengths are on the device): above 64, 128 share a pass over the cache.
+    const long long rows_per_head = seqs->row_start ? static_cast<long long>(rows) * a.share / seqs->n_seqs : a.share;
+    if (rows_per_head <= 64) return launch_shape<1>(ctx, s, a, cache->head_dim, cache->quant_group, static_cast<unsigned char*>(ws));
+    return launch_shape<2>(ctx, s, a, cache->head_dim, cache->quant_group, static_cast<unsigned char*>(ws));
+}

@@ -251,3 +251,7 @@ size_t wide_attn_cache_workspace(int rows, int n_q, int n_kv, int head_dim);
 int wide_launch_attn_cache(wide_ctx* ctx, cudaStream_t s, const wide_cache* cache, const wide_seqs* seqs, const void* q,
                            int rows, long long qs, int n_q, int hpg, const uint32_t* mask_bits, int causal, float scale,
                            void* o, void* ws);
+size_t wide_attn_tree_workspace();
+int wide_launch_attn_tree(wide_ctx* ctx, cudaStream_t s, const wide_cache* cache, const wide_seqs* seqs, const void* q, int rows,
+                          long long qs, int n_q, int hpg, const uint32_t* mask_bits, const uint32_t* tree_bits, int tree_words, float scale,
+                          void* o, void* ws);
