@@ -18,6 +18,7 @@
 //
 // Items are cut into equal pieces for the CTAs and joined as in wide_attn_cache (attn_plan.cuh).
 #include <atomic>
+#include <type_traits>
 
 #include "cache.cuh"
 
@@ -39,6 +40,8 @@ constexpr int kDescs = 8;           // tiles that are known: the ring's, and at 
 constexpr int kUnpackWarps = 8, kSoftWarps = 8;
 constexpr int kLoadWarp = 16, kScoreWarp = 17, kValueWarp = 18, kWarps = 20;   // (whole groups of four warps)
 constexpr float kSlack = 8.f;
+constexpr float kNothing = 1e38f;    // minus the reference of a row that has seen nothing yet: a logit of any size passes it
+constexpr int kOnes = 3 * 1024;      // bytes of ones: two blocks of 64 rows and two groups of 8 keys, each 1024 further on
 constexpr int kHalf = 16384;        // bytes of [128 keys][64 channels or rows]
 
 struct TreeArgs : AttnArgs {
@@ -64,11 +67,11 @@ struct alignas(16) Shared {
     int abort;
     Cursor start;
     Tile tiles[kDescs];
-    alignas(16) float ref[2][128];              // of a row, twice: the one in use and the next
-    float most[4][128];             // of a row, per warp of a group: the largest logit; at the end the sum of P
+    alignas(16) float minus_ref[2][128];        // of a row, twice: the one in use and the next
+    float most[4][128];             // of a row, per warp of a group: the largest logit
     alignas(16) int flag[2][2][4];              // [tile parity][group][warp]: a logit passed its reference
     uint32_t odd[2][kKeys];         // sub-groups of a new token's values that are not finite (their values are 0 in the tile)
-    uint32_t spoilt[128];           // rows that see such a sub-group
+    uint32_t spoilt[2][128];        // rows that see such a sub-group, of this item and the next
 };
 
 template <int D, int G, int NB>
@@ -77,11 +80,11 @@ struct Layout {
     static constexpr int kTileBytes = kBlocks * kHalf;                 // of unpacked keys, or values
     static constexpr int kRing = D == 128 && NB == 2 && G == 32 ? 2 : kMostRing;     // (no room for three)
     static constexpr int kQ = 0, kK = kQ + kBlocks * kRows * 128, kV = kK + kTileBytes, kP = kV + 2 * kTileBytes, kCodes = kP + NB * kHalf,
-                         kPlan = kCodes + kRing * kStage;
+                         kOnesAt = (kCodes + kRing * kStage + 1023) & ~1023, kPlan = kOnesAt + kOnes;
     static constexpr int kPlanRoom = 227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512 < 16384
                                          ? (227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512) / 256 * 256 : 16384;
     static constexpr int kSmem = kPlan + kPlanRoom + 1024;
-    static constexpr uint32_t kCols = NB == 1 ? 256 : 512, kO = 2 * kRows;
+    static constexpr uint32_t kCols = 4 * kRows, kO = 2 * kRows, kSum = 3 * kRows;     // two buffers of scores, outputs, sums
     static_assert(kPlanRoom >= 1024 && kSmem + sizeof(Shared) <= 227 * 1024, "shared memory");
 };
 
@@ -111,12 +114,33 @@ __device__ __forceinline__ uint32_t unpack_two(uint32_t w, uint32_t s, uint32_t 
 }
 __device__ __forceinline__ bool not_finite(uint32_t word) { return (word & 0x7F80u) == 0x7F80u || (word & 0x7F800000u) == 0x7F800000u; }
 
+__device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&r)[4]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+
 // order of fp32 numbers as that of integers, NaN aside
 __device__ __forceinline__ int ordered(float x) {
     const int b = __float_as_int(x);
     return b ^ ((b >> 31) & 0x7fffffff);
 }
 __device__ __forceinline__ float unordered(int b) { return __int_as_float(b ^ ((b >> 31) & 0x7fffffff)); }
+
+// Bit e: query row 16 c + e of the tile's item sees its key `key`.  Out of line: few tiles have keys that not every row sees.
+__device__ __noinline__ uint32_t sees_of(const TreeArgs* a, const Tile* d, int first, int key) {
+    const RowBlock rows = row_block(*a, first);
+    const int pos = d->blk * 16 + key, node = pos - (d->len - d->n_rows);
+    const bool is = (key >> 4) < d->nb && ((d->present >> (key >> 4)) & 1u) && pos < d->len;
+    uint32_t m = 0;
+#pragma unroll 4
+    for (int e = 0; e < 16; ++e) {
+        const int tok = row_of(*a, rows, e).tok;
+        bool s = is && tok < d->n_rows;
+        if (s && node >= 0)
+            s = node < 32 * a->tree_words && ((a->tree[static_cast<size_t>(d->row0 + tok) * a->tree_words + (node >> 5)] >> (node & 31)) & 1u);
+        m |= s ? 1u << e : 0u;
+    }
+    return m;
+}
 
 template <int D, int G, int NB>
 __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_constant__ TreeArgs a) {
@@ -149,7 +173,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
         sh.abort = 0;
         fence_barrier_init();
     }
-    if (tid < 128) sh.spoilt[tid] = 0;
+    if (tid < 256) sh.spoilt[tid >> 7][tid & 127] = 0;
+    for (int i = tid; i < kOnes / 4; i += 32 * kWarps) reinterpret_cast<uint32_t*>(base + L::kOnesAt)[i] = 0x3F803F80u;
+    fence_proxy_async_smem();
     grid_dep_wait();
     // (Tensor memory is taken after the kernel before has ended and before the next may come: no two wait for each other's.)
     if (warp == kScoreWarp) {
@@ -301,16 +327,12 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp < kUnpackWarps + kSoftWarps) {
             // ------------------------------------------------------------------------ softmax, outputs
+            // (Loops over the runs of 16 rows stay loops: unrolled, the code of the roles is more than the instruction caches hold, and
+            // every instruction of a tile came from far away: 11000 clocks a tile of 128 rows.)
             const int group = (warp - kUnpackWarps) >> 2, quarter = warp & 3;
             const int key = quarter * 32 + lane;                                    // of a tile
-            const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-            constexpr int kChunks = NB * 2;                                         // of 16 rows, of this group: group, group + 2, ..
-            float l[kChunks][16];
-#pragma unroll
-            for (int i = 0; i < kChunks; ++i)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) l[i][e] = 0.f;
-            int use = 0, meets = 0;
+            const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+            int use = 0, meets = 0, item = 0;
             bool ok = true;
             auto meet = [&]() {             // the four warps of the group
                 __syncwarp();
@@ -319,140 +341,106 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             };
             for (int n = 0;; ++n) {
                 if (!(ok = mbar_wait_warp(bar(sh.s_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                // the products of the tile before have read P, and O and the sums hold the tiles up to it
+                if (n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done), (n - 1) & 1, a.wait_ns, abort_flag))) break;
                 tc_fence_after_sync();
                 const Tile& d = sh.tiles[n % kDescs];
                 const int n_rows = min(kRows, d.n_rows * a.share - d.rb * kRows);   // query rows of the item
-                const uint32_t scores = tmem + lanes + (n & 1) * kRows;
-                const bool masked = d.masked;
-                const RowBlock rows = row_block(a, d.rb * kRows);
-                const int pos = d.blk * 16 + key, node = pos - (d.len - d.n_rows);
-                const bool is = (key >> 4) < d.nb && ((d.present >> (key >> 4)) & 1u) && pos < d.len;
-                // bit e: row 16 c + e sees this thread's key
-                auto sees = [&](int c) -> uint32_t {
-                    uint32_t m = 0;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int tok = row_of(a, rows, 16 * c + e).tok;
-                        bool s = is && tok < d.n_rows;
-                        if (s && node >= 0)
-                            s = node < 32 * a.tree_words && ((a.tree[static_cast<size_t>(d.row0 + tok) * a.tree_words + (node >> 5)] >> (node & 31)) & 1u);
-                        m |= s ? 1u << e : 0u;
-                    }
-                    return m;
-                };
-                uint32_t seen[kChunks];
-                bool change = d.first;
-                // ---- does a logit pass its reference?
-#pragma unroll
-                for (int i = 0; i < kChunks; ++i) {
-                    const int c = group + 2 * i;
-                    seen[i] = 0xffffu;
-                    if (16 * c >= n_rows) continue;
-                    if (masked) seen[i] = sees(c);
-                    if (d.first) continue;
-                    uint32_t s[16];
-                    tmem_ld_32x16(scores + 16 * c, s);
-                    tmem_ld_wait();
-                    float most = -CUDART_INF_F;
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const float4 r = *reinterpret_cast<const float4*>(&sh.ref[use][16 * c + e]);
-                        const float rr[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) {
-                            const float x = fmaf(__uint_as_float(s[e + f]), a.scale_log2e, -(rr[f] == -CUDART_INF_F ? -1e38f : rr[f]));
-                            most = fmaxf(most, (seen[i] >> (e + f)) & 1u ? x : -CUDART_INF_F);
-                        }
-                    }
-                    change = change || most > kSlack;
+                const uint32_t scores = lanes + (n & 1) * kRows;
+                uint32_t bad = 0;
+                if (d.masked) {        // values that are not finite, of keys that some row may not see
+                    if (!(ok = mbar_wait_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                    bad = sh.odd[n & 1][key];
                 }
-                change = __any_sync(0xffffffffu, change);
-                if (lane == 0) sh.flag[n & 1][group][quarter] = change;
-                if (!(ok = meet())) break;
-                const int4 flags = *reinterpret_cast<const int4*>(sh.flag[n & 1][group]);
-                if (flags.x | flags.y | flags.z | flags.w) {
-                    // ---- new references: the largest logits so far; what is summed is scaled
-#pragma unroll
-                    for (int i = 0; i < kChunks; ++i) {
-                        const int c = group + 2 * i;
-                        if (16 * c >= n_rows) continue;
+                // P of all rows; whether a logit passed its reference
+                auto make_p = [&](auto masked_c) {
+                    constexpr bool masked = decltype(masked_c)::value;
+                    bool change = false;
+#pragma unroll 1
+                    for (int c = group; 16 * c < n_rows; c += 2) {
+                        const uint32_t see = masked ? sees_of(&a, &d, d.rb * kRows + 16 * c, key) : 0u;
                         uint32_t s[16];
                         tmem_ld_32x16(scores + 16 * c, s);
+                        float x[16];
+#pragma unroll
+                        for (int e = 0; e < 16; e += 4) {
+                            const float4 r = *reinterpret_cast<const float4*>(&sh.minus_ref[use][16 * c + e]);
+                            x[e] = r.x, x[e + 1] = r.y, x[e + 2] = r.z, x[e + 3] = r.w;
+                        }
                         tmem_ld_wait();
+                        float most = -CUDART_INF_F;
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
-                            const float x = __uint_as_float(s[e]) * a.scale_log2e;
-                            const int top = __reduce_max_sync(0xffffffffu, ordered((seen[i] >> e) & 1u && x == x ? x : -CUDART_INF_F));
-                            if (lane == e) sh.most[quarter][16 * c + e] = unordered(top);
+                            x[e] = fmaf(__uint_as_float(s[e]), a.scale_log2e, x[e]);
+                            if (masked) x[e] = (see >> e) & 1u ? x[e] : -CUDART_INF_F;
+                            most = fmaxf(most, x[e]);
                         }
-                    }
-                    if (!(ok = meet())) break;
-                    // O holds the tiles up to the one before
-                    if (n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done), (n - 1) & 1, a.wait_ns, abort_flag))) break;
-                    tc_fence_after_sync();
+                        change = change || most > kSlack;
+                        uint32_t p[8];
 #pragma unroll
-                    for (int i = 0; i < kChunks; ++i) {
-                        const int c = group + 2 * i;
-                        if (16 * c >= n_rows) continue;
-                        float alpha = 1.f;          // of row 16 c + lane % 16
-                        {
-                            const int r = 16 * c + (lane & 15);
-                            const float old = d.first ? -CUDART_INF_F : sh.ref[use][r];
-                            const float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])), old);
-                            alpha = now == -CUDART_INF_F ? 1.f : exp2_fast(old - now);
-                            if (lane < 16) sh.ref[use ^ 1][r] = now;     // every warp of the group writes the same
-                        }
-                        uint32_t o[16];
-                        if (!d.first) {
-                            tmem_ld_32x16(tmem + lanes + L::kO + 16 * c, o);
+                        for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(exp2_fast(x[2 * e]), exp2_fast(x[2 * e + 1])));
+                        const uint32_t row = sm + L::kP + (c >> 2) * kHalf + key * 128;
+                        sts128(row + (((2 * c) & 7) ^ (key & 7)) * 16, p[0], p[1], p[2], p[3]);
+                        sts128(row + (((2 * c + 1) & 7) ^ (key & 7)) * 16, p[4], p[5], p[6], p[7]);
+                        if (masked && bad)
+#pragma unroll 1
+                            for (int e = 0; e < 16; ++e)
+                                if ((see >> e) & 1u) atomicOr(&sh.spoilt[item & 1][16 * c + e], bad);
+                    }
+                    return change;
+                };
+                bool again = d.first;
+                while (true) {
+                    if (again) {
+                        // ---- new references: the largest logits so far; what is summed is scaled
+#pragma unroll 1
+                        for (int c = group; 16 * c < n_rows; c += 2) {
+                            const uint32_t see = d.masked ? sees_of(&a, &d, d.rb * kRows + 16 * c, key) : 0xffffu;
+                            uint32_t s[16];
+                            tmem_ld_32x16(scores + 16 * c, s);
                             tmem_ld_wait();
-                        }
+                            int mine = 0;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float f = __shfl_sync(0xffffffffu, alpha, e);
-                            l[i][e] *= f;
-                            if (!d.first) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            for (int e = 0; e < 16; ++e) {
+                                const float x = __uint_as_float(s[e]) * a.scale_log2e;
+                                const int top = __reduce_max_sync(0xffffffffu, ordered((see >> e) & 1u && x == x ? x : -CUDART_INF_F));
+                                if (lane == e) mine = top;
+                            }
+                            if (lane < 16) sh.most[quarter][16 * c + lane] = unordered(mine);
                         }
-                        if (!d.first) tmem_st_32x16(tmem + lanes + L::kO + 16 * c, o);
+                        if (!(ok = meet())) break;
+#pragma unroll 1
+                        for (int c = group; 16 * c < n_rows; c += 2) {
+                            const int r = 16 * c + (lane & 15);
+                            const float old = d.first ? -CUDART_INF_F : -sh.minus_ref[use][r];
+                            float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])), old);
+                            now = fmaxf(now, -kNothing);     // of a row that has seen nothing: below every logit
+                            if (lane < 16) sh.minus_ref[use ^ 1][r] = -now;     // every warp of the group writes the same
+                            if (d.first) continue;
+                            const float alpha = exp2_fast(old - now);
+#pragma unroll 1
+                            for (uint32_t at = L::kO; at <= L::kSum; at += L::kSum - L::kO) {
+                                uint32_t o[16];
+                                tmem_ld_32x16(lanes + at + 16 * c, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * __shfl_sync(0xffffffffu, alpha, e));
+                                tmem_st_32x16(lanes + at + 16 * c, o);
+                            }
+                            tmem_st_wait();
+                        }
+                        __syncwarp();
+                        use ^= 1;
                     }
-                    tmem_st_wait();
-                    __syncwarp();
-                    use ^= 1;
+                    const bool change = __any_sync(0xffffffffu, d.masked ? make_p(std::true_type{}) : make_p(std::false_type{}));
+                    if (again) break;
+                    if (lane == 0) sh.flag[n & 1][group][quarter] = change;
+                    if (!(ok = meet())) break;
+                    const int4 flags = *reinterpret_cast<const int4*>(sh.flag[n & 1][group]);
+                    if (!(flags.x | flags.y | flags.z | flags.w)) break;
+                    again = true;
                 }
-                // ---- P; the product of the tile before has read its own
-                if (n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done), (n - 1) & 1, a.wait_ns, abort_flag))) break;
-                if (masked) {          // values that are not finite, of keys that some row may not see
-                    if (!(ok = mbar_wait_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
-                }
-                const uint32_t bad = masked ? sh.odd[n & 1][key] : 0u;
-#pragma unroll
-                for (int i = 0; i < kChunks; ++i) {
-                    const int c = group + 2 * i;
-                    if (16 * c >= n_rows) continue;
-                    uint32_t s[16], p[8];
-                    tmem_ld_32x16(scores + 16 * c, s);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4) {
-                        const float4 r = *reinterpret_cast<const float4*>(&sh.ref[use][16 * c + e]);
-                        const float rr[4] = {r.x, r.y, r.z, r.w};
-                        float x[4];
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) {
-                            x[f] = exp2_fast(fmaf(__uint_as_float(s[e + f]), a.scale_log2e, rr[f] == -CUDART_INF_F ? 0.f : -rr[f]));
-                            if (masked && !((seen[i] >> (e + f)) & 1u)) x[f] = 0.f;
-                            l[i][e + f] += x[f];
-                        }
-                        p[e / 2] = as_word(__floats2bfloat162_rn(x[0], x[1]));
-                        p[e / 2 + 1] = as_word(__floats2bfloat162_rn(x[2], x[3]));
-                    }
-                    const uint32_t row = sm + L::kP + (c >> 2) * kHalf + key * 128;
-                    sts128(row + (((2 * c) & 7) ^ (key & 7)) * 16, p[0], p[1], p[2], p[3]);
-                    sts128(row + (((2 * c + 1) & 7) ^ (key & 7)) * 16, p[4], p[5], p[6], p[7]);
-                    if (bad)
-                        for (int e = 0; e < 16; ++e)
-                            if ((seen[i] >> e) & 1u) atomicOr(&sh.spoilt[16 * c + e], bad);
-                }
+                if (!ok) break;
                 fence_proxy_async_smem();
                 tc_fence_before_sync();
                 __syncwarp();
@@ -462,52 +450,39 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 }
                 if (!d.last) continue;          // (the CTA's last tile is the last of its part)
                 // ---- end of the item or of the piece
-#pragma unroll
-                for (int i = 0; i < kChunks; ++i) {
-                    const int c = group + 2 * i;
-                    if (16 * c >= n_rows) continue;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float x = l[i][e];
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-                        if (lane == e) sh.most[quarter][16 * c + e] = x;
-                        l[i][e] = 0.f;
-                    }
-                }
-                if (!(ok = meet())) break;
                 if (!(ok = mbar_wait_warp(bar(sh.pv_done), n & 1, a.wait_ns, abort_flag))) break;
                 tc_fence_after_sync();
-                // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j
+                // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j; all lanes of the sums are alike
                 const int at = quarter * 32 + lane, channel = (at & ~31) + 4 * (lane & 7) + (lane >> 3);
                 const bool whole = d.begins && d.ends;
                 float* dst = parts + (d.begins ? slot_floats(kRows, D) : 0);
-#pragma unroll
-                for (int i = 0; i < kChunks; ++i) {
-                    const int c = group + 2 * i;
-                    if (16 * c >= n_rows) continue;
-                    uint32_t o[16];
-                    tmem_ld_32x16(tmem + lanes + L::kO + 16 * c, o);
+                const RowBlock rows = row_block(a, d.rb * kRows);
+#pragma unroll 1
+                for (int r0 = 16 * group; r0 < n_rows; r0 += (r0 & 12) == 12 ? 20 : 4) {
+                    uint32_t o[4], l[4];
+                    tmem_ld_32x4(lanes + L::kO + r0, o);
+                    tmem_ld_32x4(lanes + L::kSum + r0, l);
                     tmem_ld_wait();
-                    if (at >= D) continue;
+                    if (at < D)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int r = 16 * c + e;
-                        const float sum = (sh.most[0][r] + sh.most[1][r]) + (sh.most[2][r] + sh.most[3][r]);
-                        float x = __uint_as_float(o[e]);
-                        if ((sh.spoilt[r] >> (channel / G)) & 1u) x = CUDART_NAN_F;
-                        if (whole) {
-                            const RowOut ro = row_out(a, d.row0, d.n_rows, d.kvh, row_of(a, rows, r), D);
-                            if (ro.o) ro.o[channel] = __float2bfloat16_rn(ro.on && sum != 0.f ? x / sum : 0.f);
-                        } else if (r < n_rows) {
-                            dst[r * D + channel] = x;
-                            if (at == 0) *reinterpret_cast<float2*>(dst + kRows * D + 2 * r) = make_float2(sh.ref[use][r], sum);
+                        for (int e = 0; e < 4; ++e) {
+                            const int r = r0 + e;
+                            const float sum = __uint_as_float(l[e]);
+                            float x = __uint_as_float(o[e]);
+                            if ((sh.spoilt[item & 1][r] >> (channel / G)) & 1u) x = CUDART_NAN_F;
+                            if (whole) {
+                                const RowOut ro = row_out(a, d.row0, d.n_rows, d.kvh, row_of(a, rows, r), D);
+                                if (ro.o) ro.o[channel] = __float2bfloat16_rn(ro.on && sum != 0.f ? x / sum : 0.f);
+                            } else if (r < n_rows) {
+                                dst[r * D + channel] = x;
+                                // (a row that has seen nothing has no weight among its other pieces)
+                                if (at == 0) *reinterpret_cast<float2*>(dst + kRows * D + 2 * r) = make_float2(sum == 0.f ? -CUDART_INF_F : -sh.minus_ref[use][r], sum);
+                            }
                         }
-                    }
                 }
-                if (!(ok = meet())) break;          // all have read sums and spoilt rows
-                for (int r = quarter * 32 + lane; r < kRows; r += 128)
-                    if (((r >> 4) & 1) == group) sh.spoilt[r] = 0;
+                ++item;
+                for (int r = quarter * 32 + lane; r < kRows; r += 128)      // (nobody reads what the item before left any more)
+                    if (((r >> 4) & 1) == group) sh.spoilt[item & 1][r] = 0;
                 tc_fence_before_sync();
                 if (d.final) break;
             }
@@ -608,10 +583,13 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     if (!(ok = mbar_wait(bar(sh.p_full), n & 1, a.wait_ns, abort_flag))) break;
                     tc_fence_after_sync();
                     // (heads of 64: the upper 64 lanes take whatever lies behind the tile, and nobody reads them)
-                    const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf), pd = desc_mn(sm + L::kP, kHalf);
+                    const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf), pd = desc_mn(sm + L::kP, kHalf), ones = desc_mn(sm + L::kOnesAt, 1024);
                     const bool first = sh.tiles[n % kDescs].first, final = sh.tiles[n % kDescs].final;
 #pragma unroll
                     for (int i = 0; i < kKeys / 16; ++i) umma_bf16(tmem + L::kO, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(kRows, true), first && i == 0 ? 0u : 1u);
+                    // the sums of P over the keys: 128 rows of ones in V's place
+#pragma unroll
+                    for (int i = 0; i < kKeys / 16; ++i) umma_bf16(tmem + L::kSum, ones, pd + i * (2048 >> 4), idesc(kRows, true), first && i == 0 ? 0u : 1u);
                     umma_commit(bar(sh.v_free[n & 1]));
                     umma_commit(bar(sh.pv_done));
                     if (final) break;
