@@ -18,7 +18,6 @@
 //
 // Items are cut into equal pieces for the CTAs and joined as in wide_attn_cache (attn_plan.cuh).
 #include <atomic>
-#include <type_traits>
 
 #include "cache.cuh"
 
@@ -41,7 +40,9 @@ constexpr int kUnpackWarps = 8, kSoftWarps = 8;
 constexpr int kLoadWarp = 16, kScoreWarp = 17, kValueWarp = 18, kWarps = 20;   // (whole groups of four warps)
 constexpr float kSlack = 8.f;
 constexpr float kNothing = 1e38f;    // minus the reference of a row that has seen nothing yet: a logit of any size passes it
-constexpr int kOnes = 3 * 1024;      // bytes of ones: two blocks of 64 rows and two groups of 8 keys, each 1024 further on
+// Registers a thread: the launch has 20 warps of 96; eight warps of 72, eight of 136 and four of 56 are less than that together.
+constexpr int kUnpackRegs = 72, kSoftRegs = 136, kOtherRegs = 56;
+static_assert(8 * kUnpackRegs + 8 * kSoftRegs + 4 * kOtherRegs <= 20 * 96, "registers");
 constexpr int kHalf = 16384;        // bytes of [128 keys][64 channels or rows]
 
 struct TreeArgs : AttnArgs {
@@ -57,19 +58,20 @@ struct Tile {                       // what the roles are told of a tile
     int first, last;                // of the item's part in this CTA
     int masked;                     // not all rows see all 128 keys
     int seq, kvh, rb, row0, n_rows, len;
+    int item_rows, rows_a_block;    // query rows of the item; of a whole one
     int begins, ends;               // whether the part has the item's first, last block
     int final;                      // the CTA's last tile
 };
 
 struct alignas(16) Shared {
-    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full, pv_done, meet[2];
+    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full[2], pv_done[2], meet[2];
     uint32_t tmem;
     int abort;
     Cursor start;
     Tile tiles[kDescs];
     alignas(16) float minus_ref[2][128];        // of a row, twice: the one in use and the next
-    float most[4][128];             // of a row, per warp of a group: the largest logit
-    alignas(16) int flag[2][2][4];              // [tile parity][group][warp]: a logit passed its reference
+    float most[4][128];             // of a row, per warp of a group: the largest logit, at the end of an item the sum of P
+    alignas(16) int flag[4][2][4];              // [which block of rows][group][warp]: a logit passed its reference
     uint32_t odd[2][kKeys];         // sub-groups of a new token's values that are not finite (their values are 0 in the tile)
     uint32_t spoilt[2][128];        // rows that see such a sub-group, of this item and the next
 };
@@ -79,12 +81,12 @@ struct Layout {
     static constexpr int kRows = 64 * NB, kNS = D / G, kSB = 16 * D + 128 * kNS, kStage = kTile * kSB, kBlocks = D / 64;
     static constexpr int kTileBytes = kBlocks * kHalf;                 // of unpacked keys, or values
     static constexpr int kRing = D == 128 && NB == 2 && G == 32 ? 2 : kMostRing;     // (no room for three)
-    static constexpr int kQ = 0, kK = kQ + kBlocks * kRows * 128, kV = kK + kTileBytes, kP = kV + 2 * kTileBytes, kCodes = kP + NB * kHalf,
-                         kOnesAt = (kCodes + kRing * kStage + 1023) & ~1023, kPlan = kOnesAt + kOnes;
+    static constexpr int kQ = 0, kK = kQ + kBlocks * kRows * 128, kV = kK + kTileBytes, kP = kV + 2 * kTileBytes, kCodes = kP + 2 * kHalf,
+                         kPlan = kCodes + kRing * kStage;
     static constexpr int kPlanRoom = 227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512 < 16384
                                          ? (227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512) / 256 * 256 : 16384;
     static constexpr int kSmem = kPlan + kPlanRoom + 1024;
-    static constexpr uint32_t kCols = 4 * kRows, kO = 2 * kRows, kSum = 3 * kRows;     // two buffers of scores, outputs, sums
+    static constexpr uint32_t kCols = NB == 1 ? 256 : 512, kO = 2 * kRows;     // two buffers of scores, outputs
     static_assert(kPlanRoom >= 1024 && kSmem + sizeof(Shared) <= 227 * 1024, "shared memory");
 };
 
@@ -118,29 +120,42 @@ __device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&r)[4]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
 }
 
-// order of fp32 numbers as that of integers, NaN aside
-__device__ __forceinline__ int ordered(float x) {
-    const int b = __float_as_int(x);
-    return b ^ ((b >> 31) & 0x7fffffff);
-}
-__device__ __forceinline__ float unordered(int b) { return __int_as_float(b ^ ((b >> 31) & 0x7fffffff)); }
-
-// Bit e: query row 16 c + e of the tile's item sees its key `key`.  Out of line: few tiles have keys that not every row sees.
-__device__ __noinline__ uint32_t sees_of(const TreeArgs* a, const Tile* d, int first, int key) {
-    const RowBlock rows = row_block(*a, first);
-    const int pos = d->blk * 16 + key, node = pos - (d->len - d->n_rows);
-    const bool is = (key >> 4) < d->nb && ((d->present >> (key >> 4)) & 1u) && pos < d->len;
-    uint32_t m = 0;
-#pragma unroll 4
-    for (int e = 0; e < 16; ++e) {
-        const int tok = row_of(*a, rows, e).tok;
-        bool s = is && tok < d->n_rows;
-        if (s && node >= 0)
-            s = node < 32 * a->tree_words && ((a->tree[static_cast<size_t>(d->row0 + tok) * a->tree_words + (node >> 5)] >> (node & 31)) & 1u);
-        m |= s ? 1u << e : 0u;
+// Bit e: query row r0 + e of the tile's item sees the key key0 + lane of the tile.  Lane e gets the bits of row e for the 32 keys, and then
+// all lanes get each row's.  Out of line: few tiles have keys that not every row sees.
+__device__ __noinline__ uint32_t sees_of(const TreeArgs* a, const Tile* d, int r0, int key0) {
+    const int lane = threadIdx.x & 31, key = key0 + lane;
+    const RowBlock rows = row_block(*a, d->rb * d->rows_a_block + r0);
+    const int tok = row_of(*a, rows, lane & 15).tok, node = d->blk * 16 + key0 - (d->len - d->n_rows);   // of lane 0; negative in the prefix
+    uint32_t bits = 0;
+    if (tok < d->n_rows) {
+        const uint32_t* row = a->tree + static_cast<size_t>(d->row0 + tok) * a->tree_words;
+        const int w = node >> 5;           // rounds down
+        const uint32_t lo = w < 0 ? 0xffffffffu : w < a->tree_words ? row[w] : 0u, hi = w + 1 < 0 ? 0xffffffffu : w + 1 < a->tree_words ? row[w + 1] : 0u;
+        bits = __funnelshift_r(lo, hi, node & 31);
     }
-    return m;
+    const bool is = (key >> 4) < d->nb && ((d->present >> (key >> 4)) & 1u) && d->blk * 16 + key < d->len;
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) m |= ((__shfl_sync(0xffffffffu, bits, e) >> lane) & 1u) << e;
+    return is ? m : 0u;
 }
+
+// Joins the 16 values of every lane over the 32 lanes: lanes 2 e and 2 e + 1 get that of value e.  x is used up.
+template <typename Join>
+__device__ __forceinline__ float across_lanes(float (&x)[16], int lane, const Join& join) {
+#pragma unroll
+    for (int half = 8; half > 0; half >>= 1)
+#pragma unroll
+        for (int e = 0; e < half; ++e) {
+            const bool up = lane & (2 * half);
+            const float give = up ? x[e] : x[e + half], keep = up ? x[e + half] : x[e];
+            x[e] = join(keep, __shfl_xor_sync(0xffffffffu, give, 2 * half));
+        }
+    return join(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
+}
+
+template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 template <int D, int G, int NB>
 __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_constant__ TreeArgs a) {
@@ -167,15 +182,14 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             mbar_init(bar(sh.s_full[i]), 1);
             mbar_init(bar(sh.s_free[i]), kSoftWarps);
             mbar_init(bar(sh.meet[i]), 4);
+            mbar_init(bar(sh.p_full[i]), kSoftWarps);
+            mbar_init(bar(sh.pv_done[i]), 1);
         }
-        mbar_init(bar(sh.p_full), kSoftWarps);
-        mbar_init(bar(sh.pv_done), 1);
         sh.abort = 0;
         fence_barrier_init();
     }
     if (tid < 256) sh.spoilt[tid >> 7][tid & 127] = 0;
-    for (int i = tid; i < kOnes / 4; i += 32 * kWarps) reinterpret_cast<uint32_t*>(base + L::kOnesAt)[i] = 0x3F803F80u;
-    fence_proxy_async_smem();
+
     grid_dep_wait();
     // (Tensor memory is taken after the kernel before has ended and before the next may come: no two wait for each other's.)
     if (warp == kScoreWarp) {
@@ -219,6 +233,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
     if (u0 < u1 && sh.start.blk < sh.start.end) {
         if (warp < kUnpackWarps) {
             // ------------------------------------------------------------------------ codes to bf16 tiles
+            registers_down<kUnpackRegs>();
             const int kr = ((lane >> 2) & 1) * 4 + (lane >> 3), kc = lane & 3;     // key (and key + 8), 8-channel piece: no bank twice in a store
             const int g = lane >> 2, t = lane & 3;
             bool ok = true;
@@ -327,147 +342,185 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp < kUnpackWarps + kSoftWarps) {
             // ------------------------------------------------------------------------ softmax, outputs
-            // (Loops over the runs of 16 rows stay loops: unrolled, the code of the roles is more than the instruction caches hold, and
-            // every instruction of a tile came from far away: 11000 clocks a tile of 128 rows.)
+            registers_up<kSoftRegs>();
             const int group = (warp - kUnpackWarps) >> 2, quarter = warp & 3;
             const int key = quarter * 32 + lane;                                    // of a tile
             const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-            int use = 0, meets = 0, item = 0;
+            // Sums of P over this thread's keys.  Of a block of 64 rows a group has the runs of 16 rows `group` and group + 2.
+            unsigned long long l[NB][2][8];
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) l[b][e >> 3][e & 7] = 0;
+            uint32_t refs = 0;               // bit b: which of the two references block b uses
+            int meets = 0, item = 0, uses1 = 0;     // uses1: of the second buffer of P where the blocks have one each
             bool ok = true;
-            auto meet = [&]() {             // the four warps of the group
+            auto meet = [&]() {              // the four warps of the group
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sh.meet[group]));
                 return mbar_wait_warp(bar(sh.meet[group]), meets++ & 1, a.wait_ns, abort_flag);
             };
-            for (int n = 0;; ++n) {
+            for (int n = 0; ok; ++n) {
                 if (!(ok = mbar_wait_warp(bar(sh.s_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
-                // the products of the tile before have read P, and O and the sums hold the tiles up to it
-                if (n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done), (n - 1) & 1, a.wait_ns, abort_flag))) break;
                 tc_fence_after_sync();
                 const Tile& d = sh.tiles[n % kDescs];
-                const int n_rows = min(kRows, d.n_rows * a.share - d.rb * kRows);   // query rows of the item
+                const int n_rows = d.item_rows;
+                const bool masked = d.masked, first = d.first, last = d.last, final = d.final;
                 const uint32_t scores = lanes + (n & 1) * kRows;
                 uint32_t bad = 0;
-                if (d.masked) {        // values that are not finite, of keys that some row may not see
+                if (masked) {          // values that are not finite, of keys that some row may not see
                     if (!(ok = mbar_wait_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
                     bad = sh.odd[n & 1][key];
                 }
-                // P of all rows; whether a logit passed its reference
-                auto make_p = [&](auto masked_c) {
-                    constexpr bool masked = decltype(masked_c)::value;
-                    bool change = false;
-#pragma unroll 1
-                    for (int c = group; 16 * c < n_rows; c += 2) {
-                        const uint32_t see = masked ? sees_of(&a, &d, d.rb * kRows + 16 * c, key) : 0u;
-                        uint32_t s[16];
-                        tmem_ld_32x16(scores + 16 * c, s);
-                        float x[16];
 #pragma unroll
-                        for (int e = 0; e < 16; e += 4) {
-                            const float4 r = *reinterpret_cast<const float4*>(&sh.minus_ref[use][16 * c + e]);
-                            x[e] = r.x, x[e + 1] = r.y, x[e + 2] = r.z, x[e + 3] = r.w;
-                        }
-                        tmem_ld_wait();
-                        float most = -CUDART_INF_F;
+                for (int b = 0; b < NB; ++b) {
+                    if (64 * b >= n_rows) break;
+                    const int c0 = 4 * b + group, pb = NB == 1 ? n & 1 : b;
+                    // the product that read this buffer of P before is done
+                    const int used = NB == 1 ? n >> 1 : b == 0 ? n : uses1;
+                    if (used > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[pb]), (used - 1) & 1, a.wait_ns, abort_flag))) break;
+                    bool again = first;
+                    float x[2][16];
+                    while (true) {
+                        if (again) {
+                            // ---- new references: the largest logits so far; what is summed is scaled
+                            if (NB == 1 && n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[pb ^ 1]), (((n + 1) >> 1) - 1) & 1, a.wait_ns, abort_flag))) break;
+                            tc_fence_after_sync();
+                            const float* old_ref = sh.minus_ref[(refs >> b) & 1];
+                            float* new_ref = sh.minus_ref[((refs >> b) & 1) ^ 1];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            x[e] = fmaf(__uint_as_float(s[e]), a.scale_log2e, x[e]);
-                            if (masked) x[e] = (see >> e) & 1u ? x[e] : -CUDART_INF_F;
-                            most = fmaxf(most, x[e]);
-                        }
-                        change = change || most > kSlack;
-                        uint32_t p[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(exp2_fast(x[2 * e]), exp2_fast(x[2 * e + 1])));
-                        const uint32_t row = sm + L::kP + (c >> 2) * kHalf + key * 128;
-                        sts128(row + (((2 * c) & 7) ^ (key & 7)) * 16, p[0], p[1], p[2], p[3]);
-                        sts128(row + (((2 * c + 1) & 7) ^ (key & 7)) * 16, p[4], p[5], p[6], p[7]);
-                        if (masked && bad)
-#pragma unroll 1
-                            for (int e = 0; e < 16; ++e)
-                                if ((see >> e) & 1u) atomicOr(&sh.spoilt[item & 1][16 * c + e], bad);
-                    }
-                    return change;
-                };
-                bool again = d.first;
-                while (true) {
-                    if (again) {
-                        // ---- new references: the largest logits so far; what is summed is scaled
-#pragma unroll 1
-                        for (int c = group; 16 * c < n_rows; c += 2) {
-                            const uint32_t see = d.masked ? sees_of(&a, &d, d.rb * kRows + 16 * c, key) : 0xffffu;
-                            uint32_t s[16];
-                            tmem_ld_32x16(scores + 16 * c, s);
-                            tmem_ld_wait();
-                            int mine = 0;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const float x = __uint_as_float(s[e]) * a.scale_log2e;
-                                const int top = __reduce_max_sync(0xffffffffu, ordered((see >> e) & 1u && x == x ? x : -CUDART_INF_F));
-                                if (lane == e) mine = top;
-                            }
-                            if (lane < 16) sh.most[quarter][16 * c + lane] = unordered(mine);
-                        }
-                        if (!(ok = meet())) break;
-#pragma unroll 1
-                        for (int c = group; 16 * c < n_rows; c += 2) {
-                            const int r = 16 * c + (lane & 15);
-                            const float old = d.first ? -CUDART_INF_F : -sh.minus_ref[use][r];
-                            float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])), old);
-                            now = fmaxf(now, -kNothing);     // of a row that has seen nothing: below every logit
-                            if (lane < 16) sh.minus_ref[use ^ 1][r] = -now;     // every warp of the group writes the same
-                            if (d.first) continue;
-                            const float alpha = exp2_fast(old - now);
-#pragma unroll 1
-                            for (uint32_t at = L::kO; at <= L::kSum; at += L::kSum - L::kO) {
-                                uint32_t o[16];
-                                tmem_ld_32x16(lanes + at + 16 * c, o);
+                            for (int i = 0; i < 2; ++i) {
+                                const int c = c0 + 2 * i;
+                                const uint32_t see = masked ? sees_of(&a, &d, 16 * c, quarter * 32) : 0xffffu;
+                                uint32_t s[16];
+                                tmem_ld_32x16(scores + 16 * c, s);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * __shfl_sync(0xffffffffu, alpha, e));
-                                tmem_st_32x16(lanes + at + 16 * c, o);
+                                for (int e = 0; e < 16; ++e) x[i][e] = (see >> e) & 1u ? __uint_as_float(s[e]) * a.scale_log2e : -CUDART_INF_F;
+                                const float top = across_lanes(x[i], lane, [](float u, float v) { return fmaxf(u, v); });
+                                if (!(lane & 1)) sh.most[quarter][16 * c + (lane >> 1)] = top;
+                            }
+                            if (!(ok = meet())) break;
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const int c = c0 + 2 * i, r = 16 * c + (lane & 15);
+                                const float old = first ? -CUDART_INF_F : -old_ref[r];
+                                float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])), old);
+                                now = fmaxf(now, -kNothing);              // of a row that has seen nothing: below every logit
+                                if (lane < 16) new_ref[r] = -now;         // (every warp of the group writes the same)
+                                if (first) continue;
+                                const float alpha = exp2_fast(old - now);
+                                uint32_t o[16];
+                                tmem_ld_32x16(lanes + L::kO + 16 * c, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int e = 0; e < 16; e += 2) {
+                                    const float f0 = __shfl_sync(0xffffffffu, alpha, e), f1 = __shfl_sync(0xffffffffu, alpha, e + 1);
+                                    o[e] = __float_as_uint(__uint_as_float(o[e]) * f0);
+                                    o[e + 1] = __float_as_uint(__uint_as_float(o[e + 1]) * f1);
+                                    l[b][i][e / 2] = mul2(l[b][i][e / 2], pair(f0, f1));
+                                }
+                                tmem_st_32x16(lanes + L::kO + 16 * c, o);
                             }
                             tmem_st_wait();
+                            __syncwarp();
+                            refs ^= 1u << b;
                         }
-                        __syncwarp();
-                        use ^= 1;
+                        // ---- P, and whether a logit passed its reference
+                        const float* ref = sh.minus_ref[(refs >> b) & 1];
+                        uint32_t s[2][16];
+                        tmem_ld_32x16(scores + 16 * c0, s[0]);
+                        tmem_ld_32x16(scores + 16 * c0 + 32, s[1]);
+                        float most[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int c = c0 + 2 * i;
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) {
+                                const float4 r = *reinterpret_cast<const float4*>(ref + 16 * c + e);
+                                const unsigned long long scale2 = pair(a.scale_log2e, a.scale_log2e);
+                                unpair(fma2(pair(__uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1])), scale2, pair(r.x, r.y)), x[i][e], x[i][e + 1]);
+                                unpair(fma2(pair(__uint_as_float(s[i][e + 2]), __uint_as_float(s[i][e + 3])), scale2, pair(r.z, r.w)), x[i][e + 2], x[i][e + 3]);
+                            }
+                            if (masked) {
+                                const uint32_t see = sees_of(&a, &d, 16 * c, quarter * 32);
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) x[i][e] = (see >> e) & 1u ? x[i][e] : -CUDART_INF_F;
+                                if (bad)
+#pragma unroll 1
+                                    for (int e = 0; e < 16; ++e)
+                                        if ((see >> e) & 1u) atomicOr(&sh.spoilt[item & 1][16 * c + e], bad);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) most[e & 3] = fmaxf(most[e & 3], x[i][e]);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) x[i][e] = exp2_fast(x[i][e]);
+                            uint32_t p[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(x[i][2 * e], x[i][2 * e + 1]));
+                            const uint32_t row = sm + L::kP + pb * kHalf + key * 128;
+                            const int piece = 2 * (c & 3);
+                            sts128(row + ((piece ^ (key & 7)) << 4), p[0], p[1], p[2], p[3]);
+                            sts128(row + (((piece + 1) ^ (key & 7)) << 4), p[4], p[5], p[6], p[7]);
+                        }
+                        if (again) break;
+                        const bool change = __any_sync(0xffffffffu, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) > kSlack);
+                        int* flag = sh.flag[(n * NB + b) & 3][group];
+                        if (lane == 0) flag[quarter] = change;
+                        if (!(ok = meet())) break;
+                        const int4 flags = *reinterpret_cast<const int4*>(flag);
+                        if (!(flags.x | flags.y | flags.z | flags.w)) break;
+                        again = true;
                     }
-                    const bool change = __any_sync(0xffffffffu, d.masked ? make_p(std::true_type{}) : make_p(std::false_type{}));
-                    if (again) break;
-                    if (lane == 0) sh.flag[n & 1][group][quarter] = change;
-                    if (!(ok = meet())) break;
-                    const int4 flags = *reinterpret_cast<const int4*>(sh.flag[n & 1][group]);
-                    if (!(flags.x | flags.y | flags.z | flags.w)) break;
-                    again = true;
+                    if (!ok) break;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) l[b][i][e] = add2(l[b][i][e], pair(x[i][2 * e], x[i][2 * e + 1]));
+                    fence_proxy_async_smem();
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(sh.p_full[pb]));
+                    if (b == 1) ++uses1;
                 }
                 if (!ok) break;
-                fence_proxy_async_smem();
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(bar(sh.s_free[n & 1]));
-                    mbar_arrive(bar(sh.p_full));
-                }
-                if (!d.last) continue;          // (the CTA's last tile is the last of its part)
+                if (lane == 0) mbar_arrive(bar(sh.s_free[n & 1]));
+                if (!last) continue;          // (the CTA's last tile is the last of its part)
                 // ---- end of the item or of the piece
-                if (!(ok = mbar_wait_warp(bar(sh.pv_done), n & 1, a.wait_ns, abort_flag))) break;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float x[16];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            unpair(l[b][i][e], x[2 * e], x[2 * e + 1]);
+                            l[b][i][e] = 0;
+                        }
+                        const float sum = across_lanes(x, lane, [](float u, float v) { return u + v; });
+                        if (!(lane & 1)) sh.most[quarter][16 * (4 * b + group + 2 * i) + (lane >> 1)] = sum;
+                    }
+                if (!(ok = meet())) break;
+                const int used0 = NB == 1 ? (n + 2) >> 1 : n + 1, used1 = NB == 1 ? (n + 1) >> 1 : uses1;
+                if (!(ok = mbar_wait_warp(bar(sh.pv_done[0]), (used0 - 1) & 1, a.wait_ns, abort_flag))) break;
+                if (used1 > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[1]), (used1 - 1) & 1, a.wait_ns, abort_flag))) break;
                 tc_fence_after_sync();
-                // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j; all lanes of the sums are alike
+                // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j
                 const int at = quarter * 32 + lane, channel = (at & ~31) + 4 * (lane & 7) + (lane >> 3);
                 const bool whole = d.begins && d.ends;
                 float* dst = parts + (d.begins ? slot_floats(kRows, D) : 0);
                 const RowBlock rows = row_block(a, d.rb * kRows);
 #pragma unroll 1
                 for (int r0 = 16 * group; r0 < n_rows; r0 += (r0 & 12) == 12 ? 20 : 4) {
-                    uint32_t o[4], l[4];
+                    uint32_t o[4];
                     tmem_ld_32x4(lanes + L::kO + r0, o);
-                    tmem_ld_32x4(lanes + L::kSum + r0, l);
                     tmem_ld_wait();
                     if (at < D)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int r = r0 + e;
-                            const float sum = __uint_as_float(l[e]);
+                            const float sum = (sh.most[0][r] + sh.most[1][r]) + (sh.most[2][r] + sh.most[3][r]);
                             float x = __uint_as_float(o[e]);
                             if ((sh.spoilt[item & 1][r] >> (channel / G)) & 1u) x = CUDART_NAN_F;
                             if (whole) {
@@ -476,7 +529,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                             } else if (r < n_rows) {
                                 dst[r * D + channel] = x;
                                 // (a row that has seen nothing has no weight among its other pieces)
-                                if (at == 0) *reinterpret_cast<float2*>(dst + kRows * D + 2 * r) = make_float2(sum == 0.f ? -CUDART_INF_F : -sh.minus_ref[use][r], sum);
+                                if (at == 0)
+                                    *reinterpret_cast<float2*>(dst + kRows * D + 2 * r) = make_float2(sum == 0.f ? -CUDART_INF_F : -sh.minus_ref[(refs >> (r >> 6)) & 1][r], sum);
                             }
                         }
                 }
@@ -484,11 +538,13 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 for (int r = quarter * 32 + lane; r < kRows; r += 128)      // (nobody reads what the item before left any more)
                     if (((r >> 4) & 1) == group) sh.spoilt[item & 1][r] = 0;
                 tc_fence_before_sync();
-                if (d.final) break;
+                if (!(ok = meet())) break;       // (all have read the sums)
+                if (final) break;
             }
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp == kLoadWarp) {
             // ------------------------------------------------------------------------ items, codes
+            registers_down<kOtherRegs>();
             Cursor k = sh.start;
             const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
             bool ok = true, first = true;
@@ -527,6 +583,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     d.blk = k.blk, d.nb = nb, d.present = present, d.first = first, d.last = last;
                     d.masked = present != (1u << kTile) - 1u || (k.blk + nb) * 16 > info.z - info.y;
                     d.seq = k.seq, d.kvh = k.kvh, d.rb = k.rb, d.row0 = info.x, d.n_rows = info.y, d.len = info.z;
+                    d.item_rows = min(kRows, info.y * a.share - k.rb * kRows), d.rows_a_block = kRows;
                     d.begins = begins, d.ends = ends, d.final = final;
                     mbar_arrive_expect_tx(bar(sh.ring_full[st]), __popc(present) * kSB);
                 }
@@ -557,6 +614,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp == kScoreWarp) {
             // ------------------------------------------------------------------------ S^T = K Q^T
+            registers_down<kOtherRegs>();
             if (lane == 0) {
                 bool ok = true;
                 for (int n = 0;; ++n) {
@@ -564,9 +622,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     if (n >= 2 && !(ok = mbar_wait(bar(sh.s_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                     tc_fence_after_sync();
                     const uint64_t kd = umma_desc_sw128(sm + L::kK), qd = umma_desc_sw128(sm + L::kQ);
+                    const uint32_t shape = NB == 2 && sh.tiles[n % kDescs].item_rows <= 64 ? idesc(64, false) : idesc(kRows, false);
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i)
-                        umma_bf16(tmem + (n & 1) * kRows, kd + (i / 4) * (kHalf >> 4) + 2 * (i % 4), qd + (i / 4) * (kRows * 128 >> 4) + 2 * (i % 4), idesc(kRows, false),
+                        umma_bf16(tmem + (n & 1) * kRows, kd + (i / 4) * (kHalf >> 4) + 2 * (i % 4), qd + (i / 4) * (kRows * 128 >> 4) + 2 * (i % 4), shape,
                                   i > 0 ? 1u : 0u);
                     umma_commit(bar(sh.k_free));
                     umma_commit(bar(sh.s_full[n & 1]));
@@ -576,28 +635,40 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             }
         } else if (warp == kValueWarp) {
             // ------------------------------------------------------------------------ O^T += V^T P^T
+            registers_down<kOtherRegs>();
             if (lane == 0) {
                 bool ok = true;
-                for (int n = 0;; ++n) {
+                int uses1 = 0;
+                for (int n = 0; ok; ++n) {
                     if (!(ok = mbar_wait(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
-                    if (!(ok = mbar_wait(bar(sh.p_full), n & 1, a.wait_ns, abort_flag))) break;
-                    tc_fence_after_sync();
                     // (heads of 64: the upper 64 lanes take whatever lies behind the tile, and nobody reads them)
-                    const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf), pd = desc_mn(sm + L::kP, kHalf), ones = desc_mn(sm + L::kOnesAt, 1024);
-                    const bool first = sh.tiles[n % kDescs].first, final = sh.tiles[n % kDescs].final;
+                    const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf);
+                    const Tile& d = sh.tiles[n % kDescs];
+                    const bool first = d.first, final = d.final;
+                    const int blocks = (d.item_rows + 63) >> 6;
+                    for (int b = 0; b < blocks; ++b) {
+                        const int pb = NB == 1 ? n & 1 : b;
+                        if (!(ok = mbar_wait(bar(sh.p_full[pb]), (NB == 1 ? n >> 1 : b == 0 ? n : uses1) & 1, a.wait_ns, abort_flag))) break;
+                        if (b == 1) ++uses1;
+                        tc_fence_after_sync();
+                        const uint64_t pd = desc_mn(sm + L::kP + pb * kHalf, kHalf);
 #pragma unroll
-                    for (int i = 0; i < kKeys / 16; ++i) umma_bf16(tmem + L::kO, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(kRows, true), first && i == 0 ? 0u : 1u);
-                    // the sums of P over the keys: 128 rows of ones in V's place
-#pragma unroll
-                    for (int i = 0; i < kKeys / 16; ++i) umma_bf16(tmem + L::kSum, ones, pd + i * (2048 >> 4), idesc(kRows, true), first && i == 0 ? 0u : 1u);
-                    umma_commit(bar(sh.v_free[n & 1]));
-                    umma_commit(bar(sh.pv_done));
+                        for (int i = 0; i < kKeys / 16; ++i)
+                            umma_bf16(tmem + L::kO + 64 * b, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(64, true), first && i == 0 ? 0u : 1u);
+                        if (b + 1 == blocks) umma_commit(bar(sh.v_free[n & 1]));
+                        umma_commit(bar(sh.pv_done[pb]));
+                    }
                     if (final) break;
                 }
                 if (!ok) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
             }
+        } else {
+            registers_down<kOtherRegs>();
         }
+        // what follows is compiled for all warps alike
         __syncwarp();
+        if (warp < kUnpackWarps || warp >= kLoadWarp) registers_up<96>();
+        else registers_down<96>();
     }
     if (warp == kLoadWarp && lane == 0) {
         if (!(open & 1)) meta[0] = 0;
