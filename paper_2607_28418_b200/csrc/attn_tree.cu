@@ -37,12 +37,10 @@ constexpr int kKeys = 16 * kTile;
 constexpr int kMostRing = 3;        // tiles of codes on their way
 constexpr int kDescs = 8;           // tiles that are known: the ring's, and at most three behind it whose softmax is not done
 constexpr int kUnpackWarps = 8, kSoftWarps = 8;
-constexpr int kLoadWarp = 16, kScoreWarp = 17, kValueWarp = 18, kWarps = 20;   // (whole groups of four warps)
+constexpr int kLoadWarp = 16, kScoreWarp = 17, kValueWarp = 18, kWarps = 19;
 constexpr float kSlack = 8.f;
+constexpr int kOnes = 3 * 1024;      // bytes of ones: two blocks of 64 rows and two groups of 8 keys, each 1024 further on
 constexpr float kNothing = 1e38f;    // minus the reference of a row that has seen nothing yet: a logit of any size passes it
-// Registers a thread: the launch has 20 warps of 96; eight warps of 72, eight of 136 and four of 56 are less than that together.
-constexpr int kUnpackRegs = 72, kSoftRegs = 136, kOtherRegs = 56;
-static_assert(8 * kUnpackRegs + 8 * kSoftRegs + 4 * kOtherRegs <= 20 * 96, "registers");
 constexpr int kHalf = 16384;        // bytes of [128 keys][64 channels or rows]
 
 struct TreeArgs : AttnArgs {
@@ -70,7 +68,7 @@ struct alignas(16) Shared {
     Cursor start;
     Tile tiles[kDescs];
     alignas(16) float minus_ref[2][128];        // of a row, twice: the one in use and the next
-    float most[4][128];             // of a row, per warp of a group: the largest logit, at the end of an item the sum of P
+    float most[4][128];             // of a row, per warp of a group: the largest logit
     alignas(16) int flag[4][2][4];              // [which block of rows][group][warp]: a logit passed its reference
     uint32_t odd[2][kKeys];         // sub-groups of a new token's values that are not finite (their values are 0 in the tile)
     uint32_t spoilt[2][128];        // rows that see such a sub-group, of this item and the next
@@ -82,11 +80,11 @@ struct Layout {
     static constexpr int kTileBytes = kBlocks * kHalf;                 // of unpacked keys, or values
     static constexpr int kRing = D == 128 && NB == 2 && G == 32 ? 2 : kMostRing;     // (no room for three)
     static constexpr int kQ = 0, kK = kQ + kBlocks * kRows * 128, kV = kK + kTileBytes, kP = kV + 2 * kTileBytes, kCodes = kP + 2 * kHalf,
-                         kPlan = kCodes + kRing * kStage;
+                         kOnesAt = (kCodes + kRing * kStage + 1023) & ~1023, kPlan = kOnesAt + kOnes;
     static constexpr int kPlanRoom = 227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512 < 16384
                                          ? (227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512) / 256 * 256 : 16384;
     static constexpr int kSmem = kPlan + kPlanRoom + 1024;
-    static constexpr uint32_t kCols = NB == 1 ? 256 : 512, kO = 2 * kRows;     // two buffers of scores, outputs
+    static constexpr uint32_t kCols = 4 * kRows, kO = 2 * kRows, kSum = 3 * kRows;     // two buffers of scores, outputs, sums of P
     static_assert(kPlanRoom >= 1024 && kSmem + sizeof(Shared) <= 227 * 1024, "shared memory");
 };
 
@@ -106,6 +104,13 @@ __device__ __forceinline__ void store_transposed(uint32_t addr, uint32_t a, uint
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
+
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.u32 [%0], %1;" ::"r"(a), "r"(v) : "memory"); }
 
 __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
 __device__ __forceinline__ uint32_t as_word(__nv_bfloat162 b) { return *reinterpret_cast<const uint32_t*>(&b); }
@@ -140,22 +145,18 @@ __device__ __noinline__ uint32_t sees_of(const TreeArgs* a, const Tile* d, int r
     return is ? m : 0u;
 }
 
-// Joins the 16 values of every lane over the 32 lanes: lanes 2 e and 2 e + 1 get that of value e.  x is used up.
-template <typename Join>
-__device__ __forceinline__ float across_lanes(float (&x)[16], int lane, const Join& join) {
+// The largest of each of the 16 values over the 32 lanes: lanes 2 e and 2 e + 1 get that of value e.  x is used up.
+__device__ __forceinline__ float largest_across_lanes(float (&x)[16], int lane) {
 #pragma unroll
     for (int half = 8; half > 0; half >>= 1)
 #pragma unroll
         for (int e = 0; e < half; ++e) {
             const bool up = lane & (2 * half);
             const float give = up ? x[e] : x[e + half], keep = up ? x[e + half] : x[e];
-            x[e] = join(keep, __shfl_xor_sync(0xffffffffu, give, 2 * half));
+            x[e] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, 2 * half));
         }
-    return join(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
+    return fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
 }
-
-template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 template <int D, int G, int NB>
 __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_constant__ TreeArgs a) {
@@ -189,6 +190,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
         fence_barrier_init();
     }
     if (tid < 256) sh.spoilt[tid >> 7][tid & 127] = 0;
+    for (int i = tid; i < kOnes / 4; i += 32 * kWarps) reinterpret_cast<uint32_t*>(base + L::kOnesAt)[i] = 0x3F803F80u;
+    fence_proxy_async_smem();
 
     grid_dep_wait();
     // (Tensor memory is taken after the kernel before has ended and before the next may come: no two wait for each other's.)
@@ -233,19 +236,18 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
     if (u0 < u1 && sh.start.blk < sh.start.end) {
         if (warp < kUnpackWarps) {
             // ------------------------------------------------------------------------ codes to bf16 tiles
-            registers_down<kUnpackRegs>();
             const int kr = ((lane >> 2) & 1) * 4 + (lane >> 3), kc = lane & 3;     // key (and key + 8), 8-channel piece: no bank twice in a store
-            const int g = lane >> 2, t = lane & 3;
+            const int t = lane & 3;
             bool ok = true;
             for (int n = 0;; ++n) {
                 const int st = n % kRing;
-                if (!(ok = mbar_wait_warp(bar(sh.ring_full[st]), (n / kRing) & 1, a.wait_ns, abort_flag))) break;
+                if (!(ok = mbar_wait_asleep_warp(bar(sh.ring_full[st]), (n / kRing) & 1, a.wait_ns, abort_flag))) break;
                 const Tile& d = sh.tiles[n % kDescs];
                 const bool here = warp < d.nb && ((d.present >> warp) & 1u);
                 const int key0 = (d.blk + warp) * 16;                               // of this warp's block
                 const uint32_t codes = sm + L::kCodes + st * L::kStage + warp * kSB, words = codes + 16 * D;
                 // the scores of the tile before have been made: K, and Q at the end of an item, may change
-                if (n > 0 && !(ok = mbar_wait_warp(bar(sh.k_free), (n - 1) & 1, a.wait_ns, abort_flag))) break;
+                if (n > 0 && !(ok = mbar_wait_asleep_warp(bar(sh.k_free), (n - 1) & 1, a.wait_ns, abort_flag))) break;
                 if (d.first) {
                     const RowBlock rows = row_block(a, d.rb * kRows);
                     constexpr int kChunks = kRows * D / 8;                          // of 16 bytes
@@ -260,27 +262,19 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     }
                 }
                 if (here) {
-                    uint32_t s0[kNS], s1[kNS];
-                    lds_words<kNS>(words + kr * kNS * 4, s0);
-                    lds_words<kNS>(words + (kr + 8) * kNS * 4, s1);
-                    uint32_t m0[kNS], m1[kNS];
-#pragma unroll
-                    for (int i = 0; i < kNS; ++i) {
-                        m0[i] = __byte_perm(s0[i], 0, 0x3232), s0[i] = __byte_perm(s0[i], 0, 0x1010);
-                        m1[i] = __byte_perm(s1[i], 0, 0x3232), s1[i] = __byte_perm(s1[i], 0, 0x1010);
-                    }
                     const uint32_t row = sm + L::kK + (warp * 16 + kr) * 128;
-#pragma unroll
+#pragma unroll 1
                     for (int c = 0; c < D / 64; ++c) {
                         const uint4 v = lds128(codes + c * 512 + (kr * 4 + kc) * 16);
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {                               // channels 64 c + 32 h + 8 kc ..
                             const int i = (64 * c + 32 * h) / G;
+                            const uint32_t w0 = lds32(words + (kr * kNS + i) * 4), w1 = lds32(words + ((kr + 8) * kNS + i) * 4);
+                            const uint32_t s0 = __byte_perm(w0, 0, 0x1010), m0 = __byte_perm(w0, 0, 0x3232), s1 = __byte_perm(w1, 0, 0x1010), m1 = __byte_perm(w1, 0, 0x3232);
                             const uint32_t x = h ? v.z : v.x, y = h ? v.w : v.y;
                             const uint32_t at = row + c * kHalf + (((4 * h + kc) ^ kr) << 4);
-                            sts128(at, unpack_two(x, s0[i], m0[i]), unpack_two(x >> 4, s0[i], m0[i]), unpack_two(y, s0[i], m0[i]), unpack_two(y >> 4, s0[i], m0[i]));
-                            sts128(at + 8 * 128, unpack_two(x >> 8, s1[i], m1[i]), unpack_two(x >> 12, s1[i], m1[i]), unpack_two(y >> 8, s1[i], m1[i]),
-                                   unpack_two(y >> 12, s1[i], m1[i]));
+                            sts128(at, unpack_two(x, s0, m0), unpack_two(x >> 4, s0, m0), unpack_two(y, s0, m0), unpack_two(y >> 4, s0, m0));
+                            sts128(at + 8 * 128, unpack_two(x >> 8, s1, m1), unpack_two(x >> 12, s1, m1), unpack_two(y >> 8, s1, m1), unpack_two(y >> 12, s1, m1));
                         }
                     }
                 }
@@ -288,45 +282,40 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sh.k_full));
                 // ---- values
-                if (n >= 2 && !(ok = mbar_wait_warp(bar(sh.v_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
+                if (n >= 2 && !(ok = mbar_wait_asleep_warp(bar(sh.v_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                 {
-                    uint32_t p[4][kNS];                                             // tokens 2t, 2t + 1, 2t + 8, 2t + 9
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 2 * t + 8 * (e >> 1) + (e & 1);
-                        lds_words<kNS>(words + 64 * kNS + r * kNS * 4, p[e]);
-                        if (d.masked) {
-                            const bool is = here && key0 + r < d.len, young = key0 + r >= d.len - d.n_rows;
-                            uint32_t bad = 0;
-#pragma unroll
-                            for (int i = 0; i < kNS; ++i) {
-                                if (!is) p[e][i] = 0;
-                                if (young && not_finite(p[e][i])) {
-                                    p[e][i] = 0;
-                                    bad |= 1u << i;
-                                }
-                            }
-                            if (g == 0) sh.odd[n & 1][warp * 16 + r] = bad;
+                    // In a tile whose new tokens not every row sees, and behind the end: values of keys that are not there count as zeros, and
+                    // those of new tokens that are not finite are noted instead.
+                    if (d.masked) {
+#pragma unroll 1
+                        for (int x = lane; x < 16 * kNS; x += 32) {
+                            const int r = x / kNS;
+                            const uint32_t at = words + 64 * kNS + 4 * x, w = lds32(at);
+                            const bool is = here && key0 + r < d.len, bad = is && key0 + r >= d.len - d.n_rows && not_finite(w);
+                            if (!is || bad) sts32(at, 0u);
+                            const uint32_t bits = __ballot_sync(__activemask(), bad);
+                            if (x % kNS == 0) sh.odd[n & 1][warp * 16 + r] = (bits >> (lane & ~(kNS - 1))) & ((1u << kNS) - 1u);
                         }
-                    }
-                    uint32_t s0[kNS], m0[kNS], s1[kNS], m1[kNS];
-#pragma unroll
-                    for (int i = 0; i < kNS; ++i) {
-                        s0[i] = __byte_perm(p[0][i], p[1][i], 0x5410), m0[i] = __byte_perm(p[0][i], p[1][i], 0x7632);
-                        s1[i] = __byte_perm(p[2][i], p[3][i], 0x5410), m1[i] = __byte_perm(p[2][i], p[3][i], 0x7632);
+                        __syncwarp();
                     }
                     const int token = (lane & 7) + 8 * (lane >> 4);                 // whose row this lane's address is, and which nibble
-                    const uint32_t row = sm + L::kV + (n & 1) * L::kTileBytes + (warp * 16 + token) * 128;
-#pragma unroll
+                    const uint32_t row = sm + L::kV + (n & 1) * L::kTileBytes + (warp * 16 + token) * 128, params = words + 64 * kNS + 2 * t * kNS * 4;
+#pragma unroll 1
                     for (int c = 0; c < D / 64; ++c) {
                         const uint4 v = lds128(codes + 8 * D + c * 512 + lane * 16);
+                        uint32_t s0 = 0, m0 = 0, s1 = 0, m1 = 0;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {                               // channels 64 c + 32 (e / 2) + 4 g + 2 (e % 2) ..
-                            const int i = (64 * c + 32 * (e >> 1)) / G;
+                            if (e == 0 || (e == 2 && G == 32)) {                    // tokens 2t, 2t + 1, 2t + 8, 2t + 9
+                                const uint32_t at = params + (64 * c + 32 * (e >> 1)) / G * 4;
+                                const uint32_t p0 = lds32(at), p1 = lds32(at + kNS * 4), p2 = lds32(at + 8 * kNS * 4), p3 = lds32(at + 9 * kNS * 4);
+                                s0 = __byte_perm(p0, p1, 0x5410), m0 = __byte_perm(p0, p1, 0x7632);
+                                s1 = __byte_perm(p2, p3, 0x5410), m1 = __byte_perm(p2, p3, 0x7632);
+                            }
                             const uint32_t x = e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
                             const int piece = (e >> 1) * 4 + 2 * (e & 1) + ((lane >> 3) & 1);
-                            store_transposed(row + c * kHalf + ((piece ^ (token & 7)) << 4), unpack_two(x, s0[i], m0[i]), unpack_two(x >> 4, s0[i], m0[i]),
-                                             unpack_two(x >> 8, s1[i], m1[i]), unpack_two(x >> 12, s1[i], m1[i]));
+                            store_transposed(row + c * kHalf + ((piece ^ (token & 7)) << 4), unpack_two(x, s0, m0), unpack_two(x >> 4, s0, m0), unpack_two(x >> 8, s1, m1),
+                                             unpack_two(x >> 12, s1, m1));
                         }
                     }
                 }
@@ -342,18 +331,13 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp < kUnpackWarps + kSoftWarps) {
             // ------------------------------------------------------------------------ softmax, outputs
-            registers_up<kSoftRegs>();
             const int group = (warp - kUnpackWarps) >> 2, quarter = warp & 3;
             const int key = quarter * 32 + lane;                                    // of a tile
             const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-            // Sums of P over this thread's keys.  Of a block of 64 rows a group has the runs of 16 rows `group` and group + 2.
-            unsigned long long l[NB][2][8];
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) l[b][e >> 3][e & 7] = 0;
+            // (The loop over blocks of 64 rows stays a loop: straight-line code of all roles is more than the instruction caches hold.  Of a block a
+            // group has the runs of 16 rows `group` and group + 2.)
             uint32_t refs = 0;               // bit b: which of the two references block b uses
-            int meets = 0, item = 0, uses1 = 0;     // uses1: of the second buffer of P where the blocks have one each
+            int meets = 0, item = 0, turn = 0, uses1 = 0;     // uses1: of the second buffer of P where the blocks have one each
             bool ok = true;
             auto meet = [&]() {              // the four warps of the group
                 __syncwarp();
@@ -372,93 +356,98 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     if (!(ok = mbar_wait_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
                     bad = sh.odd[n & 1][key];
                 }
-#pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    if (64 * b >= n_rows) break;
+#pragma unroll 1
+                for (int b = 0; 64 * b < n_rows; ++b) {
                     const int c0 = 4 * b + group, pb = NB == 1 ? n & 1 : b;
                     // the product that read this buffer of P before is done
                     const int used = NB == 1 ? n >> 1 : b == 0 ? n : uses1;
                     if (used > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[pb]), (used - 1) & 1, a.wait_ns, abort_flag))) break;
                     bool again = first;
-                    float x[2][16];
+                    uint32_t see0 = 0xffffu, see1 = 0xffffu;       // rows of the two runs that see this thread's key
+                    if (masked) {
+                        see0 = sees_of(&a, &d, 16 * c0, quarter * 32);
+                        see1 = sees_of(&a, &d, 16 * c0 + 32, quarter * 32);
+                    }
                     while (true) {
                         if (again) {
                             // ---- new references: the largest logits so far; what is summed is scaled
                             if (NB == 1 && n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[pb ^ 1]), (((n + 1) >> 1) - 1) & 1, a.wait_ns, abort_flag))) break;
                             tc_fence_after_sync();
+                            // (with 64 rows the two halves are used in turn: nobody waits here for those who still read the last one)
+                            const int turned = NB == 1 ? 64 * (turn & 1) : 0;
                             const float* old_ref = sh.minus_ref[(refs >> b) & 1];
                             float* new_ref = sh.minus_ref[((refs >> b) & 1) ^ 1];
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int c = c0 + 2 * i;
-                                const uint32_t see = masked ? sees_of(&a, &d, 16 * c, quarter * 32) : 0xffffu;
+#pragma unroll 1
+                            for (int c = c0; c < c0 + 4; c += 2) {
+                                const uint32_t see = c == c0 ? see0 : see1;
                                 uint32_t s[16];
+                                float x[16];
                                 tmem_ld_32x16(scores + 16 * c, s);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) x[i][e] = (see >> e) & 1u ? __uint_as_float(s[e]) * a.scale_log2e : -CUDART_INF_F;
-                                const float top = across_lanes(x[i], lane, [](float u, float v) { return fmaxf(u, v); });
-                                if (!(lane & 1)) sh.most[quarter][16 * c + (lane >> 1)] = top;
+                                for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? __uint_as_float(s[e]) * a.scale_log2e : -CUDART_INF_F;
+                                const float top = largest_across_lanes(x, lane);
+                                if (!(lane & 1)) sh.most[quarter][turned + 16 * c + (lane >> 1)] = top;
                             }
                             if (!(ok = meet())) break;
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const int c = c0 + 2 * i, r = 16 * c + (lane & 15);
+#pragma unroll 1
+                            for (int c = c0; c < c0 + 4; c += 2) {
+                                const int r = 16 * c + (lane & 15);
                                 const float old = first ? -CUDART_INF_F : -old_ref[r];
-                                float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])), old);
+                                float now = fmaxf(fmaxf(fmaxf(sh.most[0][turned + r], sh.most[1][turned + r]), fmaxf(sh.most[2][turned + r], sh.most[3][turned + r])), old);
                                 now = fmaxf(now, -kNothing);              // of a row that has seen nothing: below every logit
                                 if (lane < 16) new_ref[r] = -now;         // (every warp of the group writes the same)
                                 if (first) continue;
                                 const float alpha = exp2_fast(old - now);
-                                uint32_t o[16];
-                                tmem_ld_32x16(lanes + L::kO + 16 * c, o);
-                                tmem_ld_wait();
+#pragma unroll 1
+                                for (uint32_t at = L::kO; at <= L::kSum; at += L::kSum - L::kO) {
+                                    uint32_t o[16];
+                                    tmem_ld_32x16(lanes + at + 16 * c, o);
+                                    tmem_ld_wait();
 #pragma unroll
-                                for (int e = 0; e < 16; e += 2) {
-                                    const float f0 = __shfl_sync(0xffffffffu, alpha, e), f1 = __shfl_sync(0xffffffffu, alpha, e + 1);
-                                    o[e] = __float_as_uint(__uint_as_float(o[e]) * f0);
-                                    o[e + 1] = __float_as_uint(__uint_as_float(o[e + 1]) * f1);
-                                    l[b][i][e / 2] = mul2(l[b][i][e / 2], pair(f0, f1));
+                                    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * __shfl_sync(0xffffffffu, alpha, e));
+                                    tmem_st_32x16(lanes + at + 16 * c, o);
                                 }
-                                tmem_st_32x16(lanes + L::kO + 16 * c, o);
                             }
                             tmem_st_wait();
                             __syncwarp();
                             refs ^= 1u << b;
+                            ++turn;
                         }
                         // ---- P, and whether a logit passed its reference
                         const float* ref = sh.minus_ref[(refs >> b) & 1];
-                        uint32_t s[2][16];
-                        tmem_ld_32x16(scores + 16 * c0, s[0]);
-                        tmem_ld_32x16(scores + 16 * c0 + 32, s[1]);
                         float most[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-                        tmem_ld_wait();
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const int c = c0 + 2 * i;
+                            uint32_t s[16];
+                            float x[16];
+                            tmem_ld_32x16(scores + 16 * c, s);
+                            tmem_ld_wait();
 #pragma unroll
                             for (int e = 0; e < 16; e += 4) {
                                 const float4 r = *reinterpret_cast<const float4*>(ref + 16 * c + e);
-                                const unsigned long long scale2 = pair(a.scale_log2e, a.scale_log2e);
-                                unpair(fma2(pair(__uint_as_float(s[i][e]), __uint_as_float(s[i][e + 1])), scale2, pair(r.x, r.y)), x[i][e], x[i][e + 1]);
-                                unpair(fma2(pair(__uint_as_float(s[i][e + 2]), __uint_as_float(s[i][e + 3])), scale2, pair(r.z, r.w)), x[i][e + 2], x[i][e + 3]);
+                                x[e] = fmaf(__uint_as_float(s[e]), a.scale_log2e, r.x);
+                                x[e + 1] = fmaf(__uint_as_float(s[e + 1]), a.scale_log2e, r.y);
+                                x[e + 2] = fmaf(__uint_as_float(s[e + 2]), a.scale_log2e, r.z);
+                                x[e + 3] = fmaf(__uint_as_float(s[e + 3]), a.scale_log2e, r.w);
                             }
                             if (masked) {
-                                const uint32_t see = sees_of(&a, &d, 16 * c, quarter * 32);
+                                const uint32_t see = i == 0 ? see0 : see1;
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) x[i][e] = (see >> e) & 1u ? x[i][e] : -CUDART_INF_F;
+                                for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? x[e] : -CUDART_INF_F;
                                 if (bad)
 #pragma unroll 1
                                     for (int e = 0; e < 16; ++e)
                                         if ((see >> e) & 1u) atomicOr(&sh.spoilt[item & 1][16 * c + e], bad);
                             }
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) most[e & 3] = fmaxf(most[e & 3], x[i][e]);
+                            for (int e = 0; e < 16; ++e) most[e & 3] = fmaxf(most[e & 3], x[e]);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) x[i][e] = exp2_fast(x[i][e]);
+                            for (int e = 0; e < 16; ++e) x[e] = exp2_fast(x[e]);
                             uint32_t p[8];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(x[i][2 * e], x[i][2 * e + 1]));
+                            for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(x[2 * e], x[2 * e + 1]));
                             const uint32_t row = sm + L::kP + pb * kHalf + key * 128;
                             const int piece = 2 * (c & 3);
                             sts128(row + ((piece ^ (key & 7)) << 4), p[0], p[1], p[2], p[3]);
@@ -474,10 +463,6 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         again = true;
                     }
                     if (!ok) break;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) l[b][i][e] = add2(l[b][i][e], pair(x[i][2 * e], x[i][2 * e + 1]));
                     fence_proxy_async_smem();
                     tc_fence_before_sync();
                     __syncwarp();
@@ -488,20 +473,6 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 if (lane == 0) mbar_arrive(bar(sh.s_free[n & 1]));
                 if (!last) continue;          // (the CTA's last tile is the last of its part)
                 // ---- end of the item or of the piece
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float x[16];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            unpair(l[b][i][e], x[2 * e], x[2 * e + 1]);
-                            l[b][i][e] = 0;
-                        }
-                        const float sum = across_lanes(x, lane, [](float u, float v) { return u + v; });
-                        if (!(lane & 1)) sh.most[quarter][16 * (4 * b + group + 2 * i) + (lane >> 1)] = sum;
-                    }
-                if (!(ok = meet())) break;
                 const int used0 = NB == 1 ? (n + 2) >> 1 : n + 1, used1 = NB == 1 ? (n + 1) >> 1 : uses1;
                 if (!(ok = mbar_wait_warp(bar(sh.pv_done[0]), (used0 - 1) & 1, a.wait_ns, abort_flag))) break;
                 if (used1 > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[1]), (used1 - 1) & 1, a.wait_ns, abort_flag))) break;
@@ -513,14 +484,15 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 const RowBlock rows = row_block(a, d.rb * kRows);
 #pragma unroll 1
                 for (int r0 = 16 * group; r0 < n_rows; r0 += (r0 & 12) == 12 ? 20 : 4) {
-                    uint32_t o[4];
+                    uint32_t o[4], l[4];       // outputs, sums of P (the same in all lanes)
                     tmem_ld_32x4(lanes + L::kO + r0, o);
+                    tmem_ld_32x4(lanes + L::kSum + r0, l);
                     tmem_ld_wait();
                     if (at < D)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int r = r0 + e;
-                            const float sum = (sh.most[0][r] + sh.most[1][r]) + (sh.most[2][r] + sh.most[3][r]);
+                            const float sum = __uint_as_float(l[e]);
                             float x = __uint_as_float(o[e]);
                             if ((sh.spoilt[item & 1][r] >> (channel / G)) & 1u) x = CUDART_NAN_F;
                             if (whole) {
@@ -538,13 +510,11 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 for (int r = quarter * 32 + lane; r < kRows; r += 128)      // (nobody reads what the item before left any more)
                     if (((r >> 4) & 1) == group) sh.spoilt[item & 1][r] = 0;
                 tc_fence_before_sync();
-                if (!(ok = meet())) break;       // (all have read the sums)
                 if (final) break;
             }
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp == kLoadWarp) {
             // ------------------------------------------------------------------------ items, codes
-            registers_down<kOtherRegs>();
             Cursor k = sh.start;
             const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
             bool ok = true, first = true;
@@ -576,7 +546,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 const bool last = next.blk >= next.end, begins = first_blk == 0, ends = k.end == k.n_blk;
                 if (last && next.left > 0) next_item(a, plan, next);
                 const bool final = last && next.blk >= next.end;
-                if (n >= kRing && !(ok = mbar_wait_warp(bar(sh.ring_empty[st]), ((n / kRing) & 1) ^ 1, a.wait_ns, abort_flag))) break;
+                if (n >= kRing && !(ok = mbar_wait_asleep_warp(bar(sh.ring_empty[st]), ((n / kRing) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                 if (lane == 0) {
                     if (present != (1u << nb) - 1u) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
                     Tile& d = sh.tiles[n % kDescs];
@@ -614,12 +584,11 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp == kScoreWarp) {
             // ------------------------------------------------------------------------ S^T = K Q^T
-            registers_down<kOtherRegs>();
             if (lane == 0) {
                 bool ok = true;
                 for (int n = 0;; ++n) {
-                    if (!(ok = mbar_wait(bar(sh.k_full), n & 1, a.wait_ns, abort_flag))) break;
-                    if (n >= 2 && !(ok = mbar_wait(bar(sh.s_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
+                    if (!(ok = mbar_wait_asleep(bar(sh.k_full), n & 1, a.wait_ns, abort_flag))) break;
+                    if (n >= 2 && !(ok = mbar_wait_asleep(bar(sh.s_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                     tc_fence_after_sync();
                     const uint64_t kd = umma_desc_sw128(sm + L::kK), qd = umma_desc_sw128(sm + L::kQ);
                     const uint32_t shape = NB == 2 && sh.tiles[n % kDescs].item_rows <= 64 ? idesc(64, false) : idesc(kRows, false);
@@ -635,12 +604,12 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             }
         } else if (warp == kValueWarp) {
             // ------------------------------------------------------------------------ O^T += V^T P^T
-            registers_down<kOtherRegs>();
             if (lane == 0) {
                 bool ok = true;
                 int uses1 = 0;
+                const uint64_t ones = desc_mn(sm + L::kOnesAt, 1024);
                 for (int n = 0; ok; ++n) {
-                    if (!(ok = mbar_wait(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                    if (!(ok = mbar_wait_asleep(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
                     // (heads of 64: the upper 64 lanes take whatever lies behind the tile, and nobody reads them)
                     const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf);
                     const Tile& d = sh.tiles[n % kDescs];
@@ -648,13 +617,17 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     const int blocks = (d.item_rows + 63) >> 6;
                     for (int b = 0; b < blocks; ++b) {
                         const int pb = NB == 1 ? n & 1 : b;
-                        if (!(ok = mbar_wait(bar(sh.p_full[pb]), (NB == 1 ? n >> 1 : b == 0 ? n : uses1) & 1, a.wait_ns, abort_flag))) break;
+                        if (!(ok = mbar_wait_asleep(bar(sh.p_full[pb]), (NB == 1 ? n >> 1 : b == 0 ? n : uses1) & 1, a.wait_ns, abort_flag))) break;
                         if (b == 1) ++uses1;
                         tc_fence_after_sync();
                         const uint64_t pd = desc_mn(sm + L::kP + pb * kHalf, kHalf);
 #pragma unroll
                         for (int i = 0; i < kKeys / 16; ++i)
                             umma_bf16(tmem + L::kO + 64 * b, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(64, true), first && i == 0 ? 0u : 1u);
+                        // the sums of P over the keys: ones in V's place
+#pragma unroll
+                        for (int i = 0; i < kKeys / 16; ++i)
+                            umma_bf16(tmem + L::kSum + 64 * b, ones, pd + i * (2048 >> 4), idesc(64, true), first && i == 0 ? 0u : 1u);
                         if (b + 1 == blocks) umma_commit(bar(sh.v_free[n & 1]));
                         umma_commit(bar(sh.pv_done[pb]));
                     }
@@ -662,13 +635,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 }
                 if (!ok) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
             }
-        } else {
-            registers_down<kOtherRegs>();
         }
-        // what follows is compiled for all warps alike
         __syncwarp();
-        if (warp < kUnpackWarps || warp >= kLoadWarp) registers_up<96>();
-        else registers_down<96>();
     }
     if (warp == kLoadWarp && lane == 0) {
         if (!(open & 1)) meta[0] = 0;

@@ -1,6 +1,9 @@
 // Thin inline-PTX wrappers for sm_100a: mbarrier, TMA (cp.async.bulk.tensor), cp.async,
 // tcgen05 (TMEM allocation, UMMA issue/commit, TMEM loads) and the descriptors they take.
 #pragma once
+#ifndef SLEEPNS
+#define SLEEPNS 40
+#endif
 
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -85,6 +88,29 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, unsigne
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, unsigned long long limit_ns,
                                                volatile int* abort_flag) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit_ns, abort_flag) ? 1 : 0) != 0;
+}
+
+// The bounded wait of a role that is not the one that all others wait for: it sleeps between polls, and so leaves issue slots and the
+// barriers to the warps that work.
+__device__ __forceinline__ bool mbar_wait_asleep(uint32_t bar, uint32_t parity, unsigned long long limit_ns, volatile int* abort_flag) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t start = globaltimer_ns();
+#pragma unroll 1
+    while (true) {
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i) {
+            __nanosleep(SLEEPNS);
+            if (mbar_try_wait(bar, parity)) return true;
+        }
+        if (*abort_flag) return false;
+        if (globaltimer_ns() - start > limit_ns) {
+            *abort_flag = 1;
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ bool mbar_wait_asleep_warp(uint32_t bar, uint32_t parity, unsigned long long limit_ns, volatile int* abort_flag) {
+    return __all_sync(0xffffffffu, mbar_wait_asleep(bar, parity, limit_ns, abort_flag) ? 1 : 0) != 0;
 }
 
 // ------------------------------------------------------------------------------- programmatic dependent launch
