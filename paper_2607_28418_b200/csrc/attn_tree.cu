@@ -24,7 +24,7 @@
 namespace {
 
 constexpr int kItemAlone = 96;     // blocks of an item that one CTA may take alone
-constexpr int kItemCost = 8;       // units that an item counts on top of its blocks: queries in, results out
+constexpr int kItemCost = 40;      // units that an item counts on top of its blocks: queries in, results out
 
 }  // namespace
 
@@ -120,10 +120,6 @@ __device__ __forceinline__ uint32_t unpack_two(uint32_t w, uint32_t s, uint32_t 
     return as_word(__hfma2(__hsub2(as_bf162(high), as_bf162(0x43004300u)), as_bf162(s), as_bf162(m)));
 }
 __device__ __forceinline__ bool not_finite(uint32_t word) { return (word & 0x7F80u) == 0x7F80u || (word & 0x7F800000u) == 0x7F800000u; }
-
-__device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&r)[4]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
-}
 
 // Bit e: query row r0 + e of the tile's item sees the key key0 + lane of the tile.  Lane e gets the bits of row e for the 32 keys, and then
 // all lanes get each row's.  Out of line: few tiles have keys that not every row sees.
@@ -250,15 +246,20 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 if (n > 0 && !(ok = mbar_wait_asleep_warp(bar(sh.k_free), (n - 1) & 1, a.wait_ns, abort_flag))) break;
                 if (d.first) {
                     const RowBlock rows = row_block(a, d.rb * kRows);
-                    constexpr int kChunks = kRows * D / 8;                          // of 16 bytes
-#pragma unroll 4
-                    for (int i = tid; i < kChunks; i += 32 * kUnpackWarps) {
-                        const int r = i / (D / 8), c = i % (D / 8);
-                        const Row w = row_of(a, rows, r);
-                        uint4 v = make_uint4(0, 0, 0, 0);
+                    constexpr int kRowLanes = D / 8, kStep = 32 * kUnpackWarps / kRowLanes;      // a thread has 16 bytes of every kStep-th row
+                    const int c = tid % kRowLanes, r0 = tid / kRowLanes;
+                    uint4 v[kRows / kStep];
+#pragma unroll
+                    for (int i = 0; i < kRows / kStep; ++i) {
+                        const Row w = row_of(a, rows, r0 + i * kStep);
+                        v[i] = make_uint4(0, 0, 0, 0);
                         if (w.tok < d.n_rows)
-                            v = *reinterpret_cast<const uint4*>(a.qm + static_cast<long long>(d.row0 + w.tok) * a.qs + (d.kvh * a.share + w.sub) * D + 8 * c);
-                        sts128(sm + L::kQ + (c >> 3) * (kRows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), v.x, v.y, v.z, v.w);
+                            v[i] = *reinterpret_cast<const uint4*>(a.qm + static_cast<long long>(d.row0 + w.tok) * a.qs + (d.kvh * a.share + w.sub) * D + 8 * c);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kRows / kStep; ++i) {
+                        const int r = r0 + i * kStep;
+                        sts128(sm + L::kQ + (c >> 3) * (kRows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
                     }
                 }
                 if (here) {
@@ -483,28 +484,36 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 float* dst = parts + (d.begins ? slot_floats(kRows, D) : 0);
                 const RowBlock rows = row_block(a, d.rb * kRows);
 #pragma unroll 1
-                for (int r0 = 16 * group; r0 < n_rows; r0 += (r0 & 12) == 12 ? 20 : 4) {
-                    uint32_t o[4], l[4];       // outputs, sums of P (the same in all lanes)
-                    tmem_ld_32x4(lanes + L::kO + r0, o);
-                    tmem_ld_32x4(lanes + L::kSum + r0, l);
+                for (int c = group; 16 * c < n_rows; c += 2) {
+                    // where the run's rows go, a row a lane: index of (row, head) in o, -1 for none; whether it is on
+                    const int r = 16 * c + (lane & 15);
+                    const Row w = row_of(a, rows, r);
+                    const int h = d.kvh * a.share + w.sub, row = d.row0 + w.tok;
+                    int place = -1;
+                    if (w.tok < d.n_rows) place = row * a.n_q + h;
+                    const bool on = place >= 0 && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, row, h / a.hpg));
+                    const uint32_t spoilt = sh.spoilt[item & 1][r], on_bits = __ballot_sync(0xffffffffu, on);
+                    uint32_t o[16], l[16];       // outputs, sums of P (the same in all lanes)
+                    tmem_ld_32x16(lanes + L::kO + 16 * c, o);
+                    tmem_ld_32x16(lanes + L::kSum + 16 * c, l);
                     tmem_ld_wait();
-                    if (at < D)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int r = r0 + e;
-                            const float sum = __uint_as_float(l[e]);
-                            float x = __uint_as_float(o[e]);
-                            if ((sh.spoilt[item & 1][r] >> (channel / G)) & 1u) x = CUDART_NAN_F;
-                            if (whole) {
-                                const RowOut ro = row_out(a, d.row0, d.n_rows, d.kvh, row_of(a, rows, r), D);
-                                if (ro.o) ro.o[channel] = __float2bfloat16_rn(ro.on && sum != 0.f ? x / sum : 0.f);
-                            } else if (r < n_rows) {
-                                dst[r * D + channel] = x;
-                                // (a row that has seen nothing has no weight among its other pieces)
-                                if (at == 0)
-                                    *reinterpret_cast<float2*>(dst + kRows * D + 2 * r) = make_float2(sum == 0.f ? -CUDART_INF_F : -sh.minus_ref[(refs >> (r >> 6)) & 1][r], sum);
-                            }
+                    for (int e = 0; e < 16; ++e) {
+                        const int to = __shfl_sync(0xffffffffu, place, e);
+                        const uint32_t bad_groups = __shfl_sync(0xffffffffu, spoilt, e);
+                        const float sum = __uint_as_float(l[e]), x = (bad_groups >> (channel / G)) & 1u ? CUDART_NAN_F : __uint_as_float(o[e]);
+                        if (at >= D) continue;
+                        if (whole) {
+                            if (to >= 0)
+                                a.o[static_cast<size_t>(to) * D + channel] = __float2bfloat16_rn((on_bits >> e) & 1u && sum != 0.f ? __fdividef(x, sum) : 0.f);
+                        } else if (to >= 0) {
+                            dst[(16 * c + e) * D + channel] = x;
+                            // (a row that has seen nothing has no weight among its other pieces)
+                            if (at == 0)
+                                *reinterpret_cast<float2*>(dst + kRows * D + 2 * (16 * c + e)) =
+                                    make_float2(sum == 0.f ? -CUDART_INF_F : -sh.minus_ref[(refs >> (c >> 2)) & 1][16 * c + e], sum);
                         }
+                    }
                 }
                 ++item;
                 for (int r = quarter * 32 + lane; r < kRows; r += 128)      // (nobody reads what the item before left any more)
@@ -662,6 +671,83 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
     }
 }
 
+// Items that more than one CTA had a piece of: block (c, .) joins the one that begins in CTA c and goes on in the next.  A warp takes a row: lane
+// e reads the maximum and sum of piece e, and every lane its channels of all pieces, eight at a time.
+constexpr int kJoinParts = 16;
+template <int ROWS, int D>
+__global__ void __launch_bounds__(256) attn_tree_join_kernel(const __grid_constant__ TreeArgs a, int ctas) {
+    grid_dep_wait();
+    const int c = blockIdx.x, lane = threadIdx.x & 31;
+    const int* mine = a.meta + (2 * c + 1) * kMeta;
+    const int4 meta = *reinterpret_cast<const int4*>(mine);
+    const int rb = mine[4];
+    int st = c + 1 + lane < ctas ? a.meta[2 * (c + 1 + lane) * kMeta] : 0;
+    if (meta.x != 1 || static_cast<unsigned>(meta.w) >= static_cast<unsigned>(a.c.n_kv_heads)) return;
+    int n = 1;         // pieces: CTAs c + 1, ... up to the one that ends the item
+    for (int k = c + 1;;) {
+        const uint32_t stop = __ballot_sync(0xffffffffu, st != 1);
+        if (stop) {
+            const int at = __ffs(stop) - 1;
+            n += at + (__shfl_sync(0xffffffffu, st, at) == 2 ? 1 : 0);
+            break;
+        }
+        n += 32;
+        k += 32;
+        st = k + lane < ctas ? a.meta[2 * (k + lane) * kMeta] : 0;
+    }
+    auto piece = [&](int i) -> const float* { return a.parts + static_cast<size_t>(i == 0 ? 2 * c + 1 : 2 * (c + i)) * slot_floats(ROWS, D); };
+    constexpr int kEach = D / 32;        // channels of a lane
+    const RowBlock rows = row_block(a, rb * ROWS);
+    for (int r = (threadIdx.x >> 5) + 8 * blockIdx.y; r < ROWS; r += 8 * kJoinParts) {
+        const RowOut ro = row_out(a, meta.y, meta.z, meta.w, row_of(a, rows, r), D);
+        if (!ro.o) break;                // (rows behind it do not exist either)
+        float m = -CUDART_INF_F, l = 0.f, x[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) x[e] = 0.f;
+        for (int e0 = 0; e0 < n; e0 += 32) {
+            const int last = min(32, n - e0);
+            const float2 ml = lane < last ? *reinterpret_cast<const float2*>(piece(e0 + lane) + ROWS * D + 2 * r) : make_float2(-CUDART_INF_F, 0.f);
+            float top = ml.x;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float m_new = fmaxf(m, top), m_use = m_new == -CUDART_INF_F ? 0.f : m_new;
+            const float old = exp2_fast(m - m_use), w = exp2_fast(ml.x - m_use);
+            float sum = ml.y * w;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            l = fmaf(l, old, sum);
+            m = m_new;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) x[e] *= old;
+            for (int p0 = 0; p0 < last; p0 += 8) {
+                float v[8][kEach];
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) v[p][e] = 0.f;
+                    if (p0 + p < last) {
+                        const float* from = piece(e0 + p0 + p) + r * D + kEach * lane;
+#pragma unroll
+                        for (int e = 0; e < kEach; e += 2) *reinterpret_cast<float2*>(&v[p][e]) = *reinterpret_cast<const float2*>(from + e);
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+                    const float we = __shfl_sync(0xffffffffu, w, (p0 + p) & 31);
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) x[e] = fmaf(v[p][e], we, x[e]);
+                }
+            }
+        }
+        const float inv = ro.on && l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+        for (int e = 0; e < kEach; e += 2) {
+            const __nv_bfloat162 b = inv != 0.f ? __floats2bfloat162_rn(x[e] * inv, x[e + 1] * inv) : __floats2bfloat162_rn(0.f, 0.f);
+            *reinterpret_cast<__nv_bfloat162*>(ro.o + kEach * lane + e) = b;
+        }
+    }
+}
+
 struct Work {
     size_t plan, parts, meta, total;
 };
@@ -708,7 +794,7 @@ int launch(wide_ctx* ctx, cudaStream_t s, TreeArgs a, unsigned char* ws) {
     const long long items = static_cast<long long>(a.c.n_kv_heads) * (static_cast<long long>(a.q.rows) * a.share / L::kRows + a.q.n_seqs);
     if (items > ctas || (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) > kItemAlone) {
         WideLaunch l(ctx, s, "attn_tree_join");
-        WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_cache_join_kernel<L::kRows, D>, dim3(ctas, L::kRows * D / 512), dim3(256), 0, s, a, ctas));
+        WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_tree_join_kernel<L::kRows, D>, dim3(ctas, kJoinParts), dim3(256), 0, s, a, ctas));
     }
     return WIDE_OK;
 }
