@@ -121,6 +121,10 @@ __device__ __forceinline__ uint32_t unpack_two(uint32_t w, uint32_t s, uint32_t 
 }
 __device__ __forceinline__ bool not_finite(uint32_t word) { return (word & 0x7F80u) == 0x7F80u || (word & 0x7F800000u) == 0x7F800000u; }
 
+__device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&r)[4]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+
 // Bit e: query row r0 + e of the tile's item sees the key key0 + lane of the tile.  Lane e gets the bits of row e for the 32 keys, and then
 // all lanes get each row's.  Out of line: few tiles have keys that not every row sees.
 __device__ __noinline__ uint32_t sees_of(const TreeArgs* a, const Tile* d, int r0, int key0) {
@@ -493,25 +497,27 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     if (w.tok < d.n_rows) place = row * a.n_q + h;
                     const bool on = place >= 0 && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, row, h / a.hpg));
                     const uint32_t spoilt = sh.spoilt[item & 1][r], on_bits = __ballot_sync(0xffffffffu, on);
-                    uint32_t o[16], l[16];       // outputs, sums of P (the same in all lanes)
-                    tmem_ld_32x16(lanes + L::kO + 16 * c, o);
-                    tmem_ld_32x16(lanes + L::kSum + 16 * c, l);
-                    tmem_ld_wait();
+#pragma unroll 1
+                    for (int e0 = 0; e0 < 16; e0 += 4) {
+                        uint32_t o[4], l[4];     // outputs, sums of P (the same in all lanes)
+                        tmem_ld_32x4(lanes + L::kO + 16 * c + e0, o);
+                        tmem_ld_32x4(lanes + L::kSum + 16 * c + e0, l);
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int to = __shfl_sync(0xffffffffu, place, e);
-                        const uint32_t bad_groups = __shfl_sync(0xffffffffu, spoilt, e);
-                        const float sum = __uint_as_float(l[e]), x = (bad_groups >> (channel / G)) & 1u ? CUDART_NAN_F : __uint_as_float(o[e]);
-                        if (at >= D) continue;
-                        if (whole) {
-                            if (to >= 0)
-                                a.o[static_cast<size_t>(to) * D + channel] = __float2bfloat16_rn((on_bits >> e) & 1u && sum != 0.f ? __fdividef(x, sum) : 0.f);
-                        } else if (to >= 0) {
-                            dst[(16 * c + e) * D + channel] = x;
-                            // (a row that has seen nothing has no weight among its other pieces)
-                            if (at == 0)
-                                *reinterpret_cast<float2*>(dst + kRows * D + 2 * (16 * c + e)) =
-                                    make_float2(sum == 0.f ? -CUDART_INF_F : -sh.minus_ref[(refs >> (c >> 2)) & 1][16 * c + e], sum);
+                        for (int e = 0; e < 4; ++e) {
+                            const int to = __shfl_sync(0xffffffffu, place, e0 + e);
+                            const uint32_t bad_groups = __shfl_sync(0xffffffffu, spoilt, e0 + e);
+                            const float sum = __uint_as_float(l[e]), x = (bad_groups >> (channel / G)) & 1u ? CUDART_NAN_F : __uint_as_float(o[e]);
+                            if (at >= D || to < 0) continue;
+                            if (whole) {
+                                a.o[static_cast<size_t>(to) * D + channel] = __float2bfloat16_rn((on_bits >> (e0 + e)) & 1u && sum != 0.f ? __fdividef(x, sum) : 0.f);
+                            } else {
+                                const int rr = 16 * c + e0 + e;
+                                dst[rr * D + channel] = x;
+                                // (a row that has seen nothing has no weight among its other pieces)
+                                if (at == 0)
+                                    *reinterpret_cast<float2*>(dst + kRows * D + 2 * rr) = make_float2(sum == 0.f ? -CUDART_INF_F : -sh.minus_ref[(refs >> (c >> 2)) & 1][rr], sum);
+                            }
                         }
                     }
                 }
