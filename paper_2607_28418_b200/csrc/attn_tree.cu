@@ -36,8 +36,8 @@ constexpr int kTile = 8;            // blocks of a tile: 128 keys
 constexpr int kKeys = 16 * kTile;
 constexpr int kMostRing = 3;        // tiles of codes on their way
 constexpr int kDescs = 8;           // tiles that are known: the ring's, and at most three behind it whose softmax is not done
-constexpr int kUnpackWarps = 8, kSoftWarps = 8;
-constexpr int kLoadWarp = 16, kScoreWarp = 17, kValueWarp = 18, kWarps = 19;
+constexpr int kUnpackWarps = 8, kSoftWarps = 16, kGroups = kSoftWarps / 4;
+constexpr int kLoadWarp = kUnpackWarps + kSoftWarps, kScoreWarp = kLoadWarp + 1, kValueWarp = kLoadWarp + 2, kWarps = kLoadWarp + 3;
 constexpr float kSlack = 8.f;
 constexpr int kOnes = 3 * 1024;      // bytes of ones: two blocks of 64 rows and two groups of 8 keys, each 1024 further on
 constexpr float kNothing = 1e38f;    // minus the reference of a row that has seen nothing yet: a logit of any size passes it
@@ -62,14 +62,14 @@ struct Tile {                       // what the roles are told of a tile
 };
 
 struct alignas(16) Shared {
-    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full[2], pv_done[2], meet[2];
+    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full[2], pv_done[2], meet[kGroups];
     uint32_t tmem;
     int abort;
     Cursor start;
     Tile tiles[kDescs];
     alignas(16) float minus_ref[2][128];        // of a row, twice: the one in use and the next
     float most[4][128];             // of a row, per warp of a group: the largest logit
-    alignas(16) int flag[4][2][4];              // [which block of rows][group][warp]: a logit passed its reference
+    alignas(16) int flag[4][kGroups][4];              // [which block of rows][group][warp]: a logit passed its reference
     uint32_t odd[2][kKeys];         // sub-groups of a new token's values that are not finite (their values are 0 in the tile)
     uint32_t spoilt[2][128];        // rows that see such a sub-group, of this item and the next
 };
@@ -182,10 +182,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             mbar_init(bar(sh.v_free[i]), 1);
             mbar_init(bar(sh.s_full[i]), 1);
             mbar_init(bar(sh.s_free[i]), kSoftWarps);
-            mbar_init(bar(sh.meet[i]), 4);
             mbar_init(bar(sh.p_full[i]), kSoftWarps);
             mbar_init(bar(sh.pv_done[i]), 1);
         }
+        for (int i = 0; i < kGroups; ++i) mbar_init(bar(sh.meet[i]), 4);
         sh.abort = 0;
         fence_barrier_init();
     }
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             const int key = quarter * 32 + lane;                                    // of a tile
             const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
             // (The loop over blocks of 64 rows stays a loop: straight-line code of all roles is more than the instruction caches hold.  Of a block a
-            // group has the runs of 16 rows `group` and group + 2.)
+            // group has a run of 16 rows.)
             uint32_t refs = 0;               // bit b: which of the two references block b uses
             int meets = 0, item = 0, turn = 0, uses1 = 0;     // uses1: of the second buffer of P where the blocks have one each
             bool ok = true;
@@ -363,17 +363,13 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 }
 #pragma unroll 1
                 for (int b = 0; 64 * b < n_rows; ++b) {
-                    const int c0 = 4 * b + group, pb = NB == 1 ? n & 1 : b;
+                    const int c = 4 * b + group, pb = NB == 1 ? n & 1 : b;
                     // the product that read this buffer of P before is done
                     const int used = NB == 1 ? n >> 1 : b == 0 ? n : uses1;
                     if (used > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[pb]), (used - 1) & 1, a.wait_ns, abort_flag))) break;
                     bool again = first;
-                    uint32_t see0 = 0xffffu, see1 = 0xffffu;       // rows of the two runs that see this thread's key
-                    if (masked) {
-                        see0 = sees_of(&a, &d, 16 * c0, quarter * 32);
-                        see1 = sees_of(&a, &d, 16 * c0 + 32, quarter * 32);
-                    }
-                    while (true) {
+                    const uint32_t see = masked && 16 * c < n_rows ? sees_of(&a, &d, 16 * c, quarter * 32) : 0xffffu;   // rows of the run that see this thread's key
+                    while (16 * c < n_rows) {
                         if (again) {
                             // ---- new references: the largest logits so far; what is summed is scaled
                             if (NB == 1 && n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[pb ^ 1]), (((n + 1) >> 1) - 1) & 1, a.wait_ns, abort_flag))) break;
@@ -382,9 +378,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                             const int turned = NB == 1 ? 64 * (turn & 1) : 0;
                             const float* old_ref = sh.minus_ref[(refs >> b) & 1];
                             float* new_ref = sh.minus_ref[((refs >> b) & 1) ^ 1];
-#pragma unroll 1
-                            for (int c = c0; c < c0 + 4; c += 2) {
-                                const uint32_t see = c == c0 ? see0 : see1;
+                            {
                                 uint32_t s[16];
                                 float x[16];
                                 tmem_ld_32x16(scores + 16 * c, s);
@@ -395,17 +389,15 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                 if (!(lane & 1)) sh.most[quarter][turned + 16 * c + (lane >> 1)] = top;
                             }
                             if (!(ok = meet())) break;
-#pragma unroll 1
-                            for (int c = c0; c < c0 + 4; c += 2) {
-                                const int r = 16 * c + (lane & 15);
+                            const int r = 16 * c + (lane & 15);
+                            {
                                 const float old = first ? -CUDART_INF_F : -old_ref[r];
                                 float now = fmaxf(fmaxf(fmaxf(sh.most[0][turned + r], sh.most[1][turned + r]), fmaxf(sh.most[2][turned + r], sh.most[3][turned + r])), old);
                                 now = fmaxf(now, -kNothing);              // of a row that has seen nothing: below every logit
                                 if (lane < 16) new_ref[r] = -now;         // (every warp of the group writes the same)
-                                if (first) continue;
                                 const float alpha = exp2_fast(old - now);
 #pragma unroll 1
-                                for (uint32_t at = L::kO; at <= L::kSum; at += L::kSum - L::kO) {
+                                for (uint32_t at = L::kO; !first && at <= L::kSum; at += L::kSum - L::kO) {
                                     uint32_t o[16];
                                     tmem_ld_32x16(lanes + at + 16 * c, o);
                                     tmem_ld_wait();
@@ -422,9 +414,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         // ---- P, and whether a logit passed its reference
                         const float* ref = sh.minus_ref[(refs >> b) & 1];
                         float most[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int c = c0 + 2 * i;
+                        {
                             uint32_t s[16];
                             float x[16];
                             tmem_ld_32x16(scores + 16 * c, s);
@@ -438,7 +428,6 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                 x[e + 3] = fmaf(__uint_as_float(s[e + 3]), a.scale_log2e, r.w);
                             }
                             if (masked) {
-                                const uint32_t see = i == 0 ? see0 : see1;
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? x[e] : -CUDART_INF_F;
                                 if (bad)
@@ -488,7 +477,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 float* dst = parts + (d.begins ? slot_floats(kRows, D) : 0);
                 const RowBlock rows = row_block(a, d.rb * kRows);
 #pragma unroll 1
-                for (int c = group; 16 * c < n_rows; c += 2) {
+                for (int c = group; 16 * c < n_rows; c += kGroups) {
                     // where the run's rows go, a row a lane: index of (row, head) in o, -1 for none; whether it is on
                     const int r = 16 * c + (lane & 15);
                     const Row w = row_of(a, rows, r);
@@ -523,7 +512,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 }
                 ++item;
                 for (int r = quarter * 32 + lane; r < kRows; r += 128)      // (nobody reads what the item before left any more)
-                    if (((r >> 4) & 1) == group) sh.spoilt[item & 1][r] = 0;
+                    if (((r >> 4) & 3) == group) sh.spoilt[item & 1][r] = 0;
                 tc_fence_before_sync();
                 if (final) break;
             }
