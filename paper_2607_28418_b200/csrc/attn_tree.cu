@@ -54,6 +54,7 @@ struct Tile {                       // what the roles are told of a tile
     int blk, nb;                    // first block, blocks
     uint32_t present;               // bit b: block b has a page
     int first, last;                // of the item's part in this CTA
+    int index, left, item;          // tiles of the part before this one; behind it (2: two or more); the part's number
     int masked;                     // not all rows see all 128 keys
     int seq, kvh, rb, row0, n_rows, len;
     int item_rows, rows_a_block;    // query rows of the item; of a whole one
@@ -62,16 +63,18 @@ struct Tile {                       // what the roles are told of a tile
 };
 
 struct alignas(16) Shared {
-    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full[2], pv_done[2], meet[kGroups];
+    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full[2], pv_done[2], read[2], meet[kGroups];
     uint32_t tmem;
     int abort;
+    int n_tiles;                    // of this CTA, once it is known
+    int ref_at[kGroups];            // which reference a group used in its last tile of an item
     Cursor start;
     Tile tiles[kDescs];
-    alignas(16) float minus_ref[2][128];        // of a row, twice: the one in use and the next
-    float most[4][128];             // of a row, per warp of a group: the largest logit
-    alignas(16) int flag[4][kGroups][4];              // [which block of rows][group][warp]: a logit passed its reference
+    alignas(16) float minus_ref[2][128];        // of a stream's row, twice: the one in use and the next
+    float most[4][128];             // of a stream's row, per warp of a group: the largest logit
+    alignas(16) int flag[4][kGroups][4];        // [tile of the stream][group][warp]: a logit passed its reference
     uint32_t odd[2][kKeys];         // sub-groups of a new token's values that are not finite (their values are 0 in the tile)
-    uint32_t spoilt[2][128];        // rows that see such a sub-group, of this item and the next
+    uint32_t spoilt[256];           // of a row: such sub-groups that it sees (for two items of 128 rows, or four of 64)
 };
 
 template <int D, int G, int NB>
@@ -84,7 +87,8 @@ struct Layout {
     static constexpr int kPlanRoom = 227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512 < 16384
                                          ? (227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512) / 256 * 256 : 16384;
     static constexpr int kSmem = kPlan + kPlanRoom + 1024;
-    static constexpr uint32_t kCols = 4 * kRows, kO = 2 * kRows, kSum = 3 * kRows;     // two buffers of scores, outputs, sums of P
+    static constexpr uint32_t kCols = 512, kO = 2 * kRows, kSum = kO + 128;     // two buffers of scores, two streams' outputs and sums of P
+    static __device__ __forceinline__ int spoilt_at(int item, int row) { return NB == 1 ? (item & 3) * 64 + row : (item & 1) * 128 + row; }
     static_assert(kPlanRoom >= 1024 && kSmem + sizeof(Shared) <= 227 * 1024, "shared memory");
 };
 
@@ -181,15 +185,17 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             mbar_init(bar(sh.v_full[i]), kUnpackWarps);
             mbar_init(bar(sh.v_free[i]), 1);
             mbar_init(bar(sh.s_full[i]), 1);
-            mbar_init(bar(sh.s_free[i]), kSoftWarps);
-            mbar_init(bar(sh.p_full[i]), kSoftWarps);
+            mbar_init(bar(sh.s_free[i]), NB == 1 ? kSoftWarps / 2 : kSoftWarps);
+            mbar_init(bar(sh.p_full[i]), kSoftWarps / 2);
+            mbar_init(bar(sh.read[i]), kSoftWarps / 2);
             mbar_init(bar(sh.pv_done[i]), 1);
         }
         for (int i = 0; i < kGroups; ++i) mbar_init(bar(sh.meet[i]), 4);
         sh.abort = 0;
+        sh.n_tiles = 0x7fffffff;
         fence_barrier_init();
     }
-    if (tid < 256) sh.spoilt[tid >> 7][tid & 127] = 0;
+    if (tid < 256) sh.spoilt[tid] = 0;
     for (int i = tid; i < kOnes / 4; i += 32 * kWarps) reinterpret_cast<uint32_t*>(base + L::kOnesAt)[i] = 0x3F803F80u;
     fence_proxy_async_smem();
 
@@ -336,49 +342,55 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp < kUnpackWarps + kSoftWarps) {
             // ------------------------------------------------------------------------ softmax, outputs
-            const int group = (warp - kUnpackWarps) >> 2, quarter = warp & 3;
+            // Two streams of eight warps, each with a buffer of P, outputs and references of its own, that wait for each other only at the end of an
+            // item: what one waits for (its product, its four warps' agreement) the other fills, and their steps of different kinds
+            // overlap.  With 128 rows a stream has 64 of them; with 64 rows it has every other tile, and the two results are joined at the end.
+            // Of its 64 rows a stream's group of four warps has the runs of 16 rows `gi` and gi + 2.  (One stream of all sixteen warps: 3400
+            // clocks a tile of 64 rows, 5000 of 128.)
+            const int stream = (warp - kUnpackWarps) >> 3, group = (warp - kUnpackWarps) >> 2, gi = group & 1, quarter = warp & 3;
             const int key = quarter * 32 + lane;                                    // of a tile
             const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
-            // (The loop over blocks of 64 rows stays a loop: straight-line code of all roles is more than the instruction caches hold.  Of a block a
-            // group has a run of 16 rows.)
-            uint32_t refs = 0;               // bit b: which of the two references block b uses
-            int meets = 0, item = 0, turn = 0, uses1 = 0;     // uses1: of the second buffer of P where the blocks have one each
+            const int row0 = NB == 1 ? 0 : 64 * stream;                             // of this stream in the item
+            uint32_t ref_at = 0;             // which of the stream's two references is in use
+            int meets = 0, uses = 0, items = 0;
             bool ok = true;
             auto meet = [&]() {              // the four warps of the group
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(sh.meet[group]));
                 return mbar_wait_warp(bar(sh.meet[group]), meets++ & 1, a.wait_ns, abort_flag);
             };
-            for (int n = 0; ok; ++n) {
+            for (int n = NB == 1 ? stream : 0;; n += NB == 1 ? 2 : 1) {
                 if (!(ok = mbar_wait_warp(bar(sh.s_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                if (NB == 1 && n >= *static_cast<volatile int*>(&sh.n_tiles)) break;
                 tc_fence_after_sync();
                 const Tile& d = sh.tiles[n % kDescs];
-                const int n_rows = d.item_rows;
-                const bool masked = d.masked, first = d.first, last = d.last, final = d.final;
-                const uint32_t scores = lanes + (n & 1) * kRows;
-                uint32_t bad = 0;
-                if (masked) {          // values that are not finite, of keys that some row may not see
-                    if (!(ok = mbar_wait_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
-                    bad = sh.odd[n & 1][key];
-                }
-#pragma unroll 1
-                for (int b = 0; 64 * b < n_rows; ++b) {
-                    const int c = 4 * b + group, pb = NB == 1 ? n & 1 : b;
-                    // the product that read this buffer of P before is done
-                    const int used = NB == 1 ? n >> 1 : b == 0 ? n : uses1;
-                    if (used > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[pb]), (used - 1) & 1, a.wait_ns, abort_flag))) break;
-                    bool again = first;
-                    const uint32_t see = masked && 16 * c < n_rows ? sees_of(&a, &d, 16 * c, quarter * 32) : 0xffffu;   // rows of the run that see this thread's key
-                    while (16 * c < n_rows) {
+                const int n_rows = d.item_rows - row0, left = d.left;
+                const bool final = d.final;
+                if (n_rows > 0) {
+                    const bool masked = d.masked, fresh = d.index < (NB == 1 ? 2 : 1);       // the stream's first tile of the item
+                    const uint32_t scores = lanes + (n & 1) * kRows + row0;
+                    uint32_t bad = 0;
+                    if (masked) {          // values that are not finite, of keys that some row may not see
+                        if (!(ok = mbar_wait_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                        bad = sh.odd[n & 1][key];
+                    }
+                    // the product before has read P, and O holds the stream's tiles up to it
+                    if (uses > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[stream]), (uses - 1) & 1, a.wait_ns, abort_flag))) break;
+                    // its outputs of the item before have been read
+                    if (NB == 1 && fresh && items > 0 && !(ok = mbar_wait_warp(bar(sh.read[stream]), (items - 1) & 1, a.wait_ns, abort_flag))) break;
+                    uint32_t see0 = 0xffffu, see1 = 0xffffu;       // rows of the two runs that see this thread's key
+                    if (masked) {
+                        see0 = sees_of(&a, &d, row0 + 16 * gi, quarter * 32);
+                        see1 = sees_of(&a, &d, row0 + 16 * gi + 32, quarter * 32);
+                    }
+                    bool again = fresh;
+                    while (16 * gi < n_rows) {
                         if (again) {
                             // ---- new references: the largest logits so far; what is summed is scaled
-                            if (NB == 1 && n > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[pb ^ 1]), (((n + 1) >> 1) - 1) & 1, a.wait_ns, abort_flag))) break;
                             tc_fence_after_sync();
-                            // (with 64 rows the two halves are used in turn: nobody waits here for those who still read the last one)
-                            const int turned = NB == 1 ? 64 * (turn & 1) : 0;
-                            const float* old_ref = sh.minus_ref[(refs >> b) & 1];
-                            float* new_ref = sh.minus_ref[((refs >> b) & 1) ^ 1];
-                            {
+#pragma unroll 1
+                            for (int c = gi; c < 4; c += 2) {
+                                const uint32_t see = c == gi ? see0 : see1;
                                 uint32_t s[16];
                                 float x[16];
                                 tmem_ld_32x16(scores + 16 * c, s);
@@ -386,35 +398,36 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? __uint_as_float(s[e]) * a.scale_log2e : -CUDART_INF_F;
                                 const float top = largest_across_lanes(x, lane);
-                                if (!(lane & 1)) sh.most[quarter][turned + 16 * c + (lane >> 1)] = top;
+                                if (!(lane & 1)) sh.most[quarter][64 * stream + 16 * c + (lane >> 1)] = top;
                             }
                             if (!(ok = meet())) break;
-                            const int r = 16 * c + (lane & 15);
-                            {
-                                const float old = first ? -CUDART_INF_F : -old_ref[r];
-                                float now = fmaxf(fmaxf(fmaxf(sh.most[0][turned + r], sh.most[1][turned + r]), fmaxf(sh.most[2][turned + r], sh.most[3][turned + r])), old);
+#pragma unroll 1
+                            for (int c = gi; c < 4; c += 2) {
+                                const int r = 64 * stream + 16 * c + (lane & 15);
+                                const float old = fresh ? -CUDART_INF_F : -sh.minus_ref[ref_at][r];
+                                float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])), old);
                                 now = fmaxf(now, -kNothing);              // of a row that has seen nothing: below every logit
-                                if (lane < 16) new_ref[r] = -now;         // (every warp of the group writes the same)
+                                if (lane < 16) sh.minus_ref[ref_at ^ 1][r] = -now;         // (every warp of the group writes the same)
                                 const float alpha = exp2_fast(old - now);
 #pragma unroll 1
-                                for (uint32_t at = L::kO; !first && at <= L::kSum; at += L::kSum - L::kO) {
+                                for (uint32_t at = L::kO; !fresh && at <= L::kSum; at += L::kSum - L::kO) {
                                     uint32_t o[16];
-                                    tmem_ld_32x16(lanes + at + 16 * c, o);
+                                    tmem_ld_32x16(lanes + at + 64 * stream + 16 * c, o);
                                     tmem_ld_wait();
 #pragma unroll
                                     for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * __shfl_sync(0xffffffffu, alpha, e));
-                                    tmem_st_32x16(lanes + at + 16 * c, o);
+                                    tmem_st_32x16(lanes + at + 64 * stream + 16 * c, o);
                                 }
                             }
                             tmem_st_wait();
                             __syncwarp();
-                            refs ^= 1u << b;
-                            ++turn;
+                            ref_at ^= 1u;
                         }
-                        // ---- P, and whether a logit passed its reference
-                        const float* ref = sh.minus_ref[(refs >> b) & 1];
-                        float most[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-                        {
+                        // ---- P, and whether a logit passed its reference (the second run may have no row, and is worked out all the same)
+                        const float* ref = sh.minus_ref[ref_at] + 64 * stream;
+                        float most = -CUDART_INF_F;
+#pragma unroll 1
+                        for (int c = gi; c < 4; c += 2) {
                             uint32_t s[16];
                             float x[16];
                             tmem_ld_32x16(scores + 16 * c, s);
@@ -428,28 +441,28 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                 x[e + 3] = fmaf(__uint_as_float(s[e + 3]), a.scale_log2e, r.w);
                             }
                             if (masked) {
+                                const uint32_t see = c == gi ? see0 : see1;
 #pragma unroll
                                 for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? x[e] : -CUDART_INF_F;
                                 if (bad)
 #pragma unroll 1
                                     for (int e = 0; e < 16; ++e)
-                                        if ((see >> e) & 1u) atomicOr(&sh.spoilt[item & 1][16 * c + e], bad);
+                                        if ((see >> e) & 1u) atomicOr(&sh.spoilt[L::spoilt_at(d.item, row0 + 16 * c + e)], bad);
                             }
+                            float top[4] = {most, x[0], x[1], x[2]};
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) most[e & 3] = fmaxf(most[e & 3], x[e]);
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) x[e] = exp2_fast(x[e]);
+                            for (int e = 3; e < 16; ++e) top[e & 3] = fmaxf(top[e & 3], x[e]);
+                            most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                             uint32_t p[8];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(x[2 * e], x[2 * e + 1]));
-                            const uint32_t row = sm + L::kP + pb * kHalf + key * 128;
-                            const int piece = 2 * (c & 3);
-                            sts128(row + ((piece ^ (key & 7)) << 4), p[0], p[1], p[2], p[3]);
-                            sts128(row + (((piece + 1) ^ (key & 7)) << 4), p[4], p[5], p[6], p[7]);
+                            for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(exp2_fast(x[2 * e]), exp2_fast(x[2 * e + 1])));
+                            const uint32_t row = sm + L::kP + stream * kHalf + key * 128;
+                            sts128(row + (((2 * c) ^ (key & 7)) << 4), p[0], p[1], p[2], p[3]);
+                            sts128(row + (((2 * c + 1) ^ (key & 7)) << 4), p[4], p[5], p[6], p[7]);
                         }
                         if (again) break;
-                        const bool change = __any_sync(0xffffffffu, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) > kSlack);
-                        int* flag = sh.flag[(n * NB + b) & 3][group];
+                        const bool change = __any_sync(0xffffffffu, most > kSlack);
+                        int* flag = sh.flag[uses & 3][group];
                         if (lane == 0) flag[quarter] = change;
                         if (!(ok = meet())) break;
                         const int4 flags = *reinterpret_cast<const int4*>(flag);
@@ -457,63 +470,94 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         again = true;
                     }
                     if (!ok) break;
+                    const bool mine = left == 0, done = left <= (NB == 1 ? 1 : 0);       // whether this stream writes the item, has its last tile of it
+                    if (done && lane == 0 && quarter == 0) sh.ref_at[group] = ref_at;
                     fence_proxy_async_smem();
                     tc_fence_before_sync();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(bar(sh.p_full[pb]));
-                    if (b == 1) ++uses1;
-                }
-                if (!ok) break;
-                if (lane == 0) mbar_arrive(bar(sh.s_free[n & 1]));
-                if (!last) continue;          // (the CTA's last tile is the last of its part)
-                // ---- end of the item or of the piece
-                const int used0 = NB == 1 ? (n + 2) >> 1 : n + 1, used1 = NB == 1 ? (n + 1) >> 1 : uses1;
-                if (!(ok = mbar_wait_warp(bar(sh.pv_done[0]), (used0 - 1) & 1, a.wait_ns, abort_flag))) break;
-                if (used1 > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[1]), (used1 - 1) & 1, a.wait_ns, abort_flag))) break;
-                tc_fence_after_sync();
-                // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j
-                const int at = quarter * 32 + lane, channel = (at & ~31) + 4 * (lane & 7) + (lane >> 3);
-                const bool whole = d.begins && d.ends;
-                float* dst = parts + (d.begins ? slot_floats(kRows, D) : 0);
-                const RowBlock rows = row_block(a, d.rb * kRows);
+                    if (lane == 0) {
+                        mbar_arrive(bar(sh.p_full[stream]));
+                        mbar_arrive(bar(sh.s_free[n & 1]));
+                    }
+                    ++uses;
+                    if (done) ++items;
+                    if (mine) {
+                        // ---- end of the item or of the piece
+                        const bool two = NB == 1 && d.index > 0;       // the other stream has a part of it
+                        const int other = stream ^ 1;
+                        if (!(ok = mbar_wait_warp(bar(sh.pv_done[stream]), (uses - 1) & 1, a.wait_ns, abort_flag))) break;
+                        // (tile n - 1 was the other's ((n - 1) / 2 + 1)-th)
+                        if (two && !(ok = mbar_wait_warp(bar(sh.pv_done[other]), ((n - 1) >> 1) & 1, a.wait_ns, abort_flag))) break;
+                        tc_fence_after_sync();
+                        // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j
+                        const int at = quarter * 32 + lane, channel = (at & ~31) + 4 * (lane & 7) + (lane >> 3);
+                        const bool whole = d.begins && d.ends;
+                        float* dst = parts + (d.begins ? slot_floats(kRows, D) : 0);
+                        const RowBlock rows = row_block(a, d.rb * kRows);
 #pragma unroll 1
-                for (int c = group; 16 * c < n_rows; c += kGroups) {
-                    // where the run's rows go, a row a lane: index of (row, head) in o, -1 for none; whether it is on
-                    const int r = 16 * c + (lane & 15);
-                    const Row w = row_of(a, rows, r);
-                    const int h = d.kvh * a.share + w.sub, row = d.row0 + w.tok;
-                    int place = -1;
-                    if (w.tok < d.n_rows) place = row * a.n_q + h;
-                    const bool on = place >= 0 && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, row, h / a.hpg));
-                    const uint32_t spoilt = sh.spoilt[item & 1][r], on_bits = __ballot_sync(0xffffffffu, on);
+                        for (int c = gi; 16 * c < n_rows && c < 4; c += 2) {
+                            // where the run's rows go, a row a lane: index of (row, head) in o, -1 for none; whether it is on; what its two parts weigh
+                            const int r = row0 + 16 * c + (lane & 15);
+                            const Row w = row_of(a, rows, r);
+                            const int h = d.kvh * a.share + w.sub, row = d.row0 + w.tok;
+                            const int place = w.tok < d.n_rows ? row * a.n_q + h : -1;
+                            const bool on = place >= 0 && (!a.mask_bits || wide_mask_bit(a.mask_bits, a.words, row, h / a.hpg));
+                            const uint32_t on_bits = __ballot_sync(0xffffffffu, on), spoilt = sh.spoilt[L::spoilt_at(d.item, r)];
+                            float top = -sh.minus_ref[ref_at][64 * stream + 16 * c + (lane & 15)], by = 1.f, by_other = 0.f;
+                            if (two) {
+                                const float that = -sh.minus_ref[sh.ref_at[2 * other + gi]][64 * other + 16 * c + (lane & 15)], most = fmaxf(top, that);
+                                by = exp2_fast(top - most);
+                                by_other = exp2_fast(that - most);
+                                top = most;
+                            }
 #pragma unroll 1
-                    for (int e0 = 0; e0 < 16; e0 += 4) {
-                        uint32_t o[4], l[4];     // outputs, sums of P (the same in all lanes)
-                        tmem_ld_32x4(lanes + L::kO + 16 * c + e0, o);
-                        tmem_ld_32x4(lanes + L::kSum + 16 * c + e0, l);
-                        tmem_ld_wait();
+                            for (int e0 = 0; e0 < 16; e0 += 4) {
+                                uint32_t o[4], l[4], o2[4], l2[4];     // outputs, sums of P (the same in all lanes)
+                                tmem_ld_32x4(lanes + L::kO + 64 * stream + 16 * c + e0, o);
+                                tmem_ld_32x4(lanes + L::kSum + 64 * stream + 16 * c + e0, l);
+                                if (two) {
+                                    tmem_ld_32x4(lanes + L::kO + 64 * other + 16 * c + e0, o2);
+                                    tmem_ld_32x4(lanes + L::kSum + 64 * other + 16 * c + e0, l2);
+                                }
+                                tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int to = __shfl_sync(0xffffffffu, place, e0 + e);
-                            const uint32_t bad_groups = __shfl_sync(0xffffffffu, spoilt, e0 + e);
-                            const float sum = __uint_as_float(l[e]), x = (bad_groups >> (channel / G)) & 1u ? CUDART_NAN_F : __uint_as_float(o[e]);
-                            if (at >= D || to < 0) continue;
-                            if (whole) {
-                                a.o[static_cast<size_t>(to) * D + channel] = __float2bfloat16_rn((on_bits >> (e0 + e)) & 1u && sum != 0.f ? __fdividef(x, sum) : 0.f);
-                            } else {
-                                const int rr = 16 * c + e0 + e;
-                                dst[rr * D + channel] = x;
-                                // (a row that has seen nothing has no weight among its other pieces)
-                                if (at == 0)
-                                    *reinterpret_cast<float2*>(dst + kRows * D + 2 * rr) = make_float2(sum == 0.f ? -CUDART_INF_F : -sh.minus_ref[(refs >> (c >> 2)) & 1][rr], sum);
+                                for (int e = 0; e < 4; ++e) {
+                                    const int to = __shfl_sync(0xffffffffu, place, e0 + e);
+                                    const uint32_t bad_groups = __shfl_sync(0xffffffffu, spoilt, e0 + e);
+                                    const float m = __shfl_sync(0xffffffffu, top, e0 + e);
+                                    float x = __uint_as_float(o[e]), sum = __uint_as_float(l[e]);
+                                    if (two) {
+                                        const float f = __shfl_sync(0xffffffffu, by, e0 + e), f2 = __shfl_sync(0xffffffffu, by_other, e0 + e);
+                                        x = fmaf(__uint_as_float(o2[e]), f2, x * f);
+                                        sum = fmaf(__uint_as_float(l2[e]), f2, sum * f);
+                                    }
+                                    if ((bad_groups >> (channel / G)) & 1u) x = CUDART_NAN_F;
+                                    if (at >= D || to < 0) continue;
+                                    if (whole) {
+                                        a.o[static_cast<size_t>(to) * D + channel] = __float2bfloat16_rn((on_bits >> (e0 + e)) & 1u && sum != 0.f ? __fdividef(x, sum) : 0.f);
+                                    } else {
+                                        const int rr = row0 + 16 * c + e0 + e;
+                                        dst[rr * D + channel] = x;
+                                        // (a row that has seen nothing has no weight among its other pieces)
+                                        if (at == 0) *reinterpret_cast<float2*>(dst + kRows * D + 2 * rr) = make_float2(sum == 0.f ? -CUDART_INF_F : m, sum);
+                                    }
+                                }
                             }
                         }
+                        if (!(ok = meet())) break;       // all have read what is cleared now
+                        for (int c = gi; c < 4; c += 2)
+                            if (quarter == 0 && lane < 16) sh.spoilt[L::spoilt_at(d.item, row0 + 16 * c + lane)] = 0;
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (NB == 1 && lane == 0) {
+                            mbar_arrive(bar(sh.read[stream]));
+                            if (two) mbar_arrive(bar(sh.read[other]));
+                        }
                     }
+                } else {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(sh.s_free[n & 1]));
                 }
-                ++item;
-                for (int r = quarter * 32 + lane; r < kRows; r += 128)      // (nobody reads what the item before left any more)
-                    if (((r >> 4) & 3) == group) sh.spoilt[item & 1][r] = 0;
-                tc_fence_before_sync();
                 if (final) break;
             }
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
@@ -522,6 +566,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             Cursor k = sh.start;
             const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
             bool ok = true, first = true;
+            int index = 0, item = 0;
             int first_blk = k.blk, pt_first = -1000000, pt = -1, pt_next = -1;
             for (int n = 0;; ++n) {
                 const int st = n % kRing, nb = min(kTile, k.end - k.blk), from = k.blk >> sub_shift, to = (k.blk + nb - 1) >> sub_shift;
@@ -559,6 +604,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     d.seq = k.seq, d.kvh = k.kvh, d.rb = k.rb, d.row0 = info.x, d.n_rows = info.y, d.len = info.z;
                     d.item_rows = min(kRows, info.y * a.share - k.rb * kRows), d.rows_a_block = kRows;
                     d.begins = begins, d.ends = ends, d.final = final;
+                    d.index = min(index, 2), d.item = item, d.left = last ? 0 : k.end - (k.blk + nb) <= kTile ? 1 : 2;
                     mbar_arrive_expect_tx(bar(sh.ring_full[st]), __popc(present) * kSB);
                 }
                 __syncwarp();
@@ -579,6 +625,11 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 }
                 if (final) break;
                 first = last;
+                ++index;
+                if (last) {
+                    index = 0;
+                    ++item;
+                }
                 if (last) {
                     if (next.seq != k.seq) pt_first = -1000000;
                     first_blk = next.blk;
@@ -602,7 +653,14 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                   i > 0 ? 1u : 0u);
                     umma_commit(bar(sh.k_free));
                     umma_commit(bar(sh.s_full[n & 1]));
-                    if (sh.tiles[n % kDescs].final) break;
+                    if (sh.tiles[n % kDescs].final) {
+                        if (NB == 1) {      // the stream that waits for the next tile learns that there is none, once it is done with its last one
+                            if (n > 0 && !(ok = mbar_wait_asleep(bar(sh.s_free[(n + 1) & 1]), ((n - 1) >> 1) & 1, a.wait_ns, abort_flag))) break;
+                            *static_cast<volatile int*>(&sh.n_tiles) = n + 1;
+                            mbar_arrive(bar(sh.s_full[(n + 1) & 1]));
+                        }
+                        break;
+                    }
                 }
                 if (!ok) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
             }
@@ -610,30 +668,30 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             // ------------------------------------------------------------------------ O^T += V^T P^T
             if (lane == 0) {
                 bool ok = true;
-                int uses1 = 0;
+                int uses[2] = {0, 0};
                 const uint64_t ones = desc_mn(sm + L::kOnesAt, 1024);
                 for (int n = 0; ok; ++n) {
                     if (!(ok = mbar_wait_asleep(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
                     // (heads of 64: the upper 64 lanes take whatever lies behind the tile, and nobody reads them)
                     const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf);
                     const Tile& d = sh.tiles[n % kDescs];
-                    const bool first = d.first, final = d.final;
+                    const bool fresh = d.index < (NB == 1 ? 2 : 1), final = d.final;
                     const int blocks = (d.item_rows + 63) >> 6;
+#pragma unroll 1
                     for (int b = 0; b < blocks; ++b) {
-                        const int pb = NB == 1 ? n & 1 : b;
-                        if (!(ok = mbar_wait_asleep(bar(sh.p_full[pb]), (NB == 1 ? n >> 1 : b == 0 ? n : uses1) & 1, a.wait_ns, abort_flag))) break;
-                        if (b == 1) ++uses1;
+                        const int stream = NB == 1 ? n & 1 : b;
+                        if (!(ok = mbar_wait_asleep(bar(sh.p_full[stream]), (stream ? uses[1]++ : uses[0]++) & 1, a.wait_ns, abort_flag))) break;
                         tc_fence_after_sync();
-                        const uint64_t pd = desc_mn(sm + L::kP + pb * kHalf, kHalf);
+                        const uint64_t pd = desc_mn(sm + L::kP + stream * kHalf, kHalf);
 #pragma unroll
                         for (int i = 0; i < kKeys / 16; ++i)
-                            umma_bf16(tmem + L::kO + 64 * b, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(64, true), first && i == 0 ? 0u : 1u);
+                            umma_bf16(tmem + L::kO + 64 * stream, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(64, true), fresh && i == 0 ? 0u : 1u);
                         // the sums of P over the keys: ones in V's place
 #pragma unroll
                         for (int i = 0; i < kKeys / 16; ++i)
-                            umma_bf16(tmem + L::kSum + 64 * b, ones, pd + i * (2048 >> 4), idesc(64, true), first && i == 0 ? 0u : 1u);
+                            umma_bf16(tmem + L::kSum + 64 * stream, ones, pd + i * (2048 >> 4), idesc(64, true), fresh && i == 0 ? 0u : 1u);
                         if (b + 1 == blocks) umma_commit(bar(sh.v_free[n & 1]));
-                        umma_commit(bar(sh.pv_done[pb]));
+                        umma_commit(bar(sh.pv_done[stream]));
                     }
                     if (final) break;
                 }
