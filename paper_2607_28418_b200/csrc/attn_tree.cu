@@ -129,6 +129,24 @@ __device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&r)[4]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
 }
 
+// By one lane of a whole, converged warp.
+__device__ __forceinline__ void umma_bf16_elect(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void umma_commit_elect(uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+        : "memory");
+}
+
 // Bit e: query row r0 + e of the tile's item sees the key key0 + lane of the tile.  Lane e gets the bits of row e for the 32 keys, and then
 // all lanes get each row's.  Out of line: few tiles have keys that not every row sees.
 __device__ __noinline__ uint32_t sees_of(const TreeArgs* a, const Tile* d, int r0, int key0) {
@@ -639,64 +657,64 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp == kScoreWarp) {
             // ------------------------------------------------------------------------ S^T = K Q^T
-            if (lane == 0) {
-                bool ok = true;
-                for (int n = 0;; ++n) {
-                    if (!(ok = mbar_wait_asleep(bar(sh.k_full), n & 1, a.wait_ns, abort_flag))) break;
-                    if (n >= 2 && !(ok = mbar_wait_asleep(bar(sh.s_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
-                    tc_fence_after_sync();
-                    const uint64_t kd = umma_desc_sw128(sm + L::kK), qd = umma_desc_sw128(sm + L::kQ);
-                    const uint32_t shape = NB == 2 && sh.tiles[n % kDescs].item_rows <= 64 ? idesc(64, false) : idesc(kRows, false);
+            // (The whole warp walks the loop and one lane is elected for each instruction: the operands, which the instruction takes from uniform
+            // registers, are then computed there.  By lane 0 alone a product took 100 clocks to issue, twice its own time.)
+            bool ok = true;
+            for (int n = 0;; ++n) {
+                if (!(ok = mbar_wait_asleep_warp(bar(sh.k_full), n & 1, a.wait_ns, abort_flag))) break;
+                if (n >= 2 && !(ok = mbar_wait_asleep_warp(bar(sh.s_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
+                tc_fence_after_sync();
+                const uint64_t kd = umma_desc_sw128(sm + L::kK), qd = umma_desc_sw128(sm + L::kQ);
+                const uint32_t shape = NB == 2 && sh.tiles[n % kDescs].item_rows <= 64 ? idesc(64, false) : idesc(kRows, false);
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i)
-                        umma_bf16(tmem + (n & 1) * kRows, kd + (i / 4) * (kHalf >> 4) + 2 * (i % 4), qd + (i / 4) * (kRows * 128 >> 4) + 2 * (i % 4), shape,
-                                  i > 0 ? 1u : 0u);
-                    umma_commit(bar(sh.k_free));
-                    umma_commit(bar(sh.s_full[n & 1]));
-                    if (sh.tiles[n % kDescs].final) {
-                        if (NB == 1) {      // the stream that waits for the next tile learns that there is none, once it is done with its last one
-                            if (n > 0 && !(ok = mbar_wait_asleep(bar(sh.s_free[(n + 1) & 1]), ((n - 1) >> 1) & 1, a.wait_ns, abort_flag))) break;
+                for (int i = 0; i < D / 16; ++i)
+                    umma_bf16_elect(tmem + (n & 1) * kRows, kd + (i / 4) * (kHalf >> 4) + 2 * (i % 4), qd + (i / 4) * (kRows * 128 >> 4) + 2 * (i % 4), shape,
+                                    i > 0 ? 1u : 0u);
+                umma_commit_elect(bar(sh.k_free));
+                umma_commit_elect(bar(sh.s_full[n & 1]));
+                if (sh.tiles[n % kDescs].final) {
+                    if (NB == 1) {      // the stream that waits for the next tile learns that there is none, once it is done with its last one
+                        if (n > 0 && !(ok = mbar_wait_asleep_warp(bar(sh.s_free[(n + 1) & 1]), ((n - 1) >> 1) & 1, a.wait_ns, abort_flag))) break;
+                        if (lane == 0) {
                             *static_cast<volatile int*>(&sh.n_tiles) = n + 1;
                             mbar_arrive(bar(sh.s_full[(n + 1) & 1]));
                         }
-                        break;
                     }
+                    break;
                 }
-                if (!ok) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
             }
+            if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         } else if (warp == kValueWarp) {
             // ------------------------------------------------------------------------ O^T += V^T P^T
-            if (lane == 0) {
-                bool ok = true;
-                int uses[2] = {0, 0};
-                const uint64_t ones = desc_mn(sm + L::kOnesAt, 1024);
-                for (int n = 0; ok; ++n) {
-                    if (!(ok = mbar_wait_asleep(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
-                    // (heads of 64: the upper 64 lanes take whatever lies behind the tile, and nobody reads them)
-                    const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf);
-                    const Tile& d = sh.tiles[n % kDescs];
-                    const bool fresh = d.index < (NB == 1 ? 2 : 1), final = d.final;
-                    const int blocks = (d.item_rows + 63) >> 6;
+            bool ok = true;
+            int uses[2] = {0, 0};
+            const uint64_t ones = desc_mn(sm + L::kOnesAt, 1024);
+            for (int n = 0; ok; ++n) {
+                if (!(ok = mbar_wait_asleep_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                // (heads of 64: the upper 64 lanes take whatever lies behind the tile, and nobody reads them)
+                const uint64_t vd = desc_mn(sm + L::kV + (n & 1) * L::kTileBytes, kHalf);
+                const Tile& d = sh.tiles[n % kDescs];
+                const bool fresh = d.index < (NB == 1 ? 2 : 1), final = d.final;
+                const int blocks = (d.item_rows + 63) >> 6;
 #pragma unroll 1
-                    for (int b = 0; b < blocks; ++b) {
-                        const int stream = NB == 1 ? n & 1 : b;
-                        if (!(ok = mbar_wait_asleep(bar(sh.p_full[stream]), (stream ? uses[1]++ : uses[0]++) & 1, a.wait_ns, abort_flag))) break;
-                        tc_fence_after_sync();
-                        const uint64_t pd = desc_mn(sm + L::kP + stream * kHalf, kHalf);
+                for (int b = 0; b < blocks; ++b) {
+                    const int stream = NB == 1 ? n & 1 : b;
+                    if (!(ok = mbar_wait_asleep_warp(bar(sh.p_full[stream]), (stream ? uses[1]++ : uses[0]++) & 1, a.wait_ns, abort_flag))) break;
+                    tc_fence_after_sync();
+                    const uint64_t pd = desc_mn(sm + L::kP + stream * kHalf, kHalf);
 #pragma unroll
-                        for (int i = 0; i < kKeys / 16; ++i)
-                            umma_bf16(tmem + L::kO + 64 * stream, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(64, true), fresh && i == 0 ? 0u : 1u);
-                        // the sums of P over the keys: ones in V's place
+                    for (int i = 0; i < kKeys / 16; ++i)
+                        umma_bf16_elect(tmem + L::kO + 64 * stream, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(64, true), fresh && i == 0 ? 0u : 1u);
+                    // the sums of P over the keys: ones in V's place
 #pragma unroll
-                        for (int i = 0; i < kKeys / 16; ++i)
-                            umma_bf16(tmem + L::kSum + 64 * stream, ones, pd + i * (2048 >> 4), idesc(64, true), fresh && i == 0 ? 0u : 1u);
-                        if (b + 1 == blocks) umma_commit(bar(sh.v_free[n & 1]));
-                        umma_commit(bar(sh.pv_done[stream]));
-                    }
-                    if (final) break;
+                    for (int i = 0; i < kKeys / 16; ++i)
+                        umma_bf16_elect(tmem + L::kSum + 64 * stream, ones, pd + i * (2048 >> 4), idesc(64, true), fresh && i == 0 ? 0u : 1u);
+                    if (b + 1 == blocks) umma_commit_elect(bar(sh.v_free[n & 1]));
+                    umma_commit_elect(bar(sh.pv_done[stream]));
                 }
-                if (!ok) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
+                if (final) break;
             }
+            if (!ok && lane == 0) atomicExch(a.timeout, WIDE_ERR_TIMEOUT);
         }
         __syncwarp();
     }
