@@ -9,6 +9,7 @@
 // depend on timing.
 #include <cuda.h>
 
+#include <algorithm>
 #include <atomic>
 
 #include "internal.h"
@@ -100,9 +101,11 @@ __device__ __forceinline__ void finish(const LinearArgs& a, long long t, int f, 
     }
 }
 
+// Stages such that two CTAs fit on an SM: with one, a cluster of four or eight often has to wait for SMs of its own (128 tokens, 4096 x 4096: 37
+// us with one, 22.5 with two; 48 tokens 24.6 and 18.4).
 template <int NT>
 struct Small {
-    static constexpr int kStages = 6, kStage = kABytes + NT * kBK * 2, kSmem = kStages * kStage + 1024;
+    static constexpr int kStages = NT == 16 ? 6 : NT == 32 ? 5 : NT == 64 ? 4 : 3, kStage = kABytes + NT * kBK * 2, kSmem = kStages * kStage + 1024;
 };
 
 // One tile of 128 channels and NT tokens a cluster.
@@ -131,6 +134,8 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
         prefetch_tmap(&tm_w);
         prefetch_tmap(&tm_x);
     }
+    grid_dep_wait();
+    // (Tensor memory is taken after the kernel before has ended and before the next may come: no two wait for each other's.)
     if (warp == 1) {
         tmem_alloc(smem_u32(&tmem_slot), kCols);
         tmem_relinquish();
@@ -143,7 +148,6 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
     const int tile = blockIdx.x / a.split, tile_n = tile % a.tiles_n, tile_t = tile / a.tiles_n;
     const int k0 = static_cast<int>(static_cast<long long>(a.nk) * rank / a.split), k1 = static_cast<int>(static_cast<long long>(a.nk) * (rank + 1) / a.split);
     grid_dep_launch();
-    grid_dep_wait();
 
     if (warp == 0) {
         if (lane == 0) {
@@ -234,6 +238,178 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
     if (warp == 1) tmem_dealloc(tmem, kCols);
 }
 
+// ------------------------------------------------------------------------------------------------ many tokens
+// Pairs of CTAs (cta_group::2) take tiles of 256 channels and 256 tokens: each brings 128 rows of both operands for a product that reads
+// the two SMs' shared memory, 7.8 bytes a kFLOP from L2, which 128 x 256 tiles of one SM exceed (they end at 1.0 PFLOP/s).  A CTA has its 128 channels
+// (TMEM lanes) of all 256 tokens in one of two accumulators, so the epilogue of a tile runs under the next one's products.  Persistent;
+// tiles go by bands of 16 token tiles, channels within them, so that a band's tokens stay in L2.
+constexpr int kPairStages = 6, kPairT = 256, kPairStage = 2 * kABytes;
+constexpr int kPairEpi = 8;                                     // epilogue warps: two for each quarter of the lanes
+constexpr int kPairThreads = 64 + 32 * kPairEpi;
+constexpr int kPairSmem = kPairStages * kPairStage + kPairEpi * 32 * 32 * 4 + 1024;
+constexpr int kBand = 16;
+
+// As tma_load_2d, the bytes counted by the even CTA's barrier of the pair (the same address with its rank cleared).
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* m, int c0, int c1, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar & 0xFEFFFFFFu), "r"(c0), "r"(c1)
+        : "memory");
+}
+__device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Arrives on the barrier at this address in both CTAs once the pair's products so far are done.
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(bar), "h"(static_cast<uint16_t>(3))
+        : "memory");
+}
+__device__ __forceinline__ void arrive_rank0(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(bar, 0)) : "memory");
+}
+
+__global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ LinearArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kPairStages + 4];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_word;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = static_cast<int>(cluster_rank());
+    uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const uint32_t full = smem_u32(bars), empty = smem_u32(bars + kPairStages), tfull = smem_u32(bars + 2 * kPairStages), tempty = smem_u32(bars + 2 * kPairStages + 2);
+    volatile int* abort_flag = &abort_word;
+    if (tid == 0) {
+        for (int s = 0; s < kPairStages; ++s) {
+            mbar_init(full + 8 * s, 1);
+            mbar_init(empty + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(tfull + 8 * s, 1);
+            mbar_init(tempty + 8 * s, 2 * kPairEpi);
+        }
+        abort_word = 0;
+        fence_barrier_init();
+        prefetch_tmap(&tm_w);
+        prefetch_tmap(&tm_x);
+    }
+    grid_dep_wait();
+    // (Tensor memory is taken after the kernel before has ended and before the next may come: no two wait for each other's.)
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();            // the other CTA's barriers and tensor memory are there
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    grid_dep_launch();
+    const int tiles_t = (a.T + kPairT - 1) / kPairT, tiles_n = (a.N + 2 * kM - 1) / (2 * kM);
+    const long long tiles = static_cast<long long>(tiles_t) * tiles_n;
+    const int pairs = gridDim.x >> 1;
+    struct At {
+        int t, n;
+    };
+    auto tile_at = [&](long long i) {
+        const long long per_band = static_cast<long long>(kBand) * tiles_n;
+        const int band = static_cast<int>(i / per_band), in = static_cast<int>(i - band * per_band);
+        const int wide = min(kBand, tiles_t - band * kBand);
+        return At{band * kBand + in % wide, in / wide};
+    };
+    bool ok = true;
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA: 128 rows of each operand
+        if (lane == 0) {
+            int it = 0;
+            for (long long i = blockIdx.x >> 1; i < tiles && ok; i += pairs) {
+                const At at = tile_at(i);
+                const int row_w = at.n * 2 * kM + rank * kM, row_x = at.t * kPairT + rank * (kPairT / 2);
+                for (int k = 0; k < a.nk; ++k, ++it) {
+                    const int s = it % kPairStages;
+                    if (!(ok = mbar_wait(empty + 8 * s, ((it / kPairStages) & 1) ^ 1u, a.wait_ns, abort_flag))) break;
+                    if (rank == 0) mbar_arrive_expect_tx(full + 8 * s, 2 * kPairStage);     // both CTAs' bytes
+                    const uint32_t to = smem_u32(base + s * kPairStage);
+                    tma_load_2d_pair(to, &tm_w, k * kBK, row_w, full + 8 * s);
+                    tma_load_2d_pair(to + kABytes, &tm_x, k * kBK, row_x, full + 8 * s);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ products, by the even CTA
+        if (rank == 0) {
+            int it = 0, n = 0;
+            for (long long i = blockIdx.x >> 1; i < tiles && ok; i += pairs, ++n) {
+                if (n >= 2 && !(ok = mbar_wait_warp(tempty + 8 * (n & 1), ((n >> 1) & 1) ^ 1u, a.wait_ns, abort_flag))) break;
+                tc_fence_after_sync();
+                for (int k = 0; k < a.nk; ++k, ++it) {
+                    const int s = it % kPairStages;
+                    if (!(ok = mbar_wait_warp(full + 8 * s, (it / kPairStages) & 1, a.wait_ns, abort_flag))) break;
+                    tc_fence_after_sync();
+                    const uint32_t from = smem_u32(base + s * kPairStage);
+                    const uint64_t wd = umma_desc_sw128(from), xd = umma_desc_sw128(from + kABytes);
+#pragma unroll
+                    for (int e = 0; e < kBK / 16; ++e)
+                        umma_bf16_pair(tmem + (n & 1) * kPairT, wd + 2 * e, xd + 2 * e, umma_idesc_bf16(2 * kM, kPairT), (k | e) ? 1u : 0u);
+                    umma_commit_pair(empty + 8 * s);
+                }
+                if (ok) umma_commit_pair(tfull + 8 * (n & 1));
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue: 32 channels of half of the tokens a warp
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        float* mine = reinterpret_cast<float*>(base + kPairStages * kPairStage) + (warp - 2) * 32 * 32;      // [token][channel]
+        int n = 0;
+        for (long long i = blockIdx.x >> 1; i < tiles; i += pairs, ++n) {
+            const At at = tile_at(i);
+            if (!(ok = mbar_wait_warp(tfull + 8 * (n & 1), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+            tc_fence_after_sync();
+            const int f = at.n * 2 * kM + rank * kM + quarter * 32 + (lane & 7) * 4;
+            float bias[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bias[e] = a.bias && f + e < a.N ? __bfloat162float(a.bias[f + e]) : 0.f;
+#pragma unroll 1
+            for (int c = half * (kPairT / 2); c < (half + 1) * (kPairT / 2); c += 32) {
+                uint32_t r[32];
+                tmem_ld_32x32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kPairT + c, r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) mine[e * 32 + lane] = __uint_as_float(r[e]);
+                __syncwarp();
+                const int t0 = at.t * kPairT + c;
+                if (f < a.N)
+#pragma unroll 2
+                    for (int e = lane >> 3; e < 32 && t0 + e < a.T; e += 4)
+                        finish(a, static_cast<long long>(t0) + e, f, *reinterpret_cast<const float4*>(mine + e * 32 + (lane & 7) * 4), bias);
+                __syncwarp();
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) arrive_rank0(tempty + 8 * (n & 1));
+        }
+    }
+    if (!ok && lane == 0) atomicExch(a.status, WIDE_ERR_TIMEOUT);
+    __syncwarp();
+    if (*abort_flag && tid == 0)
+        for (int i = 0; i < 64; ++i) __nanosleep(1000);   // copies in flight land before the shared memory is given up
+    tc_fence_before_sync();
+    __syncthreads();
+    cluster_arrive();
+    cluster_wait();            // no CTA leaves while the other may still reach into it
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
 // bf16 rows `stride` bytes apart, box [rows, 64 columns], 128-byte swizzle
 bool make_map(const wide_ctx* ctx, CUtensorMap* map, const void* base, long long rows, long long cols, long long stride, uint32_t box_rows) {
     typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -264,7 +440,8 @@ int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long
     const long long tiles = static_cast<long long>(a.tiles_n) * ((a.T + NT - 1) / NT);
     a.stream_weights = a.T <= NT;
     a.split = 1;
-    while (a.split < 8 && tiles * a.split < ctx->sm_count && a.nk / (2 * a.split) >= 4) a.split *= 2;
+    // CTAs for three quarters of the SMs at least, as long as each keeps 8 steps of K (one token, 4096 x 4096: 4 parts 16.4 us, 8 parts 18.4)
+    while (a.split < 8 && 4 * tiles * a.split < 3 * ctx->sm_count && a.nk / (2 * a.split) >= 8) a.split *= 2;
     if (tiles * a.split > 0x7fffffffLL) return WIDE_ERR_UNSUPPORTED_SHAPE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split));
@@ -281,6 +458,18 @@ int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long
     cfg.numAttrs = ctx->prof ? 1 : 2;
     WideLaunch l(ctx, s, "linear");
     WIDE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, linear_kernel<NT>, tm_w, tm_x, a));
+    return WIDE_OK;
+}
+
+int launch_pairs(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long xs, const void* w, int K) {
+    CUtensorMap tm_w, tm_x;
+    if (!make_map(ctx, &tm_w, w, a.N, K, 2LL * K, kM) || !make_map(ctx, &tm_x, x, a.T, K, 2 * xs, kPairT / 2)) return WIDE_ERR_CUDA;
+    static std::atomic<unsigned> set{0};
+    if (!allow_smem(ctx, linear_pair_kernel, kPairSmem, set)) return WIDE_ERR_CUDA;
+    const long long tiles = static_cast<long long>((a.T + kPairT - 1) / kPairT) * ((a.N + 2 * kM - 1) / (2 * kM));
+    const int pairs = static_cast<int>(std::min<long long>(tiles, ctx->sm_count / 2));
+    WideLaunch l(ctx, s, "linear_pair");
+    WIDE_CUDA_CHECK(wide_launch_after(ctx, linear_pair_kernel, dim3(2 * pairs), dim3(kPairThreads), kPairSmem, s, tm_w, tm_x, a));
     return WIDE_OK;
 }
 
@@ -305,5 +494,6 @@ int wide_launch_linear(wide_ctx* ctx, cudaStream_t s, const void* x, int T, int 
     if (T <= 16) return launch<16>(ctx, s, a, x, xs, w, K);
     if (T <= 32) return launch<32>(ctx, s, a, x, xs, w, K);
     if (T <= 64) return launch<64>(ctx, s, a, x, xs, w, K);
-    return launch<128>(ctx, s, a, x, xs, w, K);
+    if (T <= 128) return launch<128>(ctx, s, a, x, xs, w, K);
+    return launch_pairs(ctx, s, a, x, xs, w, K);
 }
