@@ -243,11 +243,64 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
 // the two SMs' shared memory, 7.8 bytes a kFLOP from L2, which 128 x 256 tiles of one SM exceed (they end at 1.0 PFLOP/s).  A CTA has its 128 channels
 // (TMEM lanes) of all 256 tokens in one of two accumulators, so the epilogue of a tile runs under the next one's products.  Persistent;
 // tiles go by bands of 16 token tiles, channels within them, so that a band's tokens stay in L2.
-constexpr int kPairStages = 6, kPairT = 256, kPairStage = 2 * kABytes;
+// Tiles of 128 tokens fill SMs that 256 leave idle (256 tokens, 4096 -> 6144: 34 us with 256, 30 with 128; 512, 4096 -> 4096: 32, 28).
 constexpr int kPairEpi = 8;                                     // epilogue warps: two for each quarter of the lanes
 constexpr int kPairThreads = 64 + 32 * kPairEpi;
-constexpr int kPairSmem = kPairStages * kPairStage + kPairEpi * 32 * 32 * 4 + 1024;
 constexpr int kBand = 16;
+template <int PT>
+struct Pair {
+    static constexpr int kStages = PT == 256 ? 6 : 8, kStage = kABytes + PT * kBK;     // (half of the tokens a CTA)
+    static constexpr int kSmem = kStages * kStage + kPairEpi * 32 * 32 * 4 + 1024;
+};
+
+// 32 tokens (from t on) of a warp's 32 channels, which lie in its shared memory as [token][channel]: a lane has channels f .. f + 3 of
+// every fourth token.  All eight together, so that loads and the activation's steps of eight overlap.
+__device__ __forceinline__ void finish_block(const LinearArgs& a, long long t, int f, const float* block, int lane, const float (&bias)[4]) {
+    float x[8][4];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float4 v = *reinterpret_cast<const float4*>(block + (4 * j + (lane >> 3)) * 32 + (lane & 7) * 4);
+        x[j][0] = v.x + bias[0], x[j][1] = v.y + bias[1], x[j][2] = v.z + bias[2], x[j][3] = v.w + bias[3];
+    }
+    if (a.act != WIDE_ACT_NONE) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[j][e] = activate(x[j][e], a.act);
+    }
+    const long long row = t + (lane >> 3);
+    if (a.out_f32) {
+        if (a.residual) {
+            const float* r = static_cast<const float*>(a.residual) + row * a.rs + f;
+            float4 z[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = *reinterpret_cast<const float4*>(r + 4 * j * a.rs);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j][0] += z[j].x, x[j][1] += z[j].y, x[j][2] += z[j].z, x[j][3] += z[j].w;
+        }
+        float* y = static_cast<float*>(a.y) + row * a.ys + f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(y + 4 * j * a.ys) = make_float4(x[j][0], x[j][1], x[j][2], x[j][3]);
+    } else {
+        if (a.residual) {
+            const __nv_bfloat16* r = static_cast<const __nv_bfloat16*>(a.residual) + row * a.rs + f;
+            uint2 z[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = *reinterpret_cast<const uint2*>(r + 4 * j * a.rs);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                x[j][0] += __uint_as_float(z[j].x << 16), x[j][1] += __uint_as_float(z[j].x & 0xFFFF0000u);
+                x[j][2] += __uint_as_float(z[j].y << 16), x[j][3] += __uint_as_float(z[j].y & 0xFFFF0000u);
+            }
+        }
+        __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + row * a.ys + f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(x[j][0], x[j][1]), q = __floats2bfloat162_rn(x[j][2], x[j][3]);
+            *reinterpret_cast<uint2*>(y + 4 * j * a.ys) = make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
+        }
+    }
+}
 
 // As tma_load_2d, the bytes counted by the even CTA's barrier of the pair (the same address with its rank cleared).
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* m, int c0, int c1, uint32_t bar) {
@@ -277,8 +330,10 @@ __device__ __forceinline__ void arrive_rank0(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(bar, 0)) : "memory");
 }
 
+template <int PT>
 __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ LinearArgs a) {
+    constexpr int kPairStages = Pair<PT>::kStages, kPairStage = Pair<PT>::kStage, kPairT = PT;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * kPairStages + 4];
     __shared__ uint32_t tmem_slot;
@@ -305,7 +360,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
     grid_dep_wait();
     // (Tensor memory is taken after the kernel before has ended and before the next may come: no two wait for each other's.)
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2u * PT) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before_sync();
@@ -388,10 +443,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                 for (int e = 0; e < 32; ++e) mine[e * 32 + lane] = __uint_as_float(r[e]);
                 __syncwarp();
                 const int t0 = at.t * kPairT + c;
-                if (f < a.N)
-#pragma unroll 2
+                if (f + 3 < a.N && t0 + 32 <= a.T) {
+                    finish_block(a, t0, f, mine, lane, bias);
+                } else if (f < a.N) {
+#pragma unroll 1
                     for (int e = lane >> 3; e < 32 && t0 + e < a.T; e += 4)
                         finish(a, static_cast<long long>(t0) + e, f, *reinterpret_cast<const float4*>(mine + e * 32 + (lane & 7) * 4), bias);
+                }
                 __syncwarp();
             }
             tc_fence_before_sync();
@@ -407,7 +465,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
     __syncthreads();
     cluster_arrive();
     cluster_wait();            // no CTA leaves while the other may still reach into it
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * PT) : "memory");
 }
 
 // bf16 rows `stride` bytes apart, box [rows, 64 columns], 128-byte swizzle
@@ -461,15 +519,20 @@ int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long
     return WIDE_OK;
 }
 
+template <int PT>
+long long pair_tiles(const LinearArgs& a) {
+    return static_cast<long long>((a.T + PT - 1) / PT) * ((a.N + 2 * kM - 1) / (2 * kM));
+}
+
+template <int PT>
 int launch_pairs(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long xs, const void* w, int K) {
     CUtensorMap tm_w, tm_x;
-    if (!make_map(ctx, &tm_w, w, a.N, K, 2LL * K, kM) || !make_map(ctx, &tm_x, x, a.T, K, 2 * xs, kPairT / 2)) return WIDE_ERR_CUDA;
+    if (!make_map(ctx, &tm_w, w, a.N, K, 2LL * K, kM) || !make_map(ctx, &tm_x, x, a.T, K, 2 * xs, PT / 2)) return WIDE_ERR_CUDA;
     static std::atomic<unsigned> set{0};
-    if (!allow_smem(ctx, linear_pair_kernel, kPairSmem, set)) return WIDE_ERR_CUDA;
-    const long long tiles = static_cast<long long>((a.T + kPairT - 1) / kPairT) * ((a.N + 2 * kM - 1) / (2 * kM));
-    const int pairs = static_cast<int>(std::min<long long>(tiles, ctx->sm_count / 2));
+    if (!allow_smem(ctx, linear_pair_kernel<PT>, Pair<PT>::kSmem, set)) return WIDE_ERR_CUDA;
+    const int pairs = static_cast<int>(std::min<long long>(pair_tiles<PT>(a), ctx->sm_count / 2));
     WideLaunch l(ctx, s, "linear_pair");
-    WIDE_CUDA_CHECK(wide_launch_after(ctx, linear_pair_kernel, dim3(2 * pairs), dim3(kPairThreads), kPairSmem, s, tm_w, tm_x, a));
+    WIDE_CUDA_CHECK(wide_launch_after(ctx, linear_pair_kernel<PT>, dim3(2 * pairs), dim3(kPairThreads), Pair<PT>::kSmem, s, tm_w, tm_x, a));
     return WIDE_OK;
 }
 
@@ -495,5 +558,9 @@ int wide_launch_linear(wide_ctx* ctx, cudaStream_t s, const void* x, int T, int 
     if (T <= 32) return launch<32>(ctx, s, a, x, xs, w, K);
     if (T <= 64) return launch<64>(ctx, s, a, x, xs, w, K);
     if (T <= 128) return launch<128>(ctx, s, a, x, xs, w, K);
-    return launch_pairs(ctx, s, a, x, xs, w, K);
+    // Rounds of the pairs; a tile of 128 tokens takes 0.65 to 0.8 of one of 256, not half, as it reads shared memory at twice the rate for its
+    // products (1024 tokens, 4096 -> 6144, three rounds of 128: 62 us, two of 256: 54).
+    const long long pairs = ctx->sm_count / 2, wide = (pair_tiles<256>(a) + pairs - 1) / pairs, narrow = (pair_tiles<128>(a) + pairs - 1) / pairs;
+    if (8 * narrow < 10 * wide) return launch_pairs<128>(ctx, s, a, x, xs, w, K);
+    return launch_pairs<256>(ctx, s, a, x, xs, w, K);
 }
