@@ -17,7 +17,10 @@
 // the codes lie, keys go out as 16-byte rows and values through transposing 8x8 stores; O's channels come out permuted within 32.
 //
 // Items are cut into equal pieces for the CTAs and joined as in wide_attn_cache (attn_plan.cuh).
+#include <cuda_fp16.h>
+
 #include <atomic>
+#include <type_traits>
 
 #include "cache.cuh"
 
@@ -39,7 +42,8 @@ constexpr int kDescs = 8;           // tiles that are known: the ring's, and at 
 constexpr int kUnpackWarps = 8, kSoftWarps = 16, kGroups = kSoftWarps / 4;
 constexpr int kLoadWarp = kUnpackWarps + kSoftWarps, kScoreWarp = kLoadWarp + 1, kValueWarp = kLoadWarp + 2, kWarps = kLoadWarp + 3;
 constexpr float kSlack = 8.f;
-constexpr int kOnes = 3 * 1024;      // bytes of ones: two blocks of 64 rows and two groups of 8 keys, each 1024 further on
+constexpr float kHigh = 7.f;         // log2 of a row's largest probability when its reference is set
+constexpr int kOnes = 1280, kOnesWide = 512;    // bytes of ones in fp16, in bf16
 constexpr float kNothing = 1e38f;    // minus the reference of a row that has seen nothing yet: a logit of any size passes it
 constexpr int kHalf = 16384;        // bytes of [128 keys][64 channels or rows]
 
@@ -56,14 +60,14 @@ struct Tile {                       // what the roles are told of a tile
     int first, last;                // of the item's part in this CTA
     int index, left, item;          // tiles of the part before this one; behind it (2: two or more); the part's number
     int masked;                     // not all rows see all 128 keys
-    int seq, kvh, rb, row0, n_rows, len;
+    int kvh, rb, row0, n_rows, len;
     int item_rows, rows_a_block;    // query rows of the item; of a whole one
     int begins, ends;               // whether the part has the item's first, last block
     int final;                      // the CTA's last tile
 };
 
 struct alignas(16) Shared {
-    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full[2], pv_done[2], read[2], meet[kGroups];
+    uint64_t ring_full[kMostRing], ring_empty[kMostRing], k_full, k_free, v_full[2], v_free[2], s_full[2], s_free[2], p_full[2], pv_done[2], read[2], meet[kGroups], q_meet;
     uint32_t tmem;
     int abort;
     int n_tiles;                    // of this CTA, once it is known
@@ -73,7 +77,10 @@ struct alignas(16) Shared {
     alignas(16) float minus_ref[2][128];        // of a stream's row, twice: the one in use and the next
     float most[4][128];             // of a stream's row, per warp of a group: the largest logit
     alignas(16) int flag[4][kGroups][4];        // [tile of the stream][group][warp]: a logit passed its reference
-    uint32_t odd[2][kKeys];         // sub-groups of a new token's values that are not finite (their values are 0 in the tile)
+    float key_by[4][kKeys];         // of a tile's key: what its products with q are taken times to be logits, in powers of two
+    uint8_t odd[4][kKeys];          // sub-groups of a new token's values that are not finite (their values are 0 in the tile)
+    alignas(8) uint8_t wide[4][kUnpackWarps];     // of a tile: whether a block's values (and probabilities) are bf16, not fp16
+    alignas(8) uint8_t q_wide[4][kUnpackWarps];   // of an item: whether queries that the warp brought do not fit fp16 (queries and keys are bf16 then)
     uint32_t spoilt[256];           // of a row: such sub-groups that it sees (for two items of 128 rows, or four of 64)
 };
 
@@ -83,7 +90,7 @@ struct Layout {
     static constexpr int kTileBytes = kBlocks * kHalf;                 // of unpacked keys, or values
     static constexpr int kRing = D == 128 && NB == 2 && G == 32 ? 2 : kMostRing;     // (no room for three)
     static constexpr int kQ = 0, kK = kQ + kBlocks * kRows * 128, kV = kK + kTileBytes, kP = kV + 2 * kTileBytes, kCodes = kP + 2 * kHalf,
-                         kOnesAt = (kCodes + kRing * kStage + 1023) & ~1023, kPlan = kOnesAt + kOnes;
+                         kOnesAt = kCodes + kRing * kStage, kPlan = kOnesAt + kOnes + kOnesWide;
     static constexpr int kPlanRoom = 227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512 < 16384
                                          ? (227 * 1024 - 1024 - kPlan - static_cast<int>(sizeof(Shared)) - 512) / 256 * 256 : 16384;
     static constexpr int kSmem = kPlan + kPlanRoom + 1024;
@@ -96,7 +103,17 @@ struct Layout {
 __device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t lbo) {
     return umma_desc_sw128(addr & ~0u) & ~(static_cast<uint64_t>(0x3FFF) << 16) | static_cast<uint64_t>(lbo >> 4) << 16;
 }
-__host__ __device__ constexpr uint32_t idesc(int n, bool mn_major) { return umma_idesc_bf16(128, n) | (mn_major ? (1u << 15) | (1u << 16) : 0u); }
+// the same where all elements are one number: groups of 8 rows 128 bytes apart
+__device__ __forceinline__ uint64_t desc_ones(uint32_t addr) {
+    return umma_desc_sw128(addr) & ~(static_cast<uint64_t>(0x3FFF) << 16 | static_cast<uint64_t>(0x3FFF) << 32) | static_cast<uint64_t>(128 >> 4) << 16 | static_cast<uint64_t>(128 >> 4) << 32;
+}
+// in less room, without a swizzle: matrices of 8 x 8 elements 16 bytes apart (a product reads them at half the speed)
+__device__ __forceinline__ uint64_t desc_ones_wide(uint32_t addr) {
+    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(1) << 16 | static_cast<uint64_t>(1) << 32 | static_cast<uint64_t>(1) << 46;
+}
+__host__ __device__ constexpr uint32_t idesc(int n, bool half, bool mn_major) {
+    return umma_idesc_bf16(128, n) & ~(half ? (1u << 7) | (1u << 10) : 0u) | (mn_major ? (1u << 15) | (1u << 16) : 0u);
+}
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
@@ -118,11 +135,28 @@ __device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st
 
 __device__ __forceinline__ __nv_bfloat162 as_bf162(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
 __device__ __forceinline__ uint32_t as_word(__nv_bfloat162 b) { return *reinterpret_cast<const uint32_t*>(&b); }
-// m + s n of the two codes in bits 0..3 and 16..19 of w
+__device__ __forceinline__ __half2 as_half2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
+__device__ __forceinline__ uint32_t as_word(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ uint32_t half_pair(float lo, float hi) { return as_word(__floats2half2_rn(lo, hi)); }
+__device__ __forceinline__ float low_of(uint32_t w) { return __uint_as_float(w << 16); }        // of two bf16 numbers
+__device__ __forceinline__ float high_of(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// m + s n in bf16 of the two codes in bits 0..3 and 16..19 of w
 __device__ __forceinline__ uint32_t unpack_two(uint32_t w, uint32_t s, uint32_t m) {
     const uint32_t high = (w & 0x000F000Fu) | 0x43004300u;       // 128 + n
     return as_word(__hfma2(__hsub2(as_bf162(high), as_bf162(0x43004300u)), as_bf162(s), as_bf162(m)));
 }
+// m + s n in fp16 of the two codes in bits 0..3 and 16..19, or, with s / 16 for s, in bits 4..7 and 20..23
+template <bool UPPER>
+__device__ __forceinline__ uint32_t unpack_half(uint32_t w, uint32_t s, uint32_t m) {
+    const uint32_t high = (w & (UPPER ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;       // 1024 + n, or 16 n
+    return as_word(__hfma2(__hsub2(as_half2(high), as_half2(0x64006400u)), as_half2(s), as_half2(m)));
+}
+__device__ __forceinline__ uint32_t sixteenth(uint32_t s) { return as_word(__hmul2(as_half2(s), as_half2(0x2C002C00u))); }
+// The exponent bits of x, so that 2^-e x is 2^8 to 2^9 and neither power leaves the normal numbers.
+__device__ __forceinline__ uint32_t exponent_of(float x) { return min(max(__float_as_uint(x) & 0x7F800000u, 9u << 23), 254u << 23); }
+__device__ __forceinline__ float times_to_256(uint32_t e) { return __uint_as_float((262u << 23) - e); }
+__device__ __forceinline__ float times_back(uint32_t e) { return __uint_as_float(e - (8u << 23)); }
 __device__ __forceinline__ bool not_finite(uint32_t word) { return (word & 0x7F80u) == 0x7F80u || (word & 0x7F800000u) == 0x7F800000u; }
 
 __device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&r)[4]) {
@@ -180,6 +214,84 @@ __device__ __forceinline__ float largest_across_lanes(float (&x)[16], int lane) 
     return fmaxf(x[0], __shfl_xor_sync(0xffffffffu, x[0], 1));
 }
 
+// The largest magnitude among eight bf16 numbers, as bits; of an infinity or a NaN: 0x7F80 or more.
+__device__ __forceinline__ uint32_t largest_bits(const uint4& v) {
+    const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+    return max(m & 0xFFFFu, m >> 16);
+}
+__device__ __forceinline__ uint32_t to_half(uint32_t w) { return half_pair(low_of(w), high_of(w)); }
+
+// Whether fp16 holds a sub-group's numbers well, from its word (step, minimum): s / 16 and what the values are rounded to.  `least`: the bits of the
+// smallest step; the largest is 2^10 and the minimum up to 2^14, so that no value is above 2^15.
+constexpr uint32_t kLeastKey = 0x3A80u, kLeastValue = 0x3900u;       // 2^-10: what is below fp16's normal numbers is 2^-18 of the key's largest; 2^-13: s / 16 is exact
+__device__ __forceinline__ bool fits_half(uint32_t w, uint32_t least) { return w == 0 || ((w & 0xFFFFu) - least < 0x4480u - least && (w & 0x7FFF0000u) < 0x46800000u); }
+
+// The words of a warp's block of which some do not fit, or whose tile has keys that not every row sees.  Out of line: few need it.  A key's are taken times
+// a power of two so that its largest number is 2^8 to 2^9 (the power goes into its logits).  Values' stay bf16 where one does not fit.  Values of
+// keys that are not there count as zeros, and those of new tokens that are not finite are noted instead.
+template <int NS>
+__device__ __noinline__ bool odd_words(Shared* sh, const Tile* d, uint32_t words, int n, int warp, bool here, bool wide_keys, float scale) {
+    const int lane = threadIdx.x & 31, key0 = (d->blk + warp) * 16;
+    uint32_t w[(NS + 1) / 2];
+    bool half = true;
+#pragma unroll
+    for (int i = 0; i < (NS + 1) / 2; ++i) {
+        const int x = 32 * i + lane, r = x / NS;
+        const bool mine = NS > 1 || lane < 16, writes = mine && x % NS == 0;
+        const uint32_t at = words + 4 * (mine ? x : 0), kw = lds32(at);
+        float top = fmaxf(fabsf(high_of(kw)), fabsf(fmaf(15.f, low_of(kw), high_of(kw))));
+#pragma unroll
+        for (int o = 1; o < NS; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const uint32_t e = exponent_of(top);
+        w[i] = lds32(at + 64 * NS);
+        __syncwarp();
+        if (mine && !wide_keys) sts32(at, half_pair(low_of(kw) * times_to_256(e), high_of(kw) * times_to_256(e)));
+        if (writes) sh->key_by[n & 3][warp * 16 + r] = wide_keys ? scale : times_back(e) * scale;
+        if (d->masked) {
+            const bool is = here && key0 + r < d->len, bad = mine && is && key0 + r >= d->len - d->n_rows && not_finite(w[i]);
+            if (!is || bad) w[i] = 0;
+            const uint32_t bits = __ballot_sync(0xffffffffu, bad);
+            if (writes) sh->odd[n & 3][warp * 16 + r] = (bits >> lane) & ((1u << NS) - 1u);
+        }
+        half = __all_sync(0xffffffffu, fits_half(w[i], kLeastValue)) && half;
+    }
+#pragma unroll
+    for (int i = 0; i < (NS + 1) / 2; ++i)
+        if (NS > 1 || lane < 16) sts32(words + 64 * NS + 4 * (32 * i + lane), half ? half_pair(low_of(w[i]), high_of(w[i])) : w[i]);
+    return half;
+}
+
+// A warp's block of keys in bf16: the form of the kernel's loop for fp16.
+template <int D, int G>
+__device__ __noinline__ void wide_keys_of(uint32_t codes, uint32_t words, uint32_t row, int kr, int kc) {
+    constexpr int kNS = D / G;
+#pragma unroll 1
+    for (int x = 0; x < D / 32; ++x) {          // channels 32 x + 8 kc ..
+        const uint32_t at = codes + (x >> 1) * 512 + (kr * 4 + kc) * 16 + (x & 1) * 8, lo = lds32(at), hi = lds32(at + 4), i = 32 * x / G;
+        const uint32_t w0 = lds32(words + (kr * kNS + i) * 4), w1 = lds32(words + ((kr + 8) * kNS + i) * 4), to = row + (x >> 1) * kHalf + (((4 * (x & 1) + kc) ^ kr) << 4);
+        const uint32_t s0 = __byte_perm(w0, 0, 0x1010), m0 = __byte_perm(w0, 0, 0x3232), s1 = __byte_perm(w1, 0, 0x1010), m1 = __byte_perm(w1, 0, 0x3232);
+        sts128(to, unpack_two(lo, s0, m0), unpack_two(lo >> 4, s0, m0), unpack_two(hi, s0, m0), unpack_two(hi >> 4, s0, m0));
+        sts128(to + 8 * 128, unpack_two(lo >> 8, s1, m1), unpack_two(lo >> 12, s1, m1), unpack_two(hi >> 8, s1, m1), unpack_two(hi >> 12, s1, m1));
+    }
+}
+
+// A warp's block of values in bf16: the form of the kernel's loop for fp16.
+template <int D, int G>
+__device__ __noinline__ void wide_values(uint32_t codes, uint32_t words, uint32_t row) {
+    constexpr int kNS = D / G;
+    const int lane = threadIdx.x & 31, t = lane & 3, token = (lane & 7) + 8 * (lane >> 4);
+    row += token * 128;
+#pragma unroll 1
+    for (int x = 0; x < D / 16; ++x) {          // channels 64 (x / 4) + 32 (x / 2 % 2) + 4 g + 2 (x % 2) ..
+        const int c = x >> 2, e = x & 3;
+        const uint32_t at = words + (2 * t * kNS + (64 * c + 32 * (e >> 1)) / G) * 4, v = lds32(codes + c * 512 + lane * 16 + 4 * e);
+        const uint32_t p0 = lds32(at), p1 = lds32(at + kNS * 4), p2 = lds32(at + 8 * kNS * 4), p3 = lds32(at + 9 * kNS * 4);
+        const uint32_t s0 = __byte_perm(p0, p1, 0x5410), m0 = __byte_perm(p0, p1, 0x7632), s1 = __byte_perm(p2, p3, 0x5410), m1 = __byte_perm(p2, p3, 0x7632);
+        const int piece = (e >> 1) * 4 + 2 * (e & 1) + ((lane >> 3) & 1);
+        store_transposed(row + c * kHalf + ((piece ^ (token & 7)) << 4), unpack_two(v, s0, m0), unpack_two(v >> 4, s0, m0), unpack_two(v >> 8, s1, m1), unpack_two(v >> 12, s1, m1));
+    }
+}
+
 template <int D, int G, int NB>
 __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_constant__ TreeArgs a) {
     using L = Layout<D, G, NB>;
@@ -209,12 +321,13 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             mbar_init(bar(sh.pv_done[i]), 1);
         }
         for (int i = 0; i < kGroups; ++i) mbar_init(bar(sh.meet[i]), 4);
+        mbar_init(bar(sh.q_meet), kUnpackWarps);
         sh.abort = 0;
         sh.n_tiles = 0x7fffffff;
         fence_barrier_init();
     }
     if (tid < 256) sh.spoilt[tid] = 0;
-    for (int i = tid; i < kOnes / 4; i += 32 * kWarps) reinterpret_cast<uint32_t*>(base + L::kOnesAt)[i] = 0x3F803F80u;
+    for (int i = tid; i < (kOnes + kOnesWide) / 4; i += 32 * kWarps) reinterpret_cast<uint32_t*>(base + L::kOnesAt)[i] = i < kOnes / 4 ? 0x3C003C00u : 0x3F803F80u;
     fence_proxy_async_smem();
 
     grid_dep_wait();
@@ -263,20 +376,24 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             const int kr = ((lane >> 2) & 1) * 4 + (lane >> 3), kc = lane & 3;     // key (and key + 8), 8-channel piece: no bank twice in a store
             const int t = lane & 3;
             bool ok = true;
+            int items = 0;
+            bool wide_keys = false;
             for (int n = 0;; ++n) {
                 const int st = n % kRing;
                 if (!(ok = mbar_wait_asleep_warp(bar(sh.ring_full[st]), (n / kRing) & 1, a.wait_ns, abort_flag))) break;
                 const Tile& d = sh.tiles[n % kDescs];
                 const bool here = warp < d.nb && ((d.present >> warp) & 1u);
-                const int key0 = (d.blk + warp) * 16;                               // of this warp's block
                 const uint32_t codes = sm + L::kCodes + st * L::kStage + warp * kSB, words = codes + 16 * D;
                 // the scores of the tile before have been made: K, and Q at the end of an item, may change
                 if (n > 0 && !(ok = mbar_wait_asleep_warp(bar(sh.k_free), (n - 1) & 1, a.wait_ns, abort_flag))) break;
                 if (d.first) {
+                    // ---- queries in fp16 where each eight neighbours are zeros or have their largest between 2^-9 (so that what falls below the type's normal
+                    // numbers is 2^-16 of it) and 2^14; one that is not leaves the item's queries and keys in bf16
                     const RowBlock rows = row_block(a, d.rb * kRows);
                     constexpr int kRowLanes = D / 8, kStep = 32 * kUnpackWarps / kRowLanes;      // a thread has 16 bytes of every kStep-th row
                     const int c = tid % kRowLanes, r0 = tid / kRowLanes;
                     uint4 v[kRows / kStep];
+                    bool odd = false;
 #pragma unroll
                     for (int i = 0; i < kRows / kStep; ++i) {
                         const Row w = row_of(a, rows, r0 + i * kStep);
@@ -286,11 +403,51 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     }
 #pragma unroll
                     for (int i = 0; i < kRows / kStep; ++i) {
+                        const uint32_t top = largest_bits(v[i]);
+                        odd |= top != 0 && top - 0x3B00u > 0x4680u - 0x3B00u;
+                    }
+                    odd = __any_sync(0xffffffffu, odd);
+                    if (lane == 0) {
+                        sh.q_wide[d.item & 3][warp] = odd;
+                        mbar_arrive(bar(sh.q_meet));
+                    }
+                    if (!(ok = mbar_wait_asleep_warp(bar(sh.q_meet), items++ & 1, a.wait_ns, abort_flag))) break;
+                    const uint2 odds = *reinterpret_cast<const uint2*>(sh.q_wide[d.item & 3]);
+                    wide_keys = (odds.x | odds.y) != 0;
+#pragma unroll
+                    for (int i = 0; i < kRows / kStep; ++i) {
                         const int r = r0 + i * kStep;
+                        if (!wide_keys) v[i] = make_uint4(to_half(v[i].x), to_half(v[i].y), to_half(v[i].z), to_half(v[i].w));
                         sts128(sm + L::kQ + (c >> 3) * (kRows * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), v[i].x, v[i].y, v[i].z, v[i].w);
                     }
                 }
-                if (here) {
+                // ---- the sub-groups' words become fp16, a word a lane
+                bool half = true;
+                {
+                    uint32_t kw[(kNS + 1) / 2], vw[(kNS + 1) / 2];
+                    bool fits = !d.masked && !wide_keys;
+#pragma unroll
+                    for (int i = 0; i < (kNS + 1) / 2; ++i) {
+                        const uint32_t at = words + 4 * (32 * i + (kNS > 1 ? lane : lane & 15));
+                        kw[i] = lds32(at);
+                        vw[i] = lds32(at + 64 * kNS);
+                        fits = fits && fits_half(kw[i], kLeastKey) && fits_half(vw[i], kLeastValue);
+                    }
+                    if (__all_sync(0xffffffffu, fits)) {
+#pragma unroll
+                        for (int i = 0; i < (kNS + 1) / 2; ++i) {
+                            const uint32_t at = words + 4 * (32 * i + (kNS > 1 ? lane : lane & 15));
+                            sts32(at, to_half(kw[i]));
+                            sts32(at + 64 * kNS, to_half(vw[i]));
+                        }
+                        if (lane < 16) sh.key_by[n & 3][warp * 16 + lane] = a.scale_log2e;
+                    } else {
+                        half = odd_words<kNS>(&sh, &d, words, n, warp, here, wide_keys, a.scale_log2e);
+                    }
+                    __syncwarp();
+                }
+                if (here && wide_keys) wide_keys_of<D, G>(codes, words, sm + L::kK + (warp * 16 + kr) * 128, kr, kc);
+                if (here && !wide_keys) {
                     const uint32_t row = sm + L::kK + (warp * 16 + kr) * 128;
 #pragma unroll 1
                     for (int c = 0; c < D / 64; ++c) {
@@ -300,52 +457,48 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                             const int i = (64 * c + 32 * h) / G;
                             const uint32_t w0 = lds32(words + (kr * kNS + i) * 4), w1 = lds32(words + ((kr + 8) * kNS + i) * 4);
                             const uint32_t s0 = __byte_perm(w0, 0, 0x1010), m0 = __byte_perm(w0, 0, 0x3232), s1 = __byte_perm(w1, 0, 0x1010), m1 = __byte_perm(w1, 0, 0x3232);
+                            const uint32_t t0 = sixteenth(s0), t1 = sixteenth(s1);
                             const uint32_t x = h ? v.z : v.x, y = h ? v.w : v.y;
                             const uint32_t at = row + c * kHalf + (((4 * h + kc) ^ kr) << 4);
-                            sts128(at, unpack_two(x, s0, m0), unpack_two(x >> 4, s0, m0), unpack_two(y, s0, m0), unpack_two(y >> 4, s0, m0));
-                            sts128(at + 8 * 128, unpack_two(x >> 8, s1, m1), unpack_two(x >> 12, s1, m1), unpack_two(y >> 8, s1, m1), unpack_two(y >> 12, s1, m1));
+                            sts128(at, unpack_half<false>(x, s0, m0), unpack_half<true>(x, t0, m0), unpack_half<false>(y, s0, m0), unpack_half<true>(y, t0, m0));
+                            sts128(at + 8 * 128, unpack_half<false>(x >> 8, s1, m1), unpack_half<true>(x >> 8, t1, m1), unpack_half<false>(y >> 8, s1, m1),
+                                   unpack_half<true>(y >> 8, t1, m1));
                         }
                     }
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(sh.k_full));
+                if (lane == 0) {
+                    sh.wide[n & 3][warp] = !half;
+                    mbar_arrive(bar(sh.k_full));
+                }
                 // ---- values
                 if (n >= 2 && !(ok = mbar_wait_asleep_warp(bar(sh.v_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                 {
-                    // In a tile whose new tokens not every row sees, and behind the end: values of keys that are not there count as zeros, and
-                    // those of new tokens that are not finite are noted instead.
-                    if (d.masked) {
-#pragma unroll 1
-                        for (int x = lane; x < 16 * kNS; x += 32) {
-                            const int r = x / kNS;
-                            const uint32_t at = words + 64 * kNS + 4 * x, w = lds32(at);
-                            const bool is = here && key0 + r < d.len, bad = is && key0 + r >= d.len - d.n_rows && not_finite(w);
-                            if (!is || bad) sts32(at, 0u);
-                            const uint32_t bits = __ballot_sync(__activemask(), bad);
-                            if (x % kNS == 0) sh.odd[n & 1][warp * 16 + r] = (bits >> (lane & ~(kNS - 1))) & ((1u << kNS) - 1u);
-                        }
-                        __syncwarp();
-                    }
                     const int token = (lane & 7) + 8 * (lane >> 4);                 // whose row this lane's address is, and which nibble
                     const uint32_t row = sm + L::kV + (n & 1) * L::kTileBytes + (warp * 16 + token) * 128, params = words + 64 * kNS + 2 * t * kNS * 4;
+                    if (half) {
 #pragma unroll 1
-                    for (int c = 0; c < D / 64; ++c) {
-                        const uint4 v = lds128(codes + 8 * D + c * 512 + lane * 16);
-                        uint32_t s0 = 0, m0 = 0, s1 = 0, m1 = 0;
+                        for (int c = 0; c < D / 64; ++c) {
+                            const uint4 v = lds128(codes + 8 * D + c * 512 + lane * 16);
+                            uint32_t s0 = 0, m0 = 0, s1 = 0, m1 = 0, t0 = 0, t1 = 0;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {                               // channels 64 c + 32 (e / 2) + 4 g + 2 (e % 2) ..
-                            if (e == 0 || (e == 2 && G == 32)) {                    // tokens 2t, 2t + 1, 2t + 8, 2t + 9
-                                const uint32_t at = params + (64 * c + 32 * (e >> 1)) / G * 4;
-                                const uint32_t p0 = lds32(at), p1 = lds32(at + kNS * 4), p2 = lds32(at + 8 * kNS * 4), p3 = lds32(at + 9 * kNS * 4);
-                                s0 = __byte_perm(p0, p1, 0x5410), m0 = __byte_perm(p0, p1, 0x7632);
-                                s1 = __byte_perm(p2, p3, 0x5410), m1 = __byte_perm(p2, p3, 0x7632);
+                            for (int e = 0; e < 4; ++e) {                               // channels 64 c + 32 (e / 2) + 4 g + 2 (e % 2) ..
+                                if (e == 0 || (e == 2 && G == 32)) {                    // tokens 2t, 2t + 1, 2t + 8, 2t + 9
+                                    const uint32_t at = params + (64 * c + 32 * (e >> 1)) / G * 4;
+                                    const uint32_t p0 = lds32(at), p1 = lds32(at + kNS * 4), p2 = lds32(at + 8 * kNS * 4), p3 = lds32(at + 9 * kNS * 4);
+                                    s0 = __byte_perm(p0, p1, 0x5410), m0 = __byte_perm(p0, p1, 0x7632);
+                                    s1 = __byte_perm(p2, p3, 0x5410), m1 = __byte_perm(p2, p3, 0x7632);
+                                    t0 = sixteenth(s0), t1 = sixteenth(s1);
+                                }
+                                const uint32_t x = e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
+                                const int piece = (e >> 1) * 4 + 2 * (e & 1) + ((lane >> 3) & 1);
+                                store_transposed(row + c * kHalf + ((piece ^ (token & 7)) << 4), unpack_half<false>(x, s0, m0), unpack_half<true>(x, t0, m0),
+                                                 unpack_half<false>(x >> 8, s1, m1), unpack_half<true>(x >> 8, t1, m1));
                             }
-                            const uint32_t x = e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w;
-                            const int piece = (e >> 1) * 4 + 2 * (e & 1) + ((lane >> 3) & 1);
-                            store_transposed(row + c * kHalf + ((piece ^ (token & 7)) << 4), unpack_two(x, s0, m0), unpack_two(x >> 4, s0, m0), unpack_two(x >> 8, s1, m1),
-                                             unpack_two(x >> 12, s1, m1));
                         }
+                    } else {
+                        wide_values<D, G>(codes + 8 * D, words + 64 * kNS, sm + L::kV + (n & 1) * L::kTileBytes + warp * 16 * 128);
                     }
                 }
                 fence_proxy_async_smem();
@@ -388,10 +541,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     const bool masked = d.masked, fresh = d.index < (NB == 1 ? 2 : 1);       // the stream's first tile of the item
                     const uint32_t scores = lanes + (n & 1) * kRows + row0;
                     uint32_t bad = 0;
-                    if (masked) {          // values that are not finite, of keys that some row may not see
-                        if (!(ok = mbar_wait_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
-                        bad = sh.odd[n & 1][key];
-                    }
+                    if (masked) bad = sh.odd[n & 3][key];          // values that are not finite, of keys that some row may not see
+                    const float by = sh.key_by[n & 3][key];
+                    const uint2 wides = *reinterpret_cast<const uint2*>(sh.wide[n & 3]);
+                    const bool plain = !masked && !(wides.x | wides.y);
                     // the product before has read P, and O holds the stream's tiles up to it
                     if (uses > 0 && !(ok = mbar_wait_warp(bar(sh.pv_done[stream]), (uses - 1) & 1, a.wait_ns, abort_flag))) break;
                     // its outputs of the item before have been read
@@ -414,7 +567,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                 tmem_ld_32x16(scores + 16 * c, s);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? __uint_as_float(s[e]) * a.scale_log2e : -CUDART_INF_F;
+                                for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? __uint_as_float(s[e]) * by : -CUDART_INF_F;
                                 const float top = largest_across_lanes(x, lane);
                                 if (!(lane & 1)) sh.most[quarter][64 * stream + 16 * c + (lane >> 1)] = top;
                             }
@@ -423,7 +576,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                             for (int c = gi; c < 4; c += 2) {
                                 const int r = 64 * stream + 16 * c + (lane & 15);
                                 const float old = fresh ? -CUDART_INF_F : -sh.minus_ref[ref_at][r];
-                                float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])), old);
+                                float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])) - kHigh, old);
                                 now = fmaxf(now, -kNothing);              // of a row that has seen nothing: below every logit
                                 if (lane < 16) sh.minus_ref[ref_at ^ 1][r] = -now;         // (every warp of the group writes the same)
                                 const float alpha = exp2_fast(old - now);
@@ -444,42 +597,53 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         // ---- P, and whether a logit passed its reference (the second run may have no row, and is worked out all the same)
                         const float* ref = sh.minus_ref[ref_at] + 64 * stream;
                         float most = -CUDART_INF_F;
+                        auto probabilities = [&](auto is_plain) {
+                            constexpr bool kPlain = decltype(is_plain)::value;
 #pragma unroll 1
-                        for (int c = gi; c < 4; c += 2) {
-                            uint32_t s[16];
-                            float x[16];
-                            tmem_ld_32x16(scores + 16 * c, s);
-                            tmem_ld_wait();
+                            for (int c = gi; c < 4; c += 2) {
+                                uint32_t s[16];
+                                float x[16];
+                                tmem_ld_32x16(scores + 16 * c, s);
+                                tmem_ld_wait();
 #pragma unroll
-                            for (int e = 0; e < 16; e += 4) {
-                                const float4 r = *reinterpret_cast<const float4*>(ref + 16 * c + e);
-                                x[e] = fmaf(__uint_as_float(s[e]), a.scale_log2e, r.x);
-                                x[e + 1] = fmaf(__uint_as_float(s[e + 1]), a.scale_log2e, r.y);
-                                x[e + 2] = fmaf(__uint_as_float(s[e + 2]), a.scale_log2e, r.z);
-                                x[e + 3] = fmaf(__uint_as_float(s[e + 3]), a.scale_log2e, r.w);
-                            }
-                            if (masked) {
-                                const uint32_t see = c == gi ? see0 : see1;
+                                for (int e = 0; e < 16; e += 4) {
+                                    const float4 r = *reinterpret_cast<const float4*>(ref + 16 * c + e);
+                                    x[e] = fmaf(__uint_as_float(s[e]), by, r.x);
+                                    x[e + 1] = fmaf(__uint_as_float(s[e + 1]), by, r.y);
+                                    x[e + 2] = fmaf(__uint_as_float(s[e + 2]), by, r.z);
+                                    x[e + 3] = fmaf(__uint_as_float(s[e + 3]), by, r.w);
+                                }
+                                if (!kPlain && masked) {
+                                    const uint32_t see = c == gi ? see0 : see1;
 #pragma unroll
-                                for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? x[e] : -CUDART_INF_F;
-                                if (bad)
+                                    for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? x[e] : -CUDART_INF_F;
+                                    if (bad)
 #pragma unroll 1
-                                    for (int e = 0; e < 16; ++e)
-                                        if ((see >> e) & 1u) atomicOr(&sh.spoilt[L::spoilt_at(d.item, row0 + 16 * c + e)], bad);
+                                        for (int e = 0; e < 16; ++e)
+                                            if ((see >> e) & 1u) atomicOr(&sh.spoilt[L::spoilt_at(d.item, row0 + 16 * c + e)], bad);
+                                }
+                                float top[4] = {most, x[0], x[1], x[2]};
+#pragma unroll
+                                for (int e = 3; e < 16; ++e) top[e & 3] = fmaxf(top[e & 3], x[e]);
+                                most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                                uint32_t p[8];
+#pragma unroll
+                                for (int e = 0; e < 16; ++e) x[e] = exp2_fast(x[e]);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) p[e] = half_pair(x[2 * e], x[2 * e + 1]);
+                                if (!kPlain && sh.wide[n & 3][key >> 4]) {
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(x[2 * e], x[2 * e + 1]));
+                                }
+                                const uint32_t row = sm + L::kP + stream * kHalf + key * 128;
+                                sts128(row + (((2 * c) ^ (key & 7)) << 4), p[0], p[1], p[2], p[3]);
+                                sts128(row + (((2 * c + 1) ^ (key & 7)) << 4), p[4], p[5], p[6], p[7]);
                             }
-                            float top[4] = {most, x[0], x[1], x[2]};
-#pragma unroll
-                            for (int e = 3; e < 16; ++e) top[e & 3] = fmaxf(top[e & 3], x[e]);
-                            most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                            uint32_t p[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) p[e] = as_word(__floats2bfloat162_rn(exp2_fast(x[2 * e]), exp2_fast(x[2 * e + 1])));
-                            const uint32_t row = sm + L::kP + stream * kHalf + key * 128;
-                            sts128(row + (((2 * c) ^ (key & 7)) << 4), p[0], p[1], p[2], p[3]);
-                            sts128(row + (((2 * c + 1) ^ (key & 7)) << 4), p[4], p[5], p[6], p[7]);
-                        }
+                        };
+                        if (plain) probabilities(std::true_type{});
+                        else probabilities(std::false_type{});
                         if (again) break;
-                        const bool change = __any_sync(0xffffffffu, most > kSlack);
+                        const bool change = __any_sync(0xffffffffu, most > kSlack + kHigh);
                         int* flag = sh.flag[uses & 3][group];
                         if (lane == 0) flag[quarter] = change;
                         if (!(ok = meet())) break;
@@ -619,7 +783,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     Tile& d = sh.tiles[n % kDescs];
                     d.blk = k.blk, d.nb = nb, d.present = present, d.first = first, d.last = last;
                     d.masked = present != (1u << kTile) - 1u || (k.blk + nb) * 16 > info.z - info.y;
-                    d.seq = k.seq, d.kvh = k.kvh, d.rb = k.rb, d.row0 = info.x, d.n_rows = info.y, d.len = info.z;
+                    d.kvh = k.kvh, d.rb = k.rb, d.row0 = info.x, d.n_rows = info.y, d.len = info.z;
                     d.item_rows = min(kRows, info.y * a.share - k.rb * kRows), d.rows_a_block = kRows;
                     d.begins = begins, d.ends = ends, d.final = final;
                     d.index = min(index, 2), d.item = item, d.left = last ? 0 : k.end - (k.blk + nb) <= kTile ? 1 : 2;
@@ -665,7 +829,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 if (n >= 2 && !(ok = mbar_wait_asleep_warp(bar(sh.s_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                 tc_fence_after_sync();
                 const uint64_t kd = umma_desc_sw128(sm + L::kK), qd = umma_desc_sw128(sm + L::kQ);
-                const uint32_t shape = NB == 2 && sh.tiles[n % kDescs].item_rows <= 64 ? idesc(64, false) : idesc(kRows, false);
+                const uint2 wides = *reinterpret_cast<const uint2*>(sh.q_wide[sh.tiles[n % kDescs].item & 3]);
+                const bool half = !(wides.x | wides.y);
+                const uint32_t shape = NB == 2 && sh.tiles[n % kDescs].item_rows <= 64 ? idesc(64, half, false) : idesc(kRows, half, false);
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
                     umma_bf16_elect(tmem + (n & 1) * kRows, kd + (i / 4) * (kHalf >> 4) + 2 * (i % 4), qd + (i / 4) * (kRows * 128 >> 4) + 2 * (i % 4), shape,
@@ -688,7 +854,6 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             // ------------------------------------------------------------------------ O^T += V^T P^T
             bool ok = true;
             int uses[2] = {0, 0};
-            const uint64_t ones = desc_mn(sm + L::kOnesAt, 1024);
             for (int n = 0; ok; ++n) {
                 if (!(ok = mbar_wait_asleep_warp(bar(sh.v_full[n & 1]), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
                 // (heads of 64: the upper 64 lanes take whatever lies behind the tile, and nobody reads them)
@@ -696,19 +861,31 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 const Tile& d = sh.tiles[n % kDescs];
                 const bool fresh = d.index < (NB == 1 ? 2 : 1), final = d.final;
                 const int blocks = (d.item_rows + 63) >> 6;
+                const uint2 wides = *reinterpret_cast<const uint2*>(sh.wide[n & 3]);
+                const uint64_t ones = desc_ones(sm + L::kOnesAt), ones_wide = desc_ones_wide(sm + L::kOnesAt + kOnes);
 #pragma unroll 1
                 for (int b = 0; b < blocks; ++b) {
                     const int stream = NB == 1 ? n & 1 : b;
                     if (!(ok = mbar_wait_asleep_warp(bar(sh.p_full[stream]), (stream ? uses[1]++ : uses[0]++) & 1, a.wait_ns, abort_flag))) break;
                     tc_fence_after_sync();
                     const uint64_t pd = desc_mn(sm + L::kP + stream * kHalf, kHalf);
+                    // and, with ones in V's place, the sums of P over the keys
+                    if (!(wides.x | wides.y)) {
 #pragma unroll
-                    for (int i = 0; i < kKeys / 16; ++i)
-                        umma_bf16_elect(tmem + L::kO + 64 * stream, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(64, true), fresh && i == 0 ? 0u : 1u);
-                    // the sums of P over the keys: ones in V's place
+                        for (int i = 0; i < kKeys / 16; ++i)
+                            umma_bf16_elect(tmem + L::kO + 64 * stream, vd + i * (2048 >> 4), pd + i * (2048 >> 4), idesc(64, true, true), fresh && i == 0 ? 0u : 1u);
 #pragma unroll
-                    for (int i = 0; i < kKeys / 16; ++i)
-                        umma_bf16_elect(tmem + L::kSum + 64 * stream, ones, pd + i * (2048 >> 4), idesc(64, true), fresh && i == 0 ? 0u : 1u);
+                        for (int i = 0; i < kKeys / 16; ++i)
+                            umma_bf16_elect(tmem + L::kSum + 64 * stream, ones, pd + i * (2048 >> 4), idesc(64, true, true), fresh && i == 0 ? 0u : 1u);
+                    } else {
+#pragma unroll 1
+                        for (int i = 0; i < kKeys / 16; ++i) {
+                            const bool bf16 = ((i < 4 ? wides.x : wides.y) >> (8 * (i & 3))) & 1u;
+                            const uint32_t type = bf16 ? idesc(64, false, true) : idesc(64, true, true), add = fresh && i == 0 ? 0u : 1u;
+                            umma_bf16_elect(tmem + L::kO + 64 * stream, vd + i * (2048 >> 4), pd + i * (2048 >> 4), type, add);
+                            umma_bf16_elect(tmem + L::kSum + 64 * stream, bf16 ? ones_wide : ones, pd + i * (2048 >> 4), type, add);
+                        }
+                    }
                     if (b + 1 == blocks) umma_commit_elect(bar(sh.v_free[n & 1]));
                     umma_commit_elect(bar(sh.pv_done[stream]));
                 }

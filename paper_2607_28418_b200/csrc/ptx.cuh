@@ -1,9 +1,6 @@
 // Thin inline-PTX wrappers for sm_100a: mbarrier, TMA (cp.async.bulk.tensor), cp.async,
 // tcgen05 (TMEM allocation, UMMA issue/commit, TMEM loads) and the descriptors they take.
 #pragma once
-#ifndef SLEEPNS
-#define SLEEPNS 40
-#endif
 
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -99,7 +96,7 @@ __device__ __forceinline__ bool mbar_wait_asleep(uint32_t bar, uint32_t parity, 
     while (true) {
 #pragma unroll 1
         for (int i = 0; i < 64; ++i) {
-            __nanosleep(SLEEPNS);
+            __nanosleep(40);
             if (mbar_try_wait(bar, parity)) return true;
         }
         if (*abort_flag) return false;

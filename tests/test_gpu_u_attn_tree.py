@@ -1,4 +1,4 @@
-"""wide_attn_tree against the softmax in 64 bits over the values that the cache holds (rounded to bf16, as wide_cache_read returns them)."""
+"""wide_attn_tree against the softmax in 64 bits over the values that the cache holds."""
 import numpy as np
 import pytest
 import torch
@@ -40,8 +40,10 @@ def seen_by(bits, n):
 
 
 def reference(c, q, on, per, sees, scale=0.0, missing=()):
-    """(reference, tolerance) [rows, hq, dim], 64 bits.  A logit sums dim / 16 steps of products in fp32 (2^-23 of their magnitudes a step, as
-    does its scaling); a probability is off by that, by the exponential (2^-21) and by its rounding to bf16 (2^-8); an output adds
+    """(reference, tolerance) [rows, hq, dim], 64 bits.  A key's number is rounded to fp16, 2^-11 of itself and 2^-18 of the key's largest, a query's
+    to 2^-16 of its row's largest, or, where some of the item's queries do not fit that type, keys to 2^-8; a logit sums dim / 16 steps of products
+    in fp32 (2^-23 of their magnitudes a step, as does its scaling).  A probability is off by that, by the exponential (2^-21) and by its rounding
+    to fp16 (2^-11, and 2^-32 of the largest), a value by 2^-11; both by 2^-8 in blocks whose values fp16 does not hold well.  An output adds
     len / 16 steps of weighed values; its own rounding is 2^-8.  missing: positions without a page."""
     dim, hq = c.dim, q.shape[1]
     share = hq // c.heads
@@ -51,7 +53,7 @@ def reference(c, q, on, per, sees, scale=0.0, missing=()):
         if n == 0 or c.lens[s] == 0:
             continue
         a = slice(c.row_start[s], c.row_start[s] + n)
-        k, v = (torch.from_numpy(co.round_bf16(x).astype(np.float64)).cuda() for x in c.held(s))
+        k, v = (torch.from_numpy(np.asarray(x, dtype=np.float64)).cuda() for x in c.held(s))
         z = torch.from_numpy(q[a].astype(np.float64)).cuda().view(n, c.heads, share, dim)
         logits = torch.einsum("mhsd,nhd->mhsn", z, k) * scale
         size = torch.einsum("mhsd,nhd->mhsn", z.abs(), k.abs()).amax(-1) * scale
@@ -63,8 +65,14 @@ def reference(c, q, on, per, sees, scale=0.0, missing=()):
         p = torch.nan_to_num(torch.softmax(logits, -1), nan=0.0)
         o = torch.einsum("mhsn,nhd->mhsd", p, v)
         weighed = torch.einsum("mhsn,nhd->mhsd", p, v.abs())
-        each = 2.0 ** -8 + 2.0 ** -20 + 2 * size * 2.0 ** -23 * (dim / 16 + 3)
-        t = 2.0 ** -8 * o.abs() + weighed * (each[..., None] + 2.0 ** -23 * (c.lens[s] / 16 + 8)) + 1e-30
+        small = (z.abs().sum(-1) * k.abs().amax() * 2.0 ** -18 + z.abs().amax(-1) * k.abs().sum(-1).amax() * 2.0 ** -16) * scale
+        tops = z.reshape(-1, 8).abs().amax(-1)
+        fits = bool(((tops == 0) | (tops >= 2.0 ** -9) & (tops <= 2.0 ** 14)).all())
+        parts = v.reshape(c.lens[s], c.heads, -1, c.group)
+        low, high = parts.amin(-1), parts.amax(-1)
+        narrow = bool((((high - low) / 15 >= 2.0 ** -12) & (torch.maximum(high, -low) <= 30000)).all())
+        each = (2.0 ** -10 if narrow else 2.0 ** -7) + 2.0 ** -20 + 2 * (size * ((2.0 ** -11 if fits else 2.0 ** -8) + 2.0 ** -23 * (dim / 16 + 3)) + small)
+        t = 2.0 ** -8 * o.abs() + weighed * (each[..., None] + 2.0 ** -23 * (c.lens[s] / 16 + 8)) + v.abs().amax() * c.lens[s] * 2.0 ** -32 + 1e-37
         live = np.ones((n, hq), dtype=bool) if on is None else np.repeat(on[a], per, axis=1)
         ref[a] = o.reshape(n, hq, dim).cpu().numpy() * live[..., None]
         tol[a] = t.reshape(n, hq, dim).cpu().numpy()
@@ -282,3 +290,41 @@ def test_strided_queries_and_nothing_to_do(ctx):
     fused[:, 128:384] = q
     assert torch.equal(binding.wide_attn_tree(ctx, fused[:, 128:384], cache, seqs, 4, 2, bits), binding.wide_attn_tree(ctx, q, cache, seqs, 4, 2, bits))
     assert binding.wide_attn_tree(ctx, q[:0], cache, seqs, 4, 2, bits[:0]).shape == (0, 256)
+
+
+@pytest.mark.parametrize("dim,group", SHAPES)
+def test_how_near_it_comes(ctx, dim, group):
+    """On ordinary values the root mean square of all errors together is hardly more than that of the output's rounding to bf16 (at most 2^-9 / sqrt(3)
+    of a number in [1, 2) and half that below the next power: 0.41 to 0.85 of 2^-9).  What else there is adds in squares: probabilities and values
+    2^-12 each, keys 2^-12 a logit of size 1."""
+    c = CacheCase([700, 90], [24, 8], 2, dim, group, 32, seed=3)
+    q = queries(c, 8, 4)
+    bits, sees = random_trees(c, 5)
+    ref, _ = reference(c, q, None, 4, sees)
+    got = run(ctx, c, q, None, 4, bits).float().cpu().numpy().reshape(ref.shape)
+    assert np.sqrt(((got - ref) ** 2).sum() / (ref ** 2).sum()) < 2.0 ** -9
+
+
+@pytest.mark.parametrize("scale_q,scale_k,scale_v", [(2.0 ** -40, 2.0 ** 40, 1.0), (2.0 ** 30, 2.0 ** -30, 2.0 ** -30), (1.0, 1.0, 2.0 ** 60), (2.0 ** 100, 2.0 ** -100, 2.0 ** -100), (2.0 ** -7, 2.0 ** 7, 2.0 ** -9)])
+def test_sizes_that_fp16_does_not_hold(ctx, scale_q, scale_k, scale_v):
+    """Queries, keys and values of any size, each alone and rows of different sizes together: only their products have to be sensible."""
+    c = CacheCase([300, 40, 150], [20, 8, 3], 2, 128, 64, 32, seed=6)
+    c.k = [co.round_bf16(x * np.float32(scale_k)) for x in c.k]
+    c.v = [co.round_bf16(x * np.float32(scale_v)) for x in c.v]
+    q = queries(c, 8, 7) * np.float32(scale_q)
+    q[::3] *= 2.0 ** -12
+    q[5] = 0
+    bits, sees = random_trees(c, 8)
+    ref, tol = reference(c, q, None, 4, sees)
+    check(run(ctx, c, q, None, 4, bits), ref, tol)
+
+
+def test_values_of_both_kinds_in_a_tile(ctx):
+    """A tile with blocks of ordinary values, of tiny and of large ones, in turn; a row's output is the sum of all."""
+    c = CacheCase([520], [12], 2, 128, 32, 32, seed=9)
+    factor = np.repeat(np.array([1.0, 2.0 ** -20, 2.0 ** 17, 1.0, 2.0 ** -14], dtype=np.float32), 16)
+    c.v = [co.round_bf16(x * np.resize(factor, len(x))[:, None, None]) for x in c.v]
+    q = queries(c, 8, 10)
+    bits, sees = random_trees(c, 11)
+    ref, tol = reference(c, q, None, 4, sees)
+    check(run(ctx, c, q, None, 4, bits), ref, tol)
