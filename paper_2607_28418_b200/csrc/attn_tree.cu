@@ -226,38 +226,29 @@ __device__ __forceinline__ uint32_t to_half(uint32_t w) { return half_pair(low_o
 constexpr uint32_t kLeastKey = 0x3A80u, kLeastValue = 0x3900u;       // 2^-10: what is below fp16's normal numbers is 2^-18 of the key's largest; 2^-13: s / 16 is exact
 __device__ __forceinline__ bool fits_half(uint32_t w, uint32_t least) { return w == 0 || ((w & 0xFFFFu) - least < 0x4480u - least && (w & 0x7FFF0000u) < 0x46800000u); }
 
-// The words of a warp's block of which some do not fit, or whose tile has keys that not every row sees.  Out of line: few need it.  A key's are taken times
-// a power of two so that its largest number is 2^8 to 2^9 (the power goes into its logits).  Values' stay bf16 where one does not fit.  Values of
-// keys that are not there count as zeros, and those of new tokens that are not finite are noted instead.
+// The words of a warp's block of which some do not fit.  Out of line: few need it.  A key's are taken times a power of two so that its largest number is
+// 2^8 to 2^9 (the power goes into its logits), unless keys are bf16.  Values' stay bf16 where one does not fit.
 template <int NS>
-__device__ __noinline__ bool odd_words(Shared* sh, const Tile* d, uint32_t words, int n, int warp, bool here, bool wide_keys, float scale) {
-    const int lane = threadIdx.x & 31, key0 = (d->blk + warp) * 16;
+__device__ __noinline__ bool odd_words(uint32_t words, float* key_by, bool wide_keys, float scale) {
+    const int lane = threadIdx.x & 31;
     uint32_t w[(NS + 1) / 2];
     bool half = true;
 #pragma unroll
     for (int i = 0; i < (NS + 1) / 2; ++i) {
-        const int x = 32 * i + lane, r = x / NS;
-        const bool mine = NS > 1 || lane < 16, writes = mine && x % NS == 0;
-        const uint32_t at = words + 4 * (mine ? x : 0), kw = lds32(at);
+        const int x = 32 * i + (NS > 1 ? lane : lane & 15);
+        const uint32_t at = words + 4 * x, kw = lds32(at);
         float top = fmaxf(fabsf(high_of(kw)), fabsf(fmaf(15.f, low_of(kw), high_of(kw))));
 #pragma unroll
         for (int o = 1; o < NS; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const uint32_t e = exponent_of(top);
         w[i] = lds32(at + 64 * NS);
-        __syncwarp();
-        if (mine && !wide_keys) sts32(at, half_pair(low_of(kw) * times_to_256(e), high_of(kw) * times_to_256(e)));
-        if (writes) sh->key_by[n & 3][warp * 16 + r] = wide_keys ? scale : times_back(e) * scale;
-        if (d->masked) {
-            const bool is = here && key0 + r < d->len, bad = mine && is && key0 + r >= d->len - d->n_rows && not_finite(w[i]);
-            if (!is || bad) w[i] = 0;
-            const uint32_t bits = __ballot_sync(0xffffffffu, bad);
-            if (writes) sh->odd[n & 3][warp * 16 + r] = (bits >> lane) & ((1u << NS) - 1u);
-        }
         half = __all_sync(0xffffffffu, fits_half(w[i], kLeastValue)) && half;
+        if (!wide_keys) sts32(at, half_pair(low_of(kw) * times_to_256(e), high_of(kw) * times_to_256(e)));
+        if (x % NS == 0) key_by[x / NS] = wide_keys ? scale : times_back(e) * scale;
     }
 #pragma unroll
     for (int i = 0; i < (NS + 1) / 2; ++i)
-        if (NS > 1 || lane < 16) sts32(words + 64 * NS + 4 * (32 * i + lane), half ? half_pair(low_of(w[i]), high_of(w[i])) : w[i]);
+        if (half) sts32(words + 64 * NS + 4 * (32 * i + (NS > 1 ? lane : lane & 15)), to_half(w[i]));
     return half;
 }
 
@@ -425,12 +416,21 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 bool half = true;
                 {
                     uint32_t kw[(kNS + 1) / 2], vw[(kNS + 1) / 2];
-                    bool fits = !d.masked && !wide_keys;
+                    bool fits = !wide_keys;
 #pragma unroll
                     for (int i = 0; i < (kNS + 1) / 2; ++i) {
                         const uint32_t at = words + 4 * (32 * i + (kNS > 1 ? lane : lane & 15));
                         kw[i] = lds32(at);
                         vw[i] = lds32(at + 64 * kNS);
+                        if (d.masked) {
+                            // keys that are not there count as zeros, and so do sub-groups of new tokens' values that are not finite, which are noted
+                            const int r = (32 * i + lane) / kNS & 15, key = (d.blk + warp) * 16 + r;
+                            const bool is = here && key < d.len, bad = is && key >= d.len - d.n_rows && not_finite(vw[i]);
+                            if (!is) kw[i] = 0;
+                            if (!is || bad) vw[i] = 0;
+                            const uint32_t bits = __ballot_sync(0xffffffffu, bad);
+                            if (lane % kNS == 0) sh.odd[n & 3][warp * 16 + r] = (bits >> lane) & ((1u << kNS) - 1u);
+                        }
                         fits = fits && fits_half(kw[i], kLeastKey) && fits_half(vw[i], kLeastValue);
                     }
                     if (__all_sync(0xffffffffu, fits)) {
@@ -442,7 +442,16 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         }
                         if (lane < 16) sh.key_by[n & 3][warp * 16 + lane] = a.scale_log2e;
                     } else {
-                        half = odd_words<kNS>(&sh, &d, words, n, warp, here, wide_keys, a.scale_log2e);
+                        if (d.masked) {
+#pragma unroll
+                            for (int i = 0; i < (kNS + 1) / 2; ++i) {
+                                const uint32_t at = words + 4 * (32 * i + (kNS > 1 ? lane : lane & 15));
+                                sts32(at, kw[i]);
+                                sts32(at + 64 * kNS, vw[i]);
+                            }
+                            __syncwarp();
+                        }
+                        half = odd_words<kNS>(words, sh.key_by[n & 3] + warp * 16, wide_keys, a.scale_log2e);
                     }
                     __syncwarp();
                 }
