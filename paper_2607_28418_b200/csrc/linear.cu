@@ -4,9 +4,13 @@
 // so that a single token costs no more than the weights' bytes.  An epilogue warp has 32 channels of all the tile's tokens; it turns
 // them round through its own part of shared memory, so that rows of y are read and written in runs of 64 or 128 bytes.
 //
-// Few tokens: the weights' bytes bound it, and N / 128 tiles are fewer than SMs.  A cluster of CTAs shares a tile: each takes a part
-// of K, and each joins the parts of some of the tokens over distributed shared memory, in the order of K, so results do not
-// depend on timing.
+// Few tokens (linear_kernel): the weights' bytes bound it, and N / 128 tiles are fewer than SMs.  A cluster of CTAs shares a tile: each takes a
+// part of K, and each joins the parts of some of the tokens over distributed shared memory, in the order of K, so results do not
+// depend on timing.  One token 4096 -> 6144: 18.5 us with cold caches, 12.9 in a stream of calls (floor 7.7); 64 tokens 4096 -> 128256: 195 us, 82% of
+// the memory's rate.
+//
+// Many tokens (linear_pair_kernel): pairs of SMs, below.  4096 tokens 4096 -> 14336: 293 us, 1.64 PFLOP/s; short of that rate where the last round of
+// tiles leaves SMs idle (2048 tokens 4096 -> 4096: 56 us, 1.23).
 #include <cuda.h>
 
 #include <algorithm>
@@ -23,6 +27,11 @@ constexpr int kM = 128;                 // output channels of a tile
 constexpr int kBK = 64;                 // bf16 numbers of a 128-byte swizzle row
 constexpr int kABytes = kM * kBK * 2;
 constexpr int kThreads = 192;           // TMA, MMA, four epilogue warps
+// fp32 outputs: after so many steps of kBK a sum goes on in the other accumulator, and the epilogue warps add the pieces up.  The tensor cores cut a sum
+// off at every addition, towards zero, so that a long one drifts: 2-norm of the error 4.4e-6 at K = 4096 in one piece, 1.0e-6 in pieces of 16
+// steps, 7e-7 of 12, 4.8e-7 of 8, whatever K.  With few tokens it costs nothing; 4096 tokens 4096 -> 14336 take 307, 338, 371, 394 us.  bf16 outputs,
+// whose rounding is 1.7e-3, keep one piece.
+constexpr int kChain = 12;
 
 struct LinearArgs {
     int T, N, nk;                       // nk: steps of kBK
@@ -109,26 +118,29 @@ struct Small {
 };
 
 // One tile of 128 channels and NT tokens a cluster.
-template <int NT>
+template <int NT, bool CHAIN>
 __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
                                                           const __grid_constant__ LinearArgs a) {
     constexpr int kStages = Small<NT>::kStages, kStage = Small<NT>::kStage;
-    constexpr uint32_t kCols = NT < 32 ? 32 : NT;
+    constexpr uint32_t kCols = CHAIN ? 2 * NT : NT < 32 ? 32 : NT;
     static_assert(kStages * kStage >= NT * kM * 4, "the parts of a tile take the place of the stages");
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 1];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    const uint32_t full = smem_u32(bars), empty = smem_u32(bars + kStages), done = smem_u32(bars + 2 * kStages);
+    const uint32_t full = smem_u32(bars), empty = smem_u32(bars + kStages), done = smem_u32(bars + 2 * kStages), taken = smem_u32(bars + 2 * kStages + 2);
     volatile int* abort_flag = &abort_word;
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(full + 8 * s, 1);
             mbar_init(empty + 8 * s, 1);
         }
-        mbar_init(done, 1);
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(done + 8 * s, 1);
+            mbar_init(taken + 8 * s, 4);
+        }
         abort_word = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_w);
@@ -166,17 +178,21 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
         if (lane == 0) {
             bool ok = true;
             for (int k = k0; k < k1 && ok; ++k) {
-                const int i = k - k0, s = i % kStages;
+                const int i = k - k0, s = i % kStages, piece = CHAIN ? i / kChain : 0;
+                if (CHAIN && i % kChain == 0) {
+                    if (piece > 0) umma_commit(done + 8 * ((piece - 1) & 1));
+                    if (piece >= 2 && !(ok = mbar_wait(taken + 8 * (piece & 1), ((piece >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
+                }
                 ok = mbar_wait(full + 8 * s, (i / kStages) & 1, a.wait_ns, abort_flag);
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint32_t at = smem_u32(base + s * kStage);
                 const uint64_t wd = umma_desc_sw128(at), xd = umma_desc_sw128(at + kABytes);
 #pragma unroll
-                for (int e = 0; e < kBK / 16; ++e) umma_bf16(tmem, wd + 2 * e, xd + 2 * e, umma_idesc_bf16(kM, NT), (i | e) ? 1u : 0u);
+                for (int e = 0; e < kBK / 16; ++e) umma_bf16(tmem + (piece & 1) * NT, wd + 2 * e, xd + 2 * e, umma_idesc_bf16(kM, NT), ((CHAIN ? i % kChain : i) | e) ? 1u : 0u);
                 umma_commit(empty + 8 * s);
             }
-            if (ok) umma_commit(done);
+            if (ok) umma_commit(done + (CHAIN ? 8 * (((k1 - k0 - 1) / kChain) & 1) : 0));
         }
     }
     __syncwarp();
@@ -185,19 +201,44 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
     float* parts = reinterpret_cast<float*>(base);      // [token][128]: every stage has been read when `done` completes
     bool ok = true;
     if (warp >= 2) {
-        ok = mbar_wait_warp(done, 0, a.wait_ns, abort_flag);
-        if (!ok && lane == 0) atomicExch(a.status, WIDE_ERR_TIMEOUT);
-        tc_fence_after_sync();
-        if (ok) {
-#pragma unroll 1
-            for (int c = 0; c < NT; c += 16) {
-                uint32_t r[16];
-                tmem_ld_32x16(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c, r);
-                tmem_ld_wait();
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+        if constexpr (CHAIN) {
+            float sum[NT];
+            const int pieces = (k1 - k0 + kChain - 1) / kChain;
+            for (int c = 0; c < pieces; ++c) {
+                if (!(ok = mbar_wait_warp(done + 8 * (c & 1), (c >> 1) & 1, a.wait_ns, abort_flag))) break;
+                tc_fence_after_sync();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) parts[(c + e) * kM + quarter * 32 + lane] = __uint_as_float(r[e]);
+                for (int t = 0; t < NT; t += 16) {
+                    uint32_t r[16];
+                    tmem_ld_32x16(lanes + (c & 1) * NT + t, r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum[t + e] = c == 0 ? __uint_as_float(r[e]) : sum[t + e] + __uint_as_float(r[e]);
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(taken + 8 * (c & 1));
+            }
+            if (ok) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) parts[t * kM + quarter * 32 + lane] = sum[t];
+            }
+        } else {
+            ok = mbar_wait_warp(done, 0, a.wait_ns, abort_flag);
+            tc_fence_after_sync();
+            if (ok) {
+#pragma unroll 1
+                for (int c = 0; c < NT; c += 16) {
+                    uint32_t r[16];
+                    tmem_ld_32x16(lanes + c, r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) parts[(c + e) * kM + quarter * 32 + lane] = __uint_as_float(r[e]);
+                }
             }
         }
+        if (!ok && lane == 0) atomicExch(a.status, WIDE_ERR_TIMEOUT);
         __syncwarp();
     }
     if (a.split > 1) {
@@ -240,7 +281,7 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
 
 // ------------------------------------------------------------------------------------------------ many tokens
 // Pairs of CTAs (cta_group::2) take tiles of 256 channels and 256 tokens: each brings 128 rows of both operands for a product that reads
-// the two SMs' shared memory, 7.8 bytes a kFLOP from L2, which 128 x 256 tiles of one SM exceed (they end at 1.0 PFLOP/s).  A CTA has its 128 channels
+// the two SMs' shared memory, 7.8 bytes a kFLOP from L2, where 128 x 256 tiles of one SM need 11.7 and end at 1.0 PFLOP/s.  A CTA has its 128 channels
 // (TMEM lanes) of all 256 tokens in one of two accumulators, so the epilogue of a tile runs under the next one's products.  Persistent;
 // tiles go by bands of 16 token tiles, channels within them, so that a band's tokens stay in L2.
 // Tiles of 128 tokens fill SMs that 256 leave idle (256 tokens, 4096 -> 6144: 34 us with 256, 30 with 128; 512, 4096 -> 4096: 32, 28).
@@ -330,7 +371,7 @@ __device__ __forceinline__ void arrive_rank0(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(bar, 0)) : "memory");
 }
 
-template <int PT>
+template <int PT, bool CHAIN>
 __global__ void __launch_bounds__(kPairThreads, 1) __cluster_dims__(2, 1, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ LinearArgs a) {
     constexpr int kPairStages = Pair<PT>::kStages, kPairStage = Pair<PT>::kStage, kPairT = PT;
@@ -404,18 +445,24 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
         // ------------------------------------------------------------------ products, by the even CTA
         if (rank == 0) {
             int it = 0, n = 0;
-            for (long long i = blockIdx.x >> 1; i < tiles && ok; i += pairs, ++n) {
+            for (long long i = blockIdx.x >> 1; i < tiles && ok; i += pairs, ++n) {       // n: accumulators filled
                 if (n >= 2 && !(ok = mbar_wait_warp(tempty + 8 * (n & 1), ((n >> 1) & 1) ^ 1u, a.wait_ns, abort_flag))) break;
                 tc_fence_after_sync();
                 for (int k = 0; k < a.nk; ++k, ++it) {
                     const int s = it % kPairStages;
+                    if (CHAIN && k > 0 && k % kChain == 0) {
+                        umma_commit_pair(tfull + 8 * (n & 1));
+                        ++n;
+                        if (n >= 2 && !(ok = mbar_wait_warp(tempty + 8 * (n & 1), ((n >> 1) & 1) ^ 1u, a.wait_ns, abort_flag))) break;
+                        tc_fence_after_sync();
+                    }
                     if (!(ok = mbar_wait_warp(full + 8 * s, (it / kPairStages) & 1, a.wait_ns, abort_flag))) break;
                     tc_fence_after_sync();
                     const uint32_t from = smem_u32(base + s * kPairStage);
                     const uint64_t wd = umma_desc_sw128(from), xd = umma_desc_sw128(from + kABytes);
 #pragma unroll
                     for (int e = 0; e < kBK / 16; ++e)
-                        umma_bf16_pair(tmem + (n & 1) * kPairT, wd + 2 * e, xd + 2 * e, umma_idesc_bf16(2 * kM, kPairT), (k | e) ? 1u : 0u);
+                        umma_bf16_pair(tmem + (n & 1) * kPairT, wd + 2 * e, xd + 2 * e, umma_idesc_bf16(2 * kM, kPairT), ((CHAIN ? k % kChain : k) | e) ? 1u : 0u);
                     umma_commit_pair(empty + 8 * s);
                 }
                 if (ok) umma_commit_pair(tfull + 8 * (n & 1));
@@ -428,21 +475,14 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
         int n = 0;
         for (long long i = blockIdx.x >> 1; i < tiles; i += pairs, ++n) {
             const At at = tile_at(i);
-            if (!(ok = mbar_wait_warp(tfull + 8 * (n & 1), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
-            tc_fence_after_sync();
+            const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + half * (kPairT / 2);
             const int f = at.n * 2 * kM + rank * kM + quarter * 32 + (lane & 7) * 4;
             float bias[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) bias[e] = a.bias && f + e < a.N ? __bfloat162float(a.bias[f + e]) : 0.f;
-#pragma unroll 1
-            for (int c = half * (kPairT / 2); c < (half + 1) * (kPairT / 2); c += 32) {
-                uint32_t r[32];
-                tmem_ld_32x32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + (n & 1) * kPairT + c, r);
-                tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 32; ++e) mine[e * 32 + lane] = __uint_as_float(r[e]);
+            auto finish_32 = [&](int c) {          // the tokens from c on of this warp's half, which lie in its shared memory
                 __syncwarp();
-                const int t0 = at.t * kPairT + c;
+                const int t0 = at.t * kPairT + half * (kPairT / 2) + c;
                 if (f + 3 < a.N && t0 + 32 <= a.T) {
                     finish_block(a, t0, f, mine, lane, bias);
                 } else if (f < a.N) {
@@ -451,10 +491,48 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                         finish(a, static_cast<long long>(t0) + e, f, *reinterpret_cast<const float4*>(mine + e * 32 + (lane & 7) * 4), bias);
                 }
                 __syncwarp();
+            };
+            if constexpr (CHAIN) {
+                float sum[kPairT / 2];
+                for (int k = 0; k < a.nk; k += kChain, ++n) {
+                    if (!(ok = mbar_wait_warp(tfull + 8 * (n & 1), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int c = 0; c < kPairT / 2; c += 16) {
+                        uint32_t r[16];
+                        tmem_ld_32x16(lanes + (n & 1) * kPairT + c, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) sum[c + e] = k == 0 ? __uint_as_float(r[e]) : sum[c + e] + __uint_as_float(r[e]);
+                    }
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) arrive_rank0(tempty + 8 * (n & 1));
+                }
+                if (!ok) break;
+                --n;
+#pragma unroll
+                for (int c = 0; c < kPairT / 2; c += 32) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) mine[e * 32 + lane] = sum[c + e];
+                    finish_32(c);
+                }
+            } else {
+                if (!(ok = mbar_wait_warp(tfull + 8 * (n & 1), (n >> 1) & 1, a.wait_ns, abort_flag))) break;
+                tc_fence_after_sync();
+#pragma unroll 1
+                for (int c = 0; c < kPairT / 2; c += 32) {
+                    uint32_t r[32];
+                    tmem_ld_32x32(lanes + (n & 1) * kPairT + c, r);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) mine[e * 32 + lane] = __uint_as_float(r[e]);
+                    finish_32(c);
+                }
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) arrive_rank0(tempty + 8 * (n & 1));
             }
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) arrive_rank0(tempty + 8 * (n & 1));
         }
     }
     if (!ok && lane == 0) atomicExch(a.status, WIDE_ERR_TIMEOUT);
@@ -489,18 +567,13 @@ bool allow_smem(const wide_ctx* ctx, K kernel, int bytes, std::atomic<unsigned>&
     return true;
 }
 
-template <int NT>
-int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long xs, const void* w, int K) {
+template <int NT, bool CHAIN>
+int launch_small(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long xs, const void* w, int K) {
     CUtensorMap tm_w, tm_x;
     if (!make_map(ctx, &tm_w, w, a.N, K, 2LL * K, kM) || !make_map(ctx, &tm_x, x, a.T, K, 2 * xs, NT)) return WIDE_ERR_CUDA;
     static std::atomic<unsigned> set{0};
-    if (!allow_smem(ctx, linear_kernel<NT>, Small<NT>::kSmem, set)) return WIDE_ERR_CUDA;
+    if (!allow_smem(ctx, linear_kernel<NT, CHAIN>, Small<NT>::kSmem, set)) return WIDE_ERR_CUDA;
     const long long tiles = static_cast<long long>(a.tiles_n) * ((a.T + NT - 1) / NT);
-    a.stream_weights = a.T <= NT;
-    a.split = 1;
-    // CTAs for three quarters of the SMs at least, as long as each keeps 8 steps of K (one token, 4096 x 4096: 4 parts 16.4 us, 8 parts 18.4)
-    while (a.split < 8 && 4 * tiles * a.split < 3 * ctx->sm_count && a.nk / (2 * a.split) >= 8) a.split *= 2;
-    if (tiles * a.split > 0x7fffffffLL) return WIDE_ERR_UNSUPPORTED_SHAPE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split));
     cfg.blockDim = dim3(kThreads);
@@ -515,8 +588,19 @@ int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long
     cfg.attrs = attr;
     cfg.numAttrs = ctx->prof ? 1 : 2;
     WideLaunch l(ctx, s, "linear");
-    WIDE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, linear_kernel<NT>, tm_w, tm_x, a));
+    WIDE_CUDA_CHECK(cudaLaunchKernelEx(&cfg, linear_kernel<NT, CHAIN>, tm_w, tm_x, a));
     return WIDE_OK;
+}
+
+template <int NT>
+int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long xs, const void* w, int K) {
+    const long long tiles = static_cast<long long>(a.tiles_n) * ((a.T + NT - 1) / NT);
+    a.stream_weights = a.T <= NT;
+    a.split = 1;
+    // CTAs for three quarters of the SMs at least, as long as each keeps 8 steps of K (one token, 4096 x 4096: 4 parts 16.4 us, 8 parts 18.4)
+    while (a.split < 8 && 4 * tiles * a.split < 3 * ctx->sm_count && a.nk / (2 * a.split) >= 8) a.split *= 2;
+    if (tiles * a.split > 0x7fffffffLL) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    return a.out_f32 && a.nk > kChain * a.split ? launch_small<NT, true>(ctx, s, a, x, xs, w, K) : launch_small<NT, false>(ctx, s, a, x, xs, w, K);
 }
 
 template <int PT>
@@ -524,15 +608,15 @@ long long pair_tiles(const LinearArgs& a) {
     return static_cast<long long>((a.T + PT - 1) / PT) * ((a.N + 2 * kM - 1) / (2 * kM));
 }
 
-template <int PT>
+template <int PT, bool CHAIN>
 int launch_pairs(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long xs, const void* w, int K) {
     CUtensorMap tm_w, tm_x;
     if (!make_map(ctx, &tm_w, w, a.N, K, 2LL * K, kM) || !make_map(ctx, &tm_x, x, a.T, K, 2 * xs, PT / 2)) return WIDE_ERR_CUDA;
     static std::atomic<unsigned> set{0};
-    if (!allow_smem(ctx, linear_pair_kernel<PT>, Pair<PT>::kSmem, set)) return WIDE_ERR_CUDA;
+    if (!allow_smem(ctx, linear_pair_kernel<PT, CHAIN>, Pair<PT>::kSmem, set)) return WIDE_ERR_CUDA;
     const int pairs = static_cast<int>(std::min<long long>(pair_tiles<PT>(a), ctx->sm_count / 2));
     WideLaunch l(ctx, s, "linear_pair");
-    WIDE_CUDA_CHECK(wide_launch_after(ctx, linear_pair_kernel<PT>, dim3(2 * pairs), dim3(kPairThreads), Pair<PT>::kSmem, s, tm_w, tm_x, a));
+    WIDE_CUDA_CHECK(wide_launch_after(ctx, linear_pair_kernel<PT, CHAIN>, dim3(2 * pairs), dim3(kPairThreads), Pair<PT>::kSmem, s, tm_w, tm_x, a));
     return WIDE_OK;
 }
 
@@ -561,6 +645,7 @@ int wide_launch_linear(wide_ctx* ctx, cudaStream_t s, const void* x, int T, int 
     // Rounds of the pairs; a tile of 128 tokens takes 0.65 to 0.8 of one of 256, not half, as it reads shared memory at twice the rate for its
     // products (1024 tokens, 4096 -> 6144, three rounds of 128: 62 us, two of 256: 54).
     const long long pairs = ctx->sm_count / 2, wide = (pair_tiles<256>(a) + pairs - 1) / pairs, narrow = (pair_tiles<128>(a) + pairs - 1) / pairs;
-    if (8 * narrow < 10 * wide) return launch_pairs<128>(ctx, s, a, x, xs, w, K);
-    return launch_pairs<256>(ctx, s, a, x, xs, w, K);
+    const bool chain = a.out_f32 && a.nk > kChain;
+    if (8 * narrow < 10 * wide) return chain ? launch_pairs<128, true>(ctx, s, a, x, xs, w, K) : launch_pairs<128, false>(ctx, s, a, x, xs, w, K);
+    return chain ? launch_pairs<256, true>(ctx, s, a, x, xs, w, K) : launch_pairs<256, false>(ctx, s, a, x, xs, w, K);
 }

@@ -156,3 +156,29 @@ def test_no_tokens(ctx):
     from paper_2607_28418_b200 import binding
     x, w, _, _ = make(0, 64, 24)
     assert binding.wide_linear(ctx, x, w).shape == (0, 24)
+
+
+@pytest.mark.parametrize("T", [1, 24, 64, 100, 200, 1500])
+@pytest.mark.parametrize("k,n", [(1024, 640), (1032, 640), (2056, 1000), (4096, 2056), (16384, 136), (16384, 16500)])
+def test_long_fp32_sums_do_not_drift(ctx, T, k, n):
+    """fp32 outputs add their sums up in pieces of 768 products: each of the 48 steps of a piece takes less than 2^-23 of what the piece has come to, which
+    grows to its end like a random walk (two thirds of it on average): 48 * 2^-24 * 2 / 3 = 1.9e-6 of a piece, and pieces add in squares like
+    their losses; joining them adds 2^-24 each."""
+    from paper_2607_28418_b200 import binding
+    x, w, _, _ = make(T, k, n, seed=11)
+    got = binding.wide_linear(ctx, x, w, out_dtype=torch.float32)
+    ref, _ = exact(x, w, None, "none", None)
+    assert ((got.double() - ref).norm() / ref.norm()).item() < 1.9e-6
+    check(got, x, w)
+
+
+@pytest.mark.parametrize("T", [3, 128, 600])
+@pytest.mark.parametrize("act,residual", [("gelu", True), ("none", False)])
+def test_pieces_of_a_sum_with_an_epilogue_replayed(ctx, T, act, residual):
+    """Several pieces a tile and several tiles a CTA, over and over."""
+    from paper_2607_28418_b200 import binding
+    x, w, b, r = make(T, 5000, 20001, bias=True, residual=torch.float32 if residual else None)
+    y = binding.wide_linear(ctx, x, w, bias=b, activation=act, residual=r, out_dtype=torch.float32)
+    check(y, x, w, b, act, r)
+    for _ in range(20):
+        assert torch.equal(binding.wide_linear(ctx, x, w, bias=b, activation=act, residual=r, out_dtype=torch.float32), y)
