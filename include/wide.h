@@ -434,8 +434,9 @@ WIDE_API int wide_qproj(wide_ctx* ctx, void* stream, const void* x, const void* 
  *   x [tokens, k] bf16, rows x_stride elements apart;  w [n, k] bf16;  bias [n] bf16 or NULL
  *   y [tokens, n] of out_dtype (bf16 or fp32), residual the same type or NULL, rows y_stride / residual_stride elements apart.
  *       residual may be y (equal strides); y must not overlap anything else that is read
- * Sums, bias, activation and residual are fp32, rounded once to out_dtype.  From one token to any number.  The same call gives the
- * same bits in every run.
+ * Sums, bias, activation and residual are fp32, rounded once to out_dtype; for fp32 outputs sums of 768 products at a time are added up
+ * (2^-20 of the result, whatever k is, on data without a trend).  From one token to any number.  The same call gives the same bits
+ * in every run.
  * Needs k % 8 == 0; x, y, residual and their rows 16-byte aligned, w and bias too.  n may be anything (columns from n on are not
  * written).  No workspace.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA; a bounded device wait that expires sets WIDE_ERR_TIMEOUT (wide_status).
@@ -600,7 +601,7 @@ WIDE_API int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cach
  * relation: row i of a sequence with n new rows and length L sees all positions j < L - n, and position L - n + j iff bit j % 32 of
  * tree_bits[row, j / 32] is 1 (its ancestors and, where the caller sets its own bit, itself):
  *     o[i, h, :] = sum_j softmax_j(scale * q[i, h, :] . k[j, h_kv, :]) v[j, h_kv, :] over the positions that it sees
- * with the keys and values that wide_cache_read returns in bf16.  Pairs whose routing group is off, and rows that see no key, give
+ * with the keys and values m + s n that the cache holds.  Pairs whose routing group is off, and rows that see no key, give
  * exact zeros; an infinity or a NaN in a new position reaches the rows that see it and no other.
  *   tree_bits uint32 [rows, tree_words], 1 <= tree_words <= 8.  A sequence with more than 32 * tree_words new rows is left out (its rows
  *       become zero) and sets WIDE_ERR_BAD_INDEX
@@ -609,8 +610,12 @@ WIDE_API int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cach
  *       need one each
  * After the accepted path is known its keys and values are written again at the positions they have in the answer
  * (wide_cache_write with the rows picked) and the length is set back.
- * Accuracy: probabilities are rounded to bf16 (2^-8 of themselves), sums are fp32, the output is rounded to bf16.  Keys, values and
- * queries of magnitude up to 2^100 such that logits and sums fit fp32.  The same call gives the same bits in every run.
+ * Accuracy: the output is rounded to bf16, sums are fp32.  Probabilities and values are rounded to fp16 (2^-11 of themselves, and 2^-32 of the
+ * largest probability), keys too (2^-11, and 2^-18 of the key's largest number), where that type holds them well: values block by block of
+ * 16 positions (sub-groups of zeros, or steps of 2^-13 to 2^10 and minima up to 2^14), keys where each eight neighbouring numbers of the queries that share
+ * a pass over them are zero or have their largest between 2^-9 and 2^14.  Elsewhere they are rounded to bf16 (2^-8).  Keys, values
+ * and queries of magnitude up to 2^100 such that logits, and 2^15 times the sum of the values, fit fp32.  The same call gives the same
+ * bits in every run.
  * Built for 16 query rows a KV head and more (up to 128 share a pass over the cache); fewer are served, wide_attn_cache
  * is quicker for a single row.  rows * n_q_heads <= 2^30.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, WORKSPACE, CUDA; WIDE_ERR_BAD_INDEX and WIDE_ERR_TIMEOUT through wide_status.

@@ -2,19 +2,29 @@
 // new tokens, those that its bits name.
 //
 // A tree of 8 to 64 tokens and 4 query heads a KV head has 32 to 256 query rows that share every key, many more than the 8 to 24 that
-// wide_attn_cache keeps in registers, so here the codes become bf16 tiles in shared memory once and the products run on
+// wide_attn_cache keeps in registers, so here the codes become 16-bit tiles in shared memory once and the products run on
 // tcgen05, 64 or 128 query rows a pass.  Keys are the 128-row operand, so what a tile costs follows the rows there are:
 //     S^T [128 keys (TMEM lanes)][rows]      = K [128 x D]   Q^T
 //     P^T = exp2(S^T scale - ref)              a thread has one key; written to shared memory as [key][row]
 //     O^T [D channels (lanes)][rows]        += V^T [D x 128] P^T   (V as unpacked, [key][channel], is the MN-major operand)
-// The reference `ref` of a row is raised (and its O rescaled in TMEM) only when a logit passes it by 2^kSlack; the sum over keys stays
-// in the threads and is made once an item.
+// The reference `ref` of a row is raised (and its O rescaled in TMEM) only when a logit passes it by 2^kSlack; the sums of P over the keys
+// are a second product, with ones in V's place.
 //
-// Roles: a warp that walks the items and brings 16-key blocks by bulk copies, eight warps that unpack them, eight that make P and
-// the outputs (four a group, the groups take turns of 16 rows), one thread for each of the two products.  K is unpacked for the next tile
-// while the softmax has this one.  Unpacking takes 3.75 instructions for two values: a code n in the low bits of the bf16 number 128
-// is 128 + n; taking 128 off is exact, and one fma rounds m + s n once, as wide_cache_read does.  With the fragment order in which
+// Everything 16-bit is fp16 where that holds it well, else bf16 (2^-11 against 2^-8: with bf16 for K, V and P the 2-norm of the error was 0.0033,
+// twice that of the output's own rounding, which is what is left now).  P is up to 2^15 (a row's largest is 2^7 when its reference is set), so that what fp16
+// loses at its lower end is 2^-32 of the largest.  A value's type goes by its block of 16 keys, a step of the product; queries' and keys' by the item; a
+// key out of the type's range is taken times a power of two, which its thread of the softmax puts into the logit.
+//
+// Roles: a warp that walks the items and brings 16-key blocks by bulk copies, eight warps that unpack them, sixteen that make P and
+// the outputs, in two streams, and a warp for each of the two products.  K is unpacked for the next tile while the softmax has this
+// one.  Unpacking takes 3.25 instructions for two values: a code n in the low bits of the fp16 number 1024 is 1024 + n, four bits further up 1024 + 16 n;
+// taking 1024 off is exact, and one fma rounds m + s n, or m + (s / 16) 16 n, once.  With the fragment order in which
 // the codes lie, keys go out as 16-byte rows and values through transposing 8x8 stores; O's channels come out permuted within 32.
+//
+// What bounds it: instruction issue.  A tile of 128 keys is some 5 thousand warp instructions to unpack and 2.6 (64 rows) or 5 thousand (128) to turn into
+// probabilities; a tile of 64 rows takes about 3400 clocks, of 128 rows 4900.  61 nodes on 32768 tokens, 32 heads on 8: 98 us in a stream of
+// calls; 32 sequences of 17 to 8192 tokens with 16 nodes each: 172 us.  What did not help: moving registers between the
+// warpgroups, unpacking K and V by warps of their own (eight left for the softmax: 117 against 100 us), packed fp32 arithmetic.
 //
 // Items are cut into equal pieces for the CTAs and joined as in wide_attn_cache (attn_plan.cuh).
 #include <cuda_fp16.h>
