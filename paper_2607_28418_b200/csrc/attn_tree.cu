@@ -21,9 +21,9 @@
 // taking 1024 off is exact, and one fma rounds m + s n, or m + (s / 16) 16 n, once.  With the fragment order in which
 // the codes lie, keys go out as 16-byte rows and values through transposing 8x8 stores; O's channels come out permuted within 32.
 //
-// What bounds it: instruction issue.  A tile of 128 keys is some 5 thousand warp instructions to unpack and 2.6 (64 rows) or 5 thousand (128) to turn into
+// What bounds it: instructions (issue slots are busy 56 % over a whole call, warps wait for their own results and hand-overs the rest).  A tile of 128 keys is some 5 thousand warp instructions to unpack and 2.6 (64 rows) or 5 thousand (128) to turn into
 // probabilities; a tile of 64 rows takes about 3400 clocks, of 128 rows 4900.  61 nodes on 32768 tokens, 32 heads on 8: 98 us in a stream of
-// calls; 32 sequences of 17 to 8192 tokens with 16 nodes each: 172 us.  What did not help: moving registers between the
+// calls; 32 sequences of 17 to 8192 tokens with 16 nodes each: 175 us.  What did not help: moving registers between the
 // warpgroups, unpacking K and V by warps of their own (eight left for the softmax: 117 against 100 us), packed fp32 arithmetic.
 //
 // Items are cut into equal pieces for the CTAs and joined as in wide_attn_cache (attn_plan.cuh).
