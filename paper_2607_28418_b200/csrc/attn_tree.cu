@@ -67,7 +67,7 @@ struct TreeArgs : AttnArgs {
 struct Tile {                       // what the roles are told of a tile
     int blk, nb;                    // first block, blocks
     uint32_t present;               // bit b: block b has a page
-    int first, last;                // of the item's part in this CTA
+    int first;                      // of the item's part in this CTA
     int index, left, item;          // tiles of the part before this one; behind it (2: two or more); the part's number
     int masked;                     // not all rows see all 128 keys
     int kvh, rb, row0, n_rows, len;
@@ -800,7 +800,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 if (lane == 0) {
                     if (present != (1u << nb) - 1u) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
                     Tile& d = sh.tiles[n % kDescs];
-                    d.blk = k.blk, d.nb = nb, d.present = present, d.first = first, d.last = last;
+                    d.blk = k.blk, d.nb = nb, d.present = present, d.first = first;
                     d.masked = present != (1u << kTile) - 1u || (k.blk + nb) * 16 > info.z - info.y;
                     d.kvh = k.kvh, d.rb = k.rb, d.row0 = info.x, d.n_rows = info.y, d.len = info.z;
                     d.item_rows = min(kRows, info.y * a.share - k.rb * kRows), d.rows_a_block = kRows;

@@ -328,3 +328,40 @@ def test_values_of_both_kinds_in_a_tile(ctx):
     bits, sees = random_trees(c, 11)
     ref, tol = reference(c, q, None, 4, sees)
     check(run(ctx, c, q, None, 4, bits), ref, tol)
+
+
+@pytest.mark.parametrize("dim,group", SHAPES)
+@pytest.mark.parametrize("new", [12, 40])
+def test_keys_of_many_sizes(ctx, dim, group, new):
+    """Keys that fp16 does not hold as they are, each with a power of two of its own, beside ordinary ones and zeros; queries that fit."""
+    c = CacheCase([530, 77], [new, 5], 2, dim, group, 32, seed=12)
+    factor = np.array([1.0, 2.0 ** -14, 0.0, 2.0 ** -40, 2.0 ** 4, 2.0 ** -9, 2.0 ** -100], dtype=np.float32)
+    c.k = [co.round_bf16(x * np.resize(factor, len(x))[:, None, None]) for x in c.k]
+    q = queries(c, 8, 13)
+    bits, sees = random_trees(c, 14)
+    ref, tol = reference(c, q, None, 4, sees)
+    check(run(ctx, c, q, None, 4, bits), ref, tol)
+
+
+def test_calls_on_two_streams(ctx):
+    """Trees of two streams at once, each with a workspace of its own, beside a linear layer: the bits of each call alone."""
+    from paper_2607_28418_b200 import binding
+    cases = [CacheCase([3000, 900], [30, 7], 4, 128, 64, 32, seed=21), CacheCase([700] * 12, [9] * 12, 4, 128, 64, 32, seed=22)]
+    x, w = torch.randn((40, 4096), device="cuda").bfloat16(), torch.randn((4096, 4096), device="cuda").bfloat16()
+    y = binding.wide_linear(ctx, x, w)
+    sets = []
+    for i, c in enumerate(cases):
+        q = to_device(queries(c, 16, 23 + i).reshape(c.rows, -1))
+        bits, _ = random_trees(c, 25 + i)
+        args = (ctx, q, c.cache(c.full_pages()), c.seqs(), 16, 4, bits.cuda())
+        work = torch.empty(binding.attn_tree_workspace_bytes(), dtype=torch.uint8, device="cuda")
+        sets.append((args, work, binding.wide_attn_tree(*args), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for args, work, _, stream in sets:
+            with torch.cuda.stream(stream):
+                got.append((binding.wide_attn_tree(*args, workspace=work), binding.wide_linear(ctx, x, w)))
+        torch.cuda.synchronize()
+        for (o, z), (_, _, alone, _) in zip(got, sets):
+            assert torch.equal(o, alone) and torch.equal(z, y)
