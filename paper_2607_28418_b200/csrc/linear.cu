@@ -46,14 +46,21 @@ struct LinearArgs {
     unsigned long long wait_ns;
 };
 
+template <int ACT>
+__device__ __forceinline__ float activate(float v) {
+    if (ACT == WIDE_ACT_SILU) return __fdividef(v, 1.f + __expf(-v));
+    if (ACT == WIDE_ACT_GELU) return 0.5f * v * erfcf(-0.70710678118654752f * v);
+    if (ACT == WIDE_ACT_GELU_TANH) {        // 0.5 v (1 + tanh u) = v / (1 + exp(-2 u))
+        const float u = 0.79788456080286536f * fmaf(0.044715f * v * v, v, v);
+        return __fdividef(v, 1.f + __expf(-2.f * u));
+    }
+    return v;
+}
 __device__ __forceinline__ float activate(float v, int act) {
     switch (act) {
-        case WIDE_ACT_SILU: return __fdividef(v, 1.f + __expf(-v));
-        case WIDE_ACT_GELU: return 0.5f * v * erfcf(-0.70710678118654752f * v);
-        case WIDE_ACT_GELU_TANH: {        // 0.5 v (1 + tanh u) = v / (1 + exp(-2 u))
-            const float u = 0.79788456080286536f * fmaf(0.044715f * v * v, v, v);
-            return __fdividef(v, 1.f + __expf(-2.f * u));
-        }
+        case WIDE_ACT_SILU: return activate<WIDE_ACT_SILU>(v);
+        case WIDE_ACT_GELU: return activate<WIDE_ACT_GELU>(v);
+        case WIDE_ACT_GELU_TANH: return activate<WIDE_ACT_GELU_TANH>(v);
         default: return v;
     }
 }
@@ -77,9 +84,8 @@ __device__ __forceinline__ float4 ld_cluster(uint32_t a) {
     return v;
 }
 
-// four neighbouring outputs of a row from channel f on
-__device__ __forceinline__ void finish(const LinearArgs& a, long long t, int f, float4 v, const float (&bias)[4]) {
-    float x[4] = {activate(v.x + bias[0], a.act), activate(v.y + bias[1], a.act), activate(v.z + bias[2], a.act), activate(v.w + bias[3], a.act)};
+// four neighbouring outputs of a row from channel f on: the residual, rounding
+__device__ __forceinline__ void put(const LinearArgs& a, long long t, int f, float (&x)[4]) {
     const int n = min(4, a.N - f);
     if (a.out_f32) {
         float* y = static_cast<float*>(a.y) + t * a.ys + f;
@@ -108,6 +114,11 @@ __device__ __forceinline__ void finish(const LinearArgs& a, long long t, int f, 
             for (int e = 0; e < n; ++e) y[e] = __float2bfloat16_rn(x[e] + (a.residual ? __bfloat162float(r[e]) : 0.f));
         }
     }
+}
+
+__device__ __forceinline__ void finish(const LinearArgs& a, long long t, int f, float4 v, const float (&bias)[4]) {
+    float x[4] = {activate(v.x + bias[0], a.act), activate(v.y + bias[1], a.act), activate(v.z + bias[2], a.act), activate(v.w + bias[3], a.act)};
+    put(a, t, f, x);
 }
 
 // Stages such that two CTAs fit on an SM: with one, a cluster of four or eight often has to wait for SMs of its own (128 tokens, 4096 x 4096: 37
@@ -294,20 +305,32 @@ struct Pair {
     static constexpr int kSmem = kStages * kStage + kPairEpi * 32 * 32 * 4 + 1024;
 };
 
-// 32 tokens (from t on) of a warp's 32 channels, which lie in its shared memory as [token][channel]: a lane has channels f .. f + 3 of
-// every fourth token.  All eight together, so that loads and the activation's steps of eight overlap.
+// 32 tokens of a warp's 32 channels, which lie in its shared memory as [token][channel]: a lane has channels f .. f + 3 of every fourth token.  Bias and
+// activation are a short loop of their own, in place: unrolled among the loads and stores below, the activation of 32 values was
+// more code than the instruction cache holds (333 tokens 1000 -> 5003 with GELU: 25.5 us against 16.8).
+template <int ACT>
+__device__ __forceinline__ void activate_block(float* block, int lane, const float (&bias)[4]) {
+#pragma unroll 1
+    for (int j = 0; j < 8; j += 2) {
+        float4* at = reinterpret_cast<float4*>(block + (4 * j + (lane >> 3)) * 32 + (lane & 7) * 4);
+        const float4 v = at[0], w = at[32];
+        at[0] = make_float4(activate<ACT>(v.x + bias[0]), activate<ACT>(v.y + bias[1]), activate<ACT>(v.z + bias[2]), activate<ACT>(v.w + bias[3]));
+        at[32] = make_float4(activate<ACT>(w.x + bias[0]), activate<ACT>(w.y + bias[1]), activate<ACT>(w.z + bias[2]), activate<ACT>(w.w + bias[3]));
+    }
+}
+__device__ __noinline__ void activate_any(float* block, int lane, int act, float b0, float b1, float b2, float b3) {
+    const float bias[4] = {b0, b1, b2, b3};
+    if (act == WIDE_ACT_SILU) activate_block<WIDE_ACT_SILU>(block, lane, bias);
+    else if (act == WIDE_ACT_GELU) activate_block<WIDE_ACT_GELU>(block, lane, bias);
+    else activate_block<WIDE_ACT_GELU_TANH>(block, lane, bias);
+}
+// All eight pieces of a lane together, from token t on, so that their loads overlap; `bias` is still to be added.
 __device__ __forceinline__ void finish_block(const LinearArgs& a, long long t, int f, const float* block, int lane, const float (&bias)[4]) {
     float x[8][4];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float4 v = *reinterpret_cast<const float4*>(block + (4 * j + (lane >> 3)) * 32 + (lane & 7) * 4);
         x[j][0] = v.x + bias[0], x[j][1] = v.y + bias[1], x[j][2] = v.z + bias[2], x[j][3] = v.w + bias[3];
-    }
-    if (a.act != WIDE_ACT_NONE) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[j][e] = activate(x[j][e], a.act);
     }
     const long long row = t + (lane >> 3);
     if (a.out_f32) {
@@ -480,15 +503,22 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
             float bias[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) bias[e] = a.bias && f + e < a.N ? __bfloat162float(a.bias[f + e]) : 0.f;
+            float left[4];          // of the bias, behind the activation
+#pragma unroll
+            for (int e = 0; e < 4; ++e) left[e] = a.act == WIDE_ACT_NONE ? bias[e] : 0.f;
             auto finish_32 = [&](int c) {          // the tokens from c on of this warp's half, which lie in its shared memory
                 __syncwarp();
                 const int t0 = at.t * kPairT + half * (kPairT / 2) + c;
+                if (a.act != WIDE_ACT_NONE && t0 < a.T) activate_any(mine, lane, a.act, bias[0], bias[1], bias[2], bias[3]);
                 if (f + 3 < a.N && t0 + 32 <= a.T) {
-                    finish_block(a, t0, f, mine, lane, bias);
+                    finish_block(a, t0, f, mine, lane, left);
                 } else if (f < a.N) {
 #pragma unroll 1
-                    for (int e = lane >> 3; e < 32 && t0 + e < a.T; e += 4)
-                        finish(a, static_cast<long long>(t0) + e, f, *reinterpret_cast<const float4*>(mine + e * 32 + (lane & 7) * 4), bias);
+                    for (int e = lane >> 3; e < 32 && t0 + e < a.T; e += 4) {
+                        const float4 v = *reinterpret_cast<const float4*>(mine + e * 32 + (lane & 7) * 4);
+                        float x[4] = {v.x + left[0], v.y + left[1], v.z + left[2], v.w + left[3]};
+                        put(a, static_cast<long long>(t0) + e, f, x);
+                    }
                 }
                 __syncwarp();
             };
