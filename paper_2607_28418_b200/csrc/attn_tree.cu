@@ -385,8 +385,6 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 const Tile& d = sh.tiles[n % kDescs];
                 const bool here = warp < d.nb && ((d.present >> warp) & 1u);
                 const uint32_t codes = sm + L::kCodes + st * L::kStage + warp * kSB, words = codes + 16 * D;
-                // the scores of the tile before have been made: K, and Q at the end of an item, may change
-                if (n > 0 && !(ok = mbar_wait_asleep_warp(bar(sh.k_free), (n - 1) & 1, a.wait_ns, abort_flag))) break;
                 if (d.first) {
                     // ---- queries in fp16 where each eight neighbours are zeros or have their largest between 2^-9 (so that what falls below the type's normal
                     // numbers is 2^-16 of it) and 2^14; one that is not leaves the item's queries and keys in bf16
@@ -415,6 +413,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     if (!(ok = mbar_wait_asleep_warp(bar(sh.q_meet), items++ & 1, a.wait_ns, abort_flag))) break;
                     const uint2 odds = *reinterpret_cast<const uint2*>(sh.q_wide[d.item & 3]);
                     wide_keys = (odds.x | odds.y) != 0;
+                    // the scores of the tile before have been made: Q may change
+                    if (n > 0 && !(ok = mbar_wait_asleep_warp(bar(sh.k_free), (n - 1) & 1, a.wait_ns, abort_flag))) break;
 #pragma unroll
                     for (int i = 0; i < kRows / kStep; ++i) {
                         const int r = r0 + i * kStep;
@@ -465,6 +465,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     }
                     __syncwarp();
                 }
+                // (K may change)
+                if (n > 0 && !d.first && !(ok = mbar_wait_asleep_warp(bar(sh.k_free), (n - 1) & 1, a.wait_ns, abort_flag))) break;
                 if (here && wide_keys) wide_keys_of<D, G>(codes, words, sm + L::kK + (warp * 16 + kr) * 128, kr, kc);
                 if (here && !wide_keys) {
                     const uint32_t row = sm + L::kK + (warp * 16 + kr) * 128;
