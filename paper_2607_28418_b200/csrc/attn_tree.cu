@@ -493,6 +493,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     sh.wide[n & 3][warp] = !half;
                     mbar_arrive(bar(sh.k_full));
                 }
+                __syncwarp();      // (whole-warp instructions behind code for some lanes: the lanes meet first, here and below)
                 // ---- values
                 if (n >= 2 && !(ok = mbar_wait_asleep_warp(bar(sh.v_free[n & 1]), ((n >> 1) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                 {
@@ -591,6 +592,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                 for (int e = 0; e < 16; ++e) x[e] = (see >> e) & 1u ? __uint_as_float(s[e]) * by : -CUDART_INF_F;
                                 const float top = largest_across_lanes(x, lane);
                                 if (!(lane & 1)) sh.most[quarter][64 * stream + 16 * c + (lane >> 1)] = top;
+                                __syncwarp();
                             }
                             if (!(ok = meet())) break;
 #pragma unroll 1
@@ -600,6 +602,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                 float now = fmaxf(fmaxf(fmaxf(sh.most[0][r], sh.most[1][r]), fmaxf(sh.most[2][r], sh.most[3][r])) - kHigh, old);
                                 now = fmaxf(now, -kNothing);              // of a row that has seen nothing: below every logit
                                 if (lane < 16) sh.minus_ref[ref_at ^ 1][r] = -now;         // (every warp of the group writes the same)
+                                __syncwarp();
                                 const float alpha = exp2_fast(old - now);
 #pragma unroll 1
                                 for (uint32_t at = L::kO; !fresh && at <= L::kSum; at += L::kSum - L::kO) {
@@ -659,6 +662,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                 const uint32_t row = sm + L::kP + stream * kHalf + key * 128;
                                 sts128(row + (((2 * c) ^ (key & 7)) << 4), p[0], p[1], p[2], p[3]);
                                 sts128(row + (((2 * c + 1) ^ (key & 7)) << 4), p[4], p[5], p[6], p[7]);
+                                if (!kPlain) __syncwarp();
                             }
                         };
                         if (plain) probabilities(std::true_type{});
@@ -745,6 +749,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                                         if (at == 0) *reinterpret_cast<float2*>(dst + kRows * D + 2 * rr) = make_float2(sum == 0.f ? -CUDART_INF_F : m, sum);
                                     }
                                 }
+                                __syncwarp();
                             }
                         }
                         if (!(ok = meet())) break;       // all have read what is cleared now
