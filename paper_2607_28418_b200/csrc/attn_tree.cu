@@ -935,10 +935,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 reinterpret_cast<uint4*>(a.o + static_cast<size_t>(i.x + r) * a.n_q * D)[v] = make_uint4(0, 0, 0, 0);
         }
     }
-    if (*abort_flag && tid == 0)
-        for (int i = 0; i < 64; ++i) __nanosleep(1000);   // copies in flight land before the shared memory is given up
     tc_fence_before_sync();
     __syncthreads();
+    if (*abort_flag) let_copies_land();
     if (warp == kScoreWarp) {
         tc_fence_after_sync();
         tmem_dealloc(tmem, L::kCols);

@@ -287,10 +287,9 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
         cluster_arrive();
         cluster_wait();
     }
-    if (*abort_flag && tid == 0)
-        for (int i = 0; i < 64; ++i) __nanosleep(1000);   // copies in flight land before the shared memory is given up
     tc_fence_before_sync();
     __syncthreads();
+    if (*abort_flag) let_copies_land();
     if (warp == 1) tmem_dealloc(tmem, kCols);
 }
 
@@ -571,10 +570,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
     }
     if (!ok && lane == 0) atomicExch(a.status, WIDE_ERR_TIMEOUT);
     __syncwarp();
-    if (*abort_flag && tid == 0)
-        for (int i = 0; i < 64; ++i) __nanosleep(1000);   // copies in flight land before the shared memory is given up
     tc_fence_before_sync();
     __syncthreads();
+    if (*abort_flag) let_copies_land();
     cluster_arrive();
     cluster_wait();            // no CTA leaves while the other may still reach into it
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * PT) : "memory");

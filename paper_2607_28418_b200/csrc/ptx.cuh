@@ -110,6 +110,13 @@ __device__ __forceinline__ bool mbar_wait_asleep_warp(uint32_t bar, uint32_t par
     return __all_sync(0xffffffffu, mbar_wait_asleep(bar, parity, limit_ns, abort_flag) ? 1 : 0) != 0;
 }
 
+// After a wait was given up, by threads behind a barrier of the whole CTA (any of its roles may have been the one that gave up, the last of them long after the others
+// were done): copies and products in flight land before the CTA returns its shared memory and its tensor memory.
+__device__ __forceinline__ void let_copies_land() {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);
+}
+
 // ------------------------------------------------------------------------------- programmatic dependent launch
 // A kernel launched with the programmatic-serialization attribute may become resident while the kernel
 // before it in the stream is still running (as soon as every CTA of that kernel has called

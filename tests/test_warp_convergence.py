@@ -73,3 +73,12 @@ def test_lanes_meet_before_whole_warp_instructions(name):
     found = []
     walk(lines, first, len(lines), False, found, meets)
     assert not sorted(set(found))
+
+
+@pytest.mark.parametrize("name,kernels", [("linear.cu", 2), ("attn_tree.cu", 1)])
+def test_a_wait_given_up_is_seen_behind_the_last_barrier(name, kernels):
+    """Copies may be in flight when any role of a kernel gives a wait up.  Whether one did is known behind the barrier that all roles come to, and not before it: a role that
+    is done early would find nothing."""
+    text = "".join(source(name))
+    assert len(re.findall(r"__syncthreads\(\);\s*if \(\*abort_flag\) let_copies_land\(\);", text)) == kernels
+    assert text.count("let_copies_land") == kernels and "__nanosleep" not in text
