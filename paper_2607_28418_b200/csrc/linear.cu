@@ -46,21 +46,39 @@ struct LinearArgs {
     unsigned long long wait_ns;
 };
 
-template <int ACT>
-__device__ __forceinline__ float activate(float v) {
-    if (ACT == WIDE_ACT_SILU) return __fdividef(v, 1.f + __expf(-v));
-    if (ACT == WIDE_ACT_GELU) return 0.5f * v * erfcf(-0.70710678118654752f * v);
-    if (ACT == WIDE_ACT_GELU_TANH) {        // 0.5 v (1 + tanh u) = v / (1 + exp(-2 u))
-        const float u = 0.79788456080286536f * fmaf(0.044715f * v * v, v, v);
-        return __fdividef(v, 1.f + __expf(-2.f * u));
+__device__ __forceinline__ float reciprocal(float x) {       // within 1 unit of the last place; 0 for x above 2^126
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// v / (1 + exp(-z)).  Divided by 1 + exp(-z) as it stands, it would be 0 from z = -87 on, where the divisor passes 2^126, though the result is a normal number down to -92.
+// EXACT keeps fp32's digits (8 units of the last place), with an exponential up to 1 (and a rounded quotient: 333 tokens 1000 -> 5003 with SiLU 24.7 us instead of
+// 14).  For bf16 the fast exponential does, though its error grows with z up to 2^-16; divisor and dividend are taken times 2^-43, so that
+// the divisor stays below 2^126 as far as there are results.
+template <bool EXACT>
+__device__ __forceinline__ float times_sigmoid(float v, float z) {
+    if (EXACT) {
+        const float e = expf(-fabsf(z)), r = reciprocal(1.f + e);
+        return v * (z >= 0.f ? r : e * r);
     }
+    constexpr float kUnit = 1.1368683772161603e-13f;
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fmaf(z, -1.4426950408889634f, -43.f)));
+    return v * (kUnit * reciprocal(kUnit + e));
+}
+template <int ACT, bool EXACT>
+__device__ __forceinline__ float activate(float v) {
+    if (ACT == WIDE_ACT_SILU) return times_sigmoid<EXACT>(v, v);
+    if (ACT == WIDE_ACT_GELU) return 0.5f * v * erfcf(-0.70710678118654752f * v);
+    if (ACT == WIDE_ACT_GELU_TANH) return times_sigmoid<EXACT>(v, 1.5957691216057307f * fmaf(0.044715f * v * v, v, v));     // v (1 + tanh u) / 2 = v / (1 + exp(-2 u))
     return v;
 }
+template <bool EXACT>
 __device__ __forceinline__ float activate(float v, int act) {
     switch (act) {
-        case WIDE_ACT_SILU: return activate<WIDE_ACT_SILU>(v);
-        case WIDE_ACT_GELU: return activate<WIDE_ACT_GELU>(v);
-        case WIDE_ACT_GELU_TANH: return activate<WIDE_ACT_GELU_TANH>(v);
+        case WIDE_ACT_SILU: return activate<WIDE_ACT_SILU, EXACT>(v);
+        case WIDE_ACT_GELU: return activate<WIDE_ACT_GELU, EXACT>(v);
+        case WIDE_ACT_GELU_TANH: return activate<WIDE_ACT_GELU_TANH, EXACT>(v);
         default: return v;
     }
 }
@@ -121,7 +139,19 @@ __device__ __forceinline__ void put(const LinearArgs& a, long long t, int f, flo
 }
 
 __device__ __forceinline__ void finish(const LinearArgs& a, long long t, int f, float4 v, const float (&bias)[4]) {
-    float x[4] = {activate(v.x + bias[0], a.act), activate(v.y + bias[1], a.act), activate(v.z + bias[2], a.act), activate(v.w + bias[3], a.act)};
+    float x[4] = {v.x + bias[0], v.y + bias[1], v.z + bias[2], v.w + bias[3]};
+    if (a.act != WIDE_ACT_NONE) {
+        if (a.out_f32) {
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {       // (a loop, as the code of four exact activations of each kind slows every call of few tokens down by a tenth)
+                const float y = activate<true>(x[0], a.act);
+                x[0] = x[1], x[1] = x[2], x[2] = x[3], x[3] = y;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = activate<false>(x[e], a.act);
+        }
+    }
     put(a, t, f, x);
 }
 
@@ -311,21 +341,23 @@ struct Pair {
 // 32 tokens of a warp's 32 channels, which lie in its shared memory as [token][channel]: a lane has channels f .. f + 3 of every fourth token.  Bias and
 // activation are a short loop of their own, in place: unrolled among the loads and stores below, the activation of 32 values was
 // more code than the instruction cache holds (333 tokens 1000 -> 5003 with GELU: 25.5 us against 16.8).
-template <int ACT>
+template <int ACT, bool EXACT>
 __device__ __forceinline__ void activate_block(float* block, int lane, const float (&bias)[4]) {
 #pragma unroll 1
     for (int j = 0; j < 8; j += 2) {
         float4* at = reinterpret_cast<float4*>(block + (4 * j + (lane >> 3)) * 32 + (lane & 7) * 4);
         const float4 v = at[0], w = at[32];
-        at[0] = make_float4(activate<ACT>(v.x + bias[0]), activate<ACT>(v.y + bias[1]), activate<ACT>(v.z + bias[2]), activate<ACT>(v.w + bias[3]));
-        at[32] = make_float4(activate<ACT>(w.x + bias[0]), activate<ACT>(w.y + bias[1]), activate<ACT>(w.z + bias[2]), activate<ACT>(w.w + bias[3]));
+        at[0] = make_float4(activate<ACT, EXACT>(v.x + bias[0]), activate<ACT, EXACT>(v.y + bias[1]), activate<ACT, EXACT>(v.z + bias[2]), activate<ACT, EXACT>(v.w + bias[3]));
+        at[32] = make_float4(activate<ACT, EXACT>(w.x + bias[0]), activate<ACT, EXACT>(w.y + bias[1]), activate<ACT, EXACT>(w.z + bias[2]), activate<ACT, EXACT>(w.w + bias[3]));
     }
 }
-__device__ __noinline__ void activate_any(float* block, int lane, int act, float b0, float b1, float b2, float b3) {
+__device__ __noinline__ void activate_any(float* block, int lane, int act, int exact, float b0, float b1, float b2, float b3) {
     const float bias[4] = {b0, b1, b2, b3};
-    if (act == WIDE_ACT_SILU) activate_block<WIDE_ACT_SILU>(block, lane, bias);
-    else if (act == WIDE_ACT_GELU) activate_block<WIDE_ACT_GELU>(block, lane, bias);
-    else activate_block<WIDE_ACT_GELU_TANH>(block, lane, bias);
+    if (act == WIDE_ACT_GELU) activate_block<WIDE_ACT_GELU, true>(block, lane, bias);       // (the same for both types)
+    else if (act == WIDE_ACT_SILU && exact) activate_block<WIDE_ACT_SILU, true>(block, lane, bias);
+    else if (act == WIDE_ACT_SILU) activate_block<WIDE_ACT_SILU, false>(block, lane, bias);
+    else if (exact) activate_block<WIDE_ACT_GELU_TANH, true>(block, lane, bias);
+    else activate_block<WIDE_ACT_GELU_TANH, false>(block, lane, bias);
 }
 // All eight pieces of a lane together, from token t on, so that their loads overlap; `bias` is still to be added.
 __device__ __forceinline__ void finish_block(const LinearArgs& a, long long t, int f, const float* block, int lane, const float (&bias)[4]) {
@@ -512,7 +544,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
             auto finish_32 = [&](int c) {          // the tokens from c on of this warp's half, which lie in its shared memory
                 __syncwarp();
                 const int t0 = at.t * kPairT + half * (kPairT / 2) + c;
-                if (a.act != WIDE_ACT_NONE && t0 < a.T) activate_any(mine, lane, a.act, bias[0], bias[1], bias[2], bias[3]);
+                if (a.act != WIDE_ACT_NONE && t0 < a.T) activate_any(mine, lane, a.act, a.out_f32, bias[0], bias[1], bias[2], bias[3]);
                 if (f + 3 < a.N && t0 + 32 <= a.T) {
                     finish_block(a, t0, f, mine, lane, left);
                 } else if (f < a.N) {
