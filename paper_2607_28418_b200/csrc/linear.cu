@@ -41,7 +41,6 @@ struct LinearArgs {
     void* y;
     long long rs, ys;                   // row strides in elements
     int act, out_f32;
-    int stream_weights;                 // one tile of tokens: weights are read once
     int* status;
     unsigned long long wait_ns;
 };
@@ -162,7 +161,7 @@ struct Small {
     static constexpr int kStages = NT == 16 ? 6 : NT == 32 ? 5 : NT == 64 ? 4 : 3, kStage = kABytes + NT * kBK * 2, kSmem = kStages * kStage + 1024;
 };
 
-// One tile of 128 channels and NT tokens a cluster.
+// A tile of 128 channels and all tokens, at most NT, a cluster: weights are read once.
 template <int NT, bool CHAIN>
 __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x,
                                                           const __grid_constant__ LinearArgs a) {
@@ -202,7 +201,7 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
     tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
     const int rank = a.split > 1 ? static_cast<int>(cluster_rank()) : 0;
-    const int tile = blockIdx.x / a.split, tile_n = tile % a.tiles_n, tile_t = tile / a.tiles_n;
+    const int tile = blockIdx.x / a.split;
     const int k0 = static_cast<int>(static_cast<long long>(a.nk) * rank / a.split), k1 = static_cast<int>(static_cast<long long>(a.nk) * (rank + 1) / a.split);
     grid_dep_launch();
 
@@ -214,9 +213,8 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
                 if (!mbar_wait(empty + 8 * s, ((i / kStages) & 1) ^ 1u, a.wait_ns, abort_flag)) break;
                 mbar_arrive_expect_tx(full + 8 * s, kStage);
                 const uint32_t at = smem_u32(base + s * kStage);
-                if (a.stream_weights) tma_load_2d_hint(at, &tm_w, k * kBK, tile_n * kM, full + 8 * s, once);
-                else tma_load_2d(at, &tm_w, k * kBK, tile_n * kM, full + 8 * s);
-                tma_load_2d(at + kABytes, &tm_x, k * kBK, tile_t * NT, full + 8 * s);
+                tma_load_2d_hint(at, &tm_w, k * kBK, tile * kM, full + 8 * s, once);
+                tma_load_2d(at + kABytes, &tm_x, k * kBK, 0, full + 8 * s);
             }
         }
     } else if (warp == 1) {
@@ -292,13 +290,13 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
     }
     if (warp >= 2 && ok) {
         const int t0 = NT * rank / a.split, t1 = NT * (rank + 1) / a.split;      // the tokens that this CTA joins
-        const int f = tile_n * kM + quarter * 32 + (lane & 7) * 4;
+        const int f = tile * kM + quarter * 32 + (lane & 7) * 4;
         float bias[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) bias[e] = a.bias && f + e < a.N ? __bfloat162float(a.bias[f + e]) : 0.f;
         const uint32_t mine = smem_u32(parts) + (quarter * 32 + (lane & 7) * 4) * 4;
         if (f < a.N) {
-            for (int t = t0 + (lane >> 3); t < t1 && tile_t * NT + t < a.T; t += 4) {
+            for (int t = t0 + (lane >> 3); t < t1 && t < a.T; t += 4) {
                 float4 v;
                 if (a.split == 1) {
                     v = *reinterpret_cast<const float4*>(parts + t * kM + quarter * 32 + (lane & 7) * 4);
@@ -309,7 +307,7 @@ __global__ void __launch_bounds__(kThreads) linear_kernel(const __grid_constant_
                         v = make_float4(v.x + z.x, v.y + z.y, v.z + z.z, v.w + z.w);
                     }
                 }
-                finish(a, static_cast<long long>(tile_t) * NT + t, f, v, bias);
+                finish(a, t, f, v, bias);
             }
         }
     }
@@ -637,9 +635,8 @@ int launch_small(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, lon
     if (!make_map(ctx, &tm_w, w, a.N, K, 2LL * K, kM) || !make_map(ctx, &tm_x, x, a.T, K, 2 * xs, NT)) return WIDE_ERR_CUDA;
     static std::atomic<unsigned> set{0};
     if (!allow_smem(ctx, linear_kernel<NT, CHAIN>, Small<NT>::kSmem, set)) return WIDE_ERR_CUDA;
-    const long long tiles = static_cast<long long>(a.tiles_n) * ((a.T + NT - 1) / NT);
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(tiles * a.split));
+    cfg.gridDim = dim3(static_cast<unsigned>(a.tiles_n * a.split));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = Small<NT>::kSmem;
     cfg.stream = s;
@@ -656,14 +653,12 @@ int launch_small(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, lon
     return WIDE_OK;
 }
 
+// T <= NT
 template <int NT>
 int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long xs, const void* w, int K) {
-    const long long tiles = static_cast<long long>(a.tiles_n) * ((a.T + NT - 1) / NT);
-    a.stream_weights = a.T <= NT;
     a.split = 1;
     // CTAs for three quarters of the SMs at least, as long as each keeps 8 steps of K (one token, 4096 x 4096: 4 parts 16.4 us, 8 parts 18.4)
-    while (a.split < 8 && 4 * tiles * a.split < 3 * ctx->sm_count && a.nk / (2 * a.split) >= 8) a.split *= 2;
-    if (tiles * a.split > 0x7fffffffLL) return WIDE_ERR_UNSUPPORTED_SHAPE;
+    while (a.split < 8 && 4LL * a.tiles_n * a.split < 3 * ctx->sm_count && a.nk / (2 * a.split) >= 8) a.split *= 2;
     return a.out_f32 && a.nk > kChain * a.split ? launch_small<NT, true>(ctx, s, a, x, xs, w, K) : launch_small<NT, false>(ctx, s, a, x, xs, w, K);
 }
 
