@@ -30,8 +30,8 @@ constexpr int kThreads = 192;           // TMA, MMA, four epilogue warps
 // fp32 outputs: after so many steps of kBK a sum goes on in the other accumulator, and the epilogue warps add the pieces up.  The tensor cores cut a sum
 // off at every addition, towards zero, so that a long one drifts: 2-norm of the error 4.4e-6 at K = 4096 in one piece, 1.0e-6 in pieces of 16
 // steps, 7e-7 of 12, 4.8e-7 of 8, whatever K.  With few tokens it costs nothing; 4096 tokens 4096 -> 14336 take 307, 338, 371, 394 us.  bf16 outputs,
-// whose rounding is 1.7e-3, keep one piece.
-constexpr int kChain = 12;
+// whose rounding is 1.7e-3 (2-norm), keep one piece up to kWhole steps: 65536 products of one sign lose 2.4e-4 there, a million would lose 2^-8.
+constexpr int kChain = 12, kWhole = 1024;
 
 struct LinearArgs {
     int T, N, nk;                       // nk: steps of kBK
@@ -659,7 +659,7 @@ int launch(wide_ctx* ctx, cudaStream_t s, LinearArgs a, const void* x, long long
     a.split = 1;
     // CTAs for three quarters of the SMs at least, as long as each keeps 8 steps of K (one token, 4096 x 4096: 4 parts 16.4 us, 8 parts 18.4)
     while (a.split < 8 && 4LL * a.tiles_n * a.split < 3 * ctx->sm_count && a.nk / (2 * a.split) >= 8) a.split *= 2;
-    return a.out_f32 && a.nk > kChain * a.split ? launch_small<NT, true>(ctx, s, a, x, xs, w, K) : launch_small<NT, false>(ctx, s, a, x, xs, w, K);
+    return a.nk > (a.out_f32 ? kChain : kWhole) * a.split ? launch_small<NT, true>(ctx, s, a, x, xs, w, K) : launch_small<NT, false>(ctx, s, a, x, xs, w, K);
 }
 
 template <int PT>
@@ -704,7 +704,7 @@ int wide_launch_linear(wide_ctx* ctx, cudaStream_t s, const void* x, int T, int 
     // Rounds of the pairs; a tile of 128 tokens takes 0.65 to 0.8 of one of 256, not half, as it reads shared memory at twice the rate for its
     // products (1024 tokens, 4096 -> 6144, three rounds of 128: 62 us, two of 256: 54).
     const long long pairs = ctx->sm_count / 2, wide = (pair_tiles<256>(a) + pairs - 1) / pairs, narrow = (pair_tiles<128>(a) + pairs - 1) / pairs;
-    const bool chain = a.out_f32 && a.nk > kChain;
+    const bool chain = a.nk > (a.out_f32 ? kChain : kWhole);
     if (8 * narrow < 10 * wide) return chain ? launch_pairs<128, true>(ctx, s, a, x, xs, w, K) : launch_pairs<128, false>(ctx, s, a, x, xs, w, K);
     return chain ? launch_pairs<256, true>(ctx, s, a, x, xs, w, K) : launch_pairs<256, false>(ctx, s, a, x, xs, w, K);
 }
