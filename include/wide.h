@@ -613,7 +613,7 @@ WIDE_API int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cach
  * (wide_cache_write with the rows picked) and the length is set back.
  * Accuracy: the output is rounded to bf16, sums are fp32.  Probabilities and values are rounded to fp16 (2^-11 of themselves, and 2^-32 of the
  * largest probability), keys too (2^-11, and 2^-18 of the key's largest number), where that type holds them well: values block by block of
- * 16 positions (sub-groups of zeros, or steps of 2^-13 to 2^10 and minima up to 2^14), keys where each eight neighbouring numbers of the queries that share
+ * 16 positions (sub-groups of zeros, of one number of 2^-14 to 2^14, or of steps of 2^-13 to 2^10 and minima up to 2^14), keys where each eight neighbouring numbers of the queries that share
  * a pass over them are zero or have their largest between 2^-9 and 2^14.  Elsewhere they are rounded to bf16 (2^-8).  Keys, values
  * and queries of magnitude up to 2^100 such that logits, and 2^15 times the sum of the values, fit fp32.  The same call gives the same
  * bits in every run.

@@ -235,6 +235,8 @@ __device__ __forceinline__ uint32_t to_half(uint32_t w) { return half_pair(low_o
 // smallest step; the largest is 2^10 and the minimum up to 2^14, so that no value is above 2^15.
 constexpr uint32_t kLeastKey = 0x3A80u, kLeastValue = 0x3900u;       // 2^-10: what is below fp16's normal numbers is 2^-18 of the key's largest; 2^-13: s / 16 is exact
 __device__ __forceinline__ bool fits_half(uint32_t w, uint32_t least) { return w == 0 || ((w & 0xFFFFu) - least < 0x4480u - least && (w & 0x7FFF0000u) < 0x46800000u); }
+// The same of a sub-group of one number (step 0): fp16 has its 8 digits as they are from 2^-14 up.
+__device__ __forceinline__ bool constant_fits_half(uint32_t w) { return (w & 0xFFFFu) == 0 && (w & 0x7FFF0000u) - 0x38800000u < 0x46800000u - 0x38800000u; }
 
 // The words of a warp's block of which some do not fit.  Out of line: few need it.  A key's are taken times a power of two so that its largest number is
 // 2^8 to 2^9 (the power goes into its logits), unless keys are bf16.  Values' stay bf16 where one does not fit.
@@ -252,7 +254,7 @@ __device__ __noinline__ bool odd_words(uint32_t words, float* key_by, bool wide_
         for (int o = 1; o < NS; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const uint32_t e = exponent_of(top);
         w[i] = lds32(at + 64 * NS);
-        half = __all_sync(0xffffffffu, fits_half(w[i], kLeastValue)) && half;
+        half = __all_sync(0xffffffffu, fits_half(w[i], kLeastValue) || constant_fits_half(w[i])) && half;
         if (!wide_keys) sts32(at, half_pair(low_of(kw) * times_to_256(e), high_of(kw) * times_to_256(e)));
         if (x % NS == 0) key_by[x / NS] = wide_keys ? scale : times_back(e) * scale;
     }
