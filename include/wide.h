@@ -611,7 +611,7 @@ WIDE_API int wide_attn_cache(wide_ctx* ctx, void* stream, const wide_cache* cach
  *       need one each
  * After the accepted path is known its keys and values are written again at the positions they have in the answer
  * (wide_cache_write with the rows picked) and the length is set back.
- * Accuracy: the output is rounded to bf16, sums are fp32.  Probabilities and values are rounded to fp16 (2^-11 of themselves, and 2^-32 of the
+ * Accuracy: the output is rounded to bf16, sums are fp32, of up to 65536 keys in a piece.  Probabilities and values are rounded to fp16 (2^-11 of themselves, and 2^-32 of the
  * largest probability), keys too (2^-11, and 2^-18 of the key's largest number), where that type holds them well: values block by block of
  * 16 positions (sub-groups of zeros, of one number of 2^-14 to 2^14, or of steps of 2^-13 to 2^10 and minima up to 2^14), keys where each eight neighbouring numbers of the queries that share
  * a pass over them are zero or have their largest between 2^-9 and 2^14.  Elsewhere they are rounded to bf16 (2^-8).  Keys, values

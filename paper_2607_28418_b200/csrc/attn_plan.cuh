@@ -29,7 +29,7 @@ struct AttnArgs {
     int* status;                   // takes WIDE_ERR_BAD_INDEX
     int plan_words;                // words of a sequence's head mask
     unsigned char* plan;           // the plan in the workspace, or NULL: every CTA makes its own in shared memory
-    float* heads;                  // partial results of warps whose first item began before their piece
+    float* heads;                  // partial results of warps whose first item began before their piece; of a portion of an item (wide_attn_tree)
     float* parts;                  // [CTA][2] partial results of CTAs
     int* meta;                     // [CTA][2][kMeta] {0 / 1 / 2: none, more follows, last piece; first row, rows, KV head, row block}
     int most_rows;                 // a sequence with more new rows is left out and reported

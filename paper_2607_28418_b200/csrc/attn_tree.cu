@@ -48,6 +48,10 @@ namespace {
 constexpr int kTile = 8;            // blocks of a tile: 128 keys
 constexpr int kKeys = 16 * kTile;
 constexpr int kMostRing = 3;        // tiles of codes on their way
+// A part of an item longer than this is taken in portions, whose results are joined in the workspace like those of CTAs.  The tensor cores cut a sum off at
+// every addition, a step of 16 keys, always towards zero: up to 2^-24 of the sum on average, so 4096 steps lose 2.4e-4.  In one portion, the 2-norm of the error over a
+// million keys was 0.0029 (64 rows, two streams) and 0.0055 (128 rows), and grew with the length (the sums of P lose more than outputs of both signs do): 0.0017 in portions, in the same time.
+constexpr int kPortion = 512;       // tiles
 constexpr int kDescs = 8;           // tiles that are known: the ring's, and at most three behind it whose softmax is not done
 constexpr int kUnpackWarps = 8, kSoftWarps = 16, kGroups = kSoftWarps / 4;
 constexpr int kLoadWarp = kUnpackWarps + kSoftWarps, kScoreWarp = kLoadWarp + 1, kValueWarp = kLoadWarp + 2, kWarps = kLoadWarp + 3;
@@ -67,12 +71,13 @@ struct TreeArgs : AttnArgs {
 struct Tile {                       // what the roles are told of a tile
     int blk, nb;                    // first block, blocks
     uint32_t present;               // bit b: block b has a page
-    int first;                      // of the item's part in this CTA
-    int index, left, item;          // tiles of the part before this one; behind it (2: two or more); the part's number
+    int first;                      // of a portion of the item's part in this CTA
+    int index, left, item;          // tiles of the portion before this one (2: two or more); behind it; the portion's number in the CTA
     int masked;                     // not all rows see all 128 keys
     int kvh, rb, row0, n_rows, len;
     int item_rows, rows_a_block;    // query rows of the item; of a whole one
     int begins, ends;               // whether the part has the item's first, last block
+    int goes_on, more;              // the portion is not the part's first, last one
     int final;                      // the CTA's last tile
 };
 
@@ -262,6 +267,45 @@ __device__ __noinline__ bool odd_words(uint32_t words, float* key_by, bool wide_
     for (int i = 0; i < (NS + 1) / 2; ++i)
         if (half) sts32(words + 64 * NS + 4 * (32 * i + (NS > 1 ? lane : lane & 15)), to_half(w[i]));
     return half;
+}
+
+// What two portions of an item's part weigh in their sum (x, y), and its reference.  -inf: the row has seen nothing.
+__device__ __forceinline__ float3 weights_of(const float2& held, const float2& now) {
+    const float top = fmaxf(held.x, now.x), use = top == -CUDART_INF_F ? 0.f : top;
+    return make_float3(exp2_fast(held.x - use), exp2_fast(now.x - use), top);
+}
+// A portion's results `now` join those before it in `held`; of an item's last portion they go out.  By the four warps of a group: a thread has a channel of the rows first .. first + 15 and 32
+// further on.  The weights in `held` change behind it (add_weights), when all have read them.  Out of line: one in 65536 keys needs it.
+template <int ROWS, int D>
+__device__ __noinline__ void add_portion(const TreeArgs* a, const Tile* d, float* held, const float* now, int first, int quarter) {
+    const int channel = quarter * 32 + (threadIdx.x & 31);
+    const bool out = d->begins && d->ends && !d->more;
+    const RowBlock rows = row_block(*a, d->rb * ROWS);
+    if (channel >= D) return;
+#pragma unroll 1
+    for (int e = 0; e < 32; ++e) {
+        const int r = first + e + (e & 16);
+        if (r >= d->item_rows) return;
+        const float2 h = *reinterpret_cast<const float2*>(held + ROWS * D + 2 * r), n = *reinterpret_cast<const float2*>(now + ROWS * D + 2 * r);
+        const float3 w = weights_of(h, n);
+        const float x = fmaf(held[r * D + channel], w.x, now[r * D + channel] * w.y);
+        if (out) {
+            const float sum = fmaf(h.y, w.x, n.y * w.y);
+            const RowOut ro = row_out(*a, d->row0, d->n_rows, d->kvh, row_of(*a, rows, r), D);
+            if (ro.o) ro.o[channel] = __float2bfloat16_rn(ro.on && sum != 0.f ? __fdividef(x, sum) : 0.f);
+        } else {
+            held[r * D + channel] = x;
+        }
+    }
+}
+// by one warp, a row a lane
+template <int ROWS, int D>
+__device__ __noinline__ void add_weights(float* held, const float* now, int first) {
+    const int r = first + (threadIdx.x & 31) + (threadIdx.x & 16);
+    float2* h = reinterpret_cast<float2*>(held + ROWS * D + 2 * r);
+    const float2 n = *reinterpret_cast<const float2*>(now + ROWS * D + 2 * r);
+    const float3 w = weights_of(*h, n);
+    *h = make_float2(w.z, fmaf(h->y, w.x, n.y * w.y));
 }
 
 // A warp's block of keys in bf16: the form of the kernel's loop for fp16.
@@ -700,8 +744,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         tc_fence_after_sync();
                         // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j
                         const int at = quarter * 32 + lane, channel = (at & ~31) + 4 * (lane & 7) + (lane >> 3);
-                        const bool whole = d.begins && d.ends;
-                        float* dst = parts + (d.begins ? slot_floats(kRows, D) : 0);
+                        const bool whole = d.begins && d.ends && !d.more && !d.goes_on;
+                        float *slot = parts + (d.begins ? slot_floats(kRows, D) : 0), *dst = d.goes_on ? a.heads + static_cast<size_t>(cta) * slot_floats(kRows, D) : slot;
                         const RowBlock rows = row_block(a, d.rb * kRows);
 #pragma unroll 1
                         for (int c = gi; 16 * c < n_rows && c < 4; c += 2) {
@@ -757,6 +801,11 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         if (!(ok = meet())) break;       // all have read what is cleared now
                         for (int c = gi; c < 4; c += 2)
                             if (quarter == 0 && lane < 16) sh.spoilt[L::spoilt_at(d.item, row0 + 16 * c + lane)] = 0;
+                        if (d.goes_on) {
+                            add_portion<kRows, D>(&a, &d, slot, dst, row0 + 16 * gi, quarter);
+                            if (!(ok = meet())) break;
+                            if (quarter == 0) add_weights<kRows, D>(slot, dst, row0 + 16 * gi);
+                        }
                         tc_fence_before_sync();
                         __syncwarp();
                         if (NB == 1 && lane == 0) {
@@ -776,7 +825,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             Cursor k = sh.start;
             const int sub_shift = a.c.page_shift - 4, sub_mask = (1 << sub_shift) - 1;
             bool ok = true, first = true;
-            int index = 0, item = 0;
+            int index = 0, item = 0, portion = 0;
             int first_blk = k.blk, pt_first = -1000000, pt = -1, pt_next = -1;
             for (int n = 0;; ++n) {
                 const int st = n % kRing, nb = min(kTile, k.end - k.blk), from = k.blk >> sub_shift, to = (k.blk + nb - 1) >> sub_shift;
@@ -804,7 +853,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 next.blk += nb;
                 const bool last = next.blk >= next.end, begins = first_blk == 0, ends = k.end == k.n_blk;
                 if (last && next.left > 0) next_item(a, plan, next);
-                const bool final = last && next.blk >= next.end;
+                const bool final = last && next.blk >= next.end, closes = last || index + 1 == kPortion;
                 if (n >= kRing && !(ok = mbar_wait_asleep_warp(bar(sh.ring_empty[st]), ((n / kRing) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                 if (lane == 0) {
                     if (present != (1u << nb) - 1u) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
@@ -813,8 +862,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     d.masked = present != (1u << kTile) - 1u || (k.blk + nb) * 16 > info.z - info.y;
                     d.kvh = k.kvh, d.rb = k.rb, d.row0 = info.x, d.n_rows = info.y, d.len = info.z;
                     d.item_rows = min(kRows, info.y * a.share - k.rb * kRows), d.rows_a_block = kRows;
-                    d.begins = begins, d.ends = ends, d.final = final;
-                    d.index = min(index, 2), d.item = item, d.left = last ? 0 : k.end - (k.blk + nb) <= kTile ? 1 : 2;
+                    d.begins = begins, d.ends = ends, d.goes_on = portion > 0, d.more = !last, d.final = final;
+                    d.index = min(index, 2), d.item = item, d.left = closes ? 0 : k.end - (k.blk + nb) <= kTile || index + 2 == kPortion ? 1 : 2;
                     mbar_arrive_expect_tx(bar(sh.ring_full[st]), __popc(present) * kSB);
                 }
                 __syncwarp();
@@ -834,11 +883,12 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     open |= begins ? 2 : 1;
                 }
                 if (final) break;
-                first = last;
+                first = closes;
                 ++index;
-                if (last) {
+                if (closes) {
                     index = 0;
                     ++item;
+                    portion = last ? 0 : portion + 1;
                 }
                 if (last) {
                     if (next.seq != k.seq) pt_first = -1000000;
@@ -1024,7 +1074,7 @@ __global__ void __launch_bounds__(256) attn_tree_join_kernel(const __grid_consta
 }
 
 struct Work {
-    size_t plan, parts, meta, total;
+    size_t plan, parts, portions, meta, total;
 };
 Work work_layout() {
     Work w;
@@ -1033,6 +1083,8 @@ Work work_layout() {
     at += wide_align_up(plan_bytes(WIDE_MAX_SEQS, 8, 8), 256);
     w.parts = at;
     at += wide_align_up(static_cast<size_t>(kMaxCtas) * 2 * slot_floats(128, 128) * 4, 256);
+    w.portions = at;
+    at += wide_align_up(static_cast<size_t>(kMaxCtas) * slot_floats(128, 128) * 4, 256);
     w.meta = at;
     at += static_cast<size_t>(kMaxCtas) * 2 * kMeta * 4;
     w.total = wide_align_up(at, 256);
@@ -1045,7 +1097,7 @@ int launch(wide_ctx* ctx, cudaStream_t s, TreeArgs a, unsigned char* ws) {
     auto kernel = attn_tree_kernel<D, G, NB>;
     const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
     const Work w = work_layout();
-    a.heads = nullptr;
+    a.heads = reinterpret_cast<float*>(ws + w.portions);
     a.parts = reinterpret_cast<float*>(ws + w.parts);
     a.meta = reinterpret_cast<int*>(ws + w.meta);
     a.plan = nullptr;
