@@ -37,6 +37,7 @@
 namespace {
 
 constexpr int kItemAlone = 96;     // blocks of an item that one CTA may take alone
+constexpr int kItemJoin = kItemAlone, kItemShort = kItemAlone;     // whenever there are CTAs for all
 constexpr int kItemCost = 4;       // units that an item counts on top of its blocks: queries in, results out
 
 }  // namespace

@@ -1,6 +1,7 @@
 // The work of an attention over the cache: items (sequence, KV head in use, block of query rows) laid end to end on a line that is cut for the
 // CTAs, and the joining of items that were cut.  The including file says how many units an item counts on top of its blocks
-// (kItemCost) and up to how many blocks one CTA may take an item alone (kItemAlone).
+// (kItemCost), up to how many blocks one CTA may take an item alone (kItemAlone), how many blocks' time it takes to join what is cut (kItemJoin), and with how many
+// blocks of room a sequence that is not asked (kItemShort).
 #pragma once
 
 #include <math_constants.h>
@@ -125,7 +126,9 @@ __device__ void make_plan(const AttnArgs& a, const Plan& p, long long* part, int
             sum += static_cast<int>(part[w] >> 32);
             same = max(same, static_cast<int>(part[w]));
         }
-        same = sum <= ctas ? same + kItemCost : 0;
+        // (an item alone, same blocks, against an even cut, sum * (same + kItemCost) / ctas, and the joining)
+        const bool brief = (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) <= kItemShort;
+        same = sum <= ctas && (brief || same * (ctas - sum) <= sum * kItemCost + kItemJoin * ctas) ? same + kItemCost : 0;
         __syncthreads();
     }
     if (tid == 0) *p.same = same;

@@ -36,8 +36,11 @@
 
 namespace {
 
-constexpr int kItemAlone = 96;     // blocks of an item that one CTA may take alone
 constexpr int kItemCost = 40;      // units that an item counts on top of its blocks: queries in, results out
+// One CTA takes an item alone where cutting it would take longer.  us alone / cut: 8 items of 32 blocks 23.8 / 20.5, of 94 38.7 / 22.4; 40 items of 32 blocks 25.2 / 26.2, of 44
+// 28.9 / 26.3, of 94 39.6 / 31.0; 96 items of 44 blocks 28.6 / 32.3, of 94 39.9 / 42.5: joining is 10 to 17 blocks.  A launch that knows that nothing is
+// cut saves the joining kernel, 2.5 us, so where page tables have room for kItemShort blocks nothing is (8 items of 19 blocks 21.5 / 20.3, 96 items 22.6 / 26.5).
+constexpr int kItemAlone = 96, kItemJoin = 14, kItemShort = 24;
 
 }  // namespace
 
@@ -1119,7 +1122,7 @@ int launch(wide_ctx* ctx, cudaStream_t s, TreeArgs a, unsigned char* ws) {
     }
     // Nothing to join where the plan is certain to give every item a CTA of its own (make_plan).
     const long long items = static_cast<long long>(a.c.n_kv_heads) * (static_cast<long long>(a.q.rows) * a.share / L::kRows + a.q.n_seqs);
-    if (items > ctas || (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) > kItemAlone) {
+    if (items > ctas || (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) > kItemShort) {
         WideLaunch l(ctx, s, "attn_tree_join");
         WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_tree_join_kernel<L::kRows, D>, dim3(ctas, kJoinParts), dim3(256), 0, s, a, ctas));
     }

@@ -1,6 +1,7 @@
 """wide_attn_tree where routing groups are not the query heads of a KV head, and with many KV heads."""
 import numpy as np
 import pytest
+import torch
 
 from tests.cache_util import CacheCase
 from tests.test_gpu_u_attn_tree import check, ctx, queries, random_trees, reference, run  # noqa: F401
@@ -58,3 +59,20 @@ def test_items_cut_between_ctas_with_such_groups(ctx, share, news):  # noqa: F81
     bits, sees = random_trees(c, 54)
     ref, tol = reference(c, q, on, per, sees)
     check(run(ctx, c, q, on, per, bits), ref, tol)
+
+
+@pytest.mark.parametrize("heads,seqs", [(1, 1), (2, 4), (8, 5)])
+@pytest.mark.parametrize("tokens", [200, 384, 400, 1540])
+@pytest.mark.parametrize("room", [0, 300])
+def test_short_items_alone_or_cut(ctx, heads, seqs, tokens, room):  # noqa: F811
+    """Few short items, around the lengths from which they are cut, with page tables that just fit and with wide ones: whatever is cut is joined."""
+    from paper_2607_28418_b200 import binding
+    from tests.cache_util import to_device
+    c = CacheCase([tokens - 3 * i for i in range(seqs)], [9] * seqs, heads, 64, 64, 16, seed=tokens)
+    q = queries(c, 4 * heads, 55)
+    bits, sees = random_trees(c, 56)
+    ref, tol = reference(c, q, None, 4, sees)
+    wide = np.pad(c.table, ((0, 0), (0, room)), constant_values=-1)
+    places = binding.Sequences(torch.from_numpy(wide).cuda(), torch.tensor(c.lens, dtype=torch.int32).cuda(), torch.from_numpy(c.row_start).cuda())
+    o = torch.full((c.rows, 4 * heads * 64), float("nan"), device="cuda").bfloat16()
+    check(binding.wide_attn_tree(ctx, to_device(q.reshape(c.rows, -1)), c.cache(c.full_pages()), places, 4 * heads, 4, bits.cuda(), o=o), ref, tol)
