@@ -53,7 +53,7 @@ constexpr int kKeys = 16 * kTile;
 constexpr int kMostRing = 3;        // tiles of codes on their way
 // A part of an item longer than this is taken in portions, whose results are joined in the workspace like those of CTAs.  The tensor cores cut a sum off at
 // every addition, a step of 16 keys, always towards zero: up to 2^-24 of the sum on average, so 4096 steps lose 2.4e-4.  In one portion, the 2-norm of the error over a
-// million keys was 0.0029 (64 rows, two streams) and 0.0055 (128 rows), and grew with the length (the sums of P lose more than outputs of both signs do): 0.0017 in portions, in the same time.
+// million keys was 0.0029 (64 rows, two streams) and 0.0055 (128 rows), and grew with the length (the sums of P lose more than outputs of both signs do): 0.0017 in portions.
 constexpr int kPortion = 512;       // tiles
 constexpr int kDescs = 8;           // tiles that are known: the ring's, and at most three behind it whose softmax is not done
 constexpr int kUnpackWarps = 8, kSoftWarps = 16, kGroups = kSoftWarps / 4;
@@ -342,7 +342,8 @@ __device__ __noinline__ void wide_values(uint32_t codes, uint32_t words, uint32_
     }
 }
 
-template <int D, int G, int NB>
+// LONG: a CTA's part of an item may be longer than a portion.  (A form of its own: the call that joins portions, which few need, costs the softmax's warps 2 to 15 %.)
+template <int D, int G, int NB, bool LONG>
 __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_constant__ TreeArgs a) {
     using L = Layout<D, G, NB>;
     constexpr int kRows = L::kRows, kNS = L::kNS, kSB = L::kSB, kRing = L::kRing;
@@ -747,8 +748,8 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         tc_fence_after_sync();
                         // lane (c, a, j, g) of O has channel 64 c + 32 a + 4 g + j
                         const int at = quarter * 32 + lane, channel = (at & ~31) + 4 * (lane & 7) + (lane >> 3);
-                        const bool whole = d.begins && d.ends && !d.more && !d.goes_on;
-                        float *slot = parts + (d.begins ? slot_floats(kRows, D) : 0), *dst = d.goes_on ? a.heads + static_cast<size_t>(cta) * slot_floats(kRows, D) : slot;
+                        const bool goes_on = LONG && d.goes_on, whole = d.begins && d.ends && !(LONG && d.more) && !goes_on;
+                        float *slot = parts + (d.begins ? slot_floats(kRows, D) : 0), *dst = goes_on ? a.heads + static_cast<size_t>(cta) * slot_floats(kRows, D) : slot;
                         const RowBlock rows = row_block(a, d.rb * kRows);
 #pragma unroll 1
                         for (int c = gi; 16 * c < n_rows && c < 4; c += 2) {
@@ -804,10 +805,12 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                         if (!(ok = meet())) break;       // all have read what is cleared now
                         for (int c = gi; c < 4; c += 2)
                             if (quarter == 0 && lane < 16) sh.spoilt[L::spoilt_at(d.item, row0 + 16 * c + lane)] = 0;
-                        if (d.goes_on) {
-                            add_portion<kRows, D>(&a, &d, slot, dst, row0 + 16 * gi, quarter);
-                            if (!(ok = meet())) break;
-                            if (quarter == 0) add_weights<kRows, D>(slot, dst, row0 + 16 * gi);
+                        if constexpr (LONG) {
+                            if (goes_on) {
+                                add_portion<kRows, D>(&a, &d, slot, dst, row0 + 16 * gi, quarter);
+                                if (!(ok = meet())) break;
+                                if (quarter == 0) add_weights<kRows, D>(slot, dst, row0 + 16 * gi);
+                            }
                         }
                         tc_fence_before_sync();
                         __syncwarp();
@@ -856,7 +859,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 next.blk += nb;
                 const bool last = next.blk >= next.end, begins = first_blk == 0, ends = k.end == k.n_blk;
                 if (last && next.left > 0) next_item(a, plan, next);
-                const bool final = last && next.blk >= next.end, closes = last || index + 1 == kPortion;
+                const bool final = last && next.blk >= next.end, closes = last || (LONG && index + 1 == kPortion);
                 if (n >= kRing && !(ok = mbar_wait_asleep_warp(bar(sh.ring_empty[st]), ((n / kRing) & 1) ^ 1, a.wait_ns, abort_flag))) break;
                 if (lane == 0) {
                     if (present != (1u << nb) - 1u) atomicExch(a.status, WIDE_ERR_BAD_INDEX);
@@ -865,8 +868,9 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                     d.masked = present != (1u << kTile) - 1u || (k.blk + nb) * 16 > info.z - info.y;
                     d.kvh = k.kvh, d.rb = k.rb, d.row0 = info.x, d.n_rows = info.y, d.len = info.z;
                     d.item_rows = min(kRows, info.y * a.share - k.rb * kRows), d.rows_a_block = kRows;
-                    d.begins = begins, d.ends = ends, d.goes_on = portion > 0, d.more = !last, d.final = final;
-                    d.index = min(index, 2), d.item = item, d.left = closes ? 0 : k.end - (k.blk + nb) <= kTile || index + 2 == kPortion ? 1 : 2;
+                    d.begins = begins, d.ends = ends, d.final = final;
+                    if (LONG) d.goes_on = portion > 0, d.more = !last;
+                    d.index = min(index, 2), d.item = item, d.left = closes ? 0 : k.end - (k.blk + nb) <= kTile || (LONG && index + 2 == kPortion) ? 1 : 2;
                     mbar_arrive_expect_tx(bar(sh.ring_full[st]), __popc(present) * kSB);
                 }
                 __syncwarp();
@@ -891,7 +895,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
                 if (closes) {
                     index = 0;
                     ++item;
-                    portion = last ? 0 : portion + 1;
+                    if (LONG) portion = last ? 0 : portion + 1;
                 }
                 if (last) {
                     if (next.seq != k.seq) pt_first = -1000000;
@@ -1094,11 +1098,10 @@ Work work_layout() {
     return w;
 }
 
-template <int D, int G, int NB>
-int launch(wide_ctx* ctx, cudaStream_t s, TreeArgs a, unsigned char* ws) {
+template <int D, int G, int NB, bool LONG>
+int launch(wide_ctx* ctx, cudaStream_t s, TreeArgs a, unsigned char* ws, int ctas, bool joins) {
     using L = Layout<D, G, NB>;
-    auto kernel = attn_tree_kernel<D, G, NB>;
-    const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
+    auto kernel = attn_tree_kernel<D, G, NB, LONG>;
     const Work w = work_layout();
     a.heads = reinterpret_cast<float*>(ws + w.portions);
     a.parts = reinterpret_cast<float*>(ws + w.parts);
@@ -1120,24 +1123,35 @@ int launch(wide_ctx* ctx, cudaStream_t s, TreeArgs a, unsigned char* ws) {
         WideLaunch l(ctx, s, "attn_tree");
         WIDE_CUDA_CHECK(wide_launch_after(ctx, kernel, dim3(ctas), dim3(32 * kWarps), L::kSmem, s, a));
     }
-    // Nothing to join where the plan is certain to give every item a CTA of its own (make_plan).
-    const long long items = static_cast<long long>(a.c.n_kv_heads) * (static_cast<long long>(a.q.rows) * a.share / L::kRows + a.q.n_seqs);
-    if (items > ctas || (static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4)) > kItemShort) {
+    if (joins) {
         WideLaunch l(ctx, s, "attn_tree_join");
         WIDE_CUDA_CHECK(wide_launch_after(ctx, attn_tree_join_kernel<L::kRows, D>, dim3(ctas, kJoinParts), dim3(256), 0, s, a, ctas));
     }
     return WIDE_OK;
 }
 
+template <int NB, bool LONG>
+int launch_dims(wide_ctx* ctx, cudaStream_t s, const TreeArgs& a, int D, int G, unsigned char* ws, int ctas, bool joins) {
+    if (D == 128) {
+        if (G == 128) return launch<128, 128, NB, LONG>(ctx, s, a, ws, ctas, joins);
+        if (G == 64) return launch<128, 64, NB, LONG>(ctx, s, a, ws, ctas, joins);
+        return launch<128, 32, NB, LONG>(ctx, s, a, ws, ctas, joins);
+    }
+    if (G == 64) return launch<64, 64, NB, LONG>(ctx, s, a, ws, ctas, joins);
+    return launch<64, 32, NB, LONG>(ctx, s, a, ws, ctas, joins);
+}
+
 template <int NB>
 int launch_shape(wide_ctx* ctx, cudaStream_t s, const TreeArgs& a, int D, int G, unsigned char* ws) {
-    if (D == 128) {
-        if (G == 128) return launch<128, 128, NB>(ctx, s, a, ws);
-        if (G == 64) return launch<128, 64, NB>(ctx, s, a, ws);
-        return launch<128, 32, NB>(ctx, s, a, ws);
-    }
-    if (G == 64) return launch<64, 64, NB>(ctx, s, a, ws);
-    return launch<64, 32, NB>(ctx, s, a, ws);
+    const int ctas = ctx->sm_count < kMaxCtas ? ctx->sm_count : kMaxCtas;
+    // What is known without the lengths: as many items at most, of as many blocks.
+    const long long items = static_cast<long long>(a.c.n_kv_heads) * (static_cast<long long>(a.q.rows) * a.share / (64 * NB) + a.q.n_seqs);
+    const long long blocks = static_cast<long long>(a.q.max_pages) << (a.c.page_shift - 4);
+    // Nothing to join where the plan is certain to give every item a CTA of its own (make_plan).
+    const bool joins = items > ctas || blocks > kItemShort;
+    // The longest part of an item that a CTA can have: all of it, or the CTA's share of the line.
+    const bool portions = blocks > kPortion * kTile && items * (blocks + kItemCost) / ctas >= kPortion * kTile;
+    return portions ? launch_dims<NB, true>(ctx, s, a, D, G, ws, ctas, joins) : launch_dims<NB, false>(ctx, s, a, D, G, ws, ctas, joins);
 }
 
 }  // namespace
