@@ -437,7 +437,8 @@ WIDE_API int wide_qproj(wide_ctx* ctx, void* stream, const void* x, const void* 
  * Sums, bias, activation and residual are fp32, rounded once to out_dtype.  Sums of 768 products at a time are added up for fp32 outputs (2-norm of the
  * error below 2^-19 of the results', whatever k is, on data without a trend), of up to 65536 for bf16.  For fp32 outputs the activation is within 2^-20 of itself, or 2^-20 + 3 z 2^-23 where
  * a GELU's lower tail is v exp(-z).  An activation of +inf is +inf, of -inf NaN (0 times infinity, as in the formulas).
- * From one token to any number.  The same call gives the same bits in every run.
+ * From one token to any number: about as fast as a library product for up to 64 tokens and from about 2000 on, up to 45 % slower between.
+ * The same call gives the same bits in every run.
  * Needs k % 8 == 0; x, y, residual and their rows 16-byte aligned, w and bias too.  n may be anything (columns from n on are not
  * written).  No workspace.
  * Errors: INVALID_ARG, UNSUPPORTED_SHAPE, ALIGNMENT, CUDA; a bounded device wait that expires sets WIDE_ERR_TIMEOUT (wide_status).

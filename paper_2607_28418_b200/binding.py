@@ -797,7 +797,7 @@ def wide_attn_tree(ctx: Context, q: torch.Tensor, cache: Cache, seqs: Sequences,
                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """wide_attn_cache for trees of drafted tokens: row i of a sequence sees its prefix and, of the sequence's new rows, those whose bits
     tree_bits int32 [rows, ceil(most new rows / 32)] names (``tree_ancestors`` makes them of parents).  ``workspace`` (uint8,
-    attn_tree_workspace_bytes) replaces the context's own scratch.  Rows that belong to no sequence are not written."""
+    attn_tree_workspace_bytes) replaces the context's own scratch, which calls on one stream share.  Rows that belong to no sequence are not written."""
     width = n_q_heads * cache.head_dim
     qp, qs = _rows(q, width, "q")
     rows = q.shape[0]

@@ -21,9 +21,10 @@
 // taking 1024 off is exact, and one fma rounds m + s n, or m + (s / 16) 16 n, once.  With the fragment order in which
 // the codes lie, keys go out as 16-byte rows and values through transposing 8x8 stores; O's channels come out permuted within 32.
 //
-// What bounds it: instructions (issue slots are busy 56 % over a whole call, warps wait for their own results and hand-overs the rest).  A tile of 128 keys is some 5 thousand warp instructions to unpack and 2.6 (64 rows) or 5 thousand (128) to turn into
-// probabilities; a tile of 64 rows takes about 3400 clocks, of 128 rows 4900.  61 nodes on 32768 tokens, 32 heads on 8: 98 us in a stream of
-// calls; 32 sequences of 17 to 8192 tokens with 16 nodes each: 175 us.  What did not help: moving registers between the
+// What bounds it: instructions and hand-overs.  In long items a tile of 128 keys is 8.5 thousand warp instructions with 64 rows and 11.3 with 128, and takes 3700 and 4800 clocks (57 and
+// 59 % of the issue slots; over a whole call 56 %).  So 64 rows' probabilities are 2.8 thousand, and 5.6 are the unpacking: 1.7 of them the arithmetic above, the rest parameters and
+// their words, addresses, stores, waits.  61 nodes on 32768 tokens, 32 heads on 8: 98 us in a stream of calls; 32 sequences of 17 to
+// 8192 tokens with 16 nodes each: 175 us.  What did not help: moving registers between the
 // warpgroups, unpacking K and V by warps of their own (eight left for the softmax: 117 against 100 us), packed fp32 arithmetic.
 //
 // Items are cut into equal pieces for the CTAs and joined as in wide_attn_cache (attn_plan.cuh).
@@ -588,8 +589,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) attn_tree_kernel(const __grid_
             // Two streams of eight warps, each with a buffer of P, outputs and references of its own, that wait for each other only at the end of an
             // item: what one waits for (its product, its four warps' agreement) the other fills, and their steps of different kinds
             // overlap.  With 128 rows a stream has 64 of them; with 64 rows it has every other tile, and the two results are joined at the end.
-            // Of its 64 rows a stream's group of four warps has the runs of 16 rows `gi` and gi + 2.  (One stream of all sixteen warps: 3400
-            // clocks a tile of 64 rows, 5000 of 128.)
+            // Of its 64 rows a stream's group of four warps has the runs of 16 rows `gi` and gi + 2.
             const int stream = (warp - kUnpackWarps) >> 3, group = (warp - kUnpackWarps) >> 2, gi = group & 1, quarter = warp & 3;
             const int key = quarter * 32 + lane;                                    // of a tile
             const uint32_t lanes = tmem + (static_cast<uint32_t>(quarter * 32) << 16);

@@ -1,9 +1,8 @@
 // New rows into the 4-bit cache with the position rotation applied on the way, and the queries rotated beside them
 // (wide_cache_append): what wide_rope and wide_cache_write do in two calls, with the same bits, in one launch.
 //
-// The rotated keys never go to memory: per token and KV head that saves 4 bytes a channel of 2 + 4 + 2 + 0.56 for bf16, and a decode step,
-// whose every call is latency, has one launch instead of two.  HBM bounds a long chunk, dependent loads (row range, length,
-// page, rows) a step.
+// A decode step, whose every call is latency, has one launch instead of two: dependent loads (row range, length, page, rows) bound it.  The rotated keys never go to
+// memory, which saves 4 bytes a channel of 2 + 4 + 2 + 0.56 for bf16, but a long chunk takes as long as the two calls, as instructions bound it.
 //
 // A CTA takes one block of the cache, up to 16 new tokens of a sequence, since these share their sines and cosines, which it works out
 // once into shared memory; its warps then take the keys and the values of a head each (as wide_cache_write does: 8 channels of a token
@@ -11,8 +10,8 @@
 // of the warp, which exchange them by shuffles.  Several CTAs share a block's heads.
 //
 // Measured with cold caches (about 8 us of each are the call's own): 64 tokens of a decode step 12.3 us (the two calls 13.3), 976 tokens
-// of 16 trees 18.4 (20.5), 8188 tokens 57 (58; floor 27), 1390 tokens of 40 heads in fp32 35 (38; floor 13).  The issue of
-// instructions bounds the long ones (levels 25 a value, rotation 7), at 57 % of the slots.
+// of 16 trees 18.4 (21), 8188 tokens 57 (58; floor 27), 1390 tokens of 40 heads in fp32 35 (39; floor 13).  The issue of
+// instructions bounds the long ones (levels 25 a value, rotation 7), at 55 % of the slots, with 24 warps an SM.
 #include "cache_levels.cuh"
 #include "rope.cuh"
 

@@ -127,7 +127,7 @@ __device__ __forceinline__ unsigned long long fma2_up(unsigned long long a, unsi
 // an integer by the addition of 2^23 and biased upwards by 2^-19 of itself, which leaves the right level or the one above
 // (the error is below 2^-21), and one comparison with the guess's lower border, n s + (m - s / 2), settles it.  Likewise the
 // scale, whose last level must reach the maximum.  The kernel is bound by the rate at which instructions issue, so the two
-// tokens share them: six a value.
+// tokens share them: six a value (and about 25 with the range over the sub-group, the scale, packing and stores).
 template <typename T>
 struct Levels {
     float m, hi, s, mh, rs;

@@ -9,8 +9,9 @@
 // depend on timing.  One token 4096 -> 6144: 18.5 us with cold caches, 12.9 in a stream of calls (floor 7.7); 64 tokens 4096 -> 128256: 195 us, 82% of
 // the memory's rate.
 //
-// Many tokens (linear_pair_kernel): pairs of SMs, below.  4096 tokens 4096 -> 14336: 293 us, 1.64 PFLOP/s; short of that rate where the last round of
-// tiles leaves SMs idle (2048 tokens 4096 -> 4096: 56 us, 1.23).
+// Many tokens (linear_pair_kernel): pairs of SMs, below.  4096 tokens 4096 -> 14336: 299 us alone (1.61 PFLOP/s, the rate that the library's product reaches alone), 330 to 360 in a
+// stream of calls, where the power cap holds the clocks down; short of that rate where the last round of tiles leaves SMs idle (2048 tokens 4096 -> 4096: 56 us,
+// 1.23), and far from it with 129 to 1000 tokens, whose tiles are fewer than the pairs (256 tokens 4096 -> 6144: 29 us, the library 21.5).
 #include <cuda.h>
 
 #include <algorithm>
